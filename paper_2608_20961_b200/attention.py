@@ -1,0 +1,210 @@
+"""Thin ctypes binding of the attention-layer calls (``include/treewy_attn.h``) and one attention
+layer's speculative round.
+
+Function names and argument order follow the C header; as in ``binding``, torch tensors supply
+device memory and the stream, every computation runs in the library's CUDA kernels, and outputs are
+written in place.  Shapes, strides and types are checked here (``ValueError``), sizes and alignment by
+the library (``binding.TreewyError``).
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as tw
+from .binding import Tree
+
+SEQ_BAD_PAGE, SEQ_BAD_LENGTH, SEQ_BAD_POSITION = 64, 128, 256
+
+
+class KVCacheStruct(ctypes.Structure):
+    """Mirror of ``treewy_kv_cache_t``."""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("stride_page", ctypes.c_int64), ("stride_slot", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+        ("page_table", ctypes.c_void_p), ("context_len", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("H_kv", ctypes.c_int32), ("d_head", ctypes.c_int32),
+    ]
+
+
+class RopeStruct(ctypes.Structure):
+    """Mirror of ``treewy_rope_t``."""
+    _fields_ = [
+        ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("pair_axis", ctypes.c_void_p),
+        ("n_axes", ctypes.c_int32), ("max_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+    ]
+
+
+_lib = None
+
+
+def load_library():
+    """The library with the attention calls' prototypes set; raises if it has not been built."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = tw.load_library()
+    vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    cache, rope, tree = ctypes.POINTER(KVCacheStruct), ctypes.POINTER(RopeStruct), ctypes.POINTER(tw.TreeStruct)
+    lib.treewy_rope.argtypes = [rope, vp, i64, vp, i64, i32, i32, i32, i32, ctypes.c_int, vp, vp]
+    lib.treewy_kv_append.argtypes = [cache, rope, i32, i32, vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, ctypes.c_int, vp, vp]
+    verify = [cache, tree, vp, i64, vp, i64, vp, i64, i32, f32, vp, i32, ctypes.c_int, vp, vp, ctypes.c_size_t, vp, vp]
+    lib.treewy_attn_verify.argtypes = verify
+    lib.treewy_attn_verify_generic.argtypes = verify
+    lib.treewy_kv_commit.argtypes = [cache, tree, vp, i64, vp, i64, vp, ctypes.c_int, vp, vp, vp]
+    for fn in (lib.treewy_rope, lib.treewy_kv_append, lib.treewy_attn_verify, lib.treewy_attn_verify_generic,
+               lib.treewy_kv_commit):
+        fn.restype = ctypes.c_int
+    lib.treewy_attn_workspace.argtypes = [cache, tree, i32, i32, ctypes.c_int]
+    lib.treewy_attn_workspace.restype = ctypes.c_size_t
+    _lib = lib
+    return lib
+
+
+def _require(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _int32(t: torch.Tensor | None, n: int, what: str) -> None:
+    _require(t is None or (t.dtype == torch.int32 and t.numel() >= n and t.is_contiguous()),
+             f"{what}: contiguous int32 tensor of at least {n} elements wanted")
+
+
+def _rows(x: torch.Tensor, T: int, H: int, d: int, dtype: torch.dtype, what: str) -> int:
+    """Checks packed rows [T, H, d] (heads contiguous, tokens at any distance); returns that distance."""
+    if x.dtype != dtype or x.dim() != 3 or tuple(x.shape[1:]) != (H, d) or x.shape[0] < T:
+        raise ValueError(f"{what}: {dtype} [{T}, {H}, {d}] wanted, got {x.dtype} {list(x.shape)}")
+    st = x.stride()
+    if (d > 1 and st[2] != 1) or (H > 1 and st[1] != d):
+        raise ValueError(f"{what}: the heads of a token have to be contiguous")
+    return st[0] if x.shape[0] > 1 else H * d
+
+
+class KVCache:
+    """A paged cache (``treewy_kv_cache_t``): k, v [n_pages, page_size, H_kv, d_head] in any order of
+    strides with d_head innermost (the same for both), page_table [B, max_pages] and context_len [B] int32.
+    The object refers to the tensors' memory: contents may change between calls, storage may not."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, context_len: torch.Tensor):
+        _require(k.dtype in tw._DTYPES and v.dtype == k.dtype, "k, v: both bfloat16 or both float32 wanted")
+        _require(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride(), "k, v: same 4-d shape and strides wanted")
+        _require(k.shape[3] == 1 or k.stride(3) == 1, "k, v: d_head has to be contiguous")
+        _require(page_table.dim() == 2 and page_table.is_contiguous() and page_table.dtype == torch.int32,
+                 "page_table: contiguous int32 [B, max_pages] wanted")
+        _int32(context_len, page_table.shape[0], "context_len")
+        _require(page_table.device == k.device == v.device == context_len.device, "cache tensors on different devices")
+        self.k, self.v, self.page_table, self.context_len = k, v, page_table, context_len
+        self.B, self.max_pages = (int(n) for n in page_table.shape)
+        self.n_pages, self.page_size, self.H_kv, self.d_head = (int(n) for n in k.shape)
+        self.dtype = k.dtype
+        self._dt = tw._DTYPES[k.dtype]
+        self._struct = KVCacheStruct(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                     page_table.data_ptr(), context_len.data_ptr(), self.n_pages, self.page_size,
+                                     self.max_pages, self.H_kv, self.d_head)
+        self._ref = ctypes.byref(self._struct)
+
+
+class Rope:
+    """Rotary positions (``treewy_rope_t``): cos_sin [max_positions, rot_dim] fp32 (cosines, then sines),
+    positions [n_axes, T] (or [T]) int32, pair_axis [rot_dim / 2] uint8 (None: one axis)."""
+
+    def __init__(self, cos_sin: torch.Tensor, positions: torch.Tensor, pair_axis: torch.Tensor | None = None,
+                 interleaved: bool = False):
+        _require(cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous(),
+                 "cos_sin: contiguous float32 [max_positions, rot_dim] wanted")
+        if positions.dim() == 1:
+            positions = positions[None]
+        _require(positions.dtype == torch.int32 and positions.dim() == 2 and positions.is_contiguous(),
+                 "positions: contiguous int32 [n_axes, T] wanted")
+        _require(pair_axis is None or (pair_axis.dtype == torch.uint8 and pair_axis.is_contiguous()
+                                       and pair_axis.numel() == cos_sin.shape[1] // 2),
+                 "pair_axis: uint8 [rot_dim / 2] wanted")
+        self.cos_sin, self.positions, self.pair_axis = cos_sin, positions, pair_axis
+        self.T = int(positions.shape[1])
+        self._struct = RopeStruct(cos_sin.data_ptr(), positions.data_ptr(),
+                                  None if pair_axis is None else pair_axis.data_ptr(), int(positions.shape[0]),
+                                  int(cos_sin.shape[0]), int(cos_sin.shape[1]), int(bool(interleaved)))
+        self._ref = ctypes.byref(self._struct)
+
+
+def treewy_rope(rope: Rope, x: torch.Tensor, y: torch.Tensor, inverse: bool = False,
+                row_status: torch.Tensor | None = None, stream=None) -> None:
+    """y [T, H, d] <- x rotated by its tokens' positions (inverse: the other way, which is the backward pass)."""
+    T, H, d = x.shape
+    _require(T == rope.T, f"x: {rope.T} tokens wanted, as rope.positions has")
+    _require(x.dtype in tw._DTYPES, "x: bfloat16 or float32 wanted")
+    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x"), _rows(y, T, H, d, x.dtype, "y")
+    tw._call("treewy_rope", load_library().treewy_rope, rope._ref, tw._p(x), ld_x, tw._p(y), ld_y, T, H, d,
+             int(inverse), tw._DTYPES[x.dtype], tw._p(row_status), tw._stream(stream))
+
+
+def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     rope: Rope | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                     seq_status: torch.Tensor | None = None, stream=None) -> None:
+    """Rows k, v [T, H_kv, d] of the sequences at row_offsets [B + 1] go behind context_len of each sequence's
+    cache, k rotated on the way; q [T, H_q, d], when given, is rotated into q_out in the same pass."""
+    T = int(k.shape[0])
+    _int32(row_offsets, cache.B + 1, "row_offsets")
+    _int32(seq_status, cache.B, "seq_status")
+    _require(rope is None or rope.T == T, "rope: as many positions as rows wanted")
+    ld_k = _rows(k, T, cache.H_kv, cache.d_head, cache.dtype, "k")
+    ld_v = _rows(v, T, cache.H_kv, cache.d_head, cache.dtype, "v")
+    H_q = ld_q = ld_qo = 0
+    if q is not None:
+        _require(q_out is not None, "q_out: wanted with q")
+        H_q = int(q.shape[1])
+        ld_q = _rows(q, T, H_q, cache.d_head, cache.dtype, "q")
+        ld_qo = _rows(q_out, T, H_q, cache.d_head, cache.dtype, "q_out")
+    tw._call("treewy_kv_append", load_library().treewy_kv_append, cache._ref, None if rope is None else rope._ref, cache.B, T,
+             tw._p(row_offsets), tw._p(k), ld_k, tw._p(v), ld_v, H_q, tw._p(q), ld_q, tw._p(q_out), ld_qo, cache._dt,
+             tw._p(seq_status), tw._stream(stream))
+
+
+def attn_workspace(cache: KVCache, tree: Tree, H_q: int, shared_len: int = 0) -> torch.Tensor:
+    """A workspace for ``treewy_attn_verify`` calls of these sizes (one per call in flight)."""
+    ts = tree.struct()
+    n = load_library().treewy_attn_workspace(cache._ref, ctypes.byref(ts), H_q, shared_len, cache._dt)
+    return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=cache.k.device)
+
+
+def treewy_attn_verify(cache: KVCache, tree: Tree, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float,
+                       O: torch.Tensor, workspace: torch.Tensor, shared_pages: torch.Tensor | None = None,
+                       shared_len: int = 0, seq_status: torch.Tensor | None = None, stream=None,
+                       generic: bool = False) -> None:
+    """O [T, H_q, d] <- attention of every draft node (q, k, v: packed rows) over its sequence's cached tokens
+    and its ancestors."""
+    lib = load_library()
+    ts = tree.struct()
+    T, H_q = tree.T, int(q.shape[1])
+    _require(tree.B == cache.B, "tree: another number of sequences than the cache's page table")
+    ld_q = _rows(q, T, H_q, cache.d_head, cache.dtype, "q")
+    ld_k = _rows(k, T, cache.H_kv, cache.d_head, cache.dtype, "k")
+    ld_v = _rows(v, T, cache.H_kv, cache.d_head, cache.dtype, "v")
+    _require(T == 0 or _rows(O, T, H_q, cache.d_head, cache.dtype, "O") == H_q * cache.d_head, "O: contiguous rows wanted")
+    _int32(shared_pages, shared_len // cache.page_size, "shared_pages")
+    _int32(seq_status, cache.B, "seq_status")
+    name = "treewy_attn_verify_generic" if generic else "treewy_attn_verify"
+    tw._call(name, lib.treewy_attn_verify_generic if generic else lib.treewy_attn_verify, cache._ref, ctypes.byref(ts),
+             tw._p(q), ld_q, tw._p(k), ld_k, tw._p(v), ld_v, H_q, scale, tw._p(shared_pages), shared_len, cache._dt,
+             tw._p(O), tw._p(workspace), workspace.numel() * workspace.element_size(), tw._p(seq_status),
+             tw._stream(stream))
+
+
+def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tensor, accepted: torch.Tensor,
+                     new_context_len: torch.Tensor | None = None, seq_status: torch.Tensor | None = None,
+                     stream=None) -> None:
+    """The accepted path's rows of k, v [T, H_kv, d] go behind context_len; new_context_len [B] receives the
+    lengths after it."""
+    ts = tree.struct()
+    _require(tree.B == cache.B, "tree: another number of sequences than the cache's page table")
+    ld_k = _rows(k, tree.T, cache.H_kv, cache.d_head, cache.dtype, "k")
+    ld_v = _rows(v, tree.T, cache.H_kv, cache.d_head, cache.dtype, "v")
+    _int32(accepted, cache.B, "accepted")
+    _int32(new_context_len, cache.B, "new_context_len")
+    _int32(seq_status, cache.B, "seq_status")
+    tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, ctypes.byref(ts), tw._p(k), ld_k, tw._p(v),
+             ld_v, tw._p(accepted), cache._dt, tw._p(new_context_len), tw._p(seq_status), tw._stream(stream))

@@ -1,0 +1,278 @@
+// Rotary positions with several axes, the append of packed rows to a paged cache, and the commit of an
+// accepted path to it.  All three move every byte once and compute next to nothing: they are bound by HBM
+// (a prompt) or by the latency of one launch (a decoding step).
+//
+// Rotation: pair p of a head turns by the angle of its own axis' position,
+//     (x, y) -> (x cos - y sin, y cos + x sin),  its transpose (the backward pass) with -sin.
+// A thread takes one unit: the two 16-byte vectors that hold 8 (bf16) or 4 (fp32) pairs of one head.  A
+// warp takes a slice of one token's heads with the same pairs in every lane throughout, so a lane reads its
+// cosines and sines once and keeps them in registers over the heads.
+#include "attn_common.cuh"
+
+namespace treewy {
+namespace {
+
+constexpr int ROWS_WARPS = 8;
+constexpr int HEAD_UNROLL = 4;  // heads a lane has in flight
+
+template <typename T, int VE> struct Vec;
+template <> struct Vec<__nv_bfloat16, 8> {
+    uint4 x;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { x = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = x; }
+    __device__ __forceinline__ void get(float (&f)[8]) const { widen8(x, f); }
+    __device__ __forceinline__ void set(const float (&f)[8])
+    {
+        x = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    }
+};
+template <> struct Vec<float, 4> {
+    float4 x;
+    __device__ __forceinline__ void load(const float *p) { x = *reinterpret_cast<const float4 *>(p); }
+    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = x; }
+    __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w; }
+    __device__ __forceinline__ void set(const float (&f)[4]) { x = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <typename T> struct Vec<T, 1> {
+    T x;
+    __device__ __forceinline__ void load(const T *p) { x = *p; }
+    __device__ __forceinline__ void store(T *p) const { *p = x; }
+    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(x); }
+    __device__ __forceinline__ void set(const float (&f)[1]) { x = from_f32<T>(f[0]); }
+};
+
+// The sequence that owns packed row t (largest b with row_offsets[b] <= t among non-decreasing offsets), found
+// by a whole warp: each round narrows the range 32-fold.  Any result is checked by the caller.
+__device__ __forceinline__ int find_sequence(const int32_t *offsets, int B, int t)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = B;
+    while (n > 1) {
+        const int step = (n + 31) / 32;
+        const int at = lo + lane * step;
+        const bool le = lane * step < n && offsets[at] <= t;
+        const unsigned m = __ballot_sync(0xffffffffu, le);
+        const int last = m ? 31 - __clz(m) : 0;
+        n = min(step, n - last * step);
+        lo += last * step;
+    }
+    return lo;
+}
+
+// VE: pairs of a unit.  Grid: one warp per (token, slice of heads).
+template <typename T, int VE>
+__global__ void __launch_bounds__(ROWS_WARPS * 32) rows_kernel(RowsArgs a, int slices, int heads_per_slice)
+{
+    const int lane = threadIdx.x & 31;
+    const long long w = (long long)blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    if (w >= (long long)a.T * slices) return;
+    const int t = (int)(w / slices), slice = (int)(w - (long long)t * slices);
+    const int heads = a.H_q + 2 * a.c.H_kv;
+    const int h_begin = slice * heads_per_slice, h_end = min(heads, h_begin + heads_per_slice);
+    const int units = a.d / (2 * VE);                 // of one head
+    const int turned = a.r.cos_sin ? a.r.rot / (2 * VE) : 0;
+    const int lph = min(units, 32), hpi = 32 / lph;   // lanes of a head, heads of a warp's step
+    const int hl = lane / lph, ul = lane - hl * lph;
+    const bool on = hl < hpi;
+    const int half = a.r.rot / 2;
+
+    // positions: one lane per axis checks its own, every lane later reads the ones its pairs need
+    bool bad_pos = false;
+    if (turned > 0) {
+        if (lane < a.r.n_axes) {
+            const int p = a.r.positions[(size_t)lane * a.T + t];
+            bad_pos = p < 0 || p >= a.r.max_positions;
+        }
+        if (a.r.pair_axis)
+            for (int p = lane; p < half; p += 32) bad_pos |= a.r.pair_axis[p] >= a.r.n_axes;
+        bad_pos = __any_sync(0xffffffffu, bad_pos);
+    }
+    // where the row goes
+    T *kd = nullptr, *vd = nullptr;
+    int bad = bad_pos ? TREEWY_SEQ_BAD_POSITION : 0, b = 0;
+    if (a.c.H_kv > 0) {
+        b = find_sequence(a.row_offsets, a.B, t);
+        const int lo = a.row_offsets[b], hi = a.row_offsets[b + 1];
+        if (t < lo || t >= hi) return;                // a row of no sequence
+        if (bad_offsets(lo, hi - lo, a.T)) {
+            bad = TREEWY_SEQ_BAD_OFFSETS;
+        } else {
+            const int len = a.c.context_len[b];
+            if (len < 0 || (long long)len + (hi - lo) > (long long)a.c.max_pages * a.c.page_size) {
+                bad = TREEWY_SEQ_BAD_LENGTH;
+            } else {
+                const int slot = len + (t - lo), pi = slot / a.c.page_size;
+                const int page = a.c.page_table[(size_t)b * a.c.max_pages + pi];
+                if (page < 0 || page >= a.c.n_pages) {
+                    bad |= TREEWY_SEQ_BAD_PAGE;
+                } else {
+                    const long long at = page * a.c.stride_page + (slot - pi * a.c.page_size) * a.c.stride_slot;
+                    kd = static_cast<T *>(a.c.k) + at, vd = static_cast<T *>(a.c.v) + at;
+                }
+            }
+        }
+    }
+    if (bad) {
+        if (lane == 0 && a.status) atomicOr(&a.status[b], bad);
+        return;
+    }
+    const T *qs = static_cast<const T *>(a.q) + t * a.ld_q;
+    const T *ks = static_cast<const T *>(a.k) + t * a.ld_k, *vs = static_cast<const T *>(a.v) + t * a.ld_v;
+    T *qd = static_cast<T *>(a.q_out) + t * a.ld_qo;
+
+    for (int u0 = 0; u0 < units; u0 += 32) {
+        const int u = u0 + ul;
+        const bool active = on && u < units;
+        const bool turn = u < turned;
+        const bool split = turn && !a.r.interleaved;  // the pair's members are rot / 2 apart
+        const int off0 = split ? u * VE : 2 * u * VE, off1 = split ? half + u * VE : off0 + VE;
+        float cs[VE], sn[VE];
+        if (active && turn) {
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                const int p = u * VE + i;
+                const int axis = a.r.pair_axis ? a.r.pair_axis[p] : 0;
+                const float *row = a.r.cos_sin + (size_t)a.r.positions[(size_t)axis * a.T + t] * a.r.rot;
+                cs[i] = row[p];
+                sn[i] = a.r.inverse ? -row[half + p] : row[half + p];
+            }
+        }
+        for (int h0 = h_begin; h0 < h_end; h0 += hpi * HEAD_UNROLL) {
+            Vec<T, VE> x[HEAD_UNROLL], y[HEAD_UNROLL];
+#pragma unroll
+            for (int i = 0; i < HEAD_UNROLL; ++i) {
+                const int h = h0 + i * hpi + hl;
+                if (!active || h >= h_end) continue;
+                const T *src = h < a.H_q ? qs + (long long)h * a.d
+                               : h < a.H_q + a.c.H_kv ? ks + (long long)(h - a.H_q) * a.d
+                                                      : vs + (long long)(h - a.H_q - a.c.H_kv) * a.d;
+                const bool is_v = h >= a.H_q + a.c.H_kv;
+                x[i].load(src + (is_v ? 2 * u * VE : off0));
+                y[i].load(src + (is_v ? 2 * u * VE + VE : off1));
+            }
+#pragma unroll
+            for (int i = 0; i < HEAD_UNROLL; ++i) {
+                const int h = h0 + i * hpi + hl;
+                if (!active || h >= h_end) continue;
+                const bool is_v = h >= a.H_q + a.c.H_kv;
+                T *dst = h < a.H_q ? qd + (long long)h * a.d
+                         : !is_v   ? kd + (h - a.H_q) * a.c.stride_head
+                                   : vd + (h - a.H_q - a.c.H_kv) * a.c.stride_head;
+                if (turn && !is_v) {
+                    float f[VE], g[VE], rf[VE], rg[VE];
+                    x[i].get(f), y[i].get(g);
+                    if (split) {
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) {
+                            rf[e] = f[e] * cs[e] - g[e] * sn[e];
+                            rg[e] = g[e] * cs[e] + f[e] * sn[e];
+                        }
+                    } else {  // pairs side by side: the 2 VE elements of x, y hold pairs 0 .. VE-1 in order
+                        if constexpr (VE == 1) {
+                            rf[0] = f[0] * cs[0] - g[0] * sn[0];
+                            rg[0] = g[0] * cs[0] + f[0] * sn[0];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VE; e += 2) {
+                                rf[e] = f[e] * cs[e / 2] - f[e + 1] * sn[e / 2];
+                                rf[e + 1] = f[e + 1] * cs[e / 2] + f[e] * sn[e / 2];
+                                rg[e] = g[e] * cs[(VE + e) / 2] - g[e + 1] * sn[(VE + e) / 2];
+                                rg[e + 1] = g[e + 1] * cs[(VE + e) / 2] + g[e] * sn[(VE + e) / 2];
+                            }
+                        }
+                    }
+                    x[i].set(rf), y[i].set(rg);
+                }
+                x[i].store(dst + (is_v ? 2 * u * VE : off0));
+                y[i].store(dst + (is_v ? 2 * u * VE + VE : off1));
+            }
+        }
+    }
+}
+
+template <typename T, int VE> cudaError_t launch_rows_ve(const RowsArgs &a, cudaStream_t stream)
+{
+    const int heads = a.H_q + 2 * a.c.H_kv, units = a.d / (2 * VE);
+    const int lph = units < 32 ? units : 32, hpi = 32 / lph;
+    const int per = hpi * HEAD_UNROLL;
+    const int slices = (heads + per - 1) / per;
+    const long long warps = (long long)a.T * slices;
+    const long long blocks = (warps + ROWS_WARPS - 1) / ROWS_WARPS;
+    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    return launch_dependent(rows_kernel<T, VE>, dim3((unsigned)blocks), dim3(ROWS_WARPS * 32), 0, stream, a, slices, per);
+}
+
+// Commit: one CTA per (sequence, slice of a row's bytes), one warp per path node.  Rows are copied as they are.
+constexpr int COMMIT_WARPS = 8;
+constexpr int COMMIT_VECS = 128;  // 16-byte vectors of k (and of v) in a slice
+
+__global__ void __launch_bounds__(COMMIT_WARPS * 32) kv_commit_kernel(KvCommitArgs a, int elem)
+{
+    const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    int lo, n, len;
+    const long long capacity = (long long)a.c.max_pages * a.c.page_size;
+    int bad = check_sequence(a.node_offsets, a.c.context_len, b, a.T, a.max_nodes, capacity, 0, &lo, &n, &len);
+    uint64_t path = 0;
+    if (!bad) {
+        const int acc = a.accepted[b];
+        if (acc < -1 || acc >= n) bad = TREEWY_SEQ_BAD_ACCEPTED;
+        else if (acc >= 0) path = a.anc_mask[lo + acc] & low_bits(n);
+    }
+    const int P = __popcll(path);
+    if (!bad && (long long)len + P > capacity) bad = TREEWY_SEQ_BAD_LENGTH;
+    bool bad_page = false;
+    if (!bad && threadIdx.x < P) {
+        const int page = a.c.page_table[(size_t)b * a.c.max_pages + (len + (int)threadIdx.x) / a.c.page_size];
+        bad_page = page < 0 || page >= a.c.n_pages;
+    }
+    if (__syncthreads_or(bad_page)) bad = TREEWY_SEQ_BAD_PAGE;  // (bad is the same in every thread before this)
+    if (bad) {
+        if (threadIdx.x == 0 && blockIdx.y == 0 && a.seq_status) atomicOr(&a.seq_status[b], bad);
+        return;
+    }
+    if (threadIdx.x == 0 && blockIdx.y == 0 && a.new_len) a.new_len[b] = len + P;
+    const int vec_elems = 16 / elem, head_vecs = a.c.d / vec_elems, row_vecs = a.c.H_kv * head_vecs;
+    const int v0 = blockIdx.y * COMMIT_VECS, v1 = min(row_vecs, v0 + COMMIT_VECS);
+    for (int r = warp; r < P; r += COMMIT_WARPS) {
+        const int node = nth_set_bit(path, r), slot = len + r, pi = slot / a.c.page_size;
+        const long long page = a.c.page_table[(size_t)b * a.c.max_pages + pi];
+        const long long at = page * a.c.stride_page + (slot - pi * a.c.page_size) * a.c.stride_slot;
+        const char *ks = static_cast<const char *>(a.k) + (lo + node) * a.ld_k * elem;
+        const char *vs = static_cast<const char *>(a.v) + (lo + node) * a.ld_v * elem;
+        for (int i = v0 + lane; i < v1; i += 32) {
+            const int h = i / head_vecs;
+            const long long dst = (at + h * a.c.stride_head) * elem + (long long)(i - h * head_vecs) * 16;
+            const uint4 x = *reinterpret_cast<const uint4 *>(ks + (long long)i * 16);
+            const uint4 y = *reinterpret_cast<const uint4 *>(vs + (long long)i * 16);
+            *reinterpret_cast<uint4 *>(static_cast<char *>(a.c.k) + dst) = x;
+            *reinterpret_cast<uint4 *>(static_cast<char *>(a.c.v) + dst) = y;
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_rows(const RowsArgs &a, treewy_dtype_t io, cudaStream_t stream)
+{
+    // 16-byte units need whole vectors on both sides of every boundary (heads of d elements stay aligned then);
+    // odd sizes go pair by pair
+    const int ve = io == TREEWY_BF16 ? 8 : 4;
+    const bool whole = a.d % (2 * ve) == 0 && (!a.r.cos_sin || a.r.rot % (2 * ve) == 0);
+    if (io == TREEWY_BF16)
+        return whole ? launch_rows_ve<__nv_bfloat16, 8>(a, stream) : launch_rows_ve<__nv_bfloat16, 1>(a, stream);
+    return whole ? launch_rows_ve<float, 4>(a, stream) : launch_rows_ve<float, 1>(a, stream);
+}
+
+cudaError_t launch_kv_commit(const KvCommitArgs &a, treewy_dtype_t io, cudaStream_t stream)
+{
+    const int elem = io == TREEWY_BF16 ? 2 : 4;
+    const int row_vecs = (int)((long long)a.c.H_kv * a.c.d * elem / 16);
+    const dim3 grid(a.B, (row_vecs + COMMIT_VECS - 1) / COMMIT_VECS);
+    return launch_dependent(kv_commit_kernel, grid, dim3(COMMIT_WARPS * 32), 0, stream, a, elem);
+}
+
+}  // namespace treewy
