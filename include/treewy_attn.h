@@ -94,7 +94,7 @@ treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_ro
  * over the sequence's context_len[b] cached tokens and the packed draft rows j whose bit is set in
  * tree->anc_mask[i] (ancestors and the node itself).  Trees of one node are ordinary decoding.  A node
  * that sees nothing (no context, an empty mask) gets o = 0; what no node may see is never multiplied, so
- * NaN or infinity there does not spread.
+ * NaN or infinity there does not spread.  scale is positive and finite.
  *   q [T,H_q,d], k, v [T,H_kv,d]   the draft rows (rotated already);  O [T,H_q,d] contiguous, io_dtype
  *   shared_pages, shared_len       the first shared_len tokens (a multiple of page_size) of EVERY sequence
  *                                  are those of shared_pages [shared_len / page_size]: a prompt common to the

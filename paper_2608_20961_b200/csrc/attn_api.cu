@@ -1,5 +1,7 @@
 // C ABI of the attention-layer calls (treewy_attn.h): argument checks and kernel dispatch.  No allocation, no
 // host synchronisation, no state kept between calls.
+#include <float.h>
+
 #include "attn_common.cuh"
 #include "treewy_kernels.cuh"
 
@@ -75,8 +77,7 @@ treewy_status_t attn_args(const treewy_kv_cache_t *cache, const treewy_tree_t *t
 
 size_t workspace_of(const AttnArgs &a, treewy_dtype_t io)
 {
-    (void)io;
-    return attn_generic_workspace(a);
+    return attn_tc_applies(a, io) ? attn_tc_workspace(a) : attn_generic_workspace(a);
 }
 
 treewy_status_t attn_common(bool force_generic, const treewy_kv_cache_t *cache, const treewy_tree_t *tree, const void *q,
@@ -88,6 +89,7 @@ treewy_status_t attn_common(bool force_generic, const treewy_kv_cache_t *cache, 
     treewy_status_t st = attn_args(cache, tree, H_q, shared_len, io, &a);
     if (st != TREEWY_OK) return st;
     if (seq_status && misaligned(seq_status)) return TREEWY_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || scale > FLT_MAX) return TREEWY_ERR_INVALID_ARG;
     if (tree->B == 0 || tree->T == 0) return TREEWY_OK;
     const int64_t kv_row = (int64_t)cache->H_kv * cache->d_head, q_row = (int64_t)H_q * cache->d_head;
     const int e = elem_size(io);
@@ -99,7 +101,8 @@ treewy_status_t attn_common(bool force_generic, const treewy_kv_cache_t *cache, 
     if (workspace_bytes < need || (need > 0 && bad_ptr(workspace))) return TREEWY_ERR_INVALID_ARG;
     a.q = q, a.k = k, a.v = v, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v, a.O = O;
     a.shared_pages = shared_pages, a.scale = scale, a.ws = static_cast<float *>(workspace), a.seq_status = seq_status;
-    a.wait_cycles = debug_inject().wait_cycles;
+    a.wait_cycles = debug_inject().wait_cycles, a.skip_item = debug_inject().skip_item;
+    if (!force_generic && attn_tc_applies(a, io)) return launched(launch_attn_tc(a, static_cast<cudaStream_t>(cuda_stream)));
     return launched(launch_attn_generic(a, io, static_cast<cudaStream_t>(cuda_stream)));
 }
 

@@ -59,13 +59,18 @@ struct AttnArgs {
     int B, T, max_nodes, H_q, G;  // G = H_q / H_kv query heads to a key/value head
     float *ws;
     int32_t *seq_status;
-    long long wait_cycles;
+    long long wait_cycles;  // limit of the bounded waits (0: the default)
+    int skip_item;          // test hook: the (b * H_kv + h) whose copies are never issued, or -1
 };
 
 cudaError_t launch_rows(const RowsArgs &a, treewy_dtype_t io, cudaStream_t stream);
 cudaError_t launch_kv_commit(const KvCommitArgs &a, treewy_dtype_t io, cudaStream_t stream);
 cudaError_t launch_attn_generic(const AttnArgs &a, treewy_dtype_t io, cudaStream_t stream);
 size_t attn_generic_workspace(const AttnArgs &a);
+// bf16 on the tensor cores, where it applies
+bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io);
+cudaError_t launch_attn_tc(const AttnArgs &a, cudaStream_t stream);
+size_t attn_tc_workspace(const AttnArgs &a);
 
 // Status bits of sequence b, and its rows and length: every kernel of the attention calls decides
 // what to skip by this one function.  The cached part is read up to context_len, so it has to fit the table.

@@ -1,0 +1,844 @@
+// treewy_attn_verify, bf16: draft-tree attention over a paged cache on the tensor cores.
+//
+// Rows.  All N nodes of a tree and the G query heads of one key/value head read the same keys, so a row of the
+// contraction is a (node, query head) pair and a tile is 128 of them (decoding: the G heads of one token).  A
+// prompt shared by the batch is the same with the rows of all sequences in one list.  Every key and value is then
+// read from HBM once for up to 128 rows, which is what bounds the kernel: 4 D bytes a key against 4 D * 128
+// operations, half of the machine's balance.
+// Keys.  A sequence's cached tokens in tiles of 64, then its draft rows as one last tile.  Only that tile and the
+// last cached one are masked.
+// One tile:  S = Q K^T (Q in tensor memory, K as the TMA left it), the softmax step in registers, P = weights as bf16
+// over S's own columns of tensor memory, O += P V (V read with its rows as the K index; O in tensor memory).
+// The running maximum m moves only when a row's new maximum exceeds it by more than 8 (in log2): until then
+// weights are at most 2^8 and nothing overflows, and the pass over O that a new m costs is rare after a
+// row's first tiles.
+//
+// Work.  (sequence, head, group of row tiles) x key tiles in one line, cut into equal parts, one for each CTA: no
+// CTA waits for a longer neighbour, whatever the lengths, and a single long sequence fills the GPU.  A cut
+// item leaves unnormalised outputs with their m and l in the workspace; a second kernel joins them in the
+// order of the keys.  When trees have more rows than a tile, `group` CTAs walk the same part with a row tile each,
+// so that the second one reads the keys out of L2.
+//
+// Roles: two softmax warpgroups that take turns at the key tiles (the maxima travel between them, row by row),
+// one warp that walks the work and issues the TMA copies, one that issues the MMAs.
+#include "attn_common.cuh"
+#include "ptx_sm100.cuh"
+#include "tma_host.cuh"
+
+namespace treewy {
+namespace {
+
+constexpr int KT = 64;                 // keys of a tile
+constexpr int MT = 128;                // rows of a tile
+constexpr int MAX_CTAS = 160;
+constexpr int THREADS = 320, PRODUCER_WARP = 8, MMA_WARP = 9;
+constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
+constexpr int MIN_TILES = 2;           // of a CTA's part: below this a part is mostly start and end
+constexpr float LAZY = 8.f;
+
+template <int D> struct Cfg {
+    static constexpr int NC = D / 64;                              // 64-column chunks of a row
+    static constexpr int CHUNK = KT * 128;                         // bytes of one chunk of a tile
+    static constexpr int STAGE = NC * CHUNK;
+    static constexpr int NST = D == 256 ? 6 : D == 128 ? 12 : 16;  // about 192 KB in flight
+    static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
+    static constexpr int TM_Q = D, TM_S = D + D / 2;
+};
+
+struct Item {
+    int b, h, lo, n, len;       // b = -1: the shared prompt
+    int row0, rows;             // this CTA's row tile: first row, rows in it
+    int kt0, tiles, kts;        // first key tile here, tiles here, tiles of the whole item
+    int slot;                   // where a cut item's part goes, or -1: the item is whole
+};
+
+struct Shared {
+    uint64_t kv_full[16], kv_empty[16], s_full[4], p_full[4], pv_done[4], q_full, o_free, item_full[ITEMS],
+        item_empty[ITEMS], hand[2][4], exch[4];
+    Item items[ITEMS];
+    float m[MT], l[2][2][MT];
+    unsigned bad_item[16];      // ordinal + 1 of an item that met a page out of range
+    unsigned nonfinite[4][2];   // draft rows of an item with NaN or infinity among their values
+    long long scan[THREADS / 32], first_off, last_off;
+    int first_b, last_b, total_fail;
+    uint32_t tmem;
+};
+
+// The workspace.
+struct Ws {
+    long long *prefix;          // [B + 2]: first unit of each sequence (shared prompts), all units, parts
+    int *desc;                  // [MAX_CTAS][8]: the item that a CTA's part cuts at its end
+    float *slot_ml, *slot_o;    // [2 * CTAs][row_cap]
+    float *row_ml, *row_o;      // [2][T * H_q]: whole items' results where a prompt is shared
+    int row_cap;
+};
+
+__device__ __forceinline__ int tiles_of(int tokens) { return (tokens + KT - 1) / KT; }
+
+struct Seq {
+    int lo, n, len, kts, row_tiles, groups;
+    long long units;
+};
+// b = -1: the shared prompt, whose rows are those of all sequences
+__device__ __forceinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status)
+{
+    Seq s;
+    *status = 0;
+    if (b < 0) {
+        s.lo = 0, s.n = 0, s.len = a.shared_len, s.kts = tiles_of(a.shared_len);
+        s.row_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT);
+    } else {
+        *status = check_sequence(a.node_offsets, a.c.context_len, b, a.T, a.max_nodes,
+                                 (long long)a.c.max_pages * a.c.page_size, a.shared_len, &s.lo, &s.n, &s.len);
+        if (*status) {
+            s.units = 0;
+            return s;
+        }
+        s.kts = tiles_of(s.len - a.shared_len) + 1;
+        s.row_tiles = (s.n * a.G + MT - 1) / MT;
+    }
+    s.groups = (s.row_tiles + R - 1) / R;
+    s.units = (long long)a.c.H_kv * s.groups * s.kts;
+    return s;
+}
+
+// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.
+__device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return g * W / parts; }
+__device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)(((unit + 1) * parts - 1) / W); }
+
+// keys of tile kt that exist
+__device__ __forceinline__ int valid_keys(const AttnArgs &a, const Item &it, int kt)
+{
+    if (it.b < 0) return min(KT, it.len - kt * KT);
+    return kt == it.kts - 1 ? it.n : min(KT, it.len - a.shared_len - kt * KT);
+}
+// position of K_j and V_j of an item of n tiles in the order of the copies: K0 K1 V0 K2 V1 ... K V V
+__device__ __forceinline__ int k_pos(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int v_pos(int j, int n) { return j < n - 1 ? 2 * j + 2 : 2 * n - 1; }
+
+__device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// a wait with one outcome for the whole warp: what follows needs all of its lanes
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity)
+{
+    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity));
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1)
+attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
+               const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
+{
+    using C = Cfg<D>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Shared sh;
+    unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int group = blockIdx.x / R, member = blockIdx.x - group * R, n_groups = gridDim.x / R;
+
+    if (tid == 0) {
+        ptx::wait_deadline_init(a.wait_cycles);
+        for (int i = 0; i < C::NST; ++i) ptx::mbar_init(&sh.kv_full[i], 1), ptx::mbar_init(&sh.kv_empty[i], 1);
+        for (int i = 0; i < C::NSB; ++i)
+            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
+        ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
+        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 9);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.hand[0][i], 1), ptx::mbar_init(&sh.hand[1][i], 1), ptx::mbar_init(&sh.exch[i], 2);
+        ptx::fence_barrier_init();
+        sh.total_fail = 0;
+        sh.first_b = sh.last_b = -2;
+        ptx::prefetch_tmap(&map_kc), ptx::prefetch_tmap(&map_vc), ptx::prefetch_tmap(&map_k), ptx::prefetch_tmap(&map_v);
+    }
+    if (tid < 16) sh.bad_item[tid] = 0;
+    if (tid < 8) sh.nonfinite[tid >> 1][tid & 1] = 0;
+    if (warp == MMA_WARP) {
+        ptx::tmem_alloc(&sh.tmem, 512);
+        ptx::tmem_relinquish();
+    }
+    grid_dependency_wait();
+    grid_dependency_trigger();
+
+    // ---- the line of work and this CTA's part of it
+    int st;
+    const long long shared_units = a.shared_len > 0 ? load_seq(a, -1, R, &st).units : 0;
+    const int chunk = (a.B + THREADS - 1) / THREADS, b_begin = min(a.B, tid * chunk), b_end = min(a.B, b_begin + chunk);
+    long long sum = 0;
+    for (int b = b_begin; b < b_end; ++b) {
+        sum += load_seq(a, b, R, &st).units;
+        if (st && blockIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[b], st);
+    }
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) sh.scan[warp] = incl;
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    long long before = shared_units, W = shared_units;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+        if (i < warp) before += sh.scan[i];
+        W += sh.scan[i];
+    }
+    before += incl - sum;
+    const int parts = (int)max(1ll, min((long long)n_groups, W / MIN_TILES));
+    const long long u0 = group < parts && W > 0 ? part_begin(group, W, parts) : 0;
+    const long long u1 = group < parts && W > 0 ? part_begin(group + 1, W, parts) : 0;
+    for (int b = b_begin; b < b_end; ++b) {
+        const long long units = load_seq(a, b, R, &st).units;
+        if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[b] = before;
+        if (u1 > u0) {
+            if (u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before;
+            if (u1 - 1 >= before && u1 - 1 < before + units) sh.last_b = b, sh.last_off = u1 - 1 - before;
+        }
+        before += units;
+    }
+    if (tid == 0) {
+        if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[a.B] = W, ws.prefix[a.B + 1] = parts;
+        if (u1 > u0 && u0 < shared_units) sh.first_b = -1, sh.first_off = u0;
+        if (u1 > u0 && u1 - 1 < shared_units) sh.last_b = -1, sh.last_off = u1 - 1;
+    }
+    __syncthreads();
+    if (tid == 0 && a.shared_len == 0) {  // what the join needs of the item that this part cuts at its end
+        int *d = ws.desc + 8 * blockIdx.x;
+        int pieces = 0;
+        if (u1 > u0) {
+            const Seq s = load_seq(a, sh.last_b, R, &st);
+            const long long it = sh.last_off / s.kts, begin = u1 - 1 - (sh.last_off - it * s.kts), end = begin + s.kts;
+            const int row0 = ((int)(it % s.groups) * R + member) * MT;
+            if (begin >= u0 && end > u1 && row0 < s.n * a.G) {
+                pieces = part_of(end - 1, W, parts) - group + 1;
+                d[1] = begin == u0 ? 2 * group : 2 * group + 1;
+                d[2] = s.lo, d[3] = (int)(it / s.groups), d[4] = row0, d[5] = min(MT, s.n * a.G - row0), d[6] = group;
+            }
+        }
+        d[0] = pieces;
+    }
+    const uint32_t tmem = sh.tmem;
+    const float sl2 = a.scale * 1.4426950408889634f;
+    auto fail = [&](int b) {
+        sh.total_fail = 1;
+        if (a.seq_status && a.B > 0) atomicOr(&a.seq_status[b < 0 ? 0 : b], TREEWY_SEQ_TIMEOUT);
+    };
+
+    if (warp == PRODUCER_WARP) {
+        // ---------------------------------------------------------------- work items and TMA copies
+        unsigned stage = 0;      // copies issued (stages filled) so far
+        auto produce = [&]() -> int {
+            int b = sh.first_b;
+            long long off = sh.first_off, u = u0;
+            unsigned ord = 0;    // items published so far
+            int item_b = -1;
+            Seq s;
+            s.units = 0;
+            if (u < u1) s = load_seq(a, b, R, &st);
+            while (u < u1) {
+                while (off >= s.units) {  // the next sequence that has work
+                    off = 0, ++b;
+                    s = load_seq(a, b, R, &st);
+                }
+                const long long it = off / s.kts;
+                const int kt0 = (int)(off - it * s.kts), h = (int)(it / s.groups), rg = (int)(it % s.groups);
+                const int tiles = (int)min((long long)(s.kts - kt0), u1 - u);
+                const long long begin = u - kt0, end = begin + s.kts;
+                const int row0 = (rg * R + member) * MT;
+                const long long rows = b < 0 ? (long long)a.T * a.G : (long long)s.n * a.G;
+                off += tiles, u += tiles;
+                if (row0 >= rows) continue;  // no row tile of this item for this member of the group
+                const unsigned r = ord % ITEMS;
+                item_b = b;
+                if (ord >= ITEMS && !wait_warp(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return item_b;
+                if (lane == 0) {
+                    Item &x = sh.items[r];
+                    x.b = b, x.h = h, x.lo = s.lo, x.n = s.n, x.len = s.len;
+                    x.row0 = row0, x.rows = (int)min((long long)MT, rows - row0);
+                    x.kt0 = kt0, x.tiles = tiles, x.kts = s.kts;
+                    x.slot = begin >= u0 && end <= u1 ? -1 : begin <= u0 ? 2 * group : 2 * group + 1;
+                    ptx::mbar_arrive(&sh.item_full[r]);
+                }
+                __syncwarp();
+                const bool withheld = b >= 0 && b * a.c.H_kv + h == a.skip_item;
+
+                // pages of a tile, one copy to a lane: (page of the tile, chunk)
+                const int ps = a.c.page_size, box = min(ps, KT), per_tile = KT / box;
+                const int pi = lane / C::NC, ch = lane % C::NC;
+                const int *table = b < 0 ? a.shared_pages : a.c.page_table + (size_t)b * a.c.max_pages;
+                const int key0 = b < 0 ? 0 : a.shared_len;
+                auto page_for = [&](int kt) -> int {  // -2: this lane has no copy in the tile
+                    if (kt >= kt0 + tiles || (b >= 0 && kt == s.kts - 1)) return -2;
+                    const int token = key0 + kt * KT + pi * box;
+                    if (pi >= per_tile || token >= s.len) return -2;
+                    return table[token / ps];
+                };
+                auto fill = [&](bool is_v, int kt, int page) -> bool {
+                    const unsigned sidx = stage % C::NST;
+                    if (stage >= C::NST && !wait_warp(&sh.kv_empty[sidx], (stage / C::NST - 1) & 1)) return false;
+                    unsigned char *dst = stages + sidx * C::STAGE + ch * C::CHUNK;
+                    const bool draft = b >= 0 && kt == s.kts - 1;
+                    const int rows_box = draft ? 8 : box;
+                    const bool mine = draft ? pi * 8 < s.n : page != -2;
+                    const unsigned copies = __popc(__ballot_sync(0xffffffffu, mine));
+                    if (lane == 0) ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], copies * rows_box * 128u);
+                    __syncwarp();
+                    if (mine) {
+                        if (draft) {
+                            ptx::tma_load_2d(dst + pi * 8 * 128, is_v ? &map_v : &map_k, h * D + ch * 64, s.lo + pi * 8, &sh.kv_full[sidx]);
+                        } else {
+                            const int token = key0 + kt * KT + pi * box;
+                            // (a page out of range reads as the one past the pool: zeros)
+                            ptx::tma_load_4d(dst + pi * box * 128, is_v ? &map_vc : &map_kc, ch * 64, token % ps, h,
+                                             page < 0 || page >= a.c.n_pages ? a.c.n_pages : page, &sh.kv_full[sidx]);
+                        }
+                    }
+                    ++stage;
+                    return true;
+                };
+                if (withheld) return -4;
+                {
+                    int prev = -2, cur = page_for(kt0), next;
+                    bool bad = false;
+                    for (int j = 0; j <= tiles; ++j) {
+                        next = page_for(kt0 + j + 1);
+                        if (j < tiles) {
+                            const bool out = cur != -2 && (cur < 0 || cur >= a.c.n_pages);
+                            if (__any_sync(0xffffffffu, out) && !bad) {
+                                bad = true;
+                                if (lane == 0) sh.bad_item[ord % 16] = ord + 1;
+                                __syncwarp();
+                            }
+                            if (!fill(false, kt0 + j, cur)) return item_b;
+                        }
+                        if (j > 0 && !fill(true, kt0 + j - 1, prev)) return item_b;
+                        prev = cur, cur = next;
+                    }
+                }
+                ++ord;
+            }
+            const unsigned r = ord % ITEMS;  // the end
+            if (ord >= ITEMS && !wait_warp(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return item_b;
+            if (lane == 0) {
+                sh.items[r].tiles = 0;
+                ptx::mbar_arrive(&sh.item_full[r]);
+            }
+            return -3;
+        };
+        const int rc = produce();
+        if (rc > -3 && lane == 0) fail(rc);
+        __syncwarp();
+        if (rc != -3) {  // copies in flight have to land before the CTA may leave
+            const unsigned have = stage < C::NST ? stage : C::NST;
+            for (unsigned i = stage - have; i != stage; ++i)
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.kv_full[i % C::NST], (i / C::NST) & 1); ++t) __nanosleep(20);
+        }
+    } else if (warp == MMA_WARP) {
+        // ---------------------------------------------------------------- MMAs, one thread
+        if (lane == 0) {
+            constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
+            int cur_b = -1;
+            unsigned commits = 0;
+            auto run = [&]() -> bool {
+                unsigned base = 0, tile = 0;  // stages and tiles of the items before
+                for (unsigned ord = 0;; ++ord) {
+                    const unsigned r = ord % ITEMS;
+                    if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return false;
+                    const Item it = sh.items[r];
+                    if (it.tiles == 0) return true;
+                    cur_b = it.b;
+                    ptx::mbar_arrive(&sh.item_empty[r]);
+                    if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
+                    const int n = it.tiles;
+                    auto qk = [&](int j) -> bool {
+                        const unsigned st_ = base + k_pos(j), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
+                        if (g >= C::NSB && !ptx::mbar_wait(&sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
+                        if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                        ptx::tc_fence_after_sync();
+                        const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+#pragma unroll
+                        for (int s = 0; s < D / 16; ++s)
+                            ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + s * 8,
+                                              ptx::umma_desc_k_sw128(kaddr + (s / 4) * C::CHUNK + (s % 4) * 32), idesc_qk, s > 0);
+                        ptx::umma_commit(&sh.kv_empty[sidx]);
+                        ptx::umma_commit(&sh.s_full[buf]);
+                        return true;
+                    };
+                    if (!qk(0)) return false;
+                    if (n > 1 && !qk(1)) return false;
+                    for (int j = 0; j < n; ++j) {
+                        const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
+                        if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                        if (j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free, (ord - 1) & 1)) return false;
+                        if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
+                        ptx::tc_fence_after_sync();
+                        const uint32_t vaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+                        const int steps = (valid_keys(a, it, it.kt0 + j) + 15) / 16;
+                        for (int s = 0; s < steps; ++s)
+                            ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8, ptx::umma_desc_mn_sw128(vaddr + s * 2048, C::CHUNK),
+                                              idesc_pv, j > 0 || s > 0);
+                        ptx::umma_commit(&sh.kv_empty[sidx]);
+                        ptx::umma_commit(&sh.pv_done[buf]);
+                        commits = g + 1;
+                        if (j + 2 < n && !qk(j + 2)) return false;
+                    }
+                    base += 2 * n, tile += n;
+                }
+            };
+            if (!run()) {
+                fail(cur_b);
+                if (commits > 0)
+                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.pv_done[(commits - 1) % C::NSB], ((commits - 1) / C::NSB) & 1); ++t)
+                        __nanosleep(20);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- softmax, epilogue
+        const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
+        int cur_b = -1;
+        auto load_q = [&](const Item &it) {
+            // this thread's half of its row: D / 2 elements into D / 4 columns
+            if (w4 * 32 < it.rows) {
+                const bool on = row < it.rows;
+                const int rr = it.row0 + (on ? row : 0), node = rr / a.G, g = rr - node * a.G;
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + (it.lo + node) * a.ld_q +
+                                                                   (long long)(it.h * a.G + g) * D + wg * (D / 2));
+                uint32_t x[D / 4];
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint4 y = on ? src[i] : make_uint4(0, 0, 0, 0);
+                    x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
+                }
+                const uint32_t dst = tmem + lane_base + C::TM_Q + wg * (D / 4);
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i)
+                    ptx::tmem_st16(dst + 16 * i, *reinterpret_cast<const uint32_t(*)[16]>(&x[16 * i]));
+                ptx::tmem_wait_st();
+            }
+            ptx::tc_fence_before_sync();
+            ptx::mbar_arrive_warp(&sh.q_full);
+        };
+        auto run = [&]() -> bool {
+            unsigned base = 0, tile = 0, handed = 0;  // handed: hand-overs of the maxima this warpgroup has received
+            if (!wait_warp(&sh.item_full[0], 0)) return false;
+            Item it = sh.items[0];
+            if (it.tiles == 0) return true;
+            load_q(it);
+            bool have = false;                        // the hand-over before this warpgroup's next tile is in
+            for (unsigned ord = 0;; ++ord) {
+                cur_b = it.b;
+                const int n = it.tiles;
+                const bool warp_on = w4 * 32 < it.rows, on = row < it.rows;
+                uint64_t tree = 0;
+                if (it.b >= 0 && on && it.kt0 + n == it.kts)
+                    tree = a.anc_mask[it.lo + (it.row0 + row) / a.G] & low_bits(it.n);
+                float m = -INFINITY, l = 0.f, m_l = -INFINITY;
+                for (int j = 0; j < n; ++j) {
+                    const unsigned g = tile + j, buf = g % C::NSB;
+                    if ((int)(g & 1) != wg) continue;
+                    const int kt = it.kt0 + j, valid = valid_keys(a, it, kt);
+                    const bool draft = it.b >= 0 && kt == it.kts - 1;
+                    if (!wait_warp(&sh.s_full[buf], (g / C::NSB) & 1)) return false;
+                    ptx::tc_fence_after_sync();
+                    const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
+                    uint32_t raw[2][32];
+                    float top = -INFINITY;
+                    if (warp_on) {
+                        ptx::tmem_ld32(ts, raw[0]);
+                        ptx::tmem_ld32(ts + 32, raw[1]);
+                        ptx::tmem_wait_ld();
+                        if (draft || valid < KT) {
+                            const uint64_t seen = draft ? tree : low_bits(valid);
+#pragma unroll
+                            for (int i = 0; i < KT; ++i)
+                                if (!((seen >> i) & 1)) raw[i >> 5][i & 31] = 0xff800000u;  // -infinity
+                        }
+                        float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            t0 = fmaxf(t0, __uint_as_float(raw[0][i])), t1 = fmaxf(t1, __uint_as_float(raw[0][i + 1]));
+                            t2 = fmaxf(t2, __uint_as_float(raw[1][i])), t3 = fmaxf(t3, __uint_as_float(raw[1][i + 1]));
+                        }
+                        top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * sl2;
+                    }
+                    if (g > 0 && !have) {
+                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
+                        ++handed;
+                    }
+                    have = false;
+                    const float m0 = j == 0 ? -INFINITY : sh.m[row];
+                    const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
+                    m = grow ? top : m0;
+                    sh.m[row] = m;
+                    ptx::mbar_arrive_warp(&sh.hand[wg ^ 1][w4]);
+                    if (warp_on) {
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                        uint32_t pk[2][16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            const float p0 = ptx::ex2(fmaf(__uint_as_float(raw[0][i]), sl2, -ref));
+                            const float p1 = ptx::ex2(fmaf(__uint_as_float(raw[0][i + 1]), sl2, -ref));
+                            const float p2 = ptx::ex2(fmaf(__uint_as_float(raw[1][i]), sl2, -ref));
+                            const float p3 = ptx::ex2(fmaf(__uint_as_float(raw[1][i + 1]), sl2, -ref));
+                            s0 += p0, s1 += p1, s2 += p2, s3 += p3;
+                            // weights as bf16: 2^-8 of each at most, averaged over the keys
+                            pk[0][i / 2] = pack_bf16(p0, p1), pk[1][i / 2] = pack_bf16(p2, p3);
+                        }
+                        ptx::tmem_st16(ts, pk[0]);
+                        ptx::tmem_st16(ts + 16, pk[1]);
+                        if (m != m_l) l *= ptx::ex2(m_l - ref);
+                        m_l = m;
+                        l += (s0 + s1) + (s2 + s3);
+                    }
+                    if (draft || valid < KT) {
+                        // Rows of V that no weight may meet: past the end (left over from the stage's last use, or the
+                        // page's unused slots), and draft rows with NaN or infinity, which the epilogue adds where they
+                        // are seen.  A zero weight would make NaN of them.
+                        const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST;
+                        if (!wait_warp(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                        unsigned char *v = stages + sidx * C::STAGE;
+                        const int upto = (valid + 15) / 16 * 16;
+                        constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
+                        for (int i = (draft ? 0 : valid * VR) + w4 * 32 + lane; i < upto * VR; i += 128) {
+                            const int key = i / VR, c = i - key * VR;
+                            uint4 *p = reinterpret_cast<uint4 *>(v + (c >> 3) * C::CHUNK + key * 128 + (c & 7) * 16);
+                            bool zero = key >= valid;
+                            if (!zero && draft) {
+                                const uint4 x = *p;
+                                if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
+                                    atomicOr(&sh.nonfinite[ord & 3][key >> 5], 1u << (key & 31));
+                                    uint4 y = x;
+                                    uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        if ((yw[e] & 0x7f80u) == 0x7f80u) yw[e] &= 0xffff0000u;
+                                        if ((yw[e] & 0x7f800000u) == 0x7f800000u) yw[e] &= 0x0000ffffu;
+                                    }
+                                    *p = y;
+                                }
+                            }
+                            if (zero) *p = make_uint4(0, 0, 0, 0);
+                        }
+                        ptx::fence_proxy_async();
+                        __syncwarp();
+                    }
+                    if (j > 0 && __any_sync(0xffffffffu, grow)) {
+                        const unsigned pg = g - 1;
+                        if (!wait_warp(&sh.pv_done[pg % C::NSB], (pg / C::NSB) & 1)) return false;
+                        ptx::tc_fence_after_sync();
+                        const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            ptx::tmem_ld32(tmem + lane_base + c, o);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            ptx::tmem_st16(tmem + lane_base + c, *reinterpret_cast<const uint32_t(*)[16]>(&o[0]));
+                            ptx::tmem_st16(tmem + lane_base + c + 16, *reinterpret_cast<const uint32_t(*)[16]>(&o[16]));
+                        }
+                    }
+                    ptx::tmem_wait_st();
+                    ptx::tc_fence_before_sync();
+                    ptx::mbar_arrive_warp(&sh.p_full[buf]);
+                }
+                // ---- end of the item: the other warpgroup's last maximum, the sum of both, the next item's queries
+                const unsigned last = tile + n - 1;
+                if ((int)(last & 1) != wg) {
+                    if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
+                    ++handed, have = true;
+                    m = sh.m[row];
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                if (m != m_l) l *= ptx::ex2(m_l - ref);
+                sh.l[ord & 1][wg][row] = l;
+                ptx::mbar_arrive_warp(&sh.exch[w4]);
+                const unsigned nr = (ord + 1) % ITEMS;
+                if (!wait_warp(&sh.item_full[nr], ((ord + 1) / ITEMS) & 1)) return false;
+                const Item next = sh.items[nr];
+                if (next.tiles > 0) load_q(next);     // (the last Q K^T of this item is done: its S has been read)
+                if (!wait_warp(&sh.exch[w4], ord & 1)) return false;
+                l += sh.l[ord & 1][wg ^ 1][row];
+                if (!wait_warp(&sh.pv_done[last % C::NSB], (last / C::NSB) & 1)) return false;
+                ptx::tc_fence_after_sync();
+                const bool bad = sh.bad_item[ord % 16] == ord + 1;
+                if (tid == 0) sh.nonfinite[(ord + 2) & 3][0] = sh.nonfinite[(ord + 2) & 3][1] = 0;
+                if (bad && it.b >= 0 && row == 0 && wg == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
+                if (warp_on) {
+                    const uint64_t nf = tree & ((uint64_t)sh.nonfinite[ord & 3][0] | (uint64_t)sh.nonfinite[ord & 3][1] << 32);
+                    const int rr = it.row0 + row, node = rr / a.G, hq = it.h * a.G + rr - node * a.G;
+                    const long long orow = (long long)(it.lo + node) * a.H_q + hq;
+                    const bool direct = it.slot < 0 && a.shared_len == 0;
+                    const float inv = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                    float *po, *pml;
+                    if (it.slot >= 0) {
+                        const long long at = ((long long)it.slot * R + member) * ws.row_cap + row;
+                        po = ws.slot_o + at * D, pml = ws.slot_ml + 2 * at;
+                    } else {
+                        const long long at = (it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow;
+                        po = ws.row_o + at * D, pml = ws.row_ml + 2 * at;
+                    }
+                    if (!direct && on && wg == 0) *reinterpret_cast<float2 *>(pml) = make_float2(m, bad ? -1.f : l);
+                    __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
+                    const bool store = on && !(direct && bad);
+#pragma unroll 1
+                    for (int c = wg * (D / 2); c < (wg + 1) * (D / 2); c += 32) {
+                        uint32_t o[32];
+                        __syncwarp();
+                        ptx::tmem_ld32(tmem + lane_base + c, o);
+                        ptx::tmem_wait_ld();
+                        if (nf) {
+                            for (uint64_t left = nf; left; left &= left - 1) {
+                                const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) +
+                                                         (it.lo + __ffsll((long long)left) - 1) * a.ld_v + (long long)it.h * D + c;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const float x = to_f32(v[i]);
+                                    if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+                                }
+                            }
+                        }
+                        if (direct) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                uint4 y;
+                                uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    yw[e] = pack_bf16(l == 0.f ? 0.f : __uint_as_float(o[i + 2 * e]) * inv,
+                                                      l == 0.f ? 0.f : __uint_as_float(o[i + 2 * e + 1]) * inv);
+                                if (store) *reinterpret_cast<uint4 *>(out + c + i) = y;
+                            }
+                        } else if (store) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                *reinterpret_cast<uint4 *>(po + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        }
+                    }
+                    __syncwarp();
+                    ptx::tc_fence_before_sync();
+                }
+                ptx::mbar_arrive_warp(&sh.o_free);
+                if (lane == 0) ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
+                if (next.tiles == 0) return true;
+                base += 2 * n, tile += n;
+                it = next;
+            }
+        };
+        const bool ok = run();
+        if (!ok && lane == 0) fail(cur_b);
+        __syncwarp();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    if (warp == MMA_WARP) ptx::tmem_dealloc(tmem, 512);
+}
+
+// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys, one
+// warp to a row, columns of a lane 4 at a time.  A part of a sequence with a bad page has l = -1: the row is left.
+template <int D> struct Join {
+    float4 acc[(D + 127) / 128];
+    float m = -INFINITY, l = 0.f;
+    bool bad = false;
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int i = 0; i < (D + 127) / 128; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ __forceinline__ void add(const float *ml, const float *o, int lane)
+    {
+        const float2 x = *reinterpret_cast<const float2 *>(ml);
+        if (x.y < 0.f) bad = true;
+        if (x.y == 0.f) return;  // saw nothing
+        const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
+        const float f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
+        m = mn, l = l * f0 + x.y * f1;
+#pragma unroll
+        for (int i = 0; i < (D + 127) / 128; ++i) {
+            const int c = i * 128 + lane * 4;
+            if (c < D) {
+                const float4 y = *reinterpret_cast<const float4 *>(o + c);
+                acc[i].x = acc[i].x * f0 + y.x * f1, acc[i].y = acc[i].y * f0 + y.y * f1;
+                acc[i].z = acc[i].z * f0 + y.z * f1, acc[i].w = acc[i].w * f0 + y.w * f1;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *out, int lane)
+    {
+        if (bad) return;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int i = 0; i < (D + 127) / 128; ++i) {
+            const int c = i * 128 + lane * 4;
+            if (c < D) *reinterpret_cast<uint2 *>(out + c) = make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+        }
+    }
+};
+
+constexpr int JOIN_WARPS = 8;
+
+// Items that a part cut: grid (CTAs of the main kernel, rows of a tile / 8).
+template <int D>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_cut_kernel(AttnArgs a, int R, Ws ws)
+{
+    const int lane = threadIdx.x & 31, row = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    const int *d = ws.desc + 8 * blockIdx.x;
+    const int pieces = d[0];
+    if (pieces == 0 || row >= d[5]) return;
+    const int member = blockIdx.x % R;
+    Join<D> jn;
+    jn.start();
+    for (int p = 0; p < pieces; ++p) {
+        const long long slot = p == 0 ? d[1] : 2 * (d[6] + p), at = (slot * R + member) * ws.row_cap + row;
+        jn.add(ws.slot_ml + 2 * at, ws.slot_o + at * D, lane);
+    }
+    const int rr = d[4] + row, node = rr / a.G;
+    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d[2] + node) * a.H_q + d[3] * a.G + rr - node * a.G) * D, lane);
+}
+
+// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: one warp to a row.
+template <int D>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(AttnArgs a, int R, Ws ws)
+{
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    if (row >= (long long)a.T * a.H_q) return;
+    const int t = (int)(row / a.H_q), hq = (int)(row - (long long)t * a.H_q), h = hq / a.G, g = hq - h * a.G;
+    int b = 0, hi = a.B;
+    while (hi - b > 1) {
+        const int mid = (b + hi) >> 1;
+        if (a.node_offsets[mid] <= t) b = mid;
+        else hi = mid;
+    }
+    int st;
+    const Seq s = load_seq(a, b, R, &st);
+    if (st || t < s.lo || t >= s.lo + s.n) return;
+    const long long W = ws.prefix[a.B];
+    const int parts = (int)ws.prefix[a.B + 1];
+    Join<D> jn;
+    jn.start();
+    auto add = [&](const Seq &q, long long first, long long r, int pass) {
+        const int tile = (int)(r / MT), in_tile = (int)(r - (long long)tile * MT), rg = tile / R, member = tile - rg * R;
+        const long long begin = first + ((long long)h * q.groups + rg) * q.kts, end = begin + q.kts;
+        const int g0 = part_of(begin, W, parts), g1 = part_of(end - 1, W, parts);
+        if (g0 == g1) {
+            const long long at = pass * (long long)a.T * a.H_q + row;
+            jn.add(ws.row_ml + 2 * at, ws.row_o + at * D, lane);
+            return;
+        }
+        for (int p = g0; p <= g1; ++p) {
+            const long long slot = p > g0 || part_begin(p, W, parts) == begin ? 2 * p : 2 * p + 1;
+            const long long at = (slot * R + member) * ws.row_cap + in_tile;
+            jn.add(ws.slot_ml + 2 * at, ws.slot_o + at * D, lane);
+        }
+    };
+    int st0;
+    add(load_seq(a, -1, R, &st0), 0, (long long)t * a.G + g, 0);
+    const bool bad_shared = jn.bad;
+    add(s, ws.prefix[b], (long long)(t - s.lo) * a.G + g, 1);
+    if (bad_shared && lane == 0 && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
+    jn.store(static_cast<__nv_bfloat16 *>(a.O) + row * D, lane);
+}
+
+struct Plan {
+    int R, row_cap, ctas;
+    size_t prefix, desc, slots, rows;  // elements
+};
+Plan plan_of(const AttnArgs &a, int ctas)
+{
+    Plan p;
+    const long long rows = (long long)a.max_nodes * a.G, tiles = (rows + MT - 1) / MT;
+    p.R = (int)(tiles < 1 ? 1 : tiles > 4 ? 4 : tiles);
+    p.ctas = ctas;
+    p.row_cap = a.shared_len > 0 || rows > MT ? MT : (int)rows;
+    p.prefix = a.B + 2 + (a.B & 1);    // (keeps what follows 16-byte aligned)
+    p.desc = 8 * MAX_CTAS;
+    p.slots = 2ull * ctas * p.row_cap;
+    p.rows = a.shared_len > 0 ? 2ull * a.T * a.H_q : 0;
+    return p;
+}
+
+template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
+{
+    using C = Cfg<D>;
+    int dev = 0, sms = 0;
+    cudaError_t e = current_device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    const Plan p = plan_of(a, MAX_CTAS);
+    const int ctas = (sms < MAX_CTAS ? sms : MAX_CTAS) / p.R * p.R;
+    Ws ws;
+    unsigned char *at = reinterpret_cast<unsigned char *>(a.ws);
+    ws.prefix = reinterpret_cast<long long *>(at), at += p.prefix * 8;
+    ws.desc = reinterpret_cast<int *>(at), at += p.desc * 4;
+    ws.slot_o = reinterpret_cast<float *>(at), at += p.slots * D * 4;
+    ws.row_o = reinterpret_cast<float *>(at), at += p.rows * D * 4;
+    ws.slot_ml = reinterpret_cast<float *>(at), at += p.slots * 8;
+    ws.row_ml = reinterpret_cast<float *>(at);
+    ws.row_cap = p.row_cap;
+
+    EncodeTiledFn enc = tma_encode_fn();
+    if (!enc) return cudaErrorNotSupported;
+    CUtensorMap kc, vc, k, v;
+    const CacheView &c = a.c;
+    auto cache_map = [&](CUtensorMap *m, const void *base) {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)c.page_size, (cuuint64_t)c.H_kv, (cuuint64_t)c.n_pages};
+        // (the stride of a dimension of one does not count, but has to be a legal one)
+        const cuuint64_t strides[3] = {(cuuint64_t)c.stride_slot * 2, c.H_kv > 1 ? (cuuint64_t)c.stride_head * 2 : 16,
+                                       c.n_pages > 1 ? (cuuint64_t)c.stride_page * 2 : 16};
+        const cuuint32_t box[4] = {64, (cuuint32_t)(c.page_size < KT ? c.page_size : KT), 1, 1}, es[4] = {1, 1, 1, 1};
+        return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    const uint64_t cols = (uint64_t)c.H_kv * D;
+    if (!cache_map(&kc, c.k) || !cache_map(&vc, c.v) ||
+        !tma_make_map_bf16(enc, &k, a.k, cols, a.T, a.ld_k * 2, 64, 8, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !tma_make_map_bf16(enc, &v, a.v, cols, a.T, a.ld_v * 2, 64, 8, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    const int smem = C::NST * C::STAGE + 1024;
+    e = ensure_dynamic_smem(reinterpret_cast<const void *>(attn_tc_kernel<D>), smem, dev);
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, kc, vc, k, v);
+    if (e != cudaSuccess) return e;
+    if (a.shared_len > 0) {
+        const long long blocks = ((long long)a.T * a.H_q + JOIN_WARPS - 1) / JOIN_WARPS;
+        return launch_dependent(attn_join_shared_kernel<D>, dim3((unsigned)blocks), dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
+    }
+    return launch_dependent(attn_join_cut_kernel<D>, dim3(ctas, (p.row_cap + JOIN_WARPS - 1) / JOIN_WARPS), dim3(JOIN_WARPS * 32), 0,
+                            stream, a, p.R, ws);
+}
+
+}  // namespace
+
+bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io)
+{
+    const CacheView &c = a.c;
+    const bool pow2 = (c.page_size & (c.page_size - 1)) == 0;
+    // 8-row groups of the swizzle have to stay whole within a page; the tensor maps want a pool that exists and real strides
+    return io == TREEWY_BF16 && (c.d == 64 || c.d == 128 || c.d == 256) && pow2 && c.page_size >= 8 && c.n_pages > 0 &&
+           c.max_pages > 0 && c.stride_slot > 0 && (c.H_kv == 1 || c.stride_head > 0) && (c.n_pages == 1 || c.stride_page > 0) &&
+           (long long)a.T * a.H_q <= 0x7fffffffll;
+}
+
+size_t attn_tc_workspace(const AttnArgs &a)
+{
+    const Plan p = plan_of(a, MAX_CTAS);
+    return p.prefix * 8 + p.desc * 4 + (p.slots + p.rows) * (a.c.d + 2) * 4;
+}
+
+cudaError_t launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
+{
+    if (a.c.d == 256) return launch_d<256>(a, stream);
+    if (a.c.d == 128) return launch_d<128>(a, stream);
+    return launch_d<64>(a, stream);
+}
+
+}  // namespace treewy
