@@ -56,6 +56,7 @@ struct AttnArgs {
     const int32_t *shared_pages;
     int shared_len;
     float scale;
+    int log_page;           // page_size = 1 << log_page (tensor-core kernel only)
     int B, T, max_nodes, H_q, G;  // G = H_q / H_kv query heads to a key/value head
     float *ws;
     int32_t *seq_status;

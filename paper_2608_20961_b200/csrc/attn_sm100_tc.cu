@@ -20,7 +20,8 @@
 // so that the second one reads the keys out of L2.
 //
 // Roles: two softmax warpgroups that take turns at the key tiles (the maxima travel between them, row by row),
-// one warp that walks the work and issues the TMA copies, one that issues the MMAs.
+// one thread that walks the work and copies K tiles, one that copies V tiles, one each for the MMAs of
+// S = Q K^T and O += P V (a single one for both was the slowest role: its waits alone took as long as a tile).
 #include "attn_common.cuh"
 #include "ptx_sm100.cuh"
 #include "tma_host.cuh"
@@ -31,7 +32,7 @@ namespace {
 constexpr int KT = 64;                 // keys of a tile
 constexpr int MT = 128;                // rows of a tile
 constexpr int MAX_CTAS = 160;
-constexpr int THREADS = 320, PRODUCER_WARP = 8, MMA_WARP = 9;
+constexpr int THREADS = 384, PRODUCER_K = 8, PRODUCER_V = 9, MMA_QK = 10, MMA_PV = 11;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
 constexpr int MIN_TILES = 2;           // of a CTA's part: below this a part is mostly start and end
 constexpr float LAZY = 8.f;
@@ -142,7 +143,7 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
         for (int i = 0; i < C::NSB; ++i)
             ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
         ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
-        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 9);
+        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.hand[0][i], 1), ptx::mbar_init(&sh.hand[1][i], 1), ptx::mbar_init(&sh.exch[i], 2);
         ptx::fence_barrier_init();
         sh.total_fail = 0;
@@ -151,7 +152,7 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
     }
     if (tid < 16) sh.bad_item[tid] = 0;
     if (tid < 8) sh.nonfinite[tid >> 1][tid & 1] = 0;
-    if (warp == MMA_WARP) {
+    if (warp == MMA_QK) {
         ptx::tmem_alloc(&sh.tmem, 512);
         ptx::tmem_relinquish();
     }
@@ -224,121 +225,129 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
         if (a.seq_status && a.B > 0) atomicOr(&a.seq_status[b < 0 ? 0 : b], TREEWY_SEQ_TIMEOUT);
     };
 
-    if (warp == PRODUCER_WARP) {
-        // ---------------------------------------------------------------- work items and TMA copies
-        unsigned stage = 0;      // copies issued (stages filled) so far
-        auto produce = [&]() -> int {
-            int b = sh.first_b;
-            long long off = sh.first_off, u = u0;
-            unsigned ord = 0;    // items published so far
-            int item_b = -1;
-            Seq s;
-            s.units = 0;
-            if (u < u1) s = load_seq(a, b, R, &st);
-            while (u < u1) {
-                while (off >= s.units) {  // the next sequence that has work
-                    off = 0, ++b;
-                    s = load_seq(a, b, R, &st);
+    if (warp == PRODUCER_K || warp == PRODUCER_V) {
+        // ---------------------------------------------------------------- work items and TMA copies: one thread each
+        if (ptx::elect_one()) {
+            const bool is_v = warp == PRODUCER_V;
+            const int ps = 1 << a.log_page, box = min(ps, KT), per_tile = KT / box;
+            unsigned base = 0;   // stages of the items before
+            long long newest = -1;  // last stage whose copies were issued
+            int cur_b = -1;
+            // the copies of one item's K tiles or V tiles
+            auto copy_item = [&](const Item &it, unsigned ord) -> bool {
+                const int *table = it.b < 0 ? a.shared_pages : a.c.page_table + (size_t)it.b * a.c.max_pages;
+                const int key0 = it.b < 0 ? 0 : a.shared_len, n = it.tiles;
+                const CUtensorMap *cache = is_v ? &map_vc : &map_kc, *rows = is_v ? &map_v : &map_k;
+                int pages[KT / 8];
+                auto load_pages = [&](int j) {
+                    const int kt = it.kt0 + j;
+                    if (j >= n || (it.b >= 0 && kt == it.kts - 1)) return;
+                    const int first = (key0 + kt * KT) >> a.log_page, end = (it.len + ps - 1) >> a.log_page;
+#pragma unroll
+                    for (int i = 0; i < KT / 8; ++i) pages[i] = i < per_tile && first + i < end ? table[first + i] : -1;
+                };
+                load_pages(0);
+                bool bad = false;
+                for (int j = 0; j < n; ++j) {
+                    const unsigned st_ = base + (is_v ? v_pos(j, n) : k_pos(j)), sidx = st_ % C::NST;
+                    const int kt = it.kt0 + j, token = key0 + kt * KT;
+                    if (st_ >= C::NST && !ptx::mbar_wait(&sh.kv_empty[sidx], (st_ / C::NST - 1) & 1)) return false;
+                    unsigned char *dst = stages + sidx * C::STAGE;
+                    newest = st_;
+                    if (it.b >= 0 && kt == it.kts - 1) {
+                        const int boxes = (it.n + 7) / 8;
+                        ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], boxes * C::NC * 1024u);
+                        for (int i = 0; i < boxes; ++i)
+#pragma unroll
+                            for (int c = 0; c < C::NC; ++c)
+                                ptx::tma_load_2d(dst + c * C::CHUNK + i * 1024, rows, it.h * D + c * 64, it.lo + i * 8, &sh.kv_full[sidx]);
+                    } else {
+                        const int boxes = min(per_tile, (it.len - token + box - 1) / box);
+#pragma unroll
+                        for (int i = 0; i < KT / 8; ++i)  // (one past the pool reads as zeros)
+                            if (i < boxes && (pages[i] < 0 || pages[i] >= a.c.n_pages)) pages[i] = a.c.n_pages, bad = true;
+                        if (bad && !is_v) sh.bad_item[ord % 16] = ord + 1;
+                        ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], boxes * C::NC * box * 128u);
+#pragma unroll
+                        for (int i = 0; i < KT / 8; ++i) {
+                            if (i >= boxes) break;
+#pragma unroll
+                            for (int c = 0; c < C::NC; ++c)
+                                ptx::tma_load_4d(dst + c * C::CHUNK + i * box * 128, cache, c * 64, token & (ps - 1), it.h, pages[i],
+                                                 &sh.kv_full[sidx]);
+                        }
+                    }
+                    load_pages(j + 1);
                 }
-                const long long it = off / s.kts;
-                const int kt0 = (int)(off - it * s.kts), h = (int)(it / s.groups), rg = (int)(it % s.groups);
-                const int tiles = (int)min((long long)(s.kts - kt0), u1 - u);
-                const long long begin = u - kt0, end = begin + s.kts;
-                const int row0 = (rg * R + member) * MT;
-                const long long rows = b < 0 ? (long long)a.T * a.G : (long long)s.n * a.G;
-                off += tiles, u += tiles;
-                if (row0 >= rows) continue;  // no row tile of this item for this member of the group
-                const unsigned r = ord % ITEMS;
-                item_b = b;
-                if (ord >= ITEMS && !wait_warp(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return item_b;
-                if (lane == 0) {
-                    Item &x = sh.items[r];
+                base += 2 * n;
+                return true;
+            };
+            auto produce_k = [&]() -> int {  // 0: all done, 1: a wait ran out, 2: stopped on purpose
+                int b = sh.first_b, st2;
+                long long off = sh.first_off, u = u0;
+                unsigned ord = 0;    // items published so far
+                Seq s;
+                s.units = 0;
+                if (u < u1) s = load_seq(a, b, R, &st2);
+                while (u < u1) {
+                    while (off >= s.units) {  // the next sequence that has work
+                        off = 0, ++b;
+                        s = load_seq(a, b, R, &st2);
+                    }
+                    const long long i_ = off / s.kts;
+                    const int kt0 = (int)(off - i_ * s.kts), h = (int)(i_ / s.groups), rg = (int)(i_ % s.groups);
+                    const int tiles = (int)min((long long)(s.kts - kt0), u1 - u);
+                    const long long begin = u - kt0, end = begin + s.kts;
+                    const int row0 = (rg * R + member) * MT;
+                    const long long rows = b < 0 ? (long long)a.T * a.G : (long long)s.n * a.G;
+                    off += tiles, u += tiles;
+                    if (row0 >= rows) continue;  // no row tile of this item for this member of the group
+                    const unsigned r = ord % ITEMS;
+                    cur_b = b;
+                    if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
+                    Item x;
                     x.b = b, x.h = h, x.lo = s.lo, x.n = s.n, x.len = s.len;
                     x.row0 = row0, x.rows = (int)min((long long)MT, rows - row0);
                     x.kt0 = kt0, x.tiles = tiles, x.kts = s.kts;
                     x.slot = begin >= u0 && end <= u1 ? -1 : begin <= u0 ? 2 * group : 2 * group + 1;
+                    sh.items[r] = x;
                     ptx::mbar_arrive(&sh.item_full[r]);
+                    if (b >= 0 && b * a.c.H_kv + h == a.skip_item) return 2;  // (test hook)
+                    if (!copy_item(x, ord)) return 1;
+                    ++ord;
                 }
-                __syncwarp();
-                const bool withheld = b >= 0 && b * a.c.H_kv + h == a.skip_item;
-
-                // pages of a tile, one copy to a lane: (page of the tile, chunk)
-                const int ps = a.c.page_size, box = min(ps, KT), per_tile = KT / box;
-                const int pi = lane / C::NC, ch = lane % C::NC;
-                const int *table = b < 0 ? a.shared_pages : a.c.page_table + (size_t)b * a.c.max_pages;
-                const int key0 = b < 0 ? 0 : a.shared_len;
-                auto page_for = [&](int kt) -> int {  // -2: this lane has no copy in the tile
-                    if (kt >= kt0 + tiles || (b >= 0 && kt == s.kts - 1)) return -2;
-                    const int token = key0 + kt * KT + pi * box;
-                    if (pi >= per_tile || token >= s.len) return -2;
-                    return table[token / ps];
-                };
-                auto fill = [&](bool is_v, int kt, int page) -> bool {
-                    const unsigned sidx = stage % C::NST;
-                    if (stage >= C::NST && !wait_warp(&sh.kv_empty[sidx], (stage / C::NST - 1) & 1)) return false;
-                    unsigned char *dst = stages + sidx * C::STAGE + ch * C::CHUNK;
-                    const bool draft = b >= 0 && kt == s.kts - 1;
-                    const int rows_box = draft ? 8 : box;
-                    const bool mine = draft ? pi * 8 < s.n : page != -2;
-                    const unsigned copies = __popc(__ballot_sync(0xffffffffu, mine));
-                    if (lane == 0) ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], copies * rows_box * 128u);
-                    __syncwarp();
-                    if (mine) {
-                        if (draft) {
-                            ptx::tma_load_2d(dst + pi * 8 * 128, is_v ? &map_v : &map_k, h * D + ch * 64, s.lo + pi * 8, &sh.kv_full[sidx]);
-                        } else {
-                            const int token = key0 + kt * KT + pi * box;
-                            // (a page out of range reads as the one past the pool: zeros)
-                            ptx::tma_load_4d(dst + pi * box * 128, is_v ? &map_vc : &map_kc, ch * 64, token % ps, h,
-                                             page < 0 || page >= a.c.n_pages ? a.c.n_pages : page, &sh.kv_full[sidx]);
-                        }
-                    }
-                    ++stage;
-                    return true;
-                };
-                if (withheld) return -4;
-                {
-                    int prev = -2, cur = page_for(kt0), next;
-                    bool bad = false;
-                    for (int j = 0; j <= tiles; ++j) {
-                        next = page_for(kt0 + j + 1);
-                        if (j < tiles) {
-                            const bool out = cur != -2 && (cur < 0 || cur >= a.c.n_pages);
-                            if (__any_sync(0xffffffffu, out) && !bad) {
-                                bad = true;
-                                if (lane == 0) sh.bad_item[ord % 16] = ord + 1;
-                                __syncwarp();
-                            }
-                            if (!fill(false, kt0 + j, cur)) return item_b;
-                        }
-                        if (j > 0 && !fill(true, kt0 + j - 1, prev)) return item_b;
-                        prev = cur, cur = next;
-                    }
-                }
-                ++ord;
-            }
-            const unsigned r = ord % ITEMS;  // the end
-            if (ord >= ITEMS && !wait_warp(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return item_b;
-            if (lane == 0) {
+                const unsigned r = ord % ITEMS;  // the end
+                if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
                 sh.items[r].tiles = 0;
                 ptx::mbar_arrive(&sh.item_full[r]);
-            }
-            return -3;
-        };
-        const int rc = produce();
-        if (rc > -3 && lane == 0) fail(rc);
-        __syncwarp();
-        if (rc != -3) {  // copies in flight have to land before the CTA may leave
-            const unsigned have = stage < C::NST ? stage : C::NST;
-            for (unsigned i = stage - have; i != stage; ++i)
-                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.kv_full[i % C::NST], (i / C::NST) & 1); ++t) __nanosleep(20);
+                return 0;
+            };
+            auto produce_v = [&]() -> int {
+                for (unsigned ord = 0;; ++ord) {
+                    const unsigned r = ord % ITEMS;
+                    if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return 1;
+                    const Item it = sh.items[r];
+                    if (it.tiles == 0) return 0;
+                    ptx::mbar_arrive(&sh.item_empty[r]);
+                    cur_b = it.b;
+                    if (it.b >= 0 && it.b * a.c.H_kv + it.h == a.skip_item) return 2;
+                    if (!copy_item(it, ord)) return 1;
+                }
+            };
+            const int rc = is_v ? produce_v() : produce_k();
+            if (rc == 1) fail(cur_b);
+            if (rc != 0)  // copies in flight have to land before the CTA may leave
+                for (long long i = max(0ll, newest - (C::NST - 1)); i <= newest; ++i)
+                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.kv_full[i % C::NST], (unsigned)(i / C::NST) & 1); ++t) __nanosleep(20);
         }
-    } else if (warp == MMA_WARP) {
-        // ---------------------------------------------------------------- MMAs, one thread
-        if (lane == 0) {
+        __syncwarp();
+    } else if (warp == MMA_QK || warp == MMA_PV) {
+        // ---------------------------------------------------------------- MMAs: one thread for Q K^T, one for P V
+        if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
             int cur_b = -1;
-            unsigned commits = 0;
+            uint64_t *newest = nullptr;  // barrier of the last commit, and its phase
+            unsigned newest_phase = 0;
             auto run = [&]() -> bool {
                 unsigned base = 0, tile = 0;  // stages and tiles of the items before
                 for (unsigned ord = 0;; ++ord) {
@@ -348,48 +357,49 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                     if (it.tiles == 0) return true;
                     cur_b = it.b;
                     ptx::mbar_arrive(&sh.item_empty[r]);
-                    if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                     const int n = it.tiles;
-                    auto qk = [&](int j) -> bool {
-                        const unsigned st_ = base + k_pos(j), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
-                        if (g >= C::NSB && !ptx::mbar_wait(&sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
-                        if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
-                        ptx::tc_fence_after_sync();
-                        const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+                    if (warp == MMA_QK) {
+                        if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
+                        for (int j = 0; j < n; ++j) {
+                            const unsigned st_ = base + k_pos(j), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
+                            if (g >= C::NSB && !ptx::mbar_wait(&sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
+                            if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                            ptx::tc_fence_after_sync();
+                            const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
 #pragma unroll
-                        for (int s = 0; s < D / 16; ++s)
-                            ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + s * 8,
-                                              ptx::umma_desc_k_sw128(kaddr + (s / 4) * C::CHUNK + (s % 4) * 32), idesc_qk, s > 0);
-                        ptx::umma_commit(&sh.kv_empty[sidx]);
-                        ptx::umma_commit(&sh.s_full[buf]);
-                        return true;
-                    };
-                    if (!qk(0)) return false;
-                    if (n > 1 && !qk(1)) return false;
-                    for (int j = 0; j < n; ++j) {
-                        const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
-                        if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
-                        if (j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free, (ord - 1) & 1)) return false;
-                        if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
-                        ptx::tc_fence_after_sync();
-                        const uint32_t vaddr = ptx::smem_u32(stages + sidx * C::STAGE);
-                        const int steps = (valid_keys(a, it, it.kt0 + j) + 15) / 16;
-                        for (int s = 0; s < steps; ++s)
-                            ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8, ptx::umma_desc_mn_sw128(vaddr + s * 2048, C::CHUNK),
-                                              idesc_pv, j > 0 || s > 0);
-                        ptx::umma_commit(&sh.kv_empty[sidx]);
-                        ptx::umma_commit(&sh.pv_done[buf]);
-                        commits = g + 1;
-                        if (j + 2 < n && !qk(j + 2)) return false;
+                            for (int s = 0; s < D / 16; ++s)
+                                ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + s * 8,
+                                                  ptx::umma_desc_k_sw128(kaddr + (s / 4) * C::CHUNK + (s % 4) * 32), idesc_qk, s > 0);
+                            ptx::umma_commit(&sh.s_full[buf]);
+                            ptx::umma_commit(&sh.kv_empty[sidx]);
+                            newest = &sh.s_full[buf], newest_phase = (g / C::NSB) & 1;
+                        }
+                    } else {
+                        for (int j = 0; j < n; ++j) {
+                            const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
+                            if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                            if (j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free, (ord - 1) & 1)) return false;
+                            if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
+                            ptx::tc_fence_after_sync();
+                            const uint32_t vaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+                            const int steps = (valid_keys(a, it, it.kt0 + j) + 15) / 16;
+#pragma unroll
+                            for (int s = 0; s < KT / 16; ++s)
+                                if (s < steps)
+                                    ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8,
+                                                      ptx::umma_desc_mn_sw128(vaddr + s * 2048, C::CHUNK), idesc_pv, j > 0 || s > 0);
+                            ptx::umma_commit(&sh.pv_done[buf]);
+                            ptx::umma_commit(&sh.kv_empty[sidx]);
+                            newest = &sh.pv_done[buf], newest_phase = (g / C::NSB) & 1;
+                        }
                     }
                     base += 2 * n, tile += n;
                 }
             };
             if (!run()) {
                 fail(cur_b);
-                if (commits > 0)
-                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.pv_done[(commits - 1) % C::NSB], ((commits - 1) / C::NSB) & 1); ++t)
-                        __nanosleep(20);
+                if (newest)  // MMAs in flight have to end before the CTA may leave
+                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(newest, newest_phase); ++t) __nanosleep(20);
             }
         }
         __syncwarp();
@@ -635,7 +645,7 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
-    if (warp == MMA_WARP) ptx::tmem_dealloc(tmem, 512);
+    if (warp == MMA_QK) ptx::tmem_dealloc(tmem, 512);
 }
 
 // The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys, one
@@ -783,6 +793,8 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     ws.slot_ml = reinterpret_cast<float *>(at), at += p.slots * 8;
     ws.row_ml = reinterpret_cast<float *>(at);
     ws.row_cap = p.row_cap;
+    a.log_page = 0;
+    while ((1 << a.log_page) < a.c.page_size) ++a.log_page;
 
     EncodeTiledFn enc = tma_encode_fn();
     if (!enc) return cudaErrorNotSupported;

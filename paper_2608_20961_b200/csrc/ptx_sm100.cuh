@@ -409,6 +409,18 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32_bmn(int M, int N)
 {
     return umma_idesc_bf16_f32(M, N) | (1u << 16);
 }
+// One thread of a converged warp, chosen by the hardware: the compiler then knows that a tcgen05 or TMA
+// instruction behind it is issued once, and takes its operands straight from uniform registers.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
