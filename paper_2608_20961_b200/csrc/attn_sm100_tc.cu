@@ -34,7 +34,8 @@ constexpr int MT = 128;                // rows of a tile
 constexpr int MAX_CTAS = 160;
 constexpr int THREADS = 384, PRODUCER_K = 8, PRODUCER_V = 9, MMA_QK = 10, MMA_PV = 11;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
-constexpr int MIN_TILES = 2;           // of a CTA's part: below this a part is mostly start and end
+constexpr int MIN_UNITS = 2;           // of a CTA's part: below this a part is mostly start and end
+constexpr int OV = 3;                  // what starting an item costs, in tiles
 constexpr float LAZY = 8.f;
 
 template <int D> struct Cfg {
@@ -43,7 +44,8 @@ template <int D> struct Cfg {
     static constexpr int STAGE = NC * CHUNK;
     static constexpr int NST = D == 256 ? 6 : D == 128 ? 12 : 16;  // about 192 KB in flight
     static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
-    static constexpr int TM_Q = D, TM_S = D + D / 2;
+    static constexpr int NQ = D == 256 ? 1 : 2;                    // Q buffers
+    static constexpr int TM_Q = D, TM_S = D + NQ * (D / 2);
 };
 
 struct Item {
@@ -78,10 +80,11 @@ __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + KT - 1) /
 
 struct Seq {
     int lo, n, len, kts, row_tiles, groups;
-    long long units;
+    unsigned units;             // H_kv * groups * (OV + kts), below 2^31 (the launcher has checked)
 };
-// b = -1: the shared prompt, whose rows are those of all sequences
-__device__ __forceinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status)
+// b = -1: the shared prompt, whose rows are those of all sequences.  (What is not called once a tile is kept out of line:
+// the roles run at the same time and share the instruction cache.)
+static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status)
 {
     Seq s;
     *status = 0;
@@ -99,13 +102,22 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *st
         s.row_tiles = (s.n * a.G + MT - 1) / MT;
     }
     s.groups = (s.row_tiles + R - 1) / R;
-    s.units = (long long)a.c.H_kv * s.groups * s.kts;
+    s.units = (unsigned)a.c.H_kv * s.groups * (OV + s.kts);
     return s;
 }
 
-// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.
-__device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return g * W / parts; }
-__device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)(((unit + 1) * parts - 1) / W); }
+// (a 64-bit division takes several times as long as a 32-bit one, and nearly every line of work is short)
+static __device__ __noinline__ long long div64(long long x, long long y)
+{
+    return ((x | y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
+}
+// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  An item takes OV + kts
+// units, tile t the (OV + t)-th of them.
+__device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return div64(g * W, parts); }
+__device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)div64((unit + 1) * parts - 1, W); }
+// Slot of part g's piece of the item that begins at `begin`: a part cuts at most two items, the one its own start
+// falls into and one more.
+__device__ __forceinline__ int slot_of(int g, long long begin, long long u0) { return begin <= u0 ? 2 * g : 2 * g + 1; }
 
 // keys of tile kt that exist
 __device__ __forceinline__ int valid_keys(const AttnArgs &a, const Item &it, int kt)
@@ -127,7 +139,7 @@ __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity)
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
-attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
+attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using C = Cfg<D>;
@@ -139,6 +151,7 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
 
     if (tid == 0) {
         ptx::wait_deadline_init(a.wait_cycles);
+#pragma unroll 1
         for (int i = 0; i < C::NST; ++i) ptx::mbar_init(&sh.kv_full[i], 1), ptx::mbar_init(&sh.kv_empty[i], 1);
         for (int i = 0; i < C::NSB; ++i)
             ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
@@ -161,11 +174,14 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
 
     // ---- the line of work and this CTA's part of it
     int st;
-    const long long shared_units = a.shared_len > 0 ? load_seq(a, -1, R, &st).units : 0;
+    const long long shared_units = a.shared_len > 0 ? (long long)load_seq(a, -1, R, &st).units : 0;
     const int chunk = (a.B + THREADS - 1) / THREADS, b_begin = min(a.B, tid * chunk), b_end = min(a.B, b_begin + chunk);
     long long sum = 0;
+    unsigned only = 0;           // a thread's one sequence is not read again
+#pragma unroll 1
     for (int b = b_begin; b < b_end; ++b) {
-        sum += load_seq(a, b, R, &st).units;
+        only = load_seq(a, b, R, &st).units;
+        sum += only;
         if (st && blockIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[b], st);
     }
     long long incl = sum;
@@ -185,11 +201,12 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
         W += sh.scan[i];
     }
     before += incl - sum;
-    const int parts = (int)max(1ll, min((long long)n_groups, W / MIN_TILES));
+    const int parts = (int)max(1ll, min((long long)n_groups, W / MIN_UNITS));
     const long long u0 = group < parts && W > 0 ? part_begin(group, W, parts) : 0;
     const long long u1 = group < parts && W > 0 ? part_begin(group + 1, W, parts) : 0;
+#pragma unroll 1
     for (int b = b_begin; b < b_end; ++b) {
-        const long long units = load_seq(a, b, R, &st).units;
+        const long long units = chunk == 1 ? only : load_seq(a, b, R, &st).units;
         if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[b] = before;
         if (u1 > u0) {
             if (u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before;
@@ -208,11 +225,12 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
         int pieces = 0;
         if (u1 > u0) {
             const Seq s = load_seq(a, sh.last_b, R, &st);
-            const long long it = sh.last_off / s.kts, begin = u1 - 1 - (sh.last_off - it * s.kts), end = begin + s.kts;
+            const unsigned last = (unsigned)sh.last_off, per = s.kts + OV, it = last / per;
+            const long long begin = u1 - 1 - (last - it * per), first = begin + OV;
             const int row0 = ((int)(it % s.groups) * R + member) * MT;
-            if (begin >= u0 && end > u1 && row0 < s.n * a.G) {
-                pieces = part_of(end - 1, W, parts) - group + 1;
-                d[1] = begin == u0 ? 2 * group : 2 * group + 1;
+            if (first >= u0 && first < u1 && first + s.kts > u1 && row0 < s.n * a.G) {
+                pieces = part_of(first + s.kts - 1, W, parts) - group + 1;
+                d[1] = slot_of(group, begin, u0);
                 d[2] = s.lo, d[3] = (int)(it / s.groups), d[4] = row0, d[5] = min(MT, s.n * a.G - row0), d[6] = group;
             }
         }
@@ -282,59 +300,53 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                 base += 2 * n;
                 return true;
             };
-            auto produce_k = [&]() -> int {  // 0: all done, 1: a wait ran out, 2: stopped on purpose
+            auto run = [&]() -> int {  // 0: all done, 1: a wait ran out, 2: stopped on purpose
                 int b = sh.first_b, st2;
-                long long off = sh.first_off, u = u0;
-                unsigned ord = 0;    // items published so far
+                unsigned off = (unsigned)sh.first_off;
+                long long u = u0;
                 Seq s;
                 s.units = 0;
-                if (u < u1) s = load_seq(a, b, R, &st2);
-                while (u < u1) {
-                    while (off >= s.units) {  // the next sequence that has work
-                        off = 0, ++b;
-                        s = load_seq(a, b, R, &st2);
-                    }
-                    const long long i_ = off / s.kts;
-                    const int kt0 = (int)(off - i_ * s.kts), h = (int)(i_ / s.groups), rg = (int)(i_ % s.groups);
-                    const int tiles = (int)min((long long)(s.kts - kt0), u1 - u);
-                    const long long begin = u - kt0, end = begin + s.kts;
-                    const int row0 = (rg * R + member) * MT;
-                    const long long rows = b < 0 ? (long long)a.T * a.G : (long long)s.n * a.G;
-                    off += tiles, u += tiles;
-                    if (row0 >= rows) continue;  // no row tile of this item for this member of the group
-                    const unsigned r = ord % ITEMS;
-                    cur_b = b;
-                    if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
-                    Item x;
-                    x.b = b, x.h = h, x.lo = s.lo, x.n = s.n, x.len = s.len;
-                    x.row0 = row0, x.rows = (int)min((long long)MT, rows - row0);
-                    x.kt0 = kt0, x.tiles = tiles, x.kts = s.kts;
-                    x.slot = begin >= u0 && end <= u1 ? -1 : begin <= u0 ? 2 * group : 2 * group + 1;
-                    sh.items[r] = x;
-                    ptx::mbar_arrive(&sh.item_full[r]);
-                    if (b >= 0 && b * a.c.H_kv + h == a.skip_item) return 2;  // (test hook)
-                    if (!copy_item(x, ord)) return 1;
-                    ++ord;
-                }
-                const unsigned r = ord % ITEMS;  // the end
-                if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
-                sh.items[r].tiles = 0;
-                ptx::mbar_arrive(&sh.item_full[r]);
-                return 0;
-            };
-            auto produce_v = [&]() -> int {
+                bool fresh = true;
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
-                    if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return 1;
-                    const Item it = sh.items[r];
-                    if (it.tiles == 0) return 0;
-                    ptx::mbar_arrive(&sh.item_empty[r]);
-                    cur_b = it.b;
-                    if (it.b >= 0 && it.b * a.c.H_kv + it.h == a.skip_item) return 2;
-                    if (!copy_item(it, ord)) return 1;
+                    Item x;
+                    if (!is_v) {
+                        // the next item that has tiles here and rows for this member of the group; 0 tiles: the end
+                        x.tiles = 0;
+                        while (u < u1 && x.tiles == 0) {
+                            if (fresh || off >= s.units) {  // (a sequence without work has no units)
+                                if (!fresh) off = 0, ++b;
+                                fresh = false;
+                                s = load_seq(a, b, R, &st2);
+                                continue;
+                            }
+                            const unsigned per = s.kts + OV, i_ = off / per, o = off - i_ * per, h = i_ / s.groups, rg = i_ - h * s.groups;
+                            const int span = (int)min((long long)(per - o), u1 - u);
+                            const int kt0 = max(0, (int)o - OV), kt1 = max(0, (int)o + span - OV);
+                            const long long begin = u - o;
+                            const long long row0 = (long long)(rg * R + member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
+                            off += span, u += span;
+                            if (row0 >= rows) continue;
+                            x.b = b, x.h = h, x.lo = s.lo, x.n = s.n, x.len = s.len;
+                            x.row0 = (int)row0, x.rows = (int)min((long long)MT, rows - row0);
+                            x.kt0 = kt0, x.tiles = kt1 - kt0, x.kts = s.kts;
+                            x.slot = kt0 == 0 && kt1 == s.kts ? -1 : slot_of(group, begin, u0);
+                        }
+                        if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
+                        sh.items[r] = x;
+                        ptx::mbar_arrive(&sh.item_full[r]);
+                    } else {
+                        if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return 1;
+                        x = sh.items[r];
+                        if (x.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
+                    }
+                    if (x.tiles == 0) return 0;
+                    cur_b = x.b;
+                    if (x.b >= 0 && x.b * a.c.H_kv + x.h == a.skip_item) return 2;  // (test hook)
+                    if (!copy_item(x, ord)) return 1;
                 }
             };
-            const int rc = is_v ? produce_v() : produce_k();
+            const int rc = run();
             if (rc == 1) fail(cur_b);
             if (rc != 0)  // copies in flight have to land before the CTA may leave
                 for (long long i = max(0ll, newest - (C::NST - 1)); i <= newest; ++i)
@@ -368,7 +380,7 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                             const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
 #pragma unroll
                             for (int s = 0; s < D / 16; ++s)
-                                ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + s * 8,
+                                ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + (ord % C::NQ) * (D / 2) + s * 8,
                                                   ptx::umma_desc_k_sw128(kaddr + (s / 4) * C::CHUNK + (s % 4) * 32), idesc_qk, s > 0);
                             ptx::umma_commit(&sh.s_full[buf]);
                             ptx::umma_commit(&sh.kv_empty[sidx]);
@@ -408,70 +420,103 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
         const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
         int cur_b = -1;
-        auto load_q = [&](const Item &it) {
-            // this thread's half of its row: D / 2 elements into D / 4 columns
+        // An item and this thread's row of it: its packed row, its query head, the draft rows it sees
+        struct Mine {
+            const Item *it;  // (stays in its slot of the ring until this warp says that it is done)
+            int t, hq;
+            uint64_t tree;
+        };
+        // Takes over item `ord`: finds this thread's row and brings its half of the row's query into tensor memory.
+        auto take = [&](unsigned ord, Mine &x) -> bool {
+            if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
+            const Item &it = sh.items[ord % ITEMS];
+            x.it = &it, x.tree = 0;
+            if (it.tiles == 0) return true;
             if (w4 * 32 < it.rows) {
                 const bool on = row < it.rows;
-                const int rr = it.row0 + (on ? row : 0), node = rr / a.G, g = rr - node * a.G;
-                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + (it.lo + node) * a.ld_q +
-                                                                   (long long)(it.h * a.G + g) * D + wg * (D / 2));
-                uint32_t x[D / 4];
+                const unsigned rr = it.row0 + (on ? row : 0), node = rr / (unsigned)a.G;
+                x.t = it.lo + (int)node, x.hq = it.h * a.G + (int)(rr - node * a.G);
+                const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + x.t * a.ld_q +
+                                                                   (long long)x.hq * D + wg * (D / 2));
+                if (it.b >= 0 && on && it.kt0 + it.tiles == it.kts) x.tree = a.anc_mask[x.t] & low_bits(it.n);
+                const uint32_t dst = tmem + lane_base + C::TM_Q + (ord % C::NQ) * (D / 2) + wg * (D / 4);
+                constexpr int QC = D / 4 < 32 ? D / 4 : 32;  // columns at a time
+#pragma unroll 1
+                for (int c = 0; c < D / 4; c += QC) {
+                    uint32_t q[QC];
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint4 y = on ? src[i] : make_uint4(0, 0, 0, 0);
-                    x[4 * i] = y.x, x[4 * i + 1] = y.y, x[4 * i + 2] = y.z, x[4 * i + 3] = y.w;
+                    for (int i = 0; i < QC / 4; ++i) {
+                        const uint4 y = on ? src[c / 4 + i] : make_uint4(0, 0, 0, 0);
+                        q[4 * i] = y.x, q[4 * i + 1] = y.y, q[4 * i + 2] = y.z, q[4 * i + 3] = y.w;
+                    }
+#pragma unroll
+                    for (int i = 0; i < QC; i += 16) ptx::tmem_st16(dst + c + i, *reinterpret_cast<const uint32_t(*)[16]>(&q[i]));
                 }
-                const uint32_t dst = tmem + lane_base + C::TM_Q + wg * (D / 4);
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i)
-                    ptx::tmem_st16(dst + 16 * i, *reinterpret_cast<const uint32_t(*)[16]>(&x[16 * i]));
                 ptx::tmem_wait_st();
             }
             ptx::tc_fence_before_sync();
             ptx::mbar_arrive_warp(&sh.q_full);
+            return true;
         };
         auto run = [&]() -> bool {
             unsigned base = 0, tile = 0, handed = 0;  // handed: hand-overs of the maxima this warpgroup has received
-            if (!wait_warp(&sh.item_full[0], 0)) return false;
-            Item it = sh.items[0];
-            if (it.tiles == 0) return true;
-            load_q(it);
+            Mine me{&sh.items[0], 0, 0, 0}, next;
             bool have = false;                        // the hand-over before this warpgroup's next tile is in
-            for (unsigned ord = 0;; ++ord) {
-                cur_b = it.b;
-                const int n = it.tiles;
-                const bool warp_on = w4 * 32 < it.rows, on = row < it.rows;
-                uint64_t tree = 0;
-                if (it.b >= 0 && on && it.kt0 + n == it.kts)
-                    tree = a.anc_mask[it.lo + (it.row0 + row) / a.G] & low_bits(it.n);
+            int n = 0;
+            // (the round before the first item only takes that one)
+            for (unsigned ord = ~0u;; ++ord) {
+                const Item &it = *me.it;
+                const bool warp_on = n > 0 && w4 * 32 < it.rows, on = n > 0 && row < it.rows;
+                const unsigned last = tile + n - 1;
+                bool taken = false;                   // the next item
                 float m = -INFINITY, l = 0.f, m_l = -INFINITY;
-                for (int j = 0; j < n; ++j) {
+                for (int j = (int)(tile & 1) == wg ? 0 : 1;; j += 2) {
                     const unsigned g = tile + j, buf = g % C::NSB;
-                    if ((int)(g & 1) != wg) continue;
+                    if (j >= n && n > 0 && (int)(last & 1) != wg) {  // the other warpgroup's last maximum
+                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
+                        ++handed, have = true;
+                        m = sh.m[row];
+                    }
+                    // With two Q buffers the next item's queries come in before this warpgroup's last tile, while it
+                    // would wait for S: the buffer's last reader was the item before this one.  With one, at the end: the
+                    // last Q K^T is done, its S has been read.
+                    if (!taken && (j >= n || (C::NQ == 2 && j + 2 >= n))) {
+                        if (!take(ord + 1, next)) return false;
+                        taken = true;
+                    }
+                    if (j >= n) break;
                     const int kt = it.kt0 + j, valid = valid_keys(a, it, kt);
                     const bool draft = it.b >= 0 && kt == it.kts - 1;
                     if (!wait_warp(&sh.s_full[buf], (g / C::NSB) & 1)) return false;
                     ptx::tc_fence_after_sync();
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
-                    uint32_t raw[2][32];
+                    if (warp_on && (draft || valid < KT)) {
+                        // masked tiles (an item has two at most): minus infinity goes into S itself, so that the step
+                        // below stays one piece of straight code
+                        const uint64_t seen = draft ? me.tree : low_bits(valid);
+#pragma unroll 1
+                        for (int c = 0; c < KT; c += 16) {
+                            const uint32_t bits = (uint32_t)(seen >> c) & 0xffffu;
+                            uint32_t x[16];
+                            ptx::tmem_ld16(ts + c, x);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (!(bits & (1u << i))) x[i] = 0xff800000u;
+                            ptx::tmem_st16(ts + c, x);
+                        }
+                        ptx::tmem_wait_st();
+                    }
+                    uint32_t raw[KT];
                     float top = -INFINITY;
                     if (warp_on) {
-                        ptx::tmem_ld32(ts, raw[0]);
-                        ptx::tmem_ld32(ts + 32, raw[1]);
+                        ptx::tmem_ld32(ts, *reinterpret_cast<uint32_t(*)[32]>(&raw[0]));
+                        ptx::tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&raw[32]));
                         ptx::tmem_wait_ld();
-                        if (draft || valid < KT) {
-                            const uint64_t seen = draft ? tree : low_bits(valid);
+                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                            for (int i = 0; i < KT; ++i)
-                                if (!((seen >> i) & 1)) raw[i >> 5][i & 31] = 0xff800000u;  // -infinity
-                        }
-                        float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            t0 = fmaxf(t0, __uint_as_float(raw[0][i])), t1 = fmaxf(t1, __uint_as_float(raw[0][i + 1]));
-                            t2 = fmaxf(t2, __uint_as_float(raw[1][i])), t3 = fmaxf(t3, __uint_as_float(raw[1][i + 1]));
-                        }
-                        top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * sl2;
+                        for (int i = 0; i < KT; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(raw[i]));
+                        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
                     }
                     if (g > 0 && !have) {
                         if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
@@ -485,23 +530,20 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                     ptx::mbar_arrive_warp(&sh.hand[wg ^ 1][w4]);
                     if (warp_on) {
                         const float ref = m == -INFINITY ? 0.f : m;
-                        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-                        uint32_t pk[2][16];
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float p0 = ptx::ex2(fmaf(__uint_as_float(raw[0][i]), sl2, -ref));
-                            const float p1 = ptx::ex2(fmaf(__uint_as_float(raw[0][i + 1]), sl2, -ref));
-                            const float p2 = ptx::ex2(fmaf(__uint_as_float(raw[1][i]), sl2, -ref));
-                            const float p3 = ptx::ex2(fmaf(__uint_as_float(raw[1][i + 1]), sl2, -ref));
-                            s0 += p0, s1 += p1, s2 += p2, s3 += p3;
-                            // weights as bf16: 2^-8 of each at most, averaged over the keys
-                            pk[0][i / 2] = pack_bf16(p0, p1), pk[1][i / 2] = pack_bf16(p2, p3);
+                        for (int i = 0; i < KT; i += 2) {
+                            const float x = ptx::ex2(fmaf(__uint_as_float(raw[i]), sl2, -ref));
+                            const float y = ptx::ex2(fmaf(__uint_as_float(raw[i + 1]), sl2, -ref));
+                            acc[i & 2] += x, acc[(i & 2) + 1] += y;
+                            // weights as bf16: at most 2^-8 of each, independent from key to key
+                            raw[i / 2] = pack_bf16(x, y);
                         }
-                        ptx::tmem_st16(ts, pk[0]);
-                        ptx::tmem_st16(ts + 16, pk[1]);
+                        ptx::tmem_st16(ts, *reinterpret_cast<const uint32_t(*)[16]>(&raw[0]));
+                        ptx::tmem_st16(ts + 16, *reinterpret_cast<const uint32_t(*)[16]>(&raw[16]));
                         if (m != m_l) l *= ptx::ex2(m_l - ref);
                         m_l = m;
-                        l += (s0 + s1) + (s2 + s3);
+                        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
                     }
                     if (draft || valid < KT) {
                         // Rows of V that no weight may meet: past the end (left over from the stage's last use, or the
@@ -515,22 +557,21 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                         for (int i = (draft ? 0 : valid * VR) + w4 * 32 + lane; i < upto * VR; i += 128) {
                             const int key = i / VR, c = i - key * VR;
                             uint4 *p = reinterpret_cast<uint4 *>(v + (c >> 3) * C::CHUNK + key * 128 + (c & 7) * 16);
-                            bool zero = key >= valid;
-                            if (!zero && draft) {
-                                const uint4 x = *p;
-                                if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
-                                    atomicOr(&sh.nonfinite[ord & 3][key >> 5], 1u << (key & 31));
-                                    uint4 y = x;
-                                    uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        if ((yw[e] & 0x7f80u) == 0x7f80u) yw[e] &= 0xffff0000u;
-                                        if ((yw[e] & 0x7f800000u) == 0x7f800000u) yw[e] &= 0x0000ffffu;
-                                    }
-                                    *p = y;
-                                }
+                            if (key >= valid) {
+                                *p = make_uint4(0, 0, 0, 0);
+                                continue;
                             }
-                            if (zero) *p = make_uint4(0, 0, 0, 0);
+                            uint4 x = *p;
+                            if (nonfinite2(x.x) || nonfinite2(x.y) || nonfinite2(x.z) || nonfinite2(x.w)) {
+                                atomicOr(&sh.nonfinite[ord & 3][key >> 5], 1u << (key & 31));
+                                uint32_t *xw = reinterpret_cast<uint32_t *>(&x);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    if ((xw[e] & 0x7f80u) == 0x7f80u) xw[e] &= 0xffff0000u;
+                                    if ((xw[e] & 0x7f800000u) == 0x7f800000u) xw[e] &= 0x0000ffffu;
+                                }
+                                *p = x;
+                            }
                         }
                         ptx::fence_proxy_async();
                         __syncwarp();
@@ -555,21 +596,12 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                     ptx::tc_fence_before_sync();
                     ptx::mbar_arrive_warp(&sh.p_full[buf]);
                 }
-                // ---- end of the item: the other warpgroup's last maximum, the sum of both, the next item's queries
-                const unsigned last = tile + n - 1;
-                if ((int)(last & 1) != wg) {
-                    if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
-                    ++handed, have = true;
-                    m = sh.m[row];
-                }
+                if (n > 0) {
+                // ---- end of the item: the sum of both, the output
                 const float ref = m == -INFINITY ? 0.f : m;
                 if (m != m_l) l *= ptx::ex2(m_l - ref);
                 sh.l[ord & 1][wg][row] = l;
                 ptx::mbar_arrive_warp(&sh.exch[w4]);
-                const unsigned nr = (ord + 1) % ITEMS;
-                if (!wait_warp(&sh.item_full[nr], ((ord + 1) / ITEMS) & 1)) return false;
-                const Item next = sh.items[nr];
-                if (next.tiles > 0) load_q(next);     // (the last Q K^T of this item is done: its S has been read)
                 if (!wait_warp(&sh.exch[w4], ord & 1)) return false;
                 l += sh.l[ord & 1][wg ^ 1][row];
                 if (!wait_warp(&sh.pv_done[last % C::NSB], (last / C::NSB) & 1)) return false;
@@ -577,65 +609,74 @@ attn_tc_kernel(AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map
                 const bool bad = sh.bad_item[ord % 16] == ord + 1;
                 if (tid == 0) sh.nonfinite[(ord + 2) & 3][0] = sh.nonfinite[(ord + 2) & 3][1] = 0;
                 if (bad && it.b >= 0 && row == 0 && wg == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
-                if (warp_on) {
-                    const uint64_t nf = tree & ((uint64_t)sh.nonfinite[ord & 3][0] | (uint64_t)sh.nonfinite[ord & 3][1] << 32);
-                    const int rr = it.row0 + row, node = rr / a.G, hq = it.h * a.G + rr - node * a.G;
-                    const long long orow = (long long)(it.lo + node) * a.H_q + hq;
-                    const bool direct = it.slot < 0 && a.shared_len == 0;
-                    const float inv = direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                    float *po, *pml;
-                    if (it.slot >= 0) {
-                        const long long at = ((long long)it.slot * R + member) * ws.row_cap + row;
-                        po = ws.slot_o + at * D, pml = ws.slot_ml + 2 * at;
-                    } else {
-                        const long long at = (it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow;
-                        po = ws.row_o + at * D, pml = ws.row_ml + 2 * at;
-                    }
-                    if (!direct && on && wg == 0) *reinterpret_cast<float2 *>(pml) = make_float2(m, bad ? -1.f : l);
-                    __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
-                    const bool store = on && !(direct && bad);
+                uint64_t nf = me.tree & ((uint64_t)sh.nonfinite[ord & 3][0] | (uint64_t)sh.nonfinite[ord & 3][1] << 32);
+                constexpr int HALF = D / 2, EC = 32;  // this warpgroup's columns, and how many at a time
 #pragma unroll 1
-                    for (int c = wg * (D / 2); c < (wg + 1) * (D / 2); c += 32) {
-                        uint32_t o[32];
-                        __syncwarp();
-                        ptx::tmem_ld32(tmem + lane_base + c, o);
-                        ptx::tmem_wait_ld();
-                        if (nf) {
-                            for (uint64_t left = nf; left; left &= left - 1) {
-                                const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) +
-                                                         (it.lo + __ffsll((long long)left) - 1) * a.ld_v + (long long)it.h * D + c;
+                for (int c = wg * HALF; c < (wg + 1) * HALF; c += EC) {
+                    uint32_t o[EC];
+                    if (warp_on) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    const float x = to_f32(v[i]);
-                                    if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+                        for (int i = 0; i < EC; i += 32) ptx::tmem_ld32(tmem + lane_base + c + i, *reinterpret_cast<uint32_t(*)[32]>(&o[i]));
+                        ptx::tmem_wait_ld();
+                    }
+                    if (c + EC == (wg + 1) * HALF) {  // all read: the next item's products may overwrite it
+                        ptx::tc_fence_before_sync();
+                        ptx::mbar_arrive_warp(&sh.o_free);
+                    }
+                    if (on) {
+                        const long long orow = (long long)me.t * a.H_q + me.hq;
+                        if (it.slot < 0 && a.shared_len == 0) {
+                            const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
+                            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c;
+                            if (!bad) {
+#pragma unroll
+                                for (int i = 0; i < EC; i += 8) {
+                                    uint4 y;
+                                    uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        yw[e] = pack_bf16(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
+                                    *reinterpret_cast<uint4 *>(out + i) = y;
                                 }
                             }
-                        }
-                        if (direct) {
+                        } else {
+                            const bool cut = it.slot >= 0;
+                            const long long at = cut ? ((long long)it.slot * R + member) * ws.row_cap + row
+                                                     : (it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow;
+                            float *po = (cut ? ws.slot_o : ws.row_o) + at * D + c, *pml = (cut ? ws.slot_ml : ws.row_ml) + 2 * at;
+                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(pml) = make_float2(m, bad ? -1.f : l);
 #pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint4 y;
-                                uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    yw[e] = pack_bf16(l == 0.f ? 0.f : __uint_as_float(o[i + 2 * e]) * inv,
-                                                      l == 0.f ? 0.f : __uint_as_float(o[i + 2 * e + 1]) * inv);
-                                if (store) *reinterpret_cast<uint4 *>(out + c + i) = y;
-                            }
-                        } else if (store) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4)
-                                *reinterpret_cast<uint4 *>(po + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                            for (int i = 0; i < EC; i += 4)
+                                *reinterpret_cast<uint4 *>(po + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                         }
                     }
                     __syncwarp();
-                    ptx::tc_fence_before_sync();
                 }
-                ptx::mbar_arrive_warp(&sh.o_free);
+                if (on)
+                    for (; nf; nf &= nf - 1) {  // seen draft rows with NaN or infinity: those elements, onto what was stored
+                        const int jn = __ffsll((long long)nf) - 1;
+                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + (it.lo + jn) * a.ld_v + (long long)it.h * D;
+                        const long long orow = (long long)me.t * a.H_q + me.hq;
+#pragma unroll 1
+                        for (int c = wg * HALF; c < (wg + 1) * HALF; ++c) {
+                            const float x = to_f32(v[c]);
+                            if (isfinite(x)) continue;
+                            if (it.slot < 0 && a.shared_len == 0) {
+                                __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c;
+                                if (!bad) *out = __float2bfloat16_rn(to_f32(*out) + x);
+                            } else {
+                                float *out = it.slot >= 0 ? ws.slot_o + (((long long)it.slot * R + member) * ws.row_cap + row) * D + c
+                                                          : ws.row_o + ((it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow) * D + c;
+                                *out += x;
+                            }
+                        }
+                    }
+                __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
-                if (next.tiles == 0) return true;
+                }
+                if (next.it->tiles == 0) return true;
                 base += 2 * n, tile += n;
-                it = next;
+                me = next, n = me.it->tiles, cur_b = me.it->b;
             }
         };
         const bool ok = run();
@@ -712,48 +753,42 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_cut_kernel(AttnArgs
     jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d[2] + node) * a.H_q + d[3] * a.G + rr - node * a.G) * D, lane);
 }
 
-// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: one warp to a row.
+// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: one warp to a row,
+// grid (rows of the longest tree / 8, sequences).
 template <int D>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(AttnArgs a, int R, Ws ws)
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
 {
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, b = blockIdx.y;
+    const int r = blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_trigger();
-    if (row >= (long long)a.T * a.H_q) return;
-    const int t = (int)(row / a.H_q), hq = (int)(row - (long long)t * a.H_q), h = hq / a.G, g = hq - h * a.G;
-    int b = 0, hi = a.B;
-    while (hi - b > 1) {
-        const int mid = (b + hi) >> 1;
-        if (a.node_offsets[mid] <= t) b = mid;
-        else hi = mid;
-    }
+    const long long W = ws.prefix[a.B], first = ws.prefix[b];
+    const int parts = (int)ws.prefix[a.B + 1];
     int st;
     const Seq s = load_seq(a, b, R, &st);
-    if (st || t < s.lo || t >= s.lo + s.n) return;
-    const long long W = ws.prefix[a.B];
-    const int parts = (int)ws.prefix[a.B + 1];
+    if (st || r >= s.n * a.H_q) return;
+    const int node = r / a.H_q, hq = r - node * a.H_q, h = hq / a.G, g = hq - h * a.G;
+    const long long row = (long long)(s.lo + node) * a.H_q + hq;
     Join<D> jn;
     jn.start();
-    auto add = [&](const Seq &q, long long first, long long r, int pass) {
-        const int tile = (int)(r / MT), in_tile = (int)(r - (long long)tile * MT), rg = tile / R, member = tile - rg * R;
-        const long long begin = first + ((long long)h * q.groups + rg) * q.kts, end = begin + q.kts;
-        const int g0 = part_of(begin, W, parts), g1 = part_of(end - 1, W, parts);
+    auto add = [&](const Seq &q, long long from, long long i, int pass) {  // i: the row in the list that q's tiles cut up
+        const int tile = (int)(i / MT), in_tile = (int)(i % MT), rg = tile / R, member = tile - rg * R;
+        const long long begin = from + (long long)(h * q.groups + rg) * (OV + q.kts);
+        const int g0 = part_of(begin + OV, W, parts), g1 = part_of(begin + OV + q.kts - 1, W, parts);
         if (g0 == g1) {
             const long long at = pass * (long long)a.T * a.H_q + row;
             jn.add(ws.row_ml + 2 * at, ws.row_o + at * D, lane);
             return;
         }
         for (int p = g0; p <= g1; ++p) {
-            const long long slot = p > g0 || part_begin(p, W, parts) == begin ? 2 * p : 2 * p + 1;
-            const long long at = (slot * R + member) * ws.row_cap + in_tile;
+            const long long at = ((long long)slot_of(p, begin, p == g0 ? part_begin(p, W, parts) : begin) * R + member) * ws.row_cap + in_tile;
             jn.add(ws.slot_ml + 2 * at, ws.slot_o + at * D, lane);
         }
     };
     int st0;
-    add(load_seq(a, -1, R, &st0), 0, (long long)t * a.G + g, 0);
+    add(load_seq(a, -1, R, &st0), 0, (long long)(s.lo + node) * a.G + g, 0);
     const bool bad_shared = jn.bad;
-    add(s, ws.prefix[b], (long long)(t - s.lo) * a.G + g, 1);
+    add(s, first, (long long)node * a.G + g, 1);
     if (bad_shared && lane == 0 && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
     jn.store(static_cast<__nv_bfloat16 *>(a.O) + row * D, lane);
 }
@@ -821,14 +856,23 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, kc, vc, k, v);
     if (e != cudaSuccess) return e;
     if (a.shared_len > 0) {
-        const long long blocks = ((long long)a.T * a.H_q + JOIN_WARPS - 1) / JOIN_WARPS;
-        return launch_dependent(attn_join_shared_kernel<D>, dim3((unsigned)blocks), dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
+        const long long blocks = ((long long)a.max_nodes * a.H_q + JOIN_WARPS - 1) / JOIN_WARPS;
+        return launch_dependent(attn_join_shared_kernel<D>, dim3((unsigned)blocks, a.B), dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
     }
     return launch_dependent(attn_join_cut_kernel<D>, dim3(ctas, (p.row_cap + JOIN_WARPS - 1) / JOIN_WARPS), dim3(JOIN_WARPS * 32), 0,
                             stream, a, p.R, ws);
 }
 
 }  // namespace
+
+// The units of one sequence, and of the shared prompt, stay below 2^31.
+static bool units_fit(const AttnArgs &a)
+{
+    const long long own = ((long long)a.max_nodes * a.G + MT - 1) / MT * (((long long)a.c.max_pages * a.c.page_size) / KT + 2 + OV);
+    const long long shared = ((long long)a.T * a.G + MT - 1) / MT * (a.shared_len / KT + 2 + OV);
+    const long long most = 0x7fffffffll / a.c.H_kv;
+    return own <= most && shared <= most;
+}
 
 bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io)
 {
@@ -837,7 +881,7 @@ bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io)
     // 8-row groups of the swizzle have to stay whole within a page; the tensor maps want a pool that exists and real strides
     return io == TREEWY_BF16 && (c.d == 64 || c.d == 128 || c.d == 256) && pow2 && c.page_size >= 8 && c.n_pages > 0 &&
            c.max_pages > 0 && c.stride_slot > 0 && (c.H_kv == 1 || c.stride_head > 0) && (c.n_pages == 1 || c.stride_page > 0) &&
-           (long long)a.T * a.H_q <= 0x7fffffffll;
+           (long long)a.T * a.H_q <= 0x7fffffffll && a.B <= 65535 && units_fit(a);
 }
 
 size_t attn_tc_workspace(const AttnArgs &a)
