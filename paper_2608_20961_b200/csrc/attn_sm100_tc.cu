@@ -67,13 +67,16 @@ struct Shared {
     uint32_t tmem;
 };
 
-// The workspace.
+// The workspace.  A block holds unnormalised outputs of up to `cap` rows of one row tile, column groups of 4 first:
+// element (row, c) at ((c / 4) * cap + row) * 4 + c % 4, so that the rows of a warp are neighbours when its threads
+// write a column group each of their own row; (m, l) of the rows beside it.
 struct Ws {
     long long *prefix;          // [B + 2]: first unit of each sequence (shared prompts), all units, parts
     int *desc;                  // [MAX_CTAS][8]: the item that a CTA's part cuts at its end
-    float *slot_ml, *slot_o;    // [2 * CTAs][row_cap]
-    float *row_ml, *row_o;      // [2][T * H_q]: whole items' results where a prompt is shared
-    int row_cap;
+    float *slot_ml, *slot_o;    // cut items: [2 * CTAs] blocks
+    float *own_ml, *own_o;      // whole items beside a shared prompt: [B][H_kv][own_tiles] blocks
+    float *shared_ml, *shared_o;  // the shared prompt's whole items: [H_kv][tiles] blocks of MT rows
+    int slot_cap, own_cap, own_tiles;
 };
 
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + KT - 1) / KT; }
@@ -82,9 +85,8 @@ struct Seq {
     int lo, n, len, kts, row_tiles, groups;
     unsigned units;             // H_kv * groups * (OV + kts), below 2^31 (the launcher has checked)
 };
-// b = -1: the shared prompt, whose rows are those of all sequences.  (What is not called once a tile is kept out of line:
-// the roles run at the same time and share the instruction cache.)
-static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status)
+// b = -1: the shared prompt, whose rows are those of all sequences
+__device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *status)
 {
     Seq s;
     *status = 0;
@@ -105,6 +107,9 @@ static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int
     s.units = (unsigned)a.c.H_kv * s.groups * (OV + s.kts);
     return s;
 }
+// (What the main kernel does not do once a tile is out of line: its roles run at the same time and share the
+// instruction cache.)
+static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status) { return read_seq(a, b, R, status); }
 
 // (a 64-bit division takes several times as long as a 32-bit one, and nearly every line of work is short)
 static __device__ __noinline__ long long div64(long long x, long long y)
@@ -610,6 +615,16 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                 if (tid == 0) sh.nonfinite[(ord + 2) & 3][0] = sh.nonfinite[(ord + 2) & 3][1] = 0;
                 if (bad && it.b >= 0 && row == 0 && wg == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
                 uint64_t nf = me.tree & ((uint64_t)sh.nonfinite[ord & 3][0] | (uint64_t)sh.nonfinite[ord & 3][1] << 32);
+                // the block of an item that is not stored as it is
+                float *blk_o = ws.slot_o, *blk_ml = ws.slot_ml;
+                int blk_cap = ws.slot_cap;
+                long long blk = (long long)it.slot * R + member;
+                if (it.slot < 0) {
+                    const int rt = it.row0 / MT;
+                    if (it.b < 0) blk_o = ws.shared_o, blk_ml = ws.shared_ml, blk_cap = MT, blk = it.h * (((long long)a.T * a.G + MT - 1) / MT) + rt;
+                    else blk_o = ws.own_o, blk_ml = ws.own_ml, blk_cap = ws.own_cap, blk = ((long long)it.b * a.c.H_kv + it.h) * ws.own_tiles + rt;
+                }
+                blk_o += blk * blk_cap * D, blk_ml += blk * blk_cap * 2;
                 constexpr int HALF = D / 2, EC = 32;  // this warpgroup's columns, and how many at a time
 #pragma unroll 1
                 for (int c = wg * HALF; c < (wg + 1) * HALF; c += EC) {
@@ -640,14 +655,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                                 }
                             }
                         } else {
-                            const bool cut = it.slot >= 0;
-                            const long long at = cut ? ((long long)it.slot * R + member) * ws.row_cap + row
-                                                     : (it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow;
-                            float *po = (cut ? ws.slot_o : ws.row_o) + at * D + c, *pml = (cut ? ws.slot_ml : ws.row_ml) + 2 * at;
-                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(pml) = make_float2(m, bad ? -1.f : l);
+                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(blk_ml + 2 * row) = make_float2(m, bad ? -1.f : l);
+                            float *po = blk_o + ((long long)(c / 4) * blk_cap + row) * 4;
 #pragma unroll
                             for (int i = 0; i < EC; i += 4)
-                                *reinterpret_cast<uint4 *>(po + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                                *reinterpret_cast<uint4 *>(po + i * blk_cap) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                         }
                     }
                     __syncwarp();
@@ -665,8 +677,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                                 __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c;
                                 if (!bad) *out = __float2bfloat16_rn(to_f32(*out) + x);
                             } else {
-                                float *out = it.slot >= 0 ? ws.slot_o + (((long long)it.slot * R + member) * ws.row_cap + row) * D + c
-                                                          : ws.row_o + ((it.b < 0 ? 0 : (long long)a.T * a.H_q) + orow) * D + c;
+                                float *out = blk_o + ((long long)(c / 4) * blk_cap + row) * 4 + c % 4;
                                 *out += x;
                             }
                         }
@@ -689,125 +700,176 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
     if (warp == MMA_QK) ptx::tmem_dealloc(tmem, 512);
 }
 
-// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys, one
-// warp to a row, columns of a lane 4 at a time.  A part of a sequence with a bad page has l = -1: the row is left.
+// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item.  Where an
+// item may be cut into many (a single sequence into as many as there are CTAs) a CTA takes 8 rows and its warps take turns at
+// the parts, since one warp would wait for each in turn; their sums meet in shared memory in the order of the warps.  Lane = row + 8 * column group, 4 groups of 4
+// columns a step, so that both the blocks (8 rows of a group are 128 bytes) and the output (4 groups of a row are 32) move in
+// whole sectors.  A part of a sequence with a bad page has l = -1: the row is left.
 template <int D> struct Join {
-    float4 acc[(D + 127) / 128];
+    static constexpr int WARPS = D == 256 ? 4 : 8, STEPS = D / 16;
+    struct Smem {
+        float4 acc[WARPS][STEPS][32];
+        float2 ml[WARPS][8];
+    };
+    float4 acc[STEPS];
     float m = -INFINITY, l = 0.f;
     bool bad = false;
     __device__ __forceinline__ void start()
     {
 #pragma unroll
-        for (int i = 0; i < (D + 127) / 128; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < STEPS; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    __device__ __forceinline__ void add(const float *ml, const float *o, int lane)
+    // block at (ml, o) of cap rows, this lane's row in it
+    __device__ __forceinline__ void add(const float *ml, const float *o, int cap, int row, int cg)
     {
-        const float2 x = *reinterpret_cast<const float2 *>(ml);
+        const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * row);
+        float4 y[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) y[i] = *reinterpret_cast<const float4 *>(o + ((long long)(4 * i + cg) * cap + row) * 4);
         if (x.y < 0.f) bad = true;
         if (x.y == 0.f) return;  // saw nothing
         const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
         const float f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
         m = mn, l = l * f0 + x.y * f1;
 #pragma unroll
-        for (int i = 0; i < (D + 127) / 128; ++i) {
-            const int c = i * 128 + lane * 4;
-            if (c < D) {
-                const float4 y = *reinterpret_cast<const float4 *>(o + c);
-                acc[i].x = acc[i].x * f0 + y.x * f1, acc[i].y = acc[i].y * f0 + y.y * f1;
-                acc[i].z = acc[i].z * f0 + y.z * f1, acc[i].w = acc[i].w * f0 + y.w * f1;
-            }
+        for (int i = 0; i < STEPS; ++i) {
+            acc[i].x = acc[i].x * f0 + y[i].x * f1, acc[i].y = acc[i].y * f0 + y[i].y * f1;
+            acc[i].z = acc[i].z * f0 + y[i].z * f1, acc[i].w = acc[i].w * f0 + y[i].w * f1;
         }
     }
-    __device__ __forceinline__ void store(__nv_bfloat16 *out, int lane)
+    // one warp's rows, joined by it alone
+    __device__ __forceinline__ void store(__nv_bfloat16 *out, int cg)
     {
         if (bad) return;
         const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-        for (int i = 0; i < (D + 127) / 128; ++i) {
-            const int c = i * 128 + lane * 4;
-            if (c < D) *reinterpret_cast<uint2 *>(out + c) = make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+        for (int i = 0; i < STEPS; ++i)
+            *reinterpret_cast<uint2 *>(out + 16 * i + 4 * cg) =
+                make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
+    }
+    // the CTA's 8 rows, joined by all of its warps; on: the row exists
+    __device__ __forceinline__ void finish(Smem &sm, __nv_bfloat16 *out, bool on)
+    {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cg = lane >> 3;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) sm.acc[warp][i][lane] = acc[i];
+        if (cg == 0) sm.ml[warp][lane & 7] = make_float2(m, bad ? -1.f : l);
+        __syncthreads();
+        float top = -INFINITY;
+        bool any_bad = false;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float2 x = sm.ml[w][lane & 7];
+            if (x.y != 0.f) top = fmaxf(top, x.x);
+            any_bad |= x.y < 0.f;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        float f[WARPS], sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float2 x = sm.ml[w][lane & 7];
+            f[w] = x.y == 0.f ? 0.f : ptx::ex2(x.x - ref);
+            sum += x.y * f[w];
+        }
+        if (!on || any_bad) return;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        for (int i = warp; i < STEPS; i += WARPS) {
+            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float4 y = sm.acc[w][i][lane];
+                t.x += y.x * f[w], t.y += y.y * f[w], t.z += y.z * f[w], t.w += y.w * f[w];
+            }
+            *reinterpret_cast<uint2 *>(out + 16 * i + 4 * cg) =
+                make_uint2(pack_bf16(t.x * inv, t.y * inv), pack_bf16(t.z * inv, t.w * inv));
         }
     }
 };
 
-constexpr int JOIN_WARPS = 8;
-
 // Items that a part cut: grid (CTAs of the main kernel, rows of a tile / 8).
 template <int D>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_cut_kernel(AttnArgs a, int R, Ws ws)
+__global__ void __launch_bounds__(Join<D>::WARPS * 32) attn_join_cut_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
 {
-    const int lane = threadIdx.x & 31, row = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5);
+    __shared__ typename Join<D>::Smem sm;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cg = lane >> 3, row = blockIdx.y * 8 + (lane & 7);
     grid_dependency_wait();
     grid_dependency_trigger();
-    const int *d = ws.desc + 8 * blockIdx.x;
-    const int pieces = d[0];
-    if (pieces == 0 || row >= d[5]) return;
+    const int4 d0 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x), d1 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x + 4);
+    const int pieces = d0.x;
+    if (pieces == 0 || (int)blockIdx.y * 8 >= d1.y) return;
     const int member = blockIdx.x % R;
+    const bool on = row < d1.y;
     Join<D> jn;
     jn.start();
-    for (int p = 0; p < pieces; ++p) {
-        const long long slot = p == 0 ? d[1] : 2 * (d[6] + p), at = (slot * R + member) * ws.row_cap + row;
-        jn.add(ws.slot_ml + 2 * at, ws.slot_o + at * D, lane);
-    }
-    const int rr = d[4] + row, node = rr / a.G;
-    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d[2] + node) * a.H_q + d[3] * a.G + rr - node * a.G) * D, lane);
+    if (on)
+#pragma unroll 1
+        for (int p = warp; p < pieces; p += Join<D>::WARPS) {
+            const long long blk = ((long long)(p == 0 ? d0.y : 2 * (d1.z + p)) * R + member) * ws.slot_cap;
+            jn.add(ws.slot_ml + blk * 2, ws.slot_o + blk * D, ws.slot_cap, row, cg);
+        }
+    const int rr = d1.x + row, node = rr / a.G;
+    jn.finish(sm, static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d0.z + node) * a.H_q + d0.w * a.G + rr - node * a.G) * D, on);
 }
 
-// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: one warp to a row,
-// grid (rows of the longest tree / 8, sequences).
+// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: rarely more than four
+// blocks, so one warp joins its 8 rows alone.  Grid (rows of the longest tree under one key/value head / 32, key/value
+// heads, sequences).
 template <int D>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
+__global__ void __launch_bounds__(128) attn_join_shared_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
 {
-    const int lane = threadIdx.x & 31, b = blockIdx.y;
-    const int r = blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, cg = lane >> 3, h = blockIdx.y, b = blockIdx.z;
+    const int r = (blockIdx.x * 4 + (threadIdx.x >> 5)) * 8 + (lane & 7);  // row among the sequence's under this head
     grid_dependency_wait();
     grid_dependency_trigger();
     const long long W = ws.prefix[a.B], first = ws.prefix[b];
     const int parts = (int)ws.prefix[a.B + 1];
-    int st;
-    const Seq s = load_seq(a, b, R, &st);
-    if (st || r >= s.n * a.H_q) return;
-    const int node = r / a.H_q, hq = r - node * a.H_q, h = hq / a.G, g = hq - h * a.G;
-    const long long row = (long long)(s.lo + node) * a.H_q + hq;
+    int st, st0;
+    const Seq own = read_seq(a, b, R, &st), prompt = read_seq(a, -1, R, &st0);
+    if (st || r >= own.n * a.G) return;
     Join<D> jn;
     jn.start();
-    auto add = [&](const Seq &q, long long from, long long i, int pass) {  // i: the row in the list that q's tiles cut up
-        const int tile = (int)(i / MT), in_tile = (int)(i % MT), rg = tile / R, member = tile - rg * R;
-        const long long begin = from + (long long)(h * q.groups + rg) * (OV + q.kts);
-        const int g0 = part_of(begin + OV, W, parts), g1 = part_of(begin + OV + q.kts - 1, W, parts);
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {  // the prompt, then the sequence's own keys
+        const int kts = pass == 0 ? prompt.kts : own.kts, groups = pass == 0 ? prompt.groups : own.groups;
+        const unsigned i = pass == 0 ? own.lo * a.G + r : r;  // the row in the list that the item's tiles cut up
+        const int tile = i / MT, in_tile = i % MT, rg = tile / R, member = tile - rg * R;
+        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (OV + kts);
+        const int g0 = part_of(begin + OV, W, parts), g1 = part_of(begin + OV + kts - 1, W, parts);
         if (g0 == g1) {
-            const long long at = pass * (long long)a.T * a.H_q + row;
-            jn.add(ws.row_ml + 2 * at, ws.row_o + at * D, lane);
-            return;
+            const long long blk = pass == 0 ? (long long)h * prompt.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
+            const int cap = pass == 0 ? MT : ws.own_cap;
+            jn.add((pass == 0 ? ws.shared_ml : ws.own_ml) + blk * cap * 2, (pass == 0 ? ws.shared_o : ws.own_o) + blk * cap * D, cap,
+                   in_tile, cg);
+        } else {
+            int slot = slot_of(g0, begin, part_begin(g0, W, parts));
+#pragma unroll 1
+            for (int p = g0; p <= g1; ++p, slot = 2 * p) {
+                const long long blk = ((long long)slot * R + member) * ws.slot_cap;
+                jn.add(ws.slot_ml + blk * 2, ws.slot_o + blk * D, ws.slot_cap, in_tile, cg);
+            }
         }
-        for (int p = g0; p <= g1; ++p) {
-            const long long at = ((long long)slot_of(p, begin, p == g0 ? part_begin(p, W, parts) : begin) * R + member) * ws.row_cap + in_tile;
-            jn.add(ws.slot_ml + 2 * at, ws.slot_o + at * D, lane);
-        }
-    };
-    int st0;
-    add(load_seq(a, -1, R, &st0), 0, (long long)(s.lo + node) * a.G + g, 0);
-    const bool bad_shared = jn.bad;
-    add(s, first, (long long)node * a.G + g, 1);
-    if (bad_shared && lane == 0 && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
-    jn.store(static_cast<__nv_bfloat16 *>(a.O) + row * D, lane);
+        if (pass == 0 && jn.bad && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
+    }
+    const int node = r / a.G;
+    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(own.lo + node) * a.H_q + h * a.G + r - node * a.G) * D, cg);
 }
 
 struct Plan {
-    int R, row_cap, ctas;
-    size_t prefix, desc, slots, rows;  // elements
+    int R, slot_cap, own_cap, own_tiles;
+    size_t prefix, desc, slots, own, shared;  // elements; rows of the three kinds of block
 };
-Plan plan_of(const AttnArgs &a, int ctas)
+Plan plan_of(const AttnArgs &a)
 {
     Plan p;
     const long long rows = (long long)a.max_nodes * a.G, tiles = (rows + MT - 1) / MT;
-    p.R = (int)(tiles < 1 ? 1 : tiles > 4 ? 4 : tiles);
-    p.ctas = ctas;
-    p.row_cap = a.shared_len > 0 || rows > MT ? MT : (int)rows;
+    p.R = (int)(tiles > 4 ? 4 : tiles);
+    p.own_cap = rows > MT ? MT : (int)rows, p.own_tiles = (int)tiles;
+    p.slot_cap = a.shared_len > 0 ? MT : p.own_cap;
     p.prefix = a.B + 2 + (a.B & 1);    // (keeps what follows 16-byte aligned)
     p.desc = 8 * MAX_CTAS;
-    p.slots = 2ull * ctas * p.row_cap;
-    p.rows = a.shared_len > 0 ? 2ull * a.T * a.H_q : 0;
+    p.slots = 2ull * MAX_CTAS * p.slot_cap;
+    p.own = a.shared_len > 0 ? (size_t)a.B * a.c.H_kv * p.own_tiles * p.own_cap : 0;
+    p.shared = a.shared_len > 0 ? a.c.H_kv * (((size_t)a.T * a.G + MT - 1) / MT) * MT : 0;
     return p;
 }
 
@@ -817,17 +879,19 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     int dev = 0, sms = 0;
     cudaError_t e = current_device_sms(&dev, &sms);
     if (e != cudaSuccess) return e;
-    const Plan p = plan_of(a, MAX_CTAS);
+    const Plan p = plan_of(a);
     const int ctas = (sms < MAX_CTAS ? sms : MAX_CTAS) / p.R * p.R;
     Ws ws;
     unsigned char *at = reinterpret_cast<unsigned char *>(a.ws);
     ws.prefix = reinterpret_cast<long long *>(at), at += p.prefix * 8;
     ws.desc = reinterpret_cast<int *>(at), at += p.desc * 4;
     ws.slot_o = reinterpret_cast<float *>(at), at += p.slots * D * 4;
-    ws.row_o = reinterpret_cast<float *>(at), at += p.rows * D * 4;
+    ws.own_o = reinterpret_cast<float *>(at), at += p.own * D * 4;
+    ws.shared_o = reinterpret_cast<float *>(at), at += p.shared * D * 4;
     ws.slot_ml = reinterpret_cast<float *>(at), at += p.slots * 8;
-    ws.row_ml = reinterpret_cast<float *>(at);
-    ws.row_cap = p.row_cap;
+    ws.own_ml = reinterpret_cast<float *>(at), at += p.own * 8;
+    ws.shared_ml = reinterpret_cast<float *>(at);
+    ws.slot_cap = p.slot_cap, ws.own_cap = p.own_cap, ws.own_tiles = p.own_tiles;
     a.log_page = 0;
     while ((1 << a.log_page) < a.c.page_size) ++a.log_page;
 
@@ -856,11 +920,10 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, kc, vc, k, v);
     if (e != cudaSuccess) return e;
     if (a.shared_len > 0) {
-        const long long blocks = ((long long)a.max_nodes * a.H_q + JOIN_WARPS - 1) / JOIN_WARPS;
-        return launch_dependent(attn_join_shared_kernel<D>, dim3((unsigned)blocks, a.B), dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
+        const unsigned x = (unsigned)(((long long)a.max_nodes * a.G + 31) / 32);
+        return launch_dependent(attn_join_shared_kernel<D>, dim3(x, a.c.H_kv, a.B), dim3(128), 0, stream, a, p.R, ws);
     }
-    return launch_dependent(attn_join_cut_kernel<D>, dim3(ctas, (p.row_cap + JOIN_WARPS - 1) / JOIN_WARPS), dim3(JOIN_WARPS * 32), 0,
-                            stream, a, p.R, ws);
+    return launch_dependent(attn_join_cut_kernel<D>, dim3(ctas, (p.slot_cap + 7) / 8), dim3(Join<D>::WARPS * 32), 0, stream, a, p.R, ws);
 }
 
 }  // namespace
@@ -881,13 +944,13 @@ bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io)
     // 8-row groups of the swizzle have to stay whole within a page; the tensor maps want a pool that exists and real strides
     return io == TREEWY_BF16 && (c.d == 64 || c.d == 128 || c.d == 256) && pow2 && c.page_size >= 8 && c.n_pages > 0 &&
            c.max_pages > 0 && c.stride_slot > 0 && (c.H_kv == 1 || c.stride_head > 0) && (c.n_pages == 1 || c.stride_page > 0) &&
-           (long long)a.T * a.H_q <= 0x7fffffffll && a.B <= 65535 && units_fit(a);
+           (long long)a.T * a.H_q <= 0x7fffffffll && a.B <= 65535 && a.c.H_kv <= 65535 && units_fit(a);
 }
 
 size_t attn_tc_workspace(const AttnArgs &a)
 {
-    const Plan p = plan_of(a, MAX_CTAS);
-    return p.prefix * 8 + p.desc * 4 + (p.slots + p.rows) * (a.c.d + 2) * 4;
+    const Plan p = plan_of(a);
+    return p.prefix * 8 + p.desc * 4 + (p.slots + p.own + p.shared) * (a.c.d + 2) * 4;
 }
 
 cudaError_t launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
