@@ -22,6 +22,8 @@
 // Roles: two softmax warpgroups that take turns at the key tiles (the maxima travel between them, row by row),
 // one thread that walks the work and copies K tiles, one that copies V tiles, one each for the MMAs of
 // S = Q K^T and O += P V (a single one for both was the slowest role: its waits alone took as long as a tile).
+#include <type_traits>
+
 #include "attn_common.cuh"
 #include "ptx_sm100.cuh"
 #include "tma_host.cuh"
@@ -40,12 +42,31 @@ constexpr float LAZY = 8.f;
 
 template <int D> struct Cfg {
     static constexpr int NC = D / 64;                              // 64-column chunks of a row
-    static constexpr int CHUNK = KT * 128;                         // bytes of one chunk of a tile
-    static constexpr int STAGE = NC * CHUNK;
-    static constexpr int NST = D == 256 ? 6 : D == 128 ? 12 : 16;  // about 192 KB in flight
+    static constexpr int STAGE = NC * KT * 128;                    // bytes of a tile
+    // Heads of 256 leave tensor memory for two S buffers only.  With the weights in S's place the Q K^T after next would
+    // wait for this tile's P V; so there P goes through shared memory and S is free as soon as it has been read.
+    static constexpr bool P_SMEM = D == 256;
+    static constexpr int P_BYTES = P_SMEM ? MT * KT * 2 : 0;       // of one of the two P buffers
+    // K tiles and V tiles have a ring of stages each, up to 192 KB together
+    static constexpr int NK = D == 256 ? 3 : D == 128 ? 6 : 8, NV = D == 256 ? 2 : NK;
     static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
     static constexpr int NQ = D == 256 ? 1 : 2;                    // Q buffers
     static constexpr int TM_Q = D, TM_S = D + NQ * (D / 2);
+};
+
+// Where the copies put a tile, and in how many pieces.  A box is rows of one page (all of it, or 64 of it) and holds the
+// chunks of its rows one after the other.  V comes so: rows are its K index, and any 16 of one page make an MMA step.  K
+// needs its 8-row groups equally far apart: whole boxes one chunk at a time, or all chunks of 8 rows, whichever makes
+// fewer copies.  (One thread issues them; a copy of 16 rows of 128 bytes takes the TMA 70 cycles, one of 64 rows 200, and
+// the kernel needs a tile in about 1400.)
+template <int D, int BOX> struct Boxes {
+    static constexpr int NC = D / 64, P = KT / BOX;  // boxes of a tile
+    static constexpr bool K_BY_CHUNK = P * NC <= KT / 8;
+    static constexpr int K_CHUNK = K_BY_CHUNK ? KT * 128 : 1024, K_GROUP = K_BY_CHUNK ? 1024 : NC * 1024;
+};
+struct Layout {                  // the same for the roles that read the tiles
+    int k_chunk, k_group;        // bytes between K's chunks, and between its 8-row groups
+    int v_rows, log_v_rows;      // rows of a V box
 };
 
 struct Item {
@@ -56,7 +77,7 @@ struct Item {
 };
 
 struct Shared {
-    uint64_t kv_full[16], kv_empty[16], s_full[4], p_full[4], pv_done[4], q_full, o_free, item_full[ITEMS],
+    uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[4], p_full[4], pv_done[4], q_full, o_free, s_free[4], item_full[ITEMS],
         item_empty[ITEMS], hand[2][4], exch[4];
     Item items[ITEMS];
     float m[MT], l[2][2][MT];
@@ -130,10 +151,6 @@ __device__ __forceinline__ int valid_keys(const AttnArgs &a, const Item &it, int
     if (it.b < 0) return min(KT, it.len - kt * KT);
     return kt == it.kts - 1 ? it.n : min(KT, it.len - a.shared_len - kt * KT);
 }
-// position of K_j and V_j of an item of n tiles in the order of the copies: K0 K1 V0 K2 V1 ... K V V
-__device__ __forceinline__ int k_pos(int j) { return j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ int v_pos(int j, int n) { return j < n - 1 ? 2 * j + 2 : 2 * n - 1; }
-
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
 // a wait with one outcome for the whole warp: what follows needs all of its lanes
@@ -144,22 +161,24 @@ __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity)
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
-attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
+attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using C = Cfg<D>;
     extern __shared__ unsigned char smem_raw[];
     __shared__ Shared sh;
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    unsigned char *v_stages = stages + C::NK * C::STAGE, *p_bufs = v_stages + C::NV * C::STAGE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int group = blockIdx.x / R, member = blockIdx.x - group * R, n_groups = gridDim.x / R;
 
     if (tid == 0) {
         ptx::wait_deadline_init(a.wait_cycles);
 #pragma unroll 1
-        for (int i = 0; i < C::NST; ++i) ptx::mbar_init(&sh.kv_full[i], 1), ptx::mbar_init(&sh.kv_empty[i], 1);
+        for (int i = 0; i < 8; ++i)
+            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_empty[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_empty[i], 1);
         for (int i = 0; i < C::NSB; ++i)
-            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
+            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.s_free[i], 4), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
         ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.hand[0][i], 1), ptx::mbar_init(&sh.hand[1][i], 1), ptx::mbar_init(&sh.exch[i], 2);
@@ -251,61 +270,18 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
     if (warp == PRODUCER_K || warp == PRODUCER_V) {
         // ---------------------------------------------------------------- work items and TMA copies: one thread each
         if (ptx::elect_one()) {
-            const bool is_v = warp == PRODUCER_V;
-            const int ps = 1 << a.log_page, box = min(ps, KT), per_tile = KT / box;
-            unsigned base = 0;   // stages of the items before
-            long long newest = -1;  // last stage whose copies were issued
+            const int ps = 1 << a.log_page;
+            unsigned filled = 0;    // tiles whose copies were issued
             int cur_b = -1;
-            // the copies of one item's K tiles or V tiles
-            auto copy_item = [&](const Item &it, unsigned ord) -> bool {
-                const int *table = it.b < 0 ? a.shared_pages : a.c.page_table + (size_t)it.b * a.c.max_pages;
-                const int key0 = it.b < 0 ? 0 : a.shared_len, n = it.tiles;
-                const CUtensorMap *cache = is_v ? &map_vc : &map_kc, *rows = is_v ? &map_v : &map_k;
-                int pages[KT / 8];
-                auto load_pages = [&](int j) {
-                    const int kt = it.kt0 + j;
-                    if (j >= n || (it.b >= 0 && kt == it.kts - 1)) return;
-                    const int first = (key0 + kt * KT) >> a.log_page, end = (it.len + ps - 1) >> a.log_page;
-#pragma unroll
-                    for (int i = 0; i < KT / 8; ++i) pages[i] = i < per_tile && first + i < end ? table[first + i] : -1;
-                };
-                load_pages(0);
-                bool bad = false;
-                for (int j = 0; j < n; ++j) {
-                    const unsigned st_ = base + (is_v ? v_pos(j, n) : k_pos(j)), sidx = st_ % C::NST;
-                    const int kt = it.kt0 + j, token = key0 + kt * KT;
-                    if (st_ >= C::NST && !ptx::mbar_wait(&sh.kv_empty[sidx], (st_ / C::NST - 1) & 1)) return false;
-                    unsigned char *dst = stages + sidx * C::STAGE;
-                    newest = st_;
-                    if (it.b >= 0 && kt == it.kts - 1) {
-                        const int boxes = (it.n + 7) / 8;
-                        ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], boxes * C::NC * 1024u);
-                        for (int i = 0; i < boxes; ++i)
-#pragma unroll
-                            for (int c = 0; c < C::NC; ++c)
-                                ptx::tma_load_2d(dst + c * C::CHUNK + i * 1024, rows, it.h * D + c * 64, it.lo + i * 8, &sh.kv_full[sidx]);
-                    } else {
-                        const int boxes = min(per_tile, (it.len - token + box - 1) / box);
-#pragma unroll
-                        for (int i = 0; i < KT / 8; ++i)  // (one past the pool reads as zeros)
-                            if (i < boxes && (pages[i] < 0 || pages[i] >= a.c.n_pages)) pages[i] = a.c.n_pages, bad = true;
-                        if (bad && !is_v) sh.bad_item[ord % 16] = ord + 1;
-                        ptx::mbar_arrive_expect_tx(&sh.kv_full[sidx], boxes * C::NC * box * 128u);
-#pragma unroll
-                        for (int i = 0; i < KT / 8; ++i) {
-                            if (i >= boxes) break;
-#pragma unroll
-                            for (int c = 0; c < C::NC; ++c)
-                                ptx::tma_load_4d(dst + c * C::CHUNK + i * box * 128, cache, c * 64, token & (ps - 1), it.h, pages[i],
-                                                 &sh.kv_full[sidx]);
-                        }
-                    }
-                    load_pages(j + 1);
-                }
-                base += 2 * n;
-                return true;
-            };
-            auto run = [&]() -> int {  // 0: all done, 1: a wait ran out, 2: stopped on purpose
+            // 0: all done, 1: a wait ran out, 2: stopped on purpose
+            auto run = [&](auto box_, auto is_v_) -> int {
+                constexpr int BOX = decltype(box_)::value;
+                constexpr bool IS_V = decltype(is_v_)::value;
+                using B = Boxes<D, BOX>;
+                const CUtensorMap *cache = IS_V ? &map_vc : &map_kc, *rows_map = IS_V ? &map_v : &map_k;
+                constexpr int NS = IS_V ? C::NV : C::NK;
+                uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *empties = IS_V ? sh.v_empty : sh.k_empty;
+                unsigned char *ring = IS_V ? v_stages : stages;
                 int b = sh.first_b, st2;
                 unsigned off = (unsigned)sh.first_off;
                 long long u = u0;
@@ -314,11 +290,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                 bool fresh = true;
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
-                    Item x;
-                    if (!is_v) {
+                    Item it;
+                    if constexpr (!IS_V) {
                         // the next item that has tiles here and rows for this member of the group; 0 tiles: the end
-                        x.tiles = 0;
-                        while (u < u1 && x.tiles == 0) {
+                        it.tiles = 0;
+                        while (u < u1 && it.tiles == 0) {
                             if (fresh || off >= s.units) {  // (a sequence without work has no units)
                                 if (!fresh) off = 0, ++b;
                                 fresh = false;
@@ -332,30 +308,112 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                             const long long row0 = (long long)(rg * R + member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
                             off += span, u += span;
                             if (row0 >= rows) continue;
-                            x.b = b, x.h = h, x.lo = s.lo, x.n = s.n, x.len = s.len;
-                            x.row0 = (int)row0, x.rows = (int)min((long long)MT, rows - row0);
-                            x.kt0 = kt0, x.tiles = kt1 - kt0, x.kts = s.kts;
-                            x.slot = kt0 == 0 && kt1 == s.kts ? -1 : slot_of(group, begin, u0);
+                            it.b = b, it.h = h, it.lo = s.lo, it.n = s.n, it.len = s.len;
+                            it.row0 = (int)row0, it.rows = (int)min((long long)MT, rows - row0);
+                            it.kt0 = kt0, it.tiles = kt1 - kt0, it.kts = s.kts;
+                            it.slot = kt0 == 0 && kt1 == s.kts ? -1 : slot_of(group, begin, u0);
                         }
                         if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
-                        sh.items[r] = x;
+                        sh.items[r] = it;
                         ptx::mbar_arrive(&sh.item_full[r]);
                     } else {
                         if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return 1;
-                        x = sh.items[r];
-                        if (x.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
+                        it = sh.items[r];
+                        if (it.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
                     }
-                    if (x.tiles == 0) return 0;
-                    cur_b = x.b;
-                    if (x.b >= 0 && x.b * a.c.H_kv + x.h == a.skip_item) return 2;  // (test hook)
-                    if (!copy_item(x, ord)) return 1;
+                    if (it.tiles == 0) return 0;
+                    cur_b = it.b;
+                    if (it.b >= 0 && it.b * a.c.H_kv + it.h == a.skip_item) return 2;  // (test hook)
+
+                    const int n = it.tiles, key0 = it.b < 0 ? 0 : a.shared_len;
+                    const int *table = it.b < 0 ? a.shared_pages : a.c.page_table + (size_t)it.b * a.c.max_pages;
+                    // whole tiles of cached tokens; the last of an item may be short, and then there are the draft rows
+                    const int whole = (it.len - key0) / KT - it.kt0;
+                    int pages[B::P];
+                    auto load_pages = [&](int j) {
+                        const int *t = table + ((key0 + (it.kt0 + j) * KT) >> a.log_page);
+                        if (j < n && j < whole)
+#pragma unroll
+                            for (int i = 0; i < B::P; ++i) pages[i] = t[i];
+                    };
+                    load_pages(0);
+                    bool bad = false;
+                    for (int j = 0; j < n; ++j) {
+                        const unsigned sidx = filled % NS;
+                        const int kt = it.kt0 + j, token = key0 + kt * KT, slot0 = token & (ps - 1);
+                        if (filled >= NS && !ptx::mbar_wait(&empties[sidx], (filled / NS - 1) & 1)) return 1;
+                        ++filled;
+                        unsigned char *dst = ring + sidx * C::STAGE;
+                        uint64_t *full = &fulls[sidx];
+                        if (j < whole) {
+                            bool out = false;
+#pragma unroll
+                            for (int i = 0; i < B::P; ++i) out |= (unsigned)pages[i] >= (unsigned)a.c.n_pages;
+                            if (out) {  // (one past the pool reads as zeros)
+                                bad = true;
+#pragma unroll
+                                for (int i = 0; i < B::P; ++i)
+                                    if ((unsigned)pages[i] >= (unsigned)a.c.n_pages) pages[i] = a.c.n_pages;
+                            }
+                            if (bad && !IS_V) sh.bad_item[ord % 16] = ord + 1;
+                            ptx::mbar_arrive_expect_tx(full, C::STAGE);
+                            if constexpr (IS_V) {
+#pragma unroll
+                                for (int i = 0; i < B::P; ++i)
+                                    ptx::tma_load_5d(dst + i * (BOX * C::NC * 128), cache, 0, slot0, 0, it.h, pages[i], full);
+                            } else if constexpr (B::K_BY_CHUNK) {
+#pragma unroll
+                                for (int i = 0; i < B::P; ++i)
+#pragma unroll
+                                    for (int c = 0; c < C::NC; ++c)
+                                        ptx::tma_load_5d(dst + i * (BOX * 128) + c * B::K_CHUNK, cache, 0, slot0, c, it.h, pages[i], full);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < KT / 8; ++i)
+                                    ptx::tma_load_5d(dst + i * B::K_GROUP, cache, 0, (8 * i) % BOX, 0, it.h, pages[8 * i / BOX], full);
+                            }
+                        } else if (it.b >= 0 && kt == it.kts - 1) {  // draft rows, 8 and one chunk at a time
+                            const int groups = (it.n + 7) / 8;
+                            ptx::mbar_arrive_expect_tx(full, groups * C::NC * 1024u);
+#pragma unroll 1
+                            for (int i = 0; i < groups; ++i) {
+                                unsigned char *to = dst + (IS_V ? (8 * i / BOX) * (BOX * C::NC * 128) + (8 * i % BOX) * 128 : i * B::K_GROUP);
+#pragma unroll
+                                for (int c = 0; c < C::NC; ++c)
+                                    ptx::tma_load_2d(to + c * (IS_V ? BOX * 128 : B::K_CHUNK), rows_map, it.h * D + c * 64, it.lo + i * 8, full);
+                            }
+                        } else {  // the short tile
+                            constexpr int ROWS = IS_V || B::K_BY_CHUNK ? BOX : 8, COPIES = !IS_V && B::K_BY_CHUNK ? C::NC : 1;
+                            const int boxes = (it.len - token + ROWS - 1) / ROWS;
+                            for (int i = 0; i < boxes; ++i) bad |= (unsigned)table[(token + i * ROWS) >> a.log_page] >= (unsigned)a.c.n_pages;
+                            if (bad && !IS_V) sh.bad_item[ord % 16] = ord + 1;
+                            ptx::mbar_arrive_expect_tx(full, boxes * ROWS * C::NC * 128u);
+#pragma unroll 1
+                            for (int i = 0; i < boxes; ++i) {
+                                int page = table[(token + i * ROWS) >> a.log_page];
+                                if ((unsigned)page >= (unsigned)a.c.n_pages) page = a.c.n_pages;
+#pragma unroll
+                                for (int c = 0; c < COPIES; ++c)
+                                    ptx::tma_load_5d(dst + i * (COPIES > 1 ? BOX * 128 : ROWS * C::NC * 128) + c * B::K_CHUNK, cache, 0,
+                                                     (token + i * ROWS) & (ps - 1), c, it.h, page, full);
+                            }
+                        }
+                        load_pages(j + 1);
+                    }
                 }
             };
-            const int rc = run();
+            auto run_box = [&](auto box_) { return warp == PRODUCER_V ? run(box_, std::true_type{}) : run(box_, std::false_type{}); };
+            const int rc = lay.v_rows == 8    ? run_box(std::integral_constant<int, 8>{})
+                           : lay.v_rows == 16 ? run_box(std::integral_constant<int, 16>{})
+                           : lay.v_rows == 32 ? run_box(std::integral_constant<int, 32>{})
+                                              : run_box(std::integral_constant<int, 64>{});
             if (rc == 1) fail(cur_b);
-            if (rc != 0)  // copies in flight have to land before the CTA may leave
-                for (long long i = max(0ll, newest - (C::NST - 1)); i <= newest; ++i)
-                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.kv_full[i % C::NST], (unsigned)(i / C::NST) & 1); ++t) __nanosleep(20);
+            if (rc != 0) {  // copies in flight have to land before the CTA may leave
+                const unsigned ns = warp == PRODUCER_V ? C::NV : C::NK;
+                uint64_t *fulls = warp == PRODUCER_V ? sh.v_full : sh.k_full;
+                for (unsigned i = filled > ns ? filled - ns : 0; i < filled; ++i)
+                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&fulls[i % ns], (i / ns) & 1); ++t) __nanosleep(20);
+            }
         }
         __syncwarp();
     } else if (warp == MMA_QK || warp == MMA_PV) {
@@ -366,7 +424,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
             uint64_t *newest = nullptr;  // barrier of the last commit, and its phase
             unsigned newest_phase = 0;
             auto run = [&]() -> bool {
-                unsigned base = 0, tile = 0;  // stages and tiles of the items before
+                unsigned tile = 0;  // tiles of the items before
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
                     if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return false;
@@ -378,39 +436,45 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                     if (warp == MMA_QK) {
                         if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                         for (int j = 0; j < n; ++j) {
-                            const unsigned st_ = base + k_pos(j), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
-                            if (g >= C::NSB && !ptx::mbar_wait(&sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
-                            if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                            const unsigned g = tile + j, sidx = g % C::NK, buf = g % C::NSB;
+                            if (g >= C::NSB && !ptx::mbar_wait(C::P_SMEM ? &sh.s_free[buf] : &sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
+                            if (!ptx::mbar_wait(&sh.k_full[sidx], (g / C::NK) & 1)) return false;
                             ptx::tc_fence_after_sync();
                             const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
 #pragma unroll
                             for (int s = 0; s < D / 16; ++s)
                                 ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + (ord % C::NQ) * (D / 2) + s * 8,
-                                                  ptx::umma_desc_k_sw128(kaddr + (s / 4) * C::CHUNK + (s % 4) * 32), idesc_qk, s > 0);
+                                                  ptx::umma_desc_k_sw128(kaddr + (s / 4) * lay.k_chunk + (s % 4) * 32, lay.k_group), idesc_qk, s > 0);
                             ptx::umma_commit(&sh.s_full[buf]);
-                            ptx::umma_commit(&sh.kv_empty[sidx]);
+                            ptx::umma_commit(&sh.k_empty[sidx]);
                             newest = &sh.s_full[buf], newest_phase = (g / C::NSB) & 1;
                         }
                     } else {
                         for (int j = 0; j < n; ++j) {
-                            const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST, g = tile + j, buf = g % C::NSB;
-                            if (!ptx::mbar_wait(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
+                            const unsigned g = tile + j, sidx = g % C::NV, buf = g % C::NSB;
+                            if (!ptx::mbar_wait(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
                             if (j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free, (ord - 1) & 1)) return false;
                             if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
                             ptx::tc_fence_after_sync();
-                            const uint32_t vaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+                            const uint32_t vaddr = ptx::smem_u32(v_stages + sidx * C::STAGE);
                             const int steps = (valid_keys(a, it, it.kt0 + j) + 15) / 16;
 #pragma unroll
                             for (int s = 0; s < KT / 16; ++s)
-                                if (s < steps)
-                                    ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8,
-                                                      ptx::umma_desc_mn_sw128(vaddr + s * 2048, C::CHUNK), idesc_pv, j > 0 || s > 0);
+                                if (s < steps) {
+                                    const uint32_t at = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
+                                    const uint64_t vd = ptx::umma_desc_mn_sw128(vaddr + at, lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
+                                    if (C::P_SMEM)
+                                        ptx::umma_bf16(tmem, ptx::umma_desc_k_sw128(ptx::smem_u32(p_bufs + (g & 1) * C::P_BYTES) + s * 32), vd,
+                                                       idesc_pv, j > 0 || s > 0);
+                                    else
+                                        ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8, vd, idesc_pv, j > 0 || s > 0);
+                                }
                             ptx::umma_commit(&sh.pv_done[buf]);
-                            ptx::umma_commit(&sh.kv_empty[sidx]);
+                            ptx::umma_commit(&sh.v_empty[sidx]);
                             newest = &sh.pv_done[buf], newest_phase = (g / C::NSB) & 1;
                         }
                     }
-                    base += 2 * n, tile += n;
+                    tile += n;
                 }
             };
             if (!run()) {
@@ -464,7 +528,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
             return true;
         };
         auto run = [&]() -> bool {
-            unsigned base = 0, tile = 0, handed = 0;  // handed: hand-overs of the maxima this warpgroup has received
+            unsigned tile = 0, handed = 0;  // handed: hand-overs of the maxima this warpgroup has received
             Mine me{&sh.items[0], 0, 0, 0}, next;
             bool have = false;                        // the hand-over before this warpgroup's next tile is in
             int n = 0;
@@ -518,6 +582,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                         ptx::tmem_ld32(ts, *reinterpret_cast<uint32_t(*)[32]>(&raw[0]));
                         ptx::tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&raw[32]));
                         ptx::tmem_wait_ld();
+                        if (C::P_SMEM) ptx::tc_fence_before_sync();
+                    }
+                    if (C::P_SMEM) ptx::mbar_arrive_warp(&sh.s_free[buf]);
+                    if (warp_on) {
                         float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                         for (int i = 0; i < KT; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(raw[i]));
@@ -544,24 +612,38 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                             // weights as bf16: at most 2^-8 of each, independent from key to key
                             raw[i / 2] = pack_bf16(x, y);
                         }
-                        ptx::tmem_st16(ts, *reinterpret_cast<const uint32_t(*)[16]>(&raw[0]));
-                        ptx::tmem_st16(ts + 16, *reinterpret_cast<const uint32_t(*)[16]>(&raw[16]));
+                        if (!C::P_SMEM) {
+                            ptx::tmem_st16(ts, *reinterpret_cast<const uint32_t(*)[16]>(&raw[0]));
+                            ptx::tmem_st16(ts + 16, *reinterpret_cast<const uint32_t(*)[16]>(&raw[16]));
+                        }
                         if (m != m_l) l *= ptx::ex2(m_l - ref);
                         m_l = m;
                         l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+                    }
+                    if (C::P_SMEM) {
+                        if (g >= 2 && !wait_warp(&sh.pv_done[buf], (g / 2 - 1) & 1)) return false;  // the buffer's last reader
+                        if (warp_on) {  // row of 128 bytes, swizzled as the MMA reads it
+                            unsigned char *p = p_bufs + (g & 1) * C::P_BYTES + row * 128;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<uint4 *>(p + ((i ^ (row & 7)) * 16)) =
+                                    make_uint4(raw[4 * i], raw[4 * i + 1], raw[4 * i + 2], raw[4 * i + 3]);
+                            ptx::fence_proxy_async();
+                        }
                     }
                     if (draft || valid < KT) {
                         // Rows of V that no weight may meet: past the end (left over from the stage's last use, or the
                         // page's unused slots), and draft rows with NaN or infinity, which the epilogue adds where they
                         // are seen.  A zero weight would make NaN of them.
-                        const unsigned st_ = base + v_pos(j, n), sidx = st_ % C::NST;
-                        if (!wait_warp(&sh.kv_full[sidx], (st_ / C::NST) & 1)) return false;
-                        unsigned char *v = stages + sidx * C::STAGE;
+                        const unsigned sidx = g % C::NV;
+                        if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
+                        unsigned char *v = v_stages + sidx * C::STAGE;
                         const int upto = (valid + 15) / 16 * 16;
                         constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
                         for (int i = (draft ? 0 : valid * VR) + w4 * 32 + lane; i < upto * VR; i += 128) {
                             const int key = i / VR, c = i - key * VR;
-                            uint4 *p = reinterpret_cast<uint4 *>(v + (c >> 3) * C::CHUNK + key * 128 + (c & 7) * 16);
+                            uint4 *p = reinterpret_cast<uint4 *>(v + (key >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) +
+                                                                 ((c >> 3) * lay.v_rows + (key & (lay.v_rows - 1))) * 128 + (c & 7) * 16);
                             if (key >= valid) {
                                 *p = make_uint4(0, 0, 0, 0);
                                 continue;
@@ -609,6 +691,9 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                 ptx::mbar_arrive_warp(&sh.exch[w4]);
                 if (!wait_warp(&sh.exch[w4], ord & 1)) return false;
                 l += sh.l[ord & 1][wg ^ 1][row];
+                // (a parity names a phase only to who has seen the one before it: where Q K^T does not wait for P V, the
+                // product before the last comes first)
+                if (C::P_SMEM && last > 0 && !wait_warp(&sh.pv_done[(last - 1) % C::NSB], ((last - 1) / C::NSB) & 1)) return false;
                 if (!wait_warp(&sh.pv_done[last % C::NSB], (last / C::NSB) & 1)) return false;
                 ptx::tc_fence_after_sync();
                 const bool bad = sh.bad_item[ord % 16] == ord + 1;
@@ -686,7 +771,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, const __grid_co
                 if (lane == 0) ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
                 }
                 if (next.it->tiles == 0) return true;
-                base += 2 * n, tile += n;
+                tile += n;
                 me = next, n = me.it->tiles, cur_b = me.it->b;
             }
         };
@@ -899,25 +984,35 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     if (!enc) return cudaErrorNotSupported;
     CUtensorMap kc, vc, k, v;
     const CacheView &c = a.c;
-    auto cache_map = [&](CUtensorMap *m, const void *base) {
-        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)c.page_size, (cuuint64_t)c.H_kv, (cuuint64_t)c.n_pages};
+    const int box = c.page_size < KT ? c.page_size : KT;
+    Layout lay;
+    lay.v_rows = box;
+    for (lay.log_v_rows = 3; (1 << lay.log_v_rows) < box; ++lay.log_v_rows) {}
+    bool by_chunk = false;
+    auto lay_k = [&](auto b) { by_chunk = decltype(b)::K_BY_CHUNK, lay.k_chunk = decltype(b)::K_CHUNK, lay.k_group = decltype(b)::K_GROUP; };
+    if (box == 8) lay_k(Boxes<D, 8>{});
+    else if (box == 16) lay_k(Boxes<D, 16>{});
+    else if (box == 32) lay_k(Boxes<D, 32>{});
+    else lay_k(Boxes<D, 64>{});
+    auto cache_map = [&](CUtensorMap *m, const void *base, int rows, int chunks) {
+        const cuuint64_t dims[5] = {64, (cuuint64_t)c.page_size, (cuuint64_t)C::NC, (cuuint64_t)c.H_kv, (cuuint64_t)c.n_pages};
         // (the stride of a dimension of one does not count, but has to be a legal one)
-        const cuuint64_t strides[3] = {(cuuint64_t)c.stride_slot * 2, c.H_kv > 1 ? (cuuint64_t)c.stride_head * 2 : 16,
+        const cuuint64_t strides[4] = {(cuuint64_t)c.stride_slot * 2, 128, c.H_kv > 1 ? (cuuint64_t)c.stride_head * 2 : 16,
                                        c.n_pages > 1 ? (cuuint64_t)c.stride_page * 2 : 16};
-        const cuuint32_t box[4] = {64, (cuuint32_t)(c.page_size < KT ? c.page_size : KT), 1, 1}, es[4] = {1, 1, 1, 1};
-        return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es,
+        const cuuint32_t bx[5] = {64, (cuuint32_t)rows, (cuuint32_t)chunks, 1, 1}, es[5] = {1, 1, 1, 1, 1};
+        return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, bx, es,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const uint64_t cols = (uint64_t)c.H_kv * D;
-    if (!cache_map(&kc, c.k) || !cache_map(&vc, c.v) ||
+    if (!cache_map(&kc, c.k, by_chunk ? box : 8, by_chunk ? 1 : C::NC) || !cache_map(&vc, c.v, box, C::NC) ||
         !tma_make_map_bf16(enc, &k, a.k, cols, a.T, a.ld_k * 2, 64, 8, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !tma_make_map_bf16(enc, &v, a.v, cols, a.T, a.ld_v * 2, 64, 8, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    const int smem = C::NST * C::STAGE + 1024;
+    const int smem = (C::NK + C::NV) * C::STAGE + 2 * C::P_BYTES + 1024;
     e = ensure_dynamic_smem(reinterpret_cast<const void *>(attn_tc_kernel<D>), smem, dev);
     if (e != cudaSuccess) return e;
-    e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, kc, vc, k, v);
+    e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, lay, kc, vc, k, v);
     if (e != cudaSuccess) return e;
     if (a.shared_len > 0) {
         const unsigned x = (unsigned)(((long long)a.max_nodes * a.G + 31) / 32);

@@ -385,23 +385,28 @@ __device__ __forceinline__ float bf16_hi(float x) { return __bfloat162float(__fl
 namespace treewy {
 namespace ptx {
 
-// tiled 4-D tensor-map load (no multicast), coordinates innermost first; x * element size must be a
+// tiled 5-D tensor-map load (no multicast), coordinates innermost first; x * element size must be a
 // multiple of 16 bytes.
-__device__ __forceinline__ void tma_load_4d(void *dst_smem, const void *tmap, int x, int y, int z, int w, uint64_t *bar)
+__device__ __forceinline__ void tma_load_5d(void *dst_smem, const void *tmap, int x, int y, int z, int w, int v, uint64_t *bar)
 {
     asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], "
-        "[%6];" ::"r"(smem_u32(dst_smem)),
-        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+        "[%7];" ::"r"(smem_u32(dst_smem)),
+        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(smem_u32(bar))
         : "memory");
 }
-// Shared-memory matrix descriptor, MN-major operand (its rows, 64 bf16 = 128 bytes of consecutive M / N, are the
-// K index) with the 128-byte swizzle the TMA writes: 8-row groups along K are 1024 bytes apart (stride byte
-// offset), neighbouring 64-element chunks along M / N `chunk` bytes (leading byte offset).  Stepping 16 along K adds
-// 2048 bytes.
-__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t addr, uint32_t chunk)
+// umma_desc_k_sw128 with 8-row groups `group` bytes apart
+__device__ __forceinline__ uint64_t umma_desc_k_sw128(uint32_t addr, uint32_t group)
 {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(chunk >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(group >> 4) << 32) | ((uint64_t)1 << 46) |
+           ((uint64_t)2 << 61);
+}
+// Shared-memory matrix descriptor, MN-major operand (its rows, 64 bf16 = 128 bytes of consecutive M / N, are the
+// K index) with the 128-byte swizzle the TMA writes: 8-row groups along K are `group` bytes apart (stride byte
+// offset), neighbouring 64-element chunks along M / N `chunk` bytes (leading byte offset).
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t addr, uint32_t chunk, uint32_t group)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(chunk >> 4) << 16) | ((uint64_t)(group >> 4) << 32) |
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 // Instruction descriptor of umma_idesc_bf16_f32 with an MN-major B operand.

@@ -198,6 +198,49 @@ def test_random_batches(seed):
     au.assert_attn(c, O, ref, size, tensor_cores=True)
 
 
+@pytest.mark.parametrize("D,page,nodes,Hkv,shared", [(64, 16, 1, 8, 0), (128, 8, 3, 4, 0), (128, 32, 64, 2, 640), (256, 16, 16, 2, 0),
+                                                     (256, 64, 5, 4, 0), (256, 8, 24, 1, 512), (256, 128, 64, 1, 0)])
+def test_long_runs_of_tiles(D, page, nodes, Hkv, shared):
+    """Batches that keep every CTA at work for dozens of tiles and several items, against the SIMT kernel (which the
+    tests above tie to 64 bits): both are within their bounds of the same value."""
+    from paper_2608_20961_b200 import attention as at, binding as tw
+    B, G = 12, 4
+    rng = np.random.default_rng(D + page)
+    gen = torch.Generator(device=DEV).manual_seed(D + page)
+    L = [int(x) for x in rng.integers(shared, 9000, B)]
+    N = [int(x) for x in rng.integers((nodes + 1) // 2, nodes + 1, B)]
+    T = sum(N)
+    need = [-(-n // page) for n in L]
+    n_pages = sum(need) + 1
+    table = torch.zeros((B, max(need)), dtype=torch.int32)
+    order, k0 = torch.from_numpy(rng.permutation(n_pages).astype(np.int32)), 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[k0:k0 + n]
+        k0 += n
+    table[:, :shared // page] = table[0, :shared // page].clone()
+    rand = lambda *s: torch.randn(s, generator=gen, device=DEV, dtype=BF16)
+    cache = at.KVCache(rand(n_pages, page, Hkv, D), rand(n_pages, page, Hkv, D), table.to(DEV), torch.tensor(L, dtype=torch.int32, device=DEV))
+    trees = [au.random_tree(n, rng) for n in N]
+    off = torch.tensor(np.concatenate([[0], np.cumsum(N)]), dtype=torch.int32, device=DEV)
+    tree = tw.Tree.empty(off, torch.tensor(sum((t[0] for t in trees), []), dtype=torch.int32, device=DEV), 1, nodes)
+    tree.anc_mask = torch.from_numpy(np.array(sum((t[1] for t in trees), []), np.uint64).view(np.int64)).to(DEV)
+    q, k, v = rand(T, Hkv * G, D), rand(T, Hkv, D), rand(T, Hkv, D)
+    ws = at.attn_workspace(cache, tree, Hkv * G, shared)
+    pages = table[0, :shared // page].contiguous().to(DEV) if shared else None
+    outs = []
+    for generic in (False, False, True):
+        O = torch.zeros((T, Hkv * G, D), dtype=BF16, device=DEV)
+        status = torch.zeros(B, dtype=torch.int32, device=DEV)
+        at.treewy_attn_verify(cache, tree, q, k, v, D ** -0.5, O, ws, pages, shared, status, generic=generic)
+        assert not status.any()
+        outs.append(O.double())
+    assert torch.equal(outs[0], outs[1])
+    # the weights' rounding is independent from key to key, so it adds up as a square root: per row, 2^-8 of the output's
+    # own size twice over (weights, store) and once for the SIMT kernel's store
+    err = (outs[0] - outs[2]).norm(dim=-1) / outs[2].norm(dim=-1)
+    assert float(err.max()) <= 3 * au.BF16_HALF_ULP, float(err.max())
+
+
 def test_cache_offsets_past_32_bits():
     """A pool of more than 2^32 elements (and bytes), the sequences' pages at its far end."""
     from paper_2608_20961_b200 import attention as at
