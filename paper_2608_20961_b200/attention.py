@@ -69,19 +69,42 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _int32(t: torch.Tensor | None, n: int, what: str) -> None:
-    _require(t is None or (t.dtype == torch.int32 and t.numel() >= n and t.is_contiguous()),
-             f"{what}: contiguous int32 tensor of at least {n} elements wanted")
+def _int32(t: torch.Tensor | None, n: int, what: str) -> int | None:
+    """Checks an optional int32 array; returns its address."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 tensor of at least {n} elements wanted")
+    return t.data_ptr()
 
 
 def _rows(x: torch.Tensor, T: int, H: int, d: int, dtype: torch.dtype, what: str) -> int:
     """Checks packed rows [T, H, d] (heads contiguous, tokens at any distance); returns that distance."""
-    if x.dtype != dtype or x.dim() != 3 or tuple(x.shape[1:]) != (H, d) or x.shape[0] < T:
-        raise ValueError(f"{what}: {dtype} [{T}, {H}, {d}] wanted, got {x.dtype} {list(x.shape)}")
-    st = x.stride()
-    if (d > 1 and st[2] != 1) or (H > 1 and st[1] != d):
+    shape, st = x.shape, x.stride()
+    if x.dtype is not dtype or len(shape) != 3 or shape[1] != H or shape[2] != d or shape[0] < T:
+        raise ValueError(f"{what}: {dtype} [{T}, {H}, {d}] wanted, got {x.dtype} {list(shape)}")
+    if (st[2] != 1 and d > 1) or (st[1] != d and H > 1):
         raise ValueError(f"{what}: the heads of a token have to be contiguous")
-    return st[0] if x.shape[0] > 1 else H * d
+    return st[0] if shape[0] > 1 else H * d
+
+
+# (These calls are a few microseconds of GPU work in a decoding step, so the host side is kept short: raw addresses,
+# structs built once where the object is kept, the stream's handle without a Stream object.)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream, x: torch.Tensor) -> int | None:
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and x.is_cuda:
+        return _raw_stream(x.get_device())
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _tree_ref(tree: Tree):
+    """The tree's struct.  Its arrays may be replaced between calls, so it is built for each."""
+    return ctypes.byref(tw.TreeStruct(tree.B, tree.T, tree.H_v, tree.max_nodes, tree.node_offsets.data_ptr(),
+                                      tree.parent.data_ptr(), None, tree.anc_mask.data_ptr(), None, None))
 
 
 class KVCache:
@@ -135,11 +158,12 @@ def treewy_rope(rope: Rope, x: torch.Tensor, y: torch.Tensor, inverse: bool = Fa
                 row_status: torch.Tensor | None = None, stream=None) -> None:
     """y [T, H, d] <- x rotated by its tokens' positions (inverse: the other way, which is the backward pass)."""
     T, H, d = x.shape
-    _require(T == rope.T, f"x: {rope.T} tokens wanted, as rope.positions has")
-    _require(x.dtype in tw._DTYPES, "x: bfloat16 or float32 wanted")
+    dt = tw._DTYPES.get(x.dtype)
+    if T != rope.T or dt is None:
+        raise ValueError(f"x: bfloat16 or float32, {rope.T} tokens as rope.positions has, wanted")
     ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x"), _rows(y, T, H, d, x.dtype, "y")
-    tw._call("treewy_rope", load_library().treewy_rope, rope._ref, tw._p(x), ld_x, tw._p(y), ld_y, T, H, d,
-             int(inverse), tw._DTYPES[x.dtype], tw._p(row_status), tw._stream(stream))
+    tw._call("treewy_rope", load_library().treewy_rope, rope._ref, x.data_ptr(), ld_x, y.data_ptr(), ld_y, T, H, d,
+             int(inverse), dt, _int32(row_status, 1, "row_status"), _stream(stream, x))
 
 
 def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -147,27 +171,26 @@ def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor,
                      seq_status: torch.Tensor | None = None, stream=None) -> None:
     """Rows k, v [T, H_kv, d] of the sequences at row_offsets [B + 1] go behind context_len of each sequence's
     cache, k rotated on the way; q [T, H_q, d], when given, is rotated into q_out in the same pass."""
-    T = int(k.shape[0])
-    _int32(row_offsets, cache.B + 1, "row_offsets")
-    _int32(seq_status, cache.B, "seq_status")
-    _require(rope is None or rope.T == T, "rope: as many positions as rows wanted")
-    ld_k = _rows(k, T, cache.H_kv, cache.d_head, cache.dtype, "k")
-    ld_v = _rows(v, T, cache.H_kv, cache.d_head, cache.dtype, "v")
+    T, H_kv, d, dtype = k.shape[0], cache.H_kv, cache.d_head, cache.dtype
+    if rope is not None and rope.T != T:
+        raise ValueError("rope: as many positions as rows wanted")
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
     H_q = ld_q = ld_qo = 0
+    q_at = qo_at = None
     if q is not None:
-        _require(q_out is not None, "q_out: wanted with q")
-        H_q = int(q.shape[1])
-        ld_q = _rows(q, T, H_q, cache.d_head, cache.dtype, "q")
-        ld_qo = _rows(q_out, T, H_q, cache.d_head, cache.dtype, "q_out")
+        if q_out is None:
+            raise ValueError("q_out: wanted with q")
+        H_q = q.shape[1]
+        ld_q, ld_qo = _rows(q, T, H_q, d, dtype, "q"), _rows(q_out, T, H_q, d, dtype, "q_out")
+        q_at, qo_at = q.data_ptr(), q_out.data_ptr()
     tw._call("treewy_kv_append", load_library().treewy_kv_append, cache._ref, None if rope is None else rope._ref, cache.B, T,
-             tw._p(row_offsets), tw._p(k), ld_k, tw._p(v), ld_v, H_q, tw._p(q), ld_q, tw._p(q_out), ld_qo, cache._dt,
-             tw._p(seq_status), tw._stream(stream))
+             _int32(row_offsets, cache.B + 1, "row_offsets"), k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, q_at, ld_q, qo_at,
+             ld_qo, cache._dt, _int32(seq_status, cache.B, "seq_status"), _stream(stream, k))
 
 
 def attn_workspace(cache: KVCache, tree: Tree, H_q: int, shared_len: int = 0) -> torch.Tensor:
     """A workspace for ``treewy_attn_verify`` calls of these sizes (one per call in flight)."""
-    ts = tree.struct()
-    n = load_library().treewy_attn_workspace(cache._ref, ctypes.byref(ts), H_q, shared_len, cache._dt)
+    n = load_library().treewy_attn_workspace(cache._ref, _tree_ref(tree), H_q, shared_len, cache._dt)
     return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=cache.k.device)
 
 
@@ -178,20 +201,20 @@ def treewy_attn_verify(cache: KVCache, tree: Tree, q: torch.Tensor, k: torch.Ten
     """O [T, H_q, d] <- attention of every draft node (q, k, v: packed rows) over its sequence's cached tokens
     and its ancestors."""
     lib = load_library()
-    ts = tree.struct()
-    T, H_q = tree.T, int(q.shape[1])
-    _require(tree.B == cache.B, "tree: another number of sequences than the cache's page table")
-    ld_q = _rows(q, T, H_q, cache.d_head, cache.dtype, "q")
-    ld_k = _rows(k, T, cache.H_kv, cache.d_head, cache.dtype, "k")
-    ld_v = _rows(v, T, cache.H_kv, cache.d_head, cache.dtype, "v")
-    _require(T == 0 or _rows(O, T, H_q, cache.d_head, cache.dtype, "O") == H_q * cache.d_head, "O: contiguous rows wanted")
-    _int32(shared_pages, shared_len // cache.page_size, "shared_pages")
-    _int32(seq_status, cache.B, "seq_status")
-    name = "treewy_attn_verify_generic" if generic else "treewy_attn_verify"
-    tw._call(name, lib.treewy_attn_verify_generic if generic else lib.treewy_attn_verify, cache._ref, ctypes.byref(ts),
-             tw._p(q), ld_q, tw._p(k), ld_k, tw._p(v), ld_v, H_q, scale, tw._p(shared_pages), shared_len, cache._dt,
-             tw._p(O), tw._p(workspace), workspace.numel() * workspace.element_size(), tw._p(seq_status),
-             tw._stream(stream))
+    T, H_kv, d, dtype = tree.T, cache.H_kv, cache.d_head, cache.dtype
+    H_q = q.shape[1]
+    if tree.B != cache.B:
+        raise ValueError("tree: another number of sequences than the cache's page table")
+    ld_q = _rows(q, T, H_q, d, dtype, "q")
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
+    if _rows(O, T, H_q, d, dtype, "O") != H_q * d and T > 0:
+        raise ValueError("O: contiguous rows wanted")
+    fn = lib.treewy_attn_verify_generic if generic else lib.treewy_attn_verify
+    tw._call("treewy_attn_verify_generic" if generic else "treewy_attn_verify", fn, cache._ref, _tree_ref(tree),
+             q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, scale,
+             _int32(shared_pages, shared_len // cache.page_size, "shared_pages"), shared_len, cache._dt, O.data_ptr(),
+             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _int32(seq_status, cache.B, "seq_status"),
+             _stream(stream, q))
 
 
 def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tensor, accepted: torch.Tensor,
@@ -199,12 +222,10 @@ def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tenso
                      stream=None) -> None:
     """The accepted path's rows of k, v [T, H_kv, d] go behind context_len; new_context_len [B] receives the
     lengths after it."""
-    ts = tree.struct()
-    _require(tree.B == cache.B, "tree: another number of sequences than the cache's page table")
-    ld_k = _rows(k, tree.T, cache.H_kv, cache.d_head, cache.dtype, "k")
-    ld_v = _rows(v, tree.T, cache.H_kv, cache.d_head, cache.dtype, "v")
-    _int32(accepted, cache.B, "accepted")
-    _int32(new_context_len, cache.B, "new_context_len")
-    _int32(seq_status, cache.B, "seq_status")
-    tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, ctypes.byref(ts), tw._p(k), ld_k, tw._p(v),
-             ld_v, tw._p(accepted), cache._dt, tw._p(new_context_len), tw._p(seq_status), tw._stream(stream))
+    if tree.B != cache.B:
+        raise ValueError("tree: another number of sequences than the cache's page table")
+    B, T, H_kv, d, dtype = cache.B, tree.T, cache.H_kv, cache.d_head, cache.dtype
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
+    tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, _tree_ref(tree), k.data_ptr(), ld_k, v.data_ptr(),
+             ld_v, _int32(accepted, B, "accepted"), cache._dt, _int32(new_context_len, B, "new_context_len"),
+             _int32(seq_status, B, "seq_status"), _stream(stream, k))

@@ -40,7 +40,8 @@ treewy_status_t check_rope(const treewy_rope_t *r, int T, int d, int inverse, Ro
     if (!r) return TREEWY_ERR_INVALID_ARG;
     if (r->n_axes < 1 || r->max_positions < 1 || r->rot_dim < 2) return TREEWY_ERR_INVALID_ARG;
     if (r->rot_dim % 2 != 0 || r->rot_dim > d || r->n_axes > 32) return TREEWY_ERR_UNSUPPORTED;
-    if (T > 0 && (bad_ptr(r->cos_sin) || bad_ptr(r->positions))) return TREEWY_ERR_INVALID_ARG;
+    if (T > 0 && (bad_ptr(r->cos_sin) || bad_ptr(r->positions) || (r->pair_axis && misaligned(r->pair_axis))))
+        return TREEWY_ERR_INVALID_ARG;
     *out = {r->cos_sin, r->positions, r->pair_axis, r->n_axes, r->max_positions, r->rot_dim, r->interleaved ? 1 : 0,
             inverse ? 1 : 0};
     return TREEWY_OK;

@@ -12,13 +12,13 @@
 namespace treewy {
 namespace {
 
-constexpr int ROWS_WARPS = 8;
-constexpr int HEAD_UNROLL = 4;  // heads a lane has in flight
+constexpr int ROWS_WARPS = 4;
+constexpr int HEAD_UNROLL = 2;  // heads a lane has in flight
 
 template <typename T, int VE> struct Vec;
 template <> struct Vec<__nv_bfloat16, 8> {
     uint4 x;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { x = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { x = __ldcs(reinterpret_cast<const uint4 *>(p)); }
     __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = x; }
     __device__ __forceinline__ void get(float (&f)[8]) const { widen8(x, f); }
     __device__ __forceinline__ void set(const float (&f)[8])
@@ -28,7 +28,7 @@ template <> struct Vec<__nv_bfloat16, 8> {
 };
 template <> struct Vec<float, 4> {
     float4 x;
-    __device__ __forceinline__ void load(const float *p) { x = *reinterpret_cast<const float4 *>(p); }
+    __device__ __forceinline__ void load(const float *p) { x = __ldcs(reinterpret_cast<const float4 *>(p)); }
     __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = x; }
     __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w; }
     __device__ __forceinline__ void set(const float (&f)[4]) { x = make_float4(f[0], f[1], f[2], f[3]); }
@@ -59,31 +59,76 @@ __device__ __forceinline__ int find_sequence(const int32_t *offsets, int B, int 
     return lo;
 }
 
-// VE: pairs of a unit.  Grid: one warp per (token, slice of heads).
-template <typename T, int VE>
-__global__ void __launch_bounds__(ROWS_WARPS * 32) rows_kernel(RowsArgs a, int slices, int heads_per_slice)
+// Four (or VE) consecutive entries of a table row
+template <int VE> __device__ __forceinline__ void load_row(const float *p, float (&f)[VE])
 {
-    const int lane = threadIdx.x & 31;
-    const long long w = (long long)blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5);
+    if constexpr (VE == 1) {
+        f[0] = *p;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE; i += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(p + i);
+            f[i] = x.x, f[i + 1] = x.y, f[i + 2] = x.z, f[i + 3] = x.w;
+        }
+    }
+}
+
+// VE: pairs of a unit.  Grid: one warp per (token, slice of heads).  A warp's first loads of x go out before anything
+// that has to be looked up for the token (positions, then the table's rows; the sequence, then its length, then its
+// page): the chains of dependent loads wait at the same time instead of one after the other.
+template <typename T, int VE>
+__global__ void __launch_bounds__(ROWS_WARPS * 32, 6) rows_kernel(const __grid_constant__ RowsArgs a, int heads_per_slice)
+{
+    const int lane = threadIdx.x & 31, t = blockIdx.x * ROWS_WARPS + (threadIdx.x >> 5);
     grid_dependency_wait();
     grid_dependency_trigger();
-    if (w >= (long long)a.T * slices) return;
-    const int t = (int)(w / slices), slice = (int)(w - (long long)t * slices);
-    const int heads = a.H_q + 2 * a.c.H_kv;
-    const int h_begin = slice * heads_per_slice, h_end = min(heads, h_begin + heads_per_slice);
+    if (t >= a.T) return;
+    const int h_begin = blockIdx.y * heads_per_slice, h_end = min(a.H_q + 2 * a.c.H_kv, h_begin + heads_per_slice);
     const int units = a.d / (2 * VE);                 // of one head
-    const int turned = a.r.cos_sin ? a.r.rot / (2 * VE) : 0;
+    const int turned = a.r.cos_sin ? a.r.rot / (2 * VE) : 0, half = a.r.rot / 2;
     const int lph = min(units, 32), hpi = 32 / lph;   // lanes of a head, heads of a warp's step
     const int hl = lane / lph, ul = lane - hl * lph;
     const bool on = hl < hpi;
-    const int half = a.r.rot / 2;
 
-    // positions: one lane per axis checks its own, every lane later reads the ones its pairs need
+    Vec<T, VE> x[HEAD_UNROLL], y[HEAD_UNROLL];
+    // a run of heads of q, k or v: the first and last of them in this slice, and where head 0 is
+    struct Run {
+        const T *src;
+        int h0, h1;
+        bool turn;
+    };
+    auto run_of = [&](int kind) {
+        const int first = kind == 0 ? 0 : a.H_q + (kind - 1) * a.c.H_kv, count = kind == 0 ? a.H_q : a.c.H_kv;
+        Run r;
+        r.src = kind == 0   ? static_cast<const T *>(a.q) + t * a.ld_q
+                : kind == 1 ? static_cast<const T *>(a.k) + t * a.ld_k
+                            : static_cast<const T *>(a.v) + t * a.ld_v;
+        r.h0 = max(h_begin - first, 0), r.h1 = min(h_end - first, count), r.turn = kind < 2;
+        return r;
+    };
+    // the two vectors of unit u in a head: the members of a pair that is split are rot / 2 apart
+    auto off0 = [&](int u, bool turn) { return turn && u < turned && !a.r.interleaved ? u * VE : 2 * u * VE; };
+    auto off1 = [&](int u, bool turn) { return turn && u < turned && !a.r.interleaved ? half + u * VE : 2 * u * VE + VE; };
+    auto load = [&](const Run &r, int h0, int u) {
+        const T *p0 = r.src + off0(u, r.turn), *p1 = r.src + off1(u, r.turn);
+#pragma unroll
+        for (int i = 0; i < HEAD_UNROLL; ++i) {
+            const int h = h0 + i * hpi + hl;
+            if (on && u < units && h < r.h1) x[i].load(p0 + h * a.d), y[i].load(p1 + h * a.d);
+        }
+    };
+    int kind = 0;
+    Run run = run_of(0);
+    while (run.h0 >= run.h1 && kind < 2) run = run_of(++kind);
+    load(run, run.h0, ul);
+
+    // positions: lane i keeps the one of axis i
+    int pos = 0;
     bool bad_pos = false;
     if (turned > 0) {
         if (lane < a.r.n_axes) {
-            const int p = a.r.positions[(size_t)lane * a.T + t];
-            bad_pos = p < 0 || p >= a.r.max_positions;
+            pos = a.r.positions[(size_t)lane * a.T + t];
+            bad_pos = pos < 0 || pos >= a.r.max_positions;
         }
         if (a.r.pair_axis)
             for (int p = lane; p < half; p += 32) bad_pos |= a.r.pair_axis[p] >= a.r.n_axes;
@@ -118,75 +163,89 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32) rows_kernel(RowsArgs a, int s
         if (lane == 0 && a.status) atomicOr(&a.status[b], bad);
         return;
     }
-    const T *qs = static_cast<const T *>(a.q) + t * a.ld_q;
-    const T *ks = static_cast<const T *>(a.k) + t * a.ld_k, *vs = static_cast<const T *>(a.v) + t * a.ld_v;
-    T *qd = static_cast<T *>(a.q_out) + t * a.ld_qo;
 
+    bool first = true;
     for (int u0 = 0; u0 < units; u0 += 32) {
         const int u = u0 + ul;
-        const bool active = on && u < units;
-        const bool turn = u < turned;
-        const bool split = turn && !a.r.interleaved;  // the pair's members are rot / 2 apart
-        const int off0 = split ? u * VE : 2 * u * VE, off1 = split ? half + u * VE : off0 + VE;
+        const bool turns = on && u < turned;
         float cs[VE], sn[VE];
-        if (active && turn) {
+        if (u0 < turned) {
+            int axis[VE], p0[VE];
+            bool one = true;                          // all pairs of the unit at one position: whole vectors of the table
+#pragma unroll
+            for (int i = 0; i < VE; ++i) axis[i] = 0;
+            if (turns && a.r.pair_axis) {
+                if constexpr (VE == 8) {              // (rot is a multiple of 2 VE here: the axes of a unit are aligned)
+                    const uint2 w = *reinterpret_cast<const uint2 *>(a.r.pair_axis + u * VE);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) axis[i] = ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 255;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) axis[i] = a.r.pair_axis[u * VE + i];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                const int p = u * VE + i;
-                const int axis = a.r.pair_axis ? a.r.pair_axis[p] : 0;
-                const float *row = a.r.cos_sin + (size_t)a.r.positions[(size_t)axis * a.T + t] * a.r.rot;
-                cs[i] = row[p];
-                sn[i] = a.r.inverse ? -row[half + p] : row[half + p];
+                p0[i] = __shfl_sync(0xffffffffu, pos, axis[i]);
+                one &= axis[i] == axis[0];
+            }
+            if (turns) {
+                if (one) {
+                    const float *row = a.r.cos_sin + (size_t)p0[0] * a.r.rot + u * VE;
+                    load_row<VE>(row, cs);
+                    load_row<VE>(row + half, sn);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) {
+                        const float *row = a.r.cos_sin + (size_t)p0[i] * a.r.rot + u * VE + i;
+                        cs[i] = row[0], sn[i] = row[half];
+                    }
+                }
+                if (a.r.inverse)
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) sn[i] = -sn[i];
             }
         }
-        for (int h0 = h_begin; h0 < h_end; h0 += hpi * HEAD_UNROLL) {
-            Vec<T, VE> x[HEAD_UNROLL], y[HEAD_UNROLL];
+        for (int kd_ = kind; kd_ < 3; ++kd_) {
+            run = run_of(kd_);
+            const bool turn = turns && run.turn, split = turn && !a.r.interleaved;
+            T *dst = kd_ == 0 ? static_cast<T *>(a.q_out) + t * a.ld_qo : kd_ == 1 ? kd : vd;
+            const long long step = kd_ == 0 ? a.d : a.c.stride_head;
+            T *d0 = dst + off0(u, run.turn), *d1 = dst + off1(u, run.turn);
+            for (int h0 = run.h0; h0 < run.h1; h0 += hpi * HEAD_UNROLL) {
+                if (!first) load(run, h0, u);         // (the very first ones are in)
+                first = false;
 #pragma unroll
-            for (int i = 0; i < HEAD_UNROLL; ++i) {
-                const int h = h0 + i * hpi + hl;
-                if (!active || h >= h_end) continue;
-                const T *src = h < a.H_q ? qs + (long long)h * a.d
-                               : h < a.H_q + a.c.H_kv ? ks + (long long)(h - a.H_q) * a.d
-                                                      : vs + (long long)(h - a.H_q - a.c.H_kv) * a.d;
-                const bool is_v = h >= a.H_q + a.c.H_kv;
-                x[i].load(src + (is_v ? 2 * u * VE : off0));
-                y[i].load(src + (is_v ? 2 * u * VE + VE : off1));
-            }
+                for (int i = 0; i < HEAD_UNROLL; ++i) {
+                    const int h = h0 + i * hpi + hl;
+                    if (!on || u >= units || h >= run.h1) continue;
+                    if (turn) {
+                        float f[VE], g[VE], rf[VE], rg[VE];
+                        x[i].get(f), y[i].get(g);
+                        if (split) {
 #pragma unroll
-            for (int i = 0; i < HEAD_UNROLL; ++i) {
-                const int h = h0 + i * hpi + hl;
-                if (!active || h >= h_end) continue;
-                const bool is_v = h >= a.H_q + a.c.H_kv;
-                T *dst = h < a.H_q ? qd + (long long)h * a.d
-                         : !is_v   ? kd + (h - a.H_q) * a.c.stride_head
-                                   : vd + (h - a.H_q - a.c.H_kv) * a.c.stride_head;
-                if (turn && !is_v) {
-                    float f[VE], g[VE], rf[VE], rg[VE];
-                    x[i].get(f), y[i].get(g);
-                    if (split) {
+                            for (int e = 0; e < VE; ++e) {
+                                rf[e] = f[e] * cs[e] - g[e] * sn[e];
+                                rg[e] = g[e] * cs[e] + f[e] * sn[e];
+                            }
+                        } else {  // pairs side by side: the 2 VE elements of x, y hold pairs 0 .. VE-1 in order
+                            if constexpr (VE == 1) {
+                                rf[0] = f[0] * cs[0] - g[0] * sn[0];
+                                rg[0] = g[0] * cs[0] + f[0] * sn[0];
+                            } else {
 #pragma unroll
-                        for (int e = 0; e < VE; ++e) {
-                            rf[e] = f[e] * cs[e] - g[e] * sn[e];
-                            rg[e] = g[e] * cs[e] + f[e] * sn[e];
-                        }
-                    } else {  // pairs side by side: the 2 VE elements of x, y hold pairs 0 .. VE-1 in order
-                        if constexpr (VE == 1) {
-                            rf[0] = f[0] * cs[0] - g[0] * sn[0];
-                            rg[0] = g[0] * cs[0] + f[0] * sn[0];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < VE; e += 2) {
-                                rf[e] = f[e] * cs[e / 2] - f[e + 1] * sn[e / 2];
-                                rf[e + 1] = f[e + 1] * cs[e / 2] + f[e] * sn[e / 2];
-                                rg[e] = g[e] * cs[(VE + e) / 2] - g[e + 1] * sn[(VE + e) / 2];
-                                rg[e + 1] = g[e + 1] * cs[(VE + e) / 2] + g[e] * sn[(VE + e) / 2];
+                                for (int e = 0; e < VE; e += 2) {
+                                    rf[e] = f[e] * cs[e / 2] - f[e + 1] * sn[e / 2];
+                                    rf[e + 1] = f[e + 1] * cs[e / 2] + f[e] * sn[e / 2];
+                                    rg[e] = g[e] * cs[(VE + e) / 2] - g[e + 1] * sn[(VE + e) / 2];
+                                    rg[e + 1] = g[e + 1] * cs[(VE + e) / 2] + g[e] * sn[(VE + e) / 2];
+                                }
                             }
                         }
+                        x[i].set(rf), y[i].set(rg);
                     }
-                    x[i].set(rf), y[i].set(rg);
+                    x[i].store(d0 + h * step), y[i].store(d1 + h * step);
                 }
-                x[i].store(dst + (is_v ? 2 * u * VE : off0));
-                y[i].store(dst + (is_v ? 2 * u * VE + VE : off1));
             }
         }
     }
@@ -196,12 +255,18 @@ template <typename T, int VE> cudaError_t launch_rows_ve(const RowsArgs &a, cuda
 {
     const int heads = a.H_q + 2 * a.c.H_kv, units = a.d / (2 * VE);
     const int lph = units < 32 ? units : 32, hpi = 32 / lph;
-    const int per = hpi * HEAD_UNROLL;
-    const int slices = (heads + per - 1) / per;
-    const long long warps = (long long)a.T * slices;
-    const long long blocks = (warps + ROWS_WARPS - 1) / ROWS_WARPS;
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    return launch_dependent(rows_kernel<T, VE>, dim3((unsigned)blocks), dim3(ROWS_WARPS * 32), 0, stream, a, slices, per);
+    // Heads of a warp: all of a token's where there are warps enough without (a warp's lookups are as much work as some
+    // twenty heads), else as many as it loads at once.
+    int dev = 0, sms = 0;
+    cudaError_t e = current_device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    const int step = hpi * HEAD_UNROLL, most = (heads + step - 1) / step;
+    long long slices = (long long)sms * 24 / a.T;
+    slices = slices < 1 ? 1 : slices > most ? most : slices;
+    const int per = (int)((most + slices - 1) / slices) * step;
+    const dim3 grid((a.T + ROWS_WARPS - 1) / ROWS_WARPS, (heads + per - 1) / per);
+    if (grid.y > 65535) return cudaErrorInvalidValue;
+    return launch_dependent(rows_kernel<T, VE>, grid, dim3(ROWS_WARPS * 32), 0, stream, a, per);
 }
 
 // Commit: one CTA per (sequence, slice of a row's bytes), one warp per path node.  Rows are copied as they are.
