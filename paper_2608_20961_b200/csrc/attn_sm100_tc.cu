@@ -76,6 +76,11 @@ struct Item {
     int slot;                   // where a cut item's part goes, or -1: the item is whole
 };
 
+struct Seq {
+    int lo, n, len, kts, row_tiles, groups;
+    unsigned units;             // H_kv * groups * (OV + kts), below 2^31 (the launcher has checked)
+};
+
 struct Shared {
     uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[4], p_full[4], pv_done[4], q_full, o_free, s_free[4], item_full[ITEMS],
         item_empty[ITEMS], hand[2][4], exch[4];
@@ -84,6 +89,7 @@ struct Shared {
     unsigned bad_item[16];      // ordinal + 1 of an item that met a page out of range
     unsigned nonfinite[4][2];   // draft rows of an item with NaN or infinity among their values
     long long scan[THREADS / 32], first_off, last_off;
+    Seq first_seq;              // of sequence first_b
     int first_b, last_b, total_fail;
     uint32_t tmem;
 };
@@ -102,10 +108,6 @@ struct Ws {
 
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + KT - 1) / KT; }
 
-struct Seq {
-    int lo, n, len, kts, row_tiles, groups;
-    unsigned units;             // H_kv * groups * (OV + kts), below 2^31 (the launcher has checked)
-};
 // b = -1: the shared prompt, whose rows are those of all sequences
 __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *status)
 {
@@ -201,11 +203,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
     const long long shared_units = a.shared_len > 0 ? (long long)load_seq(a, -1, R, &st).units : 0;
     const int chunk = (a.B + THREADS - 1) / THREADS, b_begin = min(a.B, tid * chunk), b_end = min(a.B, b_begin + chunk);
     long long sum = 0;
-    unsigned only = 0;           // a thread's one sequence is not read again
+    Seq only;                    // a thread's one sequence is not read again
 #pragma unroll 1
     for (int b = b_begin; b < b_end; ++b) {
-        only = load_seq(a, b, R, &st).units;
-        sum += only;
+        only = load_seq(a, b, R, &st);
+        sum += only.units;
         if (st && blockIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[b], st);
     }
     long long incl = sum;
@@ -230,36 +232,21 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
     const long long u1 = group < parts && W > 0 ? part_begin(group + 1, W, parts) : 0;
 #pragma unroll 1
     for (int b = b_begin; b < b_end; ++b) {
-        const long long units = chunk == 1 ? only : load_seq(a, b, R, &st).units;
+        if (chunk > 1) only = load_seq(a, b, R, &st);
+        const long long units = only.units;
         if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[b] = before;
         if (u1 > u0) {
-            if (u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before;
+            if (u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before, sh.first_seq = only;
             if (u1 - 1 >= before && u1 - 1 < before + units) sh.last_b = b, sh.last_off = u1 - 1 - before;
         }
         before += units;
     }
     if (tid == 0) {
         if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[a.B] = W, ws.prefix[a.B + 1] = parts;
-        if (u1 > u0 && u0 < shared_units) sh.first_b = -1, sh.first_off = u0;
+        if (u1 > u0 && u0 < shared_units) sh.first_b = -1, sh.first_off = u0, sh.first_seq = load_seq(a, -1, R, &st);
         if (u1 > u0 && u1 - 1 < shared_units) sh.last_b = -1, sh.last_off = u1 - 1;
     }
     __syncthreads();
-    if (tid == 0 && a.shared_len == 0) {  // what the join needs of the item that this part cuts at its end
-        int *d = ws.desc + 8 * blockIdx.x;
-        int pieces = 0;
-        if (u1 > u0) {
-            const Seq s = load_seq(a, sh.last_b, R, &st);
-            const unsigned last = (unsigned)sh.last_off, per = s.kts + OV, it = last / per;
-            const long long begin = u1 - 1 - (last - it * per), first = begin + OV;
-            const int row0 = ((int)(it % s.groups) * R + member) * MT;
-            if (first >= u0 && first < u1 && first + s.kts > u1 && row0 < s.n * a.G) {
-                pieces = part_of(first + s.kts - 1, W, parts) - group + 1;
-                d[1] = slot_of(group, begin, u0);
-                d[2] = s.lo, d[3] = (int)(it / s.groups), d[4] = row0, d[5] = min(MT, s.n * a.G - row0), d[6] = group;
-            }
-        }
-        d[0] = pieces;
-    }
     const uint32_t tmem = sh.tmem;
     const float sl2 = a.scale * 1.4426950408889634f;
     auto fail = [&](int b) {
@@ -285,9 +272,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 int b = sh.first_b, st2;
                 unsigned off = (unsigned)sh.first_off;
                 long long u = u0;
-                Seq s;
-                s.units = 0;
-                bool fresh = true;
+                Seq s = sh.first_seq;
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
                     Item it;
@@ -295,9 +280,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         // the next item that has tiles here and rows for this member of the group; 0 tiles: the end
                         it.tiles = 0;
                         while (u < u1 && it.tiles == 0) {
-                            if (fresh || off >= s.units) {  // (a sequence without work has no units)
-                                if (!fresh) off = 0, ++b;
-                                fresh = false;
+                            if (off >= s.units) {  // (a sequence without work has no units)
+                                off = 0, ++b;
                                 s = load_seq(a, b, R, &st2);
                                 continue;
                             }
@@ -421,6 +405,23 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
             int cur_b = -1;
+            if (warp == MMA_PV && a.shared_len == 0) {  // what the join needs of the item that this part cuts at its end
+                int st;
+                int *d = ws.desc + 8 * blockIdx.x;
+                int pieces = 0;
+                if (u1 > u0) {
+                    const Seq s = load_seq(a, sh.last_b, R, &st);
+                    const unsigned last = (unsigned)sh.last_off, per = s.kts + OV, it = last / per;
+                    const long long begin = u1 - 1 - (last - it * per), first = begin + OV;
+                    const int row0 = ((int)(it % s.groups) * R + member) * MT;
+                    if (first >= u0 && first < u1 && first + s.kts > u1 && row0 < s.n * a.G) {
+                        pieces = part_of(first + s.kts - 1, W, parts) - group + 1;
+                        d[1] = slot_of(group, begin, u0);
+                        d[2] = s.lo, d[3] = (int)(it / s.groups), d[4] = row0, d[5] = min(MT, s.n * a.G - row0), d[6] = group;
+                    }
+                }
+                d[0] = pieces;
+            }
             uint64_t *newest = nullptr;  // barrier of the last commit, and its phase
             unsigned newest_phase = 0;
             auto run = [&]() -> bool {
