@@ -37,7 +37,11 @@ constexpr int MAX_CTAS = 160;
 constexpr int THREADS = 384, PRODUCER_K = 8, PRODUCER_V = 9, MMA_QK = 10, MMA_PV = 11;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
 constexpr int MIN_UNITS = 2;           // of a CTA's part: below this a part is mostly start and end
-constexpr int OV = 3;                  // what starting an item costs, in tiles
+// What starting an item costs, in tiles, by the rows of its first row tile (queries into tensor memory, the pipeline's
+// start, the output): measured over 3 to 12.  Heads of 256 with full row tiles, 64 trees under one prompt: 207 us at 3,
+// 157 at 8, 156 at 12; one row of 4 heads, 64 sequences of up to 8k: 183 at 3, 172 at 5, 177 at 8.
+constexpr int OV_MAX = 9;
+__device__ __forceinline__ int start_cost(long long rows) { return rows > 32 ? OV_MAX : 5; }
 constexpr float LAZY = 8.f;
 
 template <int D> struct Cfg {
@@ -47,8 +51,9 @@ template <int D> struct Cfg {
     // wait for this tile's P V; so there P goes through shared memory and S is free as soon as it has been read.
     static constexpr bool P_SMEM = D == 256;
     static constexpr int P_BYTES = P_SMEM ? MT * KT * 2 : 0;       // of one of the two P buffers
-    // K tiles and V tiles have a ring of stages each, up to 192 KB together
-    static constexpr int NK = D == 256 ? 3 : D == 128 ? 6 : 8, NV = D == 256 ? 2 : NK;
+    // K tiles and V tiles have a ring of stages each, up to 192 KB together.  K runs further ahead: V is wanted a softmax
+    // step later (8 and 4 stages of 128: 92 us where 6 and 6 take 98).
+    static constexpr int NK = D == 256 ? 3 : 8, NV = D == 256 ? 2 : D == 128 ? 4 : 8;
     static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
     static constexpr int NQ = D == 256 ? 1 : 2;                    // Q buffers
     static constexpr int TM_Q = D, TM_S = D + NQ * (D / 2);
@@ -77,8 +82,8 @@ struct Item {
 };
 
 struct Seq {
-    int lo, n, len, kts, row_tiles, groups;
-    unsigned units;             // H_kv * groups * (OV + kts), below 2^31 (the launcher has checked)
+    int lo, n, len, kts, row_tiles, groups, ov;
+    unsigned units;             // H_kv * groups * (ov + kts), below 2^31 (the launcher has checked)
 };
 
 struct Shared {
@@ -115,7 +120,7 @@ __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *st
     *status = 0;
     if (b < 0) {
         s.lo = 0, s.n = 0, s.len = a.shared_len, s.kts = tiles_of(a.shared_len);
-        s.row_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT);
+        s.row_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT), s.ov = start_cost((long long)a.T * a.G);
     } else {
         *status = check_sequence(a.node_offsets, a.c.context_len, b, a.T, a.max_nodes,
                                  (long long)a.c.max_pages * a.c.page_size, a.shared_len, &s.lo, &s.n, &s.len);
@@ -124,10 +129,10 @@ __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *st
             return s;
         }
         s.kts = tiles_of(s.len - a.shared_len) + 1;
-        s.row_tiles = (s.n * a.G + MT - 1) / MT;
+        s.row_tiles = (s.n * a.G + MT - 1) / MT, s.ov = start_cost((long long)s.n * a.G);
     }
     s.groups = (s.row_tiles + R - 1) / R;
-    s.units = (unsigned)a.c.H_kv * s.groups * (OV + s.kts);
+    s.units = (unsigned)a.c.H_kv * s.groups * (s.ov + s.kts);
     return s;
 }
 // (What the main kernel does not do once a tile is out of line: its roles run at the same time and share the
@@ -139,8 +144,8 @@ static __device__ __noinline__ long long div64(long long x, long long y)
 {
     return ((x | y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
 }
-// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  An item takes OV + kts
-// units, tile t the (OV + t)-th of them.
+// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  An item takes ov + kts
+// units, tile t the (ov + t)-th of them.
 __device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return div64(g * W, parts); }
 __device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)div64((unit + 1) * parts - 1, W); }
 // Slot of part g's piece of the item that begins at `begin`: a part cuts at most two items, the one its own start
@@ -285,9 +290,9 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 s = load_seq(a, b, R, &st2);
                                 continue;
                             }
-                            const unsigned per = s.kts + OV, i_ = off / per, o = off - i_ * per, h = i_ / s.groups, rg = i_ - h * s.groups;
+                            const unsigned per = s.kts + s.ov, i_ = off / per, o = off - i_ * per, h = i_ / s.groups, rg = i_ - h * s.groups;
                             const int span = (int)min((long long)(per - o), u1 - u);
-                            const int kt0 = max(0, (int)o - OV), kt1 = max(0, (int)o + span - OV);
+                            const int kt0 = max(0, (int)o - s.ov), kt1 = max(0, (int)o + span - s.ov);
                             const long long begin = u - o;
                             const long long row0 = (long long)(rg * R + member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
                             off += span, u += span;
@@ -411,8 +416,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 int pieces = 0;
                 if (u1 > u0) {
                     const Seq s = load_seq(a, sh.last_b, R, &st);
-                    const unsigned last = (unsigned)sh.last_off, per = s.kts + OV, it = last / per;
-                    const long long begin = u1 - 1 - (last - it * per), first = begin + OV;
+                    const unsigned last = (unsigned)sh.last_off, per = s.kts + s.ov, it = last / per;
+                    const long long begin = u1 - 1 - (last - it * per), first = begin + s.ov;
                     const int row0 = ((int)(it % s.groups) * R + member) * MT;
                     if (first >= u0 && first < u1 && first + s.kts > u1 && row0 < s.n * a.G) {
                         pieces = part_of(first + s.kts - 1, W, parts) - group + 1;
@@ -917,10 +922,11 @@ __global__ void __launch_bounds__(128) attn_join_shared_kernel(const __grid_cons
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {  // the prompt, then the sequence's own keys
         const int kts = pass == 0 ? prompt.kts : own.kts, groups = pass == 0 ? prompt.groups : own.groups;
+        const int ov = pass == 0 ? prompt.ov : own.ov;
         const unsigned i = pass == 0 ? own.lo * a.G + r : r;  // the row in the list that the item's tiles cut up
         const int tile = i / MT, in_tile = i % MT, rg = tile / R, member = tile - rg * R;
-        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (OV + kts);
-        const int g0 = part_of(begin + OV, W, parts), g1 = part_of(begin + OV + kts - 1, W, parts);
+        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (ov + kts);
+        const int g0 = part_of(begin + ov, W, parts), g1 = part_of(begin + ov + kts - 1, W, parts);
         if (g0 == g1) {
             const long long blk = pass == 0 ? (long long)h * prompt.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
             const int cap = pass == 0 ? MT : ws.own_cap;
@@ -1027,8 +1033,8 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
 // The units of one sequence, and of the shared prompt, stay below 2^31.
 static bool units_fit(const AttnArgs &a)
 {
-    const long long own = ((long long)a.max_nodes * a.G + MT - 1) / MT * (((long long)a.c.max_pages * a.c.page_size) / KT + 2 + OV);
-    const long long shared = ((long long)a.T * a.G + MT - 1) / MT * (a.shared_len / KT + 2 + OV);
+    const long long own = ((long long)a.max_nodes * a.G + MT - 1) / MT * (((long long)a.c.max_pages * a.c.page_size) / KT + 2 + OV_MAX);
+    const long long shared = ((long long)a.T * a.G + MT - 1) / MT * (a.shared_len / KT + 2 + OV_MAX);
     const long long most = 0x7fffffffll / a.c.H_kv;
     return own <= most && shared <= most;
 }
