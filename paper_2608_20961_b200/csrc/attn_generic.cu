@@ -14,8 +14,8 @@ namespace treewy {
 namespace {
 
 constexpr int THREADS = 256, RB = 32, KB = 32;
-constexpr int TARGET_CTAS = 296;   // two to an SM
-constexpr int MIN_KEYS = 64;       // of a part
+constexpr int TARGET_CTAS = 592;   // four to an SM
+constexpr int MIN_KEYS = 32;       // of a part: one step
 constexpr int MAX_PARTS = 64;
 constexpr float MASKED = -1.f;
 
@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(THREADS) attn_generic_kernel(AttnArgs a, int p
     extern __shared__ float4 smem4[];
     __shared__ float s_alpha[RB], s_m[RB], s_l[RB], s_p[RB][KB + 1];
     __shared__ uint64_t s_mask[RB];
+    __shared__ long long s_at[2][KB];              // where a tile's keys are: elements into the cache, or -1 - the draft row's
     const int D4 = a.c.d / 4, LD4 = D4 + 1;  // one float4 of padding a row
     float4 *sQ = smem4, *sK = sQ + RB * LD4, *sV = sK + KB * LD4;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -83,6 +84,18 @@ __global__ void __launch_bounds__(THREADS) attn_generic_kernel(AttnArgs a, int p
     auto page_of = [&](int j) {
         return j < a.shared_len ? a.shared_pages[j / a.c.page_size]
                                 : a.c.page_table[(size_t)b * a.c.max_pages + j / a.c.page_size];
+    };
+    // the addresses of a tile's keys, looked up one tile ahead by one warp
+    auto locate = [&](int t0, int buf) {
+        const int j = t0 + lane;
+        long long at = 0;
+        if (j < len) {
+            const int pi = j / a.c.page_size;
+            at = page_of(j) * a.c.stride_page + (j - pi * a.c.page_size) * a.c.stride_slot + h * a.c.stride_head;
+        } else if (j < keys) {
+            at = -1 - (long long)(lo + j - len);
+        }
+        s_at[buf][lane] = at;
     };
     // every page of the sequence, whatever the part: a sequence with a bad page is skipped by all of them
     bool bad_page = false;
@@ -114,6 +127,7 @@ __global__ void __launch_bounds__(THREADS) attn_generic_kernel(AttnArgs a, int p
         s_m[tid] = -INFINITY, s_l[tid] = 0.f;
         s_mask[tid] = r0 + tid < rows ? a.anc_mask[lo + (r0 + tid) / a.G] & low_bits(n) : 0;
     }
+    if (warp == THREADS / 32 - 1 && k0 < k1) locate(k0, 0);
     float4 acc[RPT];
 #pragma unroll
     for (int i = 0; i < RPT; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -122,24 +136,20 @@ __global__ void __launch_bounds__(THREADS) attn_generic_kernel(AttnArgs a, int p
 
     for (int t0 = k0; t0 < k1; t0 += KB) {
         __syncthreads();  // the tiles of the step before are read; first round: q, masks, statistics are written
+        const int buf = ((t0 - k0) / KB) & 1;
         for (int i = tid; i < KB * D4; i += THREADS) {
-            const int r = i / D4, c = i - r * D4, j = t0 + r;
+            const int r = i / D4, c = i - r * D4;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-            if (j < k1) {
-                const T *kp, *vp;
-                if (j < len) {
-                    const int pi = j / a.c.page_size;
-                    const long long at = page_of(j) * a.c.stride_page + (j - pi * a.c.page_size) * a.c.stride_slot +
-                                         h * a.c.stride_head;
-                    kp = static_cast<const T *>(a.c.k) + at, vp = static_cast<const T *>(a.c.v) + at;
-                } else {
-                    kp = static_cast<const T *>(a.k) + (lo + j - len) * a.ld_k + (long long)h * a.c.d;
-                    vp = static_cast<const T *>(a.v) + (lo + j - len) * a.ld_v + (long long)h * a.c.d;
-                }
+            if (t0 + r < k1) {
+                const long long at = s_at[buf][r];
+                const bool cached = at >= 0;
+                const T *kp = cached ? static_cast<const T *>(a.c.k) + at : static_cast<const T *>(a.k) + (-1 - at) * a.ld_k + (long long)h * a.c.d;
+                const T *vp = cached ? static_cast<const T *>(a.c.v) + at : static_cast<const T *>(a.v) + (-1 - at) * a.ld_v + (long long)h * a.c.d;
                 x = Ld4<T>::at(kp + 4 * c), y = Ld4<T>::at(vp + 4 * c);
             }
             sK[r * LD4 + c] = x, sV[r * LD4 + c] = y;
         }
+        if (warp == THREADS / 32 - 1 && t0 + KB < k1) locate(t0 + KB, buf ^ 1);
         __syncthreads();
         {   // scores: 2 rows x 2 keys of a thread
             const int tx = tid & 15, ty = tid >> 4;
@@ -229,27 +239,38 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, int parts, c
         return;
     if (r >= (long long)n * a.H_q) return;
     const long long row = (long long)lo * a.H_q + r, stride = (long long)a.T * a.H_q;
-    if (part_ml[2 * row + 1] < 0.f) return;  // a bad page
+    // lane p has the weights of parts p and p + 32
+    float2 ml[2];
     float m = -INFINITY;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, part_ml[2 * (p * stride + row)]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int p = 0; p < parts; ++p) {
-        const float lp = part_ml[2 * (p * stride + row) + 1];
-        if (lp != 0.f) l += lp * expf(part_ml[2 * (p * stride + row)] - ref);
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = lane + 32 * i;
+        ml[i] = p < parts ? *reinterpret_cast<const float2 *>(part_ml + 2 * (p * stride + row)) : make_float2(-INFINITY, 0.f);
+        bad |= ml[i].y < 0.f;
+        if (ml[i].y != 0.f) m = fmaxf(m, ml[i].x);  // (0: this part saw nothing)
     }
+    if (__any_sync(0xffffffffu, bad)) return;       // a bad page
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = ml[i].y == 0.f ? 0.f : expf(ml[i].x - ref);
+    const float l = warp_sum(w[0] * ml[0].y + w[1] * ml[1].y);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int D4 = a.c.d / 4;
-    for (int c = lane; c < D4; c += 32) {
+    for (int c0 = 0; c0 < D4; c0 += 32) {
+        const int c = c0 + lane;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
         for (int p = 0; p < parts; ++p) {
-            const long long at = p * stride + row;
-            if (part_ml[2 * at + 1] == 0.f) continue;  // this part saw nothing
-            const float w = expf(part_ml[2 * at] - ref) * inv;
-            const float4 y = reinterpret_cast<const float4 *>(part_o)[at * D4 + c];
-            x.x += w * y.x, x.y += w * y.y, x.z += w * y.z, x.w += w * y.w;
+            const float f = __shfl_sync(0xffffffffu, p < 32 ? w[0] : w[1], p & 31);
+            if (c >= D4 || f == 0.f) continue;      // (a part that saw nothing has left nothing either)
+            const float4 y = reinterpret_cast<const float4 *>(part_o)[(p * stride + row) * D4 + c];
+            x.x += f * y.x, x.y += f * y.y, x.z += f * y.z, x.w += f * y.w;
         }
-        Ld4<T>::put(static_cast<T *>(a.O) + row * a.c.d + 4 * c, x);
+        if (c < D4) Ld4<T>::put(static_cast<T *>(a.O) + row * a.c.d + 4 * c, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
     }
 }
 
