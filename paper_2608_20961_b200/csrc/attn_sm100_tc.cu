@@ -152,12 +152,19 @@ __device__ __forceinline__ int part_of(long long unit, long long W, int parts) {
 // falls into and one more.
 __device__ __forceinline__ int slot_of(int g, long long begin, long long u0) { return begin <= u0 ? 2 * g : 2 * g + 1; }
 
-// keys of tile kt that exist
-__device__ __forceinline__ int valid_keys(const AttnArgs &a, const Item &it, int kt)
-{
-    if (it.b < 0) return min(KT, it.len - kt * KT);
-    return kt == it.kts - 1 ? it.n : min(KT, it.len - a.shared_len - kt * KT);
-}
+// The tiles of an item's part by their keys, kept in registers: tiles 0 .. full-1 are whole, the draft rows are tile
+// `draft`, and any other is the cached tokens' last one, with `rest` keys.
+struct Tiles {
+    int full, draft, rest, n;
+    __device__ __forceinline__ Tiles(const AttnArgs &a, const Item &it)
+    {
+        const int own = it.b < 0 ? it.len : it.len - a.shared_len;
+        full = own / KT - it.kt0, rest = own % KT, n = it.n;
+        draft = it.b < 0 ? 0x7fffffff : it.kts - 1 - it.kt0;
+    }
+    __device__ __forceinline__ int valid(int j) const { return j < full ? KT : j == draft ? n : rest; }
+};
+
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
 // a wait with one outcome for the whole warp: what follows needs all of its lanes
@@ -410,6 +417,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
             int cur_b = -1;
+            uint32_t v_off[KT / 16];     // 16 rows of V from one step to the next
+#pragma unroll
+            for (int s = 0; s < KT / 16; ++s)
+                v_off[s] = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
             if (warp == MMA_PV && a.shared_len == 0) {  // what the join needs of the item that this part cuts at its end
                 int st;
                 int *d = ws.desc + 8 * blockIdx.x;
@@ -439,6 +450,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     cur_b = it.b;
                     ptx::mbar_arrive(&sh.item_empty[r]);
                     const int n = it.tiles;
+                    const Tiles tiles(a, it);
                     if (warp == MMA_QK) {
                         if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                         for (int j = 0; j < n; ++j) {
@@ -463,12 +475,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
                             ptx::tc_fence_after_sync();
                             const uint32_t vaddr = ptx::smem_u32(v_stages + sidx * C::STAGE);
-                            const int steps = (valid_keys(a, it, it.kt0 + j) + 15) / 16;
+                            const int steps = (tiles.valid(j) + 15) / 16;
 #pragma unroll
                             for (int s = 0; s < KT / 16; ++s)
                                 if (s < steps) {
-                                    const uint32_t at = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
-                                    const uint64_t vd = ptx::umma_desc_mn_sw128(vaddr + at, lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
+                                    const uint64_t vd = ptx::umma_desc_mn_sw128(vaddr + v_off[s], lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
                                     if (C::P_SMEM)
                                         ptx::umma_bf16(tmem, ptx::umma_desc_k_sw128(ptx::smem_u32(p_bufs + (g & 1) * C::P_BYTES) + s * 32), vd,
                                                        idesc_pv, j > 0 || s > 0);
@@ -538,6 +549,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             Mine me{&sh.items[0], 0, 0, 0}, next;
             bool have = false;                        // the hand-over before this warpgroup's next tile is in
             int n = 0;
+            Tiles tiles(a, sh.items[0]);
             // (the round before the first item only takes that one)
             for (unsigned ord = ~0u;; ++ord) {
                 const Item &it = *me.it;
@@ -560,8 +572,14 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         taken = true;
                     }
                     if (j >= n) break;
-                    const int kt = it.kt0 + j, valid = valid_keys(a, it, kt);
-                    const bool draft = it.b >= 0 && kt == it.kts - 1;
+                    const int valid = tiles.valid(j);
+                    const bool draft = j == tiles.draft;
+                    if (g > 0 && !have) {
+                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
+                        ++handed;
+                    }
+                    have = false;
+                    const float m0 = j == 0 ? -INFINITY : sh.m[row];
                     if (!wait_warp(&sh.s_full[buf], (g / C::NSB) & 1)) return false;
                     ptx::tc_fence_after_sync();
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
@@ -597,12 +615,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         for (int i = 0; i < KT; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(raw[i]));
                         top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
                     }
-                    if (g > 0 && !have) {
-                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
-                        ++handed;
-                    }
-                    have = false;
-                    const float m0 = j == 0 ? -INFINITY : sh.m[row];
                     const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
                     m = grow ? top : m0;
                     sh.m[row] = m;
@@ -779,6 +791,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 if (next.it->tiles == 0) return true;
                 tile += n;
                 me = next, n = me.it->tiles, cur_b = me.it->b;
+                tiles = Tiles(a, *me.it);
             }
         };
         const bool ok = run();
