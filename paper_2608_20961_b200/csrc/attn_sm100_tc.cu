@@ -88,9 +88,12 @@ struct Seq {
 
 struct Shared {
     uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[4], p_full[4], pv_done[4], q_full, o_free, s_free[4], item_full[ITEMS],
-        item_empty[ITEMS], hand[2][4], exch[4];
+        item_empty[ITEMS], exch[4];
     Item items[ITEMS];
-    float m[MT], l[2][2][MT];
+    // running maximum of each row beside the number + 1 of the tile that decided it: one 64-bit word, so that a row's next
+    // tile needs no barrier to know that it reads the right one
+    unsigned long long m[MT];
+    float l[2][2][MT];
     unsigned bad_item[16];      // ordinal + 1 of an item that met a page out of range
     unsigned nonfinite[4][2];   // draft rows of an item with NaN or infinity among their values
     long long scan[THREADS / 32], first_off, last_off;
@@ -173,6 +176,26 @@ __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity)
     return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity));
 }
 
+// The maximum that tile g left for this thread's row, once it is there; for the whole warp.
+static __device__ __noinline__ bool row_max_slow(const volatile unsigned long long *p, unsigned g)
+{
+    for (;;) {
+        if (__all_sync(0xffffffffu, (unsigned)(*p >> 32) == g + 1)) return true;
+        if (__any_sync(0xffffffffu, ptx::wait_deadline_passed())) return false;
+        __nanosleep(40);
+    }
+}
+__device__ __forceinline__ bool row_max(const volatile unsigned long long *p, unsigned g, float *m)
+{
+    unsigned long long w = *p;
+    if (!__all_sync(0xffffffffu, (unsigned)(w >> 32) == g + 1)) {
+        if (!row_max_slow(p, g)) return false;
+        w = *p;
+    }
+    *m = __uint_as_float((unsigned)w);
+    return true;
+}
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
@@ -195,13 +218,14 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.s_free[i], 4), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
         ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
-        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.hand[0][i], 1), ptx::mbar_init(&sh.hand[1][i], 1), ptx::mbar_init(&sh.exch[i], 2);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.exch[i], 2);
         ptx::fence_barrier_init();
         sh.total_fail = 0;
         sh.first_b = sh.last_b = -2;
         ptx::prefetch_tmap(&map_kc), ptx::prefetch_tmap(&map_vc), ptx::prefetch_tmap(&map_k), ptx::prefetch_tmap(&map_v);
     }
     if (tid < 16) sh.bad_item[tid] = 0;
+    if (tid < MT) sh.m[tid] = 0;
     if (tid < 8) sh.nonfinite[tid >> 1][tid & 1] = 0;
     if (warp == MMA_QK) {
         ptx::tmem_alloc(&sh.tmem, 512);
@@ -545,9 +569,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             return true;
         };
         auto run = [&]() -> bool {
-            unsigned tile = 0, handed = 0;  // handed: hand-overs of the maxima this warpgroup has received
+            unsigned tile = 0;
             Mine me{&sh.items[0], 0, 0, 0}, next;
-            bool have = false;                        // the hand-over before this warpgroup's next tile is in
             int n = 0;
             Tiles tiles(a, sh.items[0]);
             // (the round before the first item only takes that one)
@@ -560,9 +583,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 for (int j = (int)(tile & 1) == wg ? 0 : 1;; j += 2) {
                     const unsigned g = tile + j, buf = g % C::NSB;
                     if (j >= n && n > 0 && (int)(last & 1) != wg) {  // the other warpgroup's last maximum
-                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
-                        ++handed, have = true;
-                        m = sh.m[row];
+                        if (!row_max(&sh.m[row], last, &m)) return false;
                     }
                     // With two Q buffers the next item's queries come in before this warpgroup's last tile, while it
                     // would wait for S: the buffer's last reader was the item before this one.  With one, at the end: the
@@ -574,12 +595,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     if (j >= n) break;
                     const int valid = tiles.valid(j);
                     const bool draft = j == tiles.draft;
-                    if (g > 0 && !have) {
-                        if (!wait_warp(&sh.hand[wg][w4], handed & 1)) return false;
-                        ++handed;
+                    float m0 = -INFINITY;
+                    if (g > 0) {
+                        if (!row_max(&sh.m[row], g - 1, &m0)) return false;
+                        if (j == 0) m0 = -INFINITY;  // (another item's)
                     }
-                    have = false;
-                    const float m0 = j == 0 ? -INFINITY : sh.m[row];
                     if (!wait_warp(&sh.s_full[buf], (g / C::NSB) & 1)) return false;
                     ptx::tc_fence_after_sync();
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
@@ -612,13 +632,13 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     if (warp_on) {
                         float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int i = 0; i < KT; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(raw[i]));
+                        for (int i = 0; i < KT; i += 2)
+                            t[(i >> 1) & 3] = ptx::max3(t[(i >> 1) & 3], __uint_as_float(raw[i]), __uint_as_float(raw[i + 1]));
                         top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
                     }
                     const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
                     m = grow ? top : m0;
-                    sh.m[row] = m;
-                    ptx::mbar_arrive_warp(&sh.hand[wg ^ 1][w4]);
+                    *reinterpret_cast<volatile unsigned long long *>(&sh.m[row]) = (unsigned long long)(g + 1) << 32 | __float_as_uint(m);
                     if (warp_on) {
                         const float ref = m == -INFINITY ? 0.f : m;
                         float acc[4] = {0.f, 0.f, 0.f, 0.f};
