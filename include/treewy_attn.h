@@ -115,6 +115,7 @@ treewy_status_t treewy_attn_verify(const treewy_kv_cache_t *cache, const treewy_
                                    float scale, const int32_t *shared_pages, int32_t shared_len,
                                    treewy_dtype_t io_dtype, void *O, void *workspace, size_t workspace_bytes,
                                    int32_t *seq_status, void *cuda_stream);
+/* (treewy_debug_inject reaches the tensor-core kernel too: skip_item is then sequence * H_kv + key/value head.) */
 /* The same contract, always through the SIMT kernel: a cross-check for the tensor-core kernel. */
 treewy_status_t treewy_attn_verify_generic(const treewy_kv_cache_t *cache, const treewy_tree_t *tree, const void *q,
                                            int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,

@@ -229,3 +229,67 @@ def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tenso
     tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, _tree_ref(tree), k.data_ptr(), ld_k, v.data_ptr(),
              ld_v, _int32(accepted, B, "accepted"), cache._dt, _int32(new_context_len, B, "new_context_len"),
              _int32(seq_status, B, "seq_status"), _stream(stream, k))
+
+
+class AttentionLayer:
+    """One attention layer's side of a speculative round, on the current stream: the paged cache, the rotary table and
+    a workspace stay with the layer; each call takes the round's packed rows.  The cache's ``context_len`` is
+    advanced by ``commit`` and ``append_and_attend``.  Layers of one model that share a context_len array have to leave
+    that to one of them: the others pass advance=False."""
+
+    def __init__(self, cache: KVCache, H_q: int, cos_sin: torch.Tensor, pair_axis: torch.Tensor | None = None,
+                 interleaved: bool = False, scale: float | None = None):
+        if H_q < 1 or H_q % cache.H_kv != 0:
+            raise ValueError("H_q: a multiple of the cache's heads wanted")
+        self.cache, self.H_q = cache, H_q
+        self.cos_sin, self.pair_axis, self.interleaved = cos_sin, pair_axis, interleaved
+        self.scale = cache.d_head ** -0.5 if scale is None else scale
+        self._new_len = torch.empty_like(cache.context_len)
+        self._ws, self._ws_for = None, None
+
+    def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
+        sizes = (tree.B, tree.T, tree.max_nodes, shared_len)
+        if self._ws_for != sizes:
+            ws = attn_workspace(self.cache, tree, self.H_q, shared_len)
+            if self._ws is None or ws.numel() > self._ws.numel():
+                self._ws = ws
+            self._ws_for = sizes
+        return self._ws
+
+    def _out(self, q: torch.Tensor) -> torch.Tensor:
+        return torch.empty((q.shape[0], self.H_q, self.cache.d_head), dtype=q.dtype, device=q.device)
+
+    def _rope(self, positions: torch.Tensor) -> Rope:
+        return Rope(self.cos_sin, positions, self.pair_axis, self.interleaved)
+
+    def verify(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               seq_status: torch.Tensor | None = None, shared_pages: torch.Tensor | None = None,
+               shared_len: int = 0) -> torch.Tensor:
+        """Rotates q and k in place (keep k and v until commit) and returns the attention's output for every node."""
+        rope = self._rope(positions)
+        treewy_rope(rope, q, q)
+        treewy_rope(rope, k, k)
+        O = self._out(q)
+        treewy_attn_verify(self.cache, tree, q, k, v, self.scale, O, self._workspace(tree, shared_len), shared_pages,
+                           shared_len, seq_status)
+        return O
+
+    def commit(self, tree: Tree, k: torch.Tensor, v: torch.Tensor, accepted: torch.Tensor,
+               seq_status: torch.Tensor | None = None, advance: bool = True) -> None:
+        """The accepted path's keys and values enter the cache (flagged sequences keep their length)."""
+        self._new_len.copy_(self.cache.context_len)
+        treewy_kv_commit(self.cache, tree, k, v, accepted, self._new_len, seq_status)
+        if advance:
+            self.cache.context_len.copy_(self._new_len)
+
+    def append_and_attend(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                          seq_status: torch.Tensor | None = None) -> torch.Tensor:
+        """Ordinary decoding: one token a sequence, written to the cache (rotated on the way) and attended from there."""
+        if tree.T != tree.B:
+            raise ValueError("tree: one node a sequence wanted")
+        q_out, O = self._out(q), self._out(q)
+        treewy_kv_append(self.cache, tree.node_offsets, k, v, self._rope(positions), q, q_out, seq_status)
+        self.cache.context_len.add_(1)
+        alone = Tree(**{**vars(tree), "anc_mask": torch.zeros_like(tree.anc_mask)})   # the token is in the cache already
+        treewy_attn_verify(self.cache, alone, q_out, k, v, self.scale, O, self._workspace(tree, 0), seq_status=seq_status)
+        return O

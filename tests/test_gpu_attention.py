@@ -520,3 +520,37 @@ def test_rounds_of_a_layer_equal_attention_over_the_accepted_tokens():
             ref, size = au.attn_reference(one)
             au.assert_attn(one, O.cpu()[lo + acc[b]][None], ref, size, tensor_cores=True)
     assert new_len.tolist() == [s[0].shape[0] for s in seen]
+
+
+def test_hybrid_example_decodes_the_same_tokens_with_and_without_trees():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "hybrid_decode.py")
+    spec = importlib.util.spec_from_file_location("hybrid_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    assert example.main(["--sequences", "3", "--tokens", "20", "--nodes", "9"]) == 0
+    assert example.main(["--sequences", "2", "--tokens", "30", "--nodes", "40"]) == 0
+
+
+@pytest.mark.parametrize("D,skip", [(64, 0), (128, 5), (256, 3)])
+def test_a_wait_that_runs_out_raises_timeout_and_leaves_the_stream_usable(D, skip):
+    """One item's copies are never issued (nothing is in flight for it) and the waits get about a millisecond: the call has
+    to return, say so in the status, and leave the stream fit for the next call."""
+    from paper_2608_20961_b200 import binding as tw
+    c = au.make_case([500, 700, 90], [3, 9, 1], Hq=8, Hkv=2, D=D, seed=12)
+    ref, size = au.attn_reference(c)
+    t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    try:
+        tw.treewy_debug_inject(2_000_000, skip)
+        t0.record()
+        _, status = au.run_attn(c)
+        t1.record()
+        torch.cuda.synchronize()
+    finally:
+        tw.treewy_debug_inject(0, -1)
+    assert t0.elapsed_time(t1) < 2000.0
+    assert any(s & tw.SEQ_TIMEOUT for s in status) and not any(s & ~tw.SEQ_TIMEOUT for s in status)
+    O, status = au.run_attn(c)
+    assert not any(status)
+    au.assert_attn(c, O, ref, size, tensor_cores=True)
