@@ -78,8 +78,14 @@ struct Item {
     int b, h, lo, n, len;       // b = -1: the shared prompt
     int row0, rows;             // this CTA's row tile: first row, rows in it
     int kt0, tiles, kts;        // first key tile here, tiles here, tiles of the whole item
-    int slot;                   // where a cut item's part goes, or -1: the item is whole
+    // tiles by their keys: 0 .. full-1 are whole, the draft rows are tile `draft`, any other is the cached tokens' last
+    // one, with `rest` keys
+    int full, draft, rest;
+    // where this part's unnormalised output goes; cap 0: the item is whole and goes to O as it is
+    float *blk_o, *blk_ml;
+    int cap;
 };
+__device__ __forceinline__ int keys_of(int j, int full, int draft, int rest, int n) { return j < full ? KT : j == draft ? n : rest; }
 
 struct Seq {
     int lo, n, len, kts, row_tiles, groups, ov;
@@ -154,19 +160,6 @@ __device__ __forceinline__ int part_of(long long unit, long long W, int parts) {
 // Slot of part g's piece of the item that begins at `begin`: a part cuts at most two items, the one its own start
 // falls into and one more.
 __device__ __forceinline__ int slot_of(int g, long long begin, long long u0) { return begin <= u0 ? 2 * g : 2 * g + 1; }
-
-// The tiles of an item's part by their keys, kept in registers: tiles 0 .. full-1 are whole, the draft rows are tile
-// `draft`, and any other is the cached tokens' last one, with `rest` keys.
-struct Tiles {
-    int full, draft, rest, n;
-    __device__ __forceinline__ Tiles(const AttnArgs &a, const Item &it)
-    {
-        const int own = it.b < 0 ? it.len : it.len - a.shared_len;
-        full = own / KT - it.kt0, rest = own % KT, n = it.n;
-        draft = it.b < 0 ? 0x7fffffff : it.kts - 1 - it.kt0;
-    }
-    __device__ __forceinline__ int valid(int j) const { return j < full ? KT : j == draft ? n : rest; }
-};
 
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
@@ -296,6 +289,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             const int ps = 1 << a.log_page;
             unsigned filled = 0;    // tiles whose copies were issued
             int cur_b = -1;
+            auto mark_bad = [&](int b, unsigned ord) {
+                sh.bad_item[ord % 16] = ord + 1;
+                if (b >= 0 && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
+            };
             // 0: all done, 1: a wait ran out, 2: stopped on purpose
             auto run = [&](auto box_, auto is_v_) -> int {
                 constexpr int BOX = decltype(box_)::value;
@@ -331,7 +328,21 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             it.b = b, it.h = h, it.lo = s.lo, it.n = s.n, it.len = s.len;
                             it.row0 = (int)row0, it.rows = (int)min((long long)MT, rows - row0);
                             it.kt0 = kt0, it.tiles = kt1 - kt0, it.kts = s.kts;
-                            it.slot = kt0 == 0 && kt1 == s.kts ? -1 : slot_of(group, begin, u0);
+                            const int own = b < 0 ? s.len : s.len - a.shared_len;
+                            it.full = own / KT - kt0, it.rest = own % KT, it.draft = b < 0 ? 0x7fffffff : s.kts - 1 - kt0;
+                            long long blk = 0;
+                            it.blk_o = it.blk_ml = nullptr, it.cap = 0;
+                            if (kt0 > 0 || kt1 < s.kts) {
+                                it.blk_o = ws.slot_o, it.blk_ml = ws.slot_ml, it.cap = ws.slot_cap;
+                                blk = (long long)slot_of(group, begin, u0) * R + member;
+                            } else if (b < 0) {
+                                it.blk_o = ws.shared_o, it.blk_ml = ws.shared_ml, it.cap = MT;
+                                blk = (long long)h * s.row_tiles + it.row0 / MT;
+                            } else if (a.shared_len > 0) {
+                                it.blk_o = ws.own_o, it.blk_ml = ws.own_ml, it.cap = ws.own_cap;
+                                blk = ((long long)b * a.c.H_kv + h) * ws.own_tiles + it.row0 / MT;
+                            }
+                            it.blk_o += blk * it.cap * D, it.blk_ml += blk * it.cap * 2;
                         }
                         if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
                         sh.items[r] = it;
@@ -348,7 +359,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     const int n = it.tiles, key0 = it.b < 0 ? 0 : a.shared_len;
                     const int *table = it.b < 0 ? a.shared_pages : a.c.page_table + (size_t)it.b * a.c.max_pages;
                     // whole tiles of cached tokens; the last of an item may be short, and then there are the draft rows
-                    const int whole = (it.len - key0) / KT - it.kt0;
+                    const int whole = it.full;
                     int pages[B::P];
                     auto load_pages = [&](int j) {
                         const int *t = table + ((key0 + (it.kt0 + j) * KT) >> a.log_page);
@@ -375,7 +386,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 for (int i = 0; i < B::P; ++i)
                                     if ((unsigned)pages[i] >= (unsigned)a.c.n_pages) pages[i] = a.c.n_pages;
                             }
-                            if (bad && !IS_V) sh.bad_item[ord % 16] = ord + 1;
+                            if (bad && !IS_V) mark_bad(it.b, ord);
                             ptx::mbar_arrive_expect_tx(full, C::STAGE);
                             if constexpr (IS_V) {
 #pragma unroll
@@ -392,7 +403,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 for (int i = 0; i < KT / 8; ++i)
                                     ptx::tma_load_5d(dst + i * B::K_GROUP, cache, 0, (8 * i) % BOX, 0, it.h, pages[8 * i / BOX], full);
                             }
-                        } else if (it.b >= 0 && kt == it.kts - 1) {  // draft rows, 8 and one chunk at a time
+                        } else if (j == it.draft) {  // draft rows, 8 and one chunk at a time
                             const int groups = (it.n + 7) / 8;
                             ptx::mbar_arrive_expect_tx(full, groups * C::NC * 1024u);
 #pragma unroll 1
@@ -406,7 +417,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             constexpr int ROWS = IS_V || B::K_BY_CHUNK ? BOX : 8, COPIES = !IS_V && B::K_BY_CHUNK ? C::NC : 1;
                             const int boxes = (it.len - token + ROWS - 1) / ROWS;
                             for (int i = 0; i < boxes; ++i) bad |= (unsigned)table[(token + i * ROWS) >> a.log_page] >= (unsigned)a.c.n_pages;
-                            if (bad && !IS_V) sh.bad_item[ord % 16] = ord + 1;
+                            if (bad && !IS_V) mark_bad(it.b, ord);
                             ptx::mbar_arrive_expect_tx(full, boxes * ROWS * C::NC * 128u);
 #pragma unroll 1
                             for (int i = 0; i < boxes; ++i) {
@@ -474,7 +485,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     cur_b = it.b;
                     ptx::mbar_arrive(&sh.item_empty[r]);
                     const int n = it.tiles;
-                    const Tiles tiles(a, it);
                     if (warp == MMA_QK) {
                         if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                         for (int j = 0; j < n; ++j) {
@@ -499,7 +509,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
                             ptx::tc_fence_after_sync();
                             const uint32_t vaddr = ptx::smem_u32(v_stages + sidx * C::STAGE);
-                            const int steps = (tiles.valid(j) + 15) / 16;
+                            const int steps = (keys_of(j, it.full, it.draft, it.rest, it.n) + 15) / 16;
 #pragma unroll
                             for (int s = 0; s < KT / 16; ++s)
                                 if (s < steps) {
@@ -572,7 +582,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             unsigned tile = 0;
             Mine me{&sh.items[0], 0, 0, 0}, next;
             int n = 0;
-            Tiles tiles(a, sh.items[0]);
+            int full = 0, draft_at = 0, rest = 0;     // (registers: read at every tile)
             // (the round before the first item only takes that one)
             for (unsigned ord = ~0u;; ++ord) {
                 const Item &it = *me.it;
@@ -593,8 +603,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         taken = true;
                     }
                     if (j >= n) break;
-                    const int valid = tiles.valid(j);
-                    const bool draft = j == tiles.draft;
+                    const int valid = keys_of(j, full, draft_at, rest, it.n);
+                    const bool draft = j == draft_at;
                     float m0 = -INFINITY;
                     if (g > 0) {
                         if (!row_max(&sh.m[row], g - 1, &m0)) return false;
@@ -736,18 +746,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 ptx::tc_fence_after_sync();
                 const bool bad = sh.bad_item[ord % 16] == ord + 1;
                 if (tid == 0) sh.nonfinite[(ord + 2) & 3][0] = sh.nonfinite[(ord + 2) & 3][1] = 0;
-                if (bad && it.b >= 0 && row == 0 && wg == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
                 uint64_t nf = me.tree & ((uint64_t)sh.nonfinite[ord & 3][0] | (uint64_t)sh.nonfinite[ord & 3][1] << 32);
-                // the block of an item that is not stored as it is
-                float *blk_o = ws.slot_o, *blk_ml = ws.slot_ml;
-                int blk_cap = ws.slot_cap;
-                long long blk = (long long)it.slot * R + member;
-                if (it.slot < 0) {
-                    const int rt = it.row0 / MT;
-                    if (it.b < 0) blk_o = ws.shared_o, blk_ml = ws.shared_ml, blk_cap = MT, blk = it.h * (((long long)a.T * a.G + MT - 1) / MT) + rt;
-                    else blk_o = ws.own_o, blk_ml = ws.own_ml, blk_cap = ws.own_cap, blk = ((long long)it.b * a.c.H_kv + it.h) * ws.own_tiles + rt;
-                }
-                blk_o += blk * blk_cap * D, blk_ml += blk * blk_cap * 2;
+                const int cap = it.cap;
+                const long long orow = (long long)me.t * a.H_q + me.hq;
+                __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
+                const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
                 constexpr int HALF = D / 2, EC = 32;  // this warpgroup's columns, and how many at a time
 #pragma unroll 1
                 for (int c = wg * HALF; c < (wg + 1) * HALF; c += EC) {
@@ -762,10 +765,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         ptx::mbar_arrive_warp(&sh.o_free);
                     }
                     if (on) {
-                        const long long orow = (long long)me.t * a.H_q + me.hq;
-                        if (it.slot < 0 && a.shared_len == 0) {
-                            const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
-                            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c;
+                        if (cap == 0) {
+                            __nv_bfloat16 *out = out_row + c;
                             if (!bad) {
 #pragma unroll
                                 for (int i = 0; i < EC; i += 8) {
@@ -778,11 +779,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 }
                             }
                         } else {
-                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(blk_ml + 2 * row) = make_float2(m, bad ? -1.f : l);
-                            float *po = blk_o + ((long long)(c / 4) * blk_cap + row) * 4;
+                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(it.blk_ml + 2 * row) = make_float2(m, bad ? -1.f : l);
+                            float *po = it.blk_o + (c / 4 * cap + row) * 4;
 #pragma unroll
                             for (int i = 0; i < EC; i += 4)
-                                *reinterpret_cast<uint4 *>(po + i * blk_cap) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                                *reinterpret_cast<uint4 *>(po + i * cap) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                         }
                     }
                     __syncwarp();
@@ -791,16 +792,15 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     for (; nf; nf &= nf - 1) {  // seen draft rows with NaN or infinity: those elements, onto what was stored
                         const int jn = __ffsll((long long)nf) - 1;
                         const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(a.v) + (it.lo + jn) * a.ld_v + (long long)it.h * D;
-                        const long long orow = (long long)me.t * a.H_q + me.hq;
 #pragma unroll 1
                         for (int c = wg * HALF; c < (wg + 1) * HALF; ++c) {
                             const float x = to_f32(v[c]);
                             if (isfinite(x)) continue;
-                            if (it.slot < 0 && a.shared_len == 0) {
-                                __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c;
+                            if (cap == 0) {
+                                __nv_bfloat16 *out = out_row + c;
                                 if (!bad) *out = __float2bfloat16_rn(to_f32(*out) + x);
                             } else {
-                                float *out = blk_o + ((long long)(c / 4) * blk_cap + row) * 4 + c % 4;
+                                float *out = it.blk_o + (c / 4 * cap + row) * 4 + c % 4;
                                 *out += x;
                             }
                         }
@@ -811,7 +811,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 if (next.it->tiles == 0) return true;
                 tile += n;
                 me = next, n = me.it->tiles, cur_b = me.it->b;
-                tiles = Tiles(a, *me.it);
+                full = me.it->full, draft_at = me.it->draft, rest = me.it->rest;
             }
         };
         const bool ok = run();
