@@ -36,12 +36,15 @@ constexpr int MT = 128;                // rows of a tile
 constexpr int MAX_CTAS = 160;
 constexpr int THREADS = 384, PRODUCER_K = 8, PRODUCER_V = 9, MMA_QK = 10, MMA_PV = 11;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
-constexpr int MIN_UNITS = 2;           // of a CTA's part: below this a part is mostly start and end
-// What starting an item costs, in tiles, by the rows of its first row tile (queries into tensor memory, the pipeline's
-// start, the output): measured over 3 to 12.  Heads of 256 with full row tiles, 64 trees under one prompt: 207 us at 3,
-// 157 at 8, 156 at 12; one row of 4 heads, 64 sequences of up to 8k: 183 at 3, 172 at 5, 177 at 8.
-constexpr int OV_MAX = 9;
-__device__ __forceinline__ int start_cost(long long rows) { return rows > 32 ? OV_MAX : 5; }
+constexpr int MAX_START = 40, MAX_TILE = 5;
+constexpr int MIN_UNITS = 8;           // of a CTA's part: below this a part is mostly start and end
+// What a tile and the start of an item cost, in quarters of a tile of few rows, by the rows of the row tile.  With up to
+// 32 rows one softmax warp in four works and a tile takes 0.47 us (0.53 where HBM bounds it); with 128 all of them share the
+// exponentials' pipe and it takes 0.63.  A start (queries into tensor memory, the pipeline's start, the output) takes 2 us,
+// 3.1 beside a shared prompt (every output is a block in fp32) and about 6 with 128 rows.  (A part's time against its tiles and
+// items, least squares over the 148 parts of the benchmark's cases.)
+__device__ __forceinline__ int tile_cost(long long rows) { return rows > 32 ? 5 : 4; }
+__device__ __forceinline__ int start_cost(long long rows, bool shared) { return rows > 32 ? MAX_START : shared ? 30 : 20; }
 constexpr float LAZY = 8.f;
 
 template <int D> struct Cfg {
@@ -88,8 +91,10 @@ struct Item {
 __device__ __forceinline__ int keys_of(int j, int full, int draft, int rest, int n) { return j < full ? KT : j == draft ? n : rest; }
 
 struct Seq {
-    int lo, n, len, kts, row_tiles, groups, ov;
-    unsigned units;             // H_kv * groups * (ov + kts), below 2^31 (the launcher has checked)
+    int lo, n, len, kts, row_tiles, groups;
+    int ov, wt;                 // cost of an item's start and of a tile
+    unsigned per;               // of an item: ov + wt * kts
+    unsigned units;             // H_kv * groups * per, below 2^31 (the launcher has checked)
 };
 
 struct Shared {
@@ -129,7 +134,7 @@ __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *st
     *status = 0;
     if (b < 0) {
         s.lo = 0, s.n = 0, s.len = a.shared_len, s.kts = tiles_of(a.shared_len);
-        s.row_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT), s.ov = start_cost((long long)a.T * a.G);
+        s.row_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT), s.ov = start_cost((long long)a.T * a.G, true), s.wt = tile_cost((long long)a.T * a.G);
     } else {
         *status = check_sequence(a.node_offsets, a.c.context_len, b, a.T, a.max_nodes,
                                  (long long)a.c.max_pages * a.c.page_size, a.shared_len, &s.lo, &s.n, &s.len);
@@ -138,10 +143,11 @@ __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *st
             return s;
         }
         s.kts = tiles_of(s.len - a.shared_len) + 1;
-        s.row_tiles = (s.n * a.G + MT - 1) / MT, s.ov = start_cost((long long)s.n * a.G);
+        s.row_tiles = (s.n * a.G + MT - 1) / MT, s.ov = start_cost((long long)s.n * a.G, a.shared_len > 0), s.wt = tile_cost((long long)s.n * a.G);
     }
     s.groups = (s.row_tiles + R - 1) / R;
-    s.units = (unsigned)a.c.H_kv * s.groups * (s.ov + s.kts);
+    s.per = s.ov + s.wt * s.kts;
+    s.units = (unsigned)a.c.H_kv * s.groups * s.per;
     return s;
 }
 // (What the main kernel does not do once a tile is out of line: its roles run at the same time and share the
@@ -153,10 +159,12 @@ static __device__ __noinline__ long long div64(long long x, long long y)
 {
     return ((x | y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
 }
-// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  An item takes ov + kts
-// units, tile t the (ov + t)-th of them.
+// parts: CTA groups that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  An item takes ov + wt kts
+// units and tile t begins at ov + wt t of them: it belongs to the part that this unit is in.
 __device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return div64(g * W, parts); }
 __device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)div64((unit + 1) * parts - 1, W); }
+// tiles of an item that begin before unit o of it
+__device__ __forceinline__ int tiles_before(int o, int ov, int wt, int kts) { return o <= ov ? 0 : min(kts, (o - ov + wt - 1) / wt); }
 // Slot of part g's piece of the item that begins at `begin`: a part cuts at most two items, the one its own start
 // falls into and one more.
 __device__ __forceinline__ int slot_of(int g, long long begin, long long u0) { return begin <= u0 ? 2 * g : 2 * g + 1; }
@@ -318,9 +326,9 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 s = load_seq(a, b, R, &st2);
                                 continue;
                             }
-                            const unsigned per = s.kts + s.ov, i_ = off / per, o = off - i_ * per, h = i_ / s.groups, rg = i_ - h * s.groups;
-                            const int span = (int)min((long long)(per - o), u1 - u);
-                            const int kt0 = max(0, (int)o - s.ov), kt1 = max(0, (int)o + span - s.ov);
+                            const unsigned i_ = off / s.per, o = off - i_ * s.per, h = i_ / s.groups, rg = i_ - h * s.groups;
+                            const int span = (int)min((long long)(s.per - o), u1 - u);
+                            const int kt0 = tiles_before(o, s.ov, s.wt, s.kts), kt1 = tiles_before(o + span, s.ov, s.wt, s.kts);
                             const long long begin = u - o;
                             const long long row0 = (long long)(rg * R + member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
                             off += span, u += span;
@@ -462,11 +470,12 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 int pieces = 0;
                 if (u1 > u0) {
                     const Seq s = load_seq(a, sh.last_b, R, &st);
-                    const unsigned last = (unsigned)sh.last_off, per = s.kts + s.ov, it = last / per;
-                    const long long begin = u1 - 1 - (last - it * per), first = begin + s.ov;
+                    const unsigned last = (unsigned)sh.last_off, per = s.per, it = last / per;
+                    const long long begin = u1 - 1 - (last - it * per);
+                    const int kt0 = tiles_before((int)max(0ll, u0 - begin), s.ov, s.wt, s.kts), kt1 = tiles_before((int)(u1 - begin), s.ov, s.wt, s.kts);
                     const int row0 = ((int)(it % s.groups) * R + member) * MT;
-                    if (first >= u0 && first < u1 && first + s.kts > u1 && row0 < s.n * a.G) {
-                        pieces = part_of(first + s.kts - 1, W, parts) - group + 1;
+                    if (kt0 == 0 && kt1 > 0 && kt1 < s.kts && row0 < s.n * a.G) {
+                        pieces = part_of(begin + s.ov + s.wt * (s.kts - 1), W, parts) - group + 1;
                         d[1] = slot_of(group, begin, u0);
                         d[2] = s.lo, d[3] = (int)(it / s.groups), d[4] = row0, d[5] = min(MT, s.n * a.G - row0), d[6] = group;
                     }
@@ -955,11 +964,11 @@ __global__ void __launch_bounds__(128) attn_join_shared_kernel(const __grid_cons
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {  // the prompt, then the sequence's own keys
         const int kts = pass == 0 ? prompt.kts : own.kts, groups = pass == 0 ? prompt.groups : own.groups;
-        const int ov = pass == 0 ? prompt.ov : own.ov;
+        const int ov = pass == 0 ? prompt.ov : own.ov, wt = pass == 0 ? prompt.wt : own.wt;
         const unsigned i = pass == 0 ? own.lo * a.G + r : r;  // the row in the list that the item's tiles cut up
         const int tile = i / MT, in_tile = i % MT, rg = tile / R, member = tile - rg * R;
-        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (ov + kts);
-        const int g0 = part_of(begin + ov, W, parts), g1 = part_of(begin + ov + kts - 1, W, parts);
+        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (ov + wt * kts);
+        const int g0 = part_of(begin + ov, W, parts), g1 = part_of(begin + ov + wt * (kts - 1), W, parts);
         if (g0 == g1) {
             const long long blk = pass == 0 ? (long long)h * prompt.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
             const int cap = pass == 0 ? MT : ws.own_cap;
@@ -1066,8 +1075,9 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
 // The units of one sequence, and of the shared prompt, stay below 2^31.
 static bool units_fit(const AttnArgs &a)
 {
-    const long long own = ((long long)a.max_nodes * a.G + MT - 1) / MT * (((long long)a.c.max_pages * a.c.page_size) / KT + 2 + OV_MAX);
-    const long long shared = ((long long)a.T * a.G + MT - 1) / MT * (a.shared_len / KT + 2 + OV_MAX);
+    const long long own = ((long long)a.max_nodes * a.G + MT - 1) / MT *
+                          (((long long)a.c.max_pages * a.c.page_size / KT + 2) * MAX_TILE + MAX_START);
+    const long long shared = ((long long)a.T * a.G + MT - 1) / MT * ((a.shared_len / KT + 2ll) * MAX_TILE + MAX_START);
     const long long most = 0x7fffffffll / a.c.H_kv;
     return own <= most && shared <= most;
 }
