@@ -117,18 +117,20 @@ struct Shared {
 // element (row, c) at ((c / 4) * cap + row) * 4 + c % 4, so that the rows of a warp are neighbours when its threads
 // write a column group each of their own row; (m, l) of the rows beside it.
 struct Ws {
-    long long *prefix;          // [B + 2]: first unit of each sequence (shared prompts), all units, parts
     int *desc;                  // [MAX_CTAS][8]: the item that a CTA's part cuts at its end
+    int4 *own_at, *shared_at;   // beside a shared prompt: where each item's parts are, [B][H_kv][own_tiles], [H_kv][tiles]
     float *slot_ml, *slot_o;    // cut items: [2 * CTAs] blocks
     float *own_ml, *own_o;      // whole items beside a shared prompt: [B][H_kv][own_tiles] blocks
     float *shared_ml, *shared_o;  // the shared prompt's whole items: [H_kv][tiles] blocks of MT rows
-    int slot_cap, own_cap, own_tiles;
+    int slot_cap, own_cap, own_tiles, shared_tiles;
 };
 
 __device__ __forceinline__ int tiles_of(int tokens) { return (tokens + KT - 1) / KT; }
 
 // b = -1: the shared prompt, whose rows are those of all sequences
-__device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *status)
+// (What the main kernel does not do once a tile is out of line: its roles run at the same time and share the
+// instruction cache.)
+static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status)
 {
     Seq s;
     *status = 0;
@@ -150,10 +152,6 @@ __device__ __forceinline__ Seq read_seq(const AttnArgs &a, int b, int R, int *st
     s.units = (unsigned)a.c.H_kv * s.groups * s.per;
     return s;
 }
-// (What the main kernel does not do once a tile is out of line: its roles run at the same time and share the
-// instruction cache.)
-static __device__ __noinline__ Seq load_seq(const AttnArgs &a, int b, int R, int *status) { return read_seq(a, b, R, status); }
-
 // (a 64-bit division takes several times as long as a 32-bit one, and nearly every line of work is short)
 static __device__ __noinline__ long long div64(long long x, long long y)
 {
@@ -271,7 +269,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
     for (int b = b_begin; b < b_end; ++b) {
         if (chunk > 1) only = load_seq(a, b, R, &st);
         const long long units = only.units;
-        if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[b] = before;
         if (u1 > u0) {
             if (u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before, sh.first_seq = only;
             if (u1 - 1 >= before && u1 - 1 < before + units) sh.last_b = b, sh.last_off = u1 - 1 - before;
@@ -279,7 +276,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         before += units;
     }
     if (tid == 0) {
-        if (blockIdx.x == 0 && a.shared_len > 0) ws.prefix[a.B] = W, ws.prefix[a.B + 1] = parts;
         if (u1 > u0 && u0 < shared_units) sh.first_b = -1, sh.first_off = u0, sh.first_seq = load_seq(a, -1, R, &st);
         if (u1 > u0 && u1 - 1 < shared_units) sh.last_b = -1, sh.last_off = u1 - 1;
     }
@@ -340,15 +336,16 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             it.full = own / KT - kt0, it.rest = own % KT, it.draft = b < 0 ? 0x7fffffff : s.kts - 1 - kt0;
                             long long blk = 0;
                             it.blk_o = it.blk_ml = nullptr, it.cap = 0;
-                            if (kt0 > 0 || kt1 < s.kts) {
-                                it.blk_o = ws.slot_o, it.blk_ml = ws.slot_ml, it.cap = ws.slot_cap;
-                                blk = (long long)slot_of(group, begin, u0) * R + member;
-                            } else if (b < 0) {
-                                it.blk_o = ws.shared_o, it.blk_ml = ws.shared_ml, it.cap = MT;
-                                blk = (long long)h * s.row_tiles + it.row0 / MT;
-                            } else if (a.shared_len > 0) {
-                                it.blk_o = ws.own_o, it.blk_ml = ws.own_ml, it.cap = ws.own_cap;
-                                blk = ((long long)b * a.c.H_kv + h) * ws.own_tiles + it.row0 / MT;
+                            const bool cut = kt0 > 0 || kt1 < s.kts;
+                            if (cut || a.shared_len > 0) {
+                                const int tile = it.row0 / MT;
+                                const long long i = b < 0 ? (long long)h * s.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
+                                blk = cut ? (long long)slot_of(group, begin, u0) * R + member : i;
+                                it.blk_o = cut ? ws.slot_o : b < 0 ? ws.shared_o : ws.own_o, it.blk_ml = cut ? ws.slot_ml : b < 0 ? ws.shared_ml : ws.own_ml;
+                                it.cap = cut ? ws.slot_cap : b < 0 ? MT : ws.own_cap;
+                                if (kt0 == 0 && kt1 > 0 && a.shared_len > 0)
+                                    (b < 0 ? ws.shared_at : ws.own_at)[i] =
+                                        make_int4((int)blk, cut ? part_of(begin + s.ov + s.wt * (s.kts - 1), W, parts) - group + 1 : 0, group, 0);
                             }
                             it.blk_o += blk * it.cap * D, it.blk_ml += blk * it.cap * 2;
                         }
@@ -833,32 +830,22 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
     if (warp == MMA_QK) ptx::tmem_dealloc(tmem, 512);
 }
 
-// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item.  Where an
-// item may be cut into many (a single sequence into as many as there are CTAs) a CTA takes 8 rows and its warps take turns at
-// the parts, since one warp would wait for each in turn; their sums meet in shared memory in the order of the warps.  Lane = row + 8 * column group, 4 groups of 4
-// columns a step, so that both the blocks (8 rows of a group are 128 bytes) and the output (4 groups of a row are 32) move in
-// whole sectors.  A part of a sequence with a bad page has l = -1: the row is left.
-template <int D> struct Join {
-    static constexpr int WARPS = D == 256 ? 4 : 8, STEPS = D / 16;
-    struct Smem {
-        float4 acc[WARPS][STEPS][32];
-        float2 ml[WARPS][8];
-    };
+// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys.  A warp
+// takes 8 rows and 16 STEPS columns of them: lane = row + 8 * column group, 4 groups of 4 columns a step, so that both the
+// blocks (8 rows of a group are 128 bytes) and the output (4 groups of a row are 32) move in whole sectors.  Warps share out
+// columns, not parts: nothing has to meet (with the parts over warps that met in shared memory, too few of a CTA's warps had
+// work; the trees above took 94 us).  The blocks come out of L2, where the main kernel left them.  A part of a sequence with a bad page has l = -1: the row is left.
+template <int STEPS> struct Join {
     float4 acc[STEPS];
     float m = -INFINITY, l = 0.f;
     bool bad = false;
-    __device__ __forceinline__ void start()
+    __device__ __forceinline__ Join()
     {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    // block at (ml, o) of cap rows, this lane's row in it
-    __device__ __forceinline__ void add(const float *ml, const float *o, int cap, int row, int cg)
+    __device__ __forceinline__ void add(float2 x, const float4 (&y)[STEPS])
     {
-        const float2 x = *reinterpret_cast<const float2 *>(ml + 2 * row);
-        float4 y[STEPS];
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) y[i] = *reinterpret_cast<const float4 *>(o + ((long long)(4 * i + cg) * cap + row) * 4);
         if (x.y < 0.f) bad = true;
         if (x.y == 0.f) return;  // saw nothing
         const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
@@ -870,7 +857,7 @@ template <int D> struct Join {
             acc[i].z = acc[i].z * f0 + y[i].z * f1, acc[i].w = acc[i].w * f0 + y[i].w * f1;
         }
     }
-    // one warp's rows, joined by it alone
+    // out: this lane's row, at the warp's first column
     __device__ __forceinline__ void store(__nv_bfloat16 *out, int cg)
     {
         if (bad) return;
@@ -880,117 +867,119 @@ template <int D> struct Join {
             *reinterpret_cast<uint2 *>(out + 16 * i + 4 * cg) =
                 make_uint2(pack_bf16(acc[i].x * inv, acc[i].y * inv), pack_bf16(acc[i].z * inv, acc[i].w * inv));
     }
-    // the CTA's 8 rows, joined by all of its warps; on: the row exists
-    __device__ __forceinline__ void finish(Smem &sm, __nv_bfloat16 *out, bool on)
-    {
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cg = lane >> 3;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) sm.acc[warp][i][lane] = acc[i];
-        if (cg == 0) sm.ml[warp][lane & 7] = make_float2(m, bad ? -1.f : l);
-        __syncthreads();
-        float top = -INFINITY;
-        bool any_bad = false;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float2 x = sm.ml[w][lane & 7];
-            if (x.y != 0.f) top = fmaxf(top, x.x);
-            any_bad |= x.y < 0.f;
-        }
-        const float ref = top == -INFINITY ? 0.f : top;
-        float f[WARPS], sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float2 x = sm.ml[w][lane & 7];
-            f[w] = x.y == 0.f ? 0.f : ptx::ex2(x.x - ref);
-            sum += x.y * f[w];
-        }
-        if (!on || any_bad) return;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        for (int i = warp; i < STEPS; i += WARPS) {
-            float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float4 y = sm.acc[w][i][lane];
-                t.x += y.x * f[w], t.y += y.y * f[w], t.z += y.z * f[w], t.w += y.w * f[w];
-            }
-            *reinterpret_cast<uint2 *>(out + 16 * i + 4 * cg) =
-                make_uint2(pack_bf16(t.x * inv, t.y * inv), pack_bf16(t.z * inv, t.w * inv));
-        }
-    }
 };
-
-// Items that a part cut: grid (CTAs of the main kernel, rows of a tile / 8).
-template <int D>
-__global__ void __launch_bounds__(Join<D>::WARPS * 32) attn_join_cut_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
+// column groups 4 i + cg from column c0 on, of one row of a block of cap rows
+template <int STEPS> __device__ __forceinline__ void load_part(float4 (&y)[STEPS], const float *block, int cap, int row, int c0, int cg)
 {
-    __shared__ typename Join<D>::Smem sm;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cg = lane >> 3, row = blockIdx.y * 8 + (lane & 7);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+        y[i] = __ldcs(reinterpret_cast<const float4 *>(block + ((long long)(c0 / 4 + 4 * i + cg) * cap + row) * 4));
+}
+
+constexpr int JOIN_WARPS = 8;
+
+// Items that a part cut: grid (CTAs of the main kernel, warps of a block / 8).  UN parts are loaded at a time: with few rows
+// there are few warps and many parts (up to one for each CTA), with many rows the other way round.
+template <int D, int STEPS, int UN>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_cut_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
+{
+    constexpr int CW = D / (16 * STEPS);         // warps that share a row
+    const int w = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31, cg = lane >> 3;
+    const int row = w / CW * 8 + (lane & 7), c0 = w % CW * (16 * STEPS);
     grid_dependency_wait();
     grid_dependency_trigger();
     const int4 d0 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x), d1 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x + 4);
     const int pieces = d0.x;
-    if (pieces == 0 || (int)blockIdx.y * 8 >= d1.y) return;
-    const int member = blockIdx.x % R;
-    const bool on = row < d1.y;
-    Join<D> jn;
-    jn.start();
-    if (on)
+    if (pieces == 0 || row >= d1.y) return;
+    const int member = blockIdx.x % R, cap = ws.slot_cap;
+    Join<STEPS> jn;
 #pragma unroll 1
-        for (int p = warp; p < pieces; p += Join<D>::WARPS) {
-            const long long blk = ((long long)(p == 0 ? d0.y : 2 * (d1.z + p)) * R + member) * ws.slot_cap;
-            jn.add(ws.slot_ml + blk * 2, ws.slot_o + blk * D, ws.slot_cap, row, cg);
+    for (int p0 = 0; p0 < pieces; p0 += UN) {
+        float2 x[UN];
+        float4 y[UN][STEPS];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int p = min(p0 + i, pieces - 1);
+            const long long blk = ((long long)(p == 0 ? d0.y : 2 * (d1.z + p)) * R + member) * cap;
+            x[i] = __ldcs(reinterpret_cast<const float2 *>(ws.slot_ml + (blk + row) * 2));
+            load_part<STEPS>(y[i], ws.slot_o + blk * D, cap, row, c0, cg);
         }
+#pragma unroll
+        for (int i = 0; i < UN; ++i)
+            if (p0 + i < pieces) jn.add(x[i], y[i]);
+    }
     const int rr = d1.x + row, node = rr / a.G;
-    jn.finish(sm, static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d0.z + node) * a.H_q + d0.w * a.G + rr - node * a.G) * D, on);
+    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(d0.z + node) * a.H_q + d0.w * a.G + rr - node * a.G) * D + c0, cg);
 }
 
-// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut: rarely more than four
-// blocks, so one warp joins its 8 rows alone.  Grid (rows of the longest tree under one key/value head / 32, key/value
-// heads, sequences).
-template <int D>
-__global__ void __launch_bounds__(128) attn_join_shared_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
+// With a shared prompt every row has two items, its sequence's and the prompt's, each whole or cut.  Grid (warps of the
+// longest tree under one key/value head / 8, key/value heads, sequences).
+template <int D, int STEPS>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws)
 {
-    const int lane = threadIdx.x & 31, cg = lane >> 3, h = blockIdx.y, b = blockIdx.z;
-    const int r = (blockIdx.x * 4 + (threadIdx.x >> 5)) * 8 + (lane & 7);  // row among the sequence's under this head
+    constexpr int CW = D / (16 * STEPS);
+    const int w = blockIdx.x * JOIN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31, cg = lane >> 3, h = blockIdx.y, b = blockIdx.z;
+    const int r = w / CW * 8 + (lane & 7), c0 = w % CW * (16 * STEPS);  // row among the sequence's under this head
     grid_dependency_wait();
     grid_dependency_trigger();
-    const long long W = ws.prefix[a.B], first = ws.prefix[b];
-    const int parts = (int)ws.prefix[a.B + 1];
-    int st, st0;
-    const Seq own = read_seq(a, b, R, &st), prompt = read_seq(a, -1, R, &st0);
-    if (st || r >= own.n * a.G) return;
-    Join<D> jn;
-    jn.start();
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {  // the prompt, then the sequence's own keys
-        const int kts = pass == 0 ? prompt.kts : own.kts, groups = pass == 0 ? prompt.groups : own.groups;
-        const int ov = pass == 0 ? prompt.ov : own.ov, wt = pass == 0 ? prompt.wt : own.wt;
-        const unsigned i = pass == 0 ? own.lo * a.G + r : r;  // the row in the list that the item's tiles cut up
-        const int tile = i / MT, in_tile = i % MT, rg = tile / R, member = tile - rg * R;
-        const long long begin = (pass == 0 ? 0 : first) + (long long)(h * groups + rg) * (ov + wt * kts);
-        const int g0 = part_of(begin + ov, W, parts), g1 = part_of(begin + ov + wt * (kts - 1), W, parts);
-        if (g0 == g1) {
-            const long long blk = pass == 0 ? (long long)h * prompt.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
-            const int cap = pass == 0 ? MT : ws.own_cap;
-            jn.add((pass == 0 ? ws.shared_ml : ws.own_ml) + blk * cap * 2, (pass == 0 ? ws.shared_o : ws.own_o) + blk * cap * D, cap,
-                   in_tile, cg);
+    int lo, n, len;
+    if (check_sequence(a.node_offsets, a.c.context_len, b, a.T, a.max_nodes, (long long)a.c.max_pages * a.c.page_size, a.shared_len, &lo, &n, &len) ||
+        r >= n * a.G)
+        return;
+    // the two items: their parts, and what is loaded first of each
+    struct Where {
+        const float *ml, *o;
+        int cap, row, slot, more;  // slot: the block of the part after the first, if there is one
+    };
+    constexpr int blocks = 2 * MAX_CTAS;
+    auto find = [&](bool is_own) {
+        const unsigned i = is_own ? r : lo * a.G + r;  // the row in the list that the item's tiles cut up
+        const int tile = i / MT, tiles = is_own ? ws.own_tiles : ws.shared_tiles;
+        const int4 at = (is_own ? ws.own_at : ws.shared_at)[((long long)(is_own ? b : 0) * a.c.H_kv + h) * tiles + tile];
+        Where x;
+        x.row = i % MT;
+        if (at.y == 0) {
+            x.ml = is_own ? ws.own_ml : ws.shared_ml, x.o = is_own ? ws.own_o : ws.shared_o, x.cap = is_own ? ws.own_cap : MT;
         } else {
-            int slot = slot_of(g0, begin, part_begin(g0, W, parts));
-#pragma unroll 1
-            for (int p = g0; p <= g1; ++p, slot = 2 * p) {
-                const long long blk = ((long long)slot * R + member) * ws.slot_cap;
-                jn.add(ws.slot_ml + blk * 2, ws.slot_o + blk * D, ws.slot_cap, in_tile, cg);
-            }
+            x.ml = ws.slot_ml, x.o = ws.slot_o, x.cap = ws.slot_cap;
         }
-        if (pass == 0 && jn.bad && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
+        // (a main kernel that ran into its time limit may have left out items: whatever lies there then stays within the workspace)
+        const unsigned most = at.y == 0 ? (is_own ? a.B : 1) * a.c.H_kv * tiles : blocks;
+        const long long blk = min((unsigned)at.x, most - 1);
+        x.slot = min((unsigned)((at.z + 1) * 2 * R + tile % R), (unsigned)blocks);
+        x.more = at.y == 0 ? 0 : at.y - 1;
+        x.ml += blk * x.cap * 2, x.o += blk * x.cap * D;
+        return x;
+    };
+    Join<STEPS> jn;
+    const Where at[2] = {find(false), find(true)};
+    float2 x[2];
+    float4 y[2][STEPS];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[i] = __ldcs(reinterpret_cast<const float2 *>(at[i].ml + 2 * at[i].row));
+        load_part<STEPS>(y[i], at[i].o, at[i].cap, at[i].row, c0, cg);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // the prompt, then the sequence's own keys
+        jn.add(x[i], y[i]);
+#pragma unroll 1
+        for (int p = 0, slot = at[i].slot; p < at[i].more && slot < blocks; ++p, slot += 2 * R) {
+            const long long blk = (long long)slot * ws.slot_cap;
+            const float2 xp = __ldcs(reinterpret_cast<const float2 *>(ws.slot_ml + (blk + at[i].row) * 2));
+            float4 yp[STEPS];
+            load_part<STEPS>(yp, ws.slot_o + blk * D, ws.slot_cap, at[i].row, c0, cg);
+            jn.add(xp, yp);
+        }
+        if (i == 0 && jn.bad && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
     }
     const int node = r / a.G;
-    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(own.lo + node) * a.H_q + h * a.G + r - node * a.G) * D, cg);
+    jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(lo + node) * a.H_q + h * a.G + r - node * a.G) * D + c0, cg);
 }
 
 struct Plan {
-    int R, slot_cap, own_cap, own_tiles;
-    size_t prefix, desc, slots, own, shared;  // elements; rows of the three kinds of block
+    int R, slot_cap, own_cap, own_tiles, shared_tiles;
+    size_t desc, at, slots, own, shared;  // elements; items beside a shared prompt; rows of the three kinds of block
 };
 Plan plan_of(const AttnArgs &a)
 {
@@ -999,11 +988,12 @@ Plan plan_of(const AttnArgs &a)
     p.R = (int)(tiles > 4 ? 4 : tiles);
     p.own_cap = rows > MT ? MT : (int)rows, p.own_tiles = (int)tiles;
     p.slot_cap = a.shared_len > 0 ? MT : p.own_cap;
-    p.prefix = a.B + 2 + (a.B & 1);    // (keeps what follows 16-byte aligned)
     p.desc = 8 * MAX_CTAS;
     p.slots = 2ull * MAX_CTAS * p.slot_cap;
     p.own = a.shared_len > 0 ? (size_t)a.B * a.c.H_kv * p.own_tiles * p.own_cap : 0;
-    p.shared = a.shared_len > 0 ? a.c.H_kv * (((size_t)a.T * a.G + MT - 1) / MT) * MT : 0;
+    p.shared_tiles = (int)(((long long)a.T * a.G + MT - 1) / MT);
+    p.shared = a.shared_len > 0 ? (size_t)a.c.H_kv * p.shared_tiles * MT : 0;
+    p.at = a.shared_len > 0 ? ((size_t)a.B * p.own_tiles + p.shared_tiles) * a.c.H_kv : 0;
     return p;
 }
 
@@ -1017,15 +1007,15 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     const int ctas = (sms < MAX_CTAS ? sms : MAX_CTAS) / p.R * p.R;
     Ws ws;
     unsigned char *at = reinterpret_cast<unsigned char *>(a.ws);
-    ws.prefix = reinterpret_cast<long long *>(at), at += p.prefix * 8;
     ws.desc = reinterpret_cast<int *>(at), at += p.desc * 4;
+    ws.own_at = reinterpret_cast<int4 *>(at), ws.shared_at = ws.own_at + (size_t)a.B * a.c.H_kv * p.own_tiles, at += p.at * 16;
     ws.slot_o = reinterpret_cast<float *>(at), at += p.slots * D * 4;
     ws.own_o = reinterpret_cast<float *>(at), at += p.own * D * 4;
     ws.shared_o = reinterpret_cast<float *>(at), at += p.shared * D * 4;
     ws.slot_ml = reinterpret_cast<float *>(at), at += p.slots * 8;
     ws.own_ml = reinterpret_cast<float *>(at), at += p.own * 8;
     ws.shared_ml = reinterpret_cast<float *>(at);
-    ws.slot_cap = p.slot_cap, ws.own_cap = p.own_cap, ws.own_tiles = p.own_tiles;
+    ws.slot_cap = p.slot_cap, ws.own_cap = p.own_cap, ws.own_tiles = p.own_tiles, ws.shared_tiles = p.shared_tiles;
     a.log_page = 0;
     while ((1 << a.log_page) < a.c.page_size) ++a.log_page;
 
@@ -1064,10 +1054,22 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
     e = launch_dependent(attn_tc_kernel<D>, dim3(ctas), dim3(THREADS), smem, stream, a, p.R, ws, lay, kc, vc, k, v);
     if (e != cudaSuccess) return e;
     if (a.shared_len > 0) {
-        const unsigned x = (unsigned)(((long long)a.max_nodes * a.G + 31) / 32);
-        return launch_dependent(attn_join_shared_kernel<D>, dim3(x, a.c.H_kv, a.B), dim3(128), 0, stream, a, p.R, ws);
+        constexpr int STEPS = 4;
+        const long long warps = ((long long)a.max_nodes * a.G + 7) / 8 * (D / (16 * STEPS));
+        return launch_dependent(attn_join_shared_kernel<D, STEPS>, dim3((unsigned)((warps + JOIN_WARPS - 1) / JOIN_WARPS), a.c.H_kv, a.B),
+                                dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
     }
-    return launch_dependent(attn_join_cut_kernel<D>, dim3(ctas, (p.slot_cap + 7) / 8), dim3(Join<D>::WARPS * 32), 0, stream, a, p.R, ws);
+    auto cut = [&](auto steps, auto un) {
+        constexpr int STEPS = decltype(steps)::value;
+        const int warps = (p.slot_cap + 7) / 8 * (D / (16 * STEPS));
+        return launch_dependent(attn_join_cut_kernel<D, STEPS, decltype(un)::value>, dim3(ctas, (warps + JOIN_WARPS - 1) / JOIN_WARPS),
+                                dim3(JOIN_WARPS * 32), 0, stream, a, p.R, ws);
+    };
+    // Few rows: many parts to an item and few warps, so little of a row to each and many parts at a time (one sequence 14.0 us
+    // instead of 15.4, two of 65537 keys 93.1 instead of 94.6).  Many rows: two or three parts and many warps (32 trees of 32
+    // nodes, heads of 256: 87 us instead of 98, of which the join is 6).
+    if (p.slot_cap <= 32) return cut(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+    return cut(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
 }
 
 }  // namespace
@@ -1095,7 +1097,7 @@ bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io)
 size_t attn_tc_workspace(const AttnArgs &a)
 {
     const Plan p = plan_of(a);
-    return p.prefix * 8 + p.desc * 4 + (p.slots + p.own + p.shared) * (a.c.d + 2) * 4;
+    return p.desc * 4 + p.at * 16 + (p.slots + p.own + p.shared) * (a.c.d + 2) * 4;
 }
 
 cudaError_t launch_attn_tc(const AttnArgs &a, cudaStream_t stream)
