@@ -58,6 +58,7 @@ template <int D> struct Cfg {
     // step later (8 and 4 stages of 128: 92 us where 6 and 6 take 98).
     static constexpr int NK = D == 256 ? 3 : 8, NV = D == 256 ? 2 : D == 128 ? 4 : 8;
     static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
+    static_assert(!P_SMEM || NV == NSB, "P's two buffers go around with the V stages");
     static constexpr int NQ = D == 256 ? 1 : 2;                    // Q buffers
     static constexpr int TM_Q = D, TM_S = D + NQ * (D / 2);
 };
@@ -98,8 +99,10 @@ struct Seq {
 };
 
 struct Shared {
-    uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[4], p_full[4], pv_done[4], q_full, o_free, s_free[4], item_full[ITEMS],
-        item_empty[ITEMS], exch[4];
+    // s_full of tile g (Q K^T done: S is there, the K stage is free) goes around with the K stages, pv_done (P V done: the V
+    // stage and P's place are free) with the V stages: one commit of the MMAs says both
+    uint64_t k_full[8], s_full[8], v_full[8], pv_done[8], p_full[4], s_free[4], q_full, o_free, item_full[ITEMS], item_empty[ITEMS],
+        exch[4];
     Item items[ITEMS];
     // running maximum of each row beside the number + 1 of the tile that decided it: one 64-bit word, so that a row's next
     // tile needs no barrier to know that it reads the right one
@@ -212,9 +215,9 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         ptx::wait_deadline_init(a.wait_cycles);
 #pragma unroll 1
         for (int i = 0; i < 8; ++i)
-            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_empty[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_empty[i], 1);
+            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.pv_done[i], 1);
         for (int i = 0; i < C::NSB; ++i)
-            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.s_free[i], 4), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
+            ptx::mbar_init(&sh.s_free[i], 4), ptx::mbar_init(&sh.p_full[i], 4);
         ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.exch[i], 2);
@@ -304,7 +307,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 using B = Boxes<D, BOX>;
                 const CUtensorMap *cache = IS_V ? &map_vc : &map_kc, *rows_map = IS_V ? &map_v : &map_k;
                 constexpr int NS = IS_V ? C::NV : C::NK;
-                uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *empties = IS_V ? sh.v_empty : sh.k_empty;
+                uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *empties = IS_V ? sh.pv_done : sh.s_full;
                 unsigned char *ring = IS_V ? v_stages : stages;
                 int b = sh.first_b, st2;
                 unsigned off = (unsigned)sh.first_off;
@@ -457,10 +460,19 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
             int cur_b = -1;
-            uint32_t v_off[KT / 16];     // 16 rows of V from one step to the next
+            // Descriptors: the stage and the step only add to the address, 16 bytes a unit in the low bits.  A step of V is 16
+            // rows.
+            const uint64_t kd = ptx::umma_desc_k_sw128(ptx::smem_u32(stages), lay.k_group);
+            const uint64_t k_hi = kd & ~0xffffffffull;
+            const uint32_t k_lo = (uint32_t)kd, k_chunk = lay.k_chunk / 16;
+            uint64_t v_hi = 0;
+            uint32_t v_lo[KT / 16];
 #pragma unroll
-            for (int s = 0; s < KT / 16; ++s)
-                v_off[s] = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
+            for (int s = 0; s < KT / 16; ++s) {
+                const uint32_t off = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
+                const uint64_t vd = ptx::umma_desc_mn_sw128(ptx::smem_u32(v_stages) + off, lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
+                v_hi = vd & ~0xffffffffull, v_lo[s] = (uint32_t)vd;
+            }
             if (warp == MMA_PV && a.shared_len == 0) {  // what the join needs of the item that this part cuts at its end
                 int st;
                 int *d = ws.desc + 8 * blockIdx.x;
@@ -481,6 +493,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             }
             uint64_t *newest = nullptr;  // barrier of the last commit, and its phase
             unsigned newest_phase = 0;
+            auto wait_pv = [&](unsigned g) { return ptx::mbar_wait(&sh.pv_done[g % C::NV], (g / C::NV) & 1); };
             auto run = [&]() -> bool {
                 unsigned tile = 0;  // tiles of the items before
                 for (unsigned ord = 0;; ++ord) {
@@ -495,17 +508,16 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                         for (int j = 0; j < n; ++j) {
                             const unsigned g = tile + j, sidx = g % C::NK, buf = g % C::NSB;
-                            if (g >= C::NSB && !ptx::mbar_wait(C::P_SMEM ? &sh.s_free[buf] : &sh.pv_done[buf], (g / C::NSB - 1) & 1)) return false;
+                            if (g >= C::NSB && !(C::P_SMEM ? ptx::mbar_wait(&sh.s_free[buf], (g / C::NSB - 1) & 1) : wait_pv(g - C::NSB))) return false;
                             if (!ptx::mbar_wait(&sh.k_full[sidx], (g / C::NK) & 1)) return false;
                             ptx::tc_fence_after_sync();
-                            const uint32_t kaddr = ptx::smem_u32(stages + sidx * C::STAGE);
+                            const uint32_t lo = k_lo + sidx * (C::STAGE / 16);
 #pragma unroll
                             for (int s = 0; s < D / 16; ++s)
                                 ptx::umma_bf16_ts(tmem + C::TM_S + buf * KT, tmem + C::TM_Q + (ord % C::NQ) * (D / 2) + s * 8,
-                                                  ptx::umma_desc_k_sw128(kaddr + (s / 4) * lay.k_chunk + (s % 4) * 32, lay.k_group), idesc_qk, s > 0);
-                            ptx::umma_commit(&sh.s_full[buf]);
-                            ptx::umma_commit(&sh.k_empty[sidx]);
-                            newest = &sh.s_full[buf], newest_phase = (g / C::NSB) & 1;
+                                                  k_hi | (lo + (s / 4) * k_chunk + (s % 4) * 2), idesc_qk, s > 0);
+                            ptx::umma_commit(&sh.s_full[sidx]);
+                            newest = &sh.s_full[sidx], newest_phase = (g / C::NK) & 1;
                         }
                     } else {
                         for (int j = 0; j < n; ++j) {
@@ -514,21 +526,19 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                             if (j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free, (ord - 1) & 1)) return false;
                             if (!ptx::mbar_wait(&sh.p_full[buf], (g / C::NSB) & 1)) return false;
                             ptx::tc_fence_after_sync();
-                            const uint32_t vaddr = ptx::smem_u32(v_stages + sidx * C::STAGE);
                             const int steps = (keys_of(j, it.full, it.draft, it.rest, it.n) + 15) / 16;
 #pragma unroll
                             for (int s = 0; s < KT / 16; ++s)
                                 if (s < steps) {
-                                    const uint64_t vd = ptx::umma_desc_mn_sw128(vaddr + v_off[s], lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
+                                    const uint64_t vd = v_hi | (v_lo[s] + sidx * (C::STAGE / 16));
                                     if (C::P_SMEM)
                                         ptx::umma_bf16(tmem, ptx::umma_desc_k_sw128(ptx::smem_u32(p_bufs + (g & 1) * C::P_BYTES) + s * 32), vd,
                                                        idesc_pv, j > 0 || s > 0);
                                     else
                                         ptx::umma_bf16_ts(tmem, tmem + C::TM_S + buf * KT + s * 8, vd, idesc_pv, j > 0 || s > 0);
                                 }
-                            ptx::umma_commit(&sh.pv_done[buf]);
-                            ptx::umma_commit(&sh.v_empty[sidx]);
-                            newest = &sh.pv_done[buf], newest_phase = (g / C::NSB) & 1;
+                            ptx::umma_commit(&sh.pv_done[sidx]);
+                            newest = &sh.pv_done[sidx], newest_phase = (g / C::NV) & 1;
                         }
                     }
                     tile += n;
@@ -616,7 +626,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         if (!row_max(&sh.m[row], g - 1, &m0)) return false;
                         if (j == 0) m0 = -INFINITY;  // (another item's)
                     }
-                    if (!wait_warp(&sh.s_full[buf], (g / C::NSB) & 1)) return false;
+                    if (!wait_warp(&sh.s_full[g % C::NK], (g / C::NK) & 1)) return false;
                     ptx::tc_fence_after_sync();
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
                     if (warp_on && (draft || valid < KT)) {
@@ -675,7 +685,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
                     }
                     if (C::P_SMEM) {
-                        if (g >= 2 && !wait_warp(&sh.pv_done[buf], (g / 2 - 1) & 1)) return false;  // the buffer's last reader
+                        if (g >= 2 && !wait_warp(&sh.pv_done[g % C::NV], (g / C::NV - 1) & 1)) return false;  // the buffer's last reader
                         if (warp_on) {  // row of 128 bytes, swizzled as the MMA reads it
                             unsigned char *p = p_bufs + (g & 1) * C::P_BYTES + row * 128;
 #pragma unroll
@@ -719,7 +729,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     }
                     if (j > 0 && __any_sync(0xffffffffu, grow)) {
                         const unsigned pg = g - 1;
-                        if (!wait_warp(&sh.pv_done[pg % C::NSB], (pg / C::NSB) & 1)) return false;
+                        if (!wait_warp(&sh.pv_done[pg % C::NV], (pg / C::NV) & 1)) return false;
                         ptx::tc_fence_after_sync();
                         const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
 #pragma unroll 1
@@ -747,8 +757,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 l += sh.l[ord & 1][wg ^ 1][row];
                 // (a parity names a phase only to who has seen the one before it: where Q K^T does not wait for P V, the
                 // product before the last comes first)
-                if (C::P_SMEM && last > 0 && !wait_warp(&sh.pv_done[(last - 1) % C::NSB], ((last - 1) / C::NSB) & 1)) return false;
-                if (!wait_warp(&sh.pv_done[last % C::NSB], (last / C::NSB) & 1)) return false;
+                if (C::P_SMEM && last > 0 && !wait_warp(&sh.pv_done[(last - 1) % C::NV], ((last - 1) / C::NV) & 1)) return false;
+                if (!wait_warp(&sh.pv_done[last % C::NV], (last / C::NV) & 1)) return false;
                 ptx::tc_fence_after_sync();
                 const bool bad = sh.bad_item[ord % 16] == ord + 1;
                 if (tid == 0) sh.nonfinite[(ord + 2) & 3][0] = sh.nonfinite[(ord + 2) & 3][1] = 0;
