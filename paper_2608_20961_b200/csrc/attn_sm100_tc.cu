@@ -53,6 +53,7 @@ template <int D> struct Cfg {
     // Heads of 256 leave tensor memory for two S buffers only.  With the weights in S's place the Q K^T after next would
     // wait for this tile's P V; so there P goes through shared memory and S is free as soon as it has been read.
     static constexpr bool P_SMEM = D == 256;
+    static constexpr bool HALVES = D == 128;
     static constexpr int P_BYTES = P_SMEM ? MT * KT * 2 : 0;       // of one of the two P buffers
     // K tiles and V tiles have a ring of stages each, up to 192 KB together.  K runs further ahead: V is wanted a softmax
     // step later (8 and 4 stages of 128: 92 us where 6 and 6 take 98).
@@ -646,45 +647,53 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                         }
                         ptx::tmem_wait_st();
                     }
-                    uint32_t raw[KT];
+                    constexpr int HK = C::HALVES ? KT / 2 : KT;  // keys of a row in registers at a time
+                    uint32_t raw[HK];
                     float top = -INFINITY;
                     if (warp_on) {
-                        ptx::tmem_ld32(ts, *reinterpret_cast<uint32_t(*)[32]>(&raw[0]));
-                        ptx::tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&raw[32]));
-                        ptx::tmem_wait_ld();
+                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                        for (int h = 0; h < KT; h += HK) {
+#pragma unroll
+                            for (int i = 0; i < HK; i += 32) ptx::tmem_ld32(ts + h + i, *reinterpret_cast<uint32_t(*)[32]>(&raw[i]));
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < HK; i += 2)
+                                t[(i >> 1) & 3] = ptx::max3(t[(i >> 1) & 3], __uint_as_float(raw[i]), __uint_as_float(raw[i + 1]));
+                        }
+                        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
                         if (C::P_SMEM) ptx::tc_fence_before_sync();
                     }
                     if (C::P_SMEM) ptx::mbar_arrive_warp(&sh.s_free[buf]);
-                    if (warp_on) {
-                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int i = 0; i < KT; i += 2)
-                            t[(i >> 1) & 3] = ptx::max3(t[(i >> 1) & 3], __uint_as_float(raw[i]), __uint_as_float(raw[i + 1]));
-                        top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
-                    }
                     const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
                     m = grow ? top : m0;
                     *reinterpret_cast<volatile unsigned long long *>(&sh.m[row]) = (unsigned long long)(g + 1) << 32 | __float_as_uint(m);
                     if (warp_on) {
                         const float ref = m == -INFINITY ? 0.f : m;
                         float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                        for (int h = 0; h < KT; h += HK) {
+                            if (C::HALVES) {
+                                ptx::tmem_ld32(ts + h, *reinterpret_cast<uint32_t(*)[32]>(&raw[0]));
+                                ptx::tmem_wait_ld();
+                            }
 #pragma unroll
-                        for (int i = 0; i < KT; i += 2) {
-                            const float x = ptx::ex2(fmaf(__uint_as_float(raw[i]), sl2, -ref));
-                            const float y = ptx::ex2(fmaf(__uint_as_float(raw[i + 1]), sl2, -ref));
-                            acc[i & 2] += x, acc[(i & 2) + 1] += y;
-                            // weights as bf16: at most 2^-8 of each, independent from key to key
-                            raw[i / 2] = pack_bf16(x, y);
-                        }
-                        if (!C::P_SMEM) {
-                            ptx::tmem_st16(ts, *reinterpret_cast<const uint32_t(*)[16]>(&raw[0]));
-                            ptx::tmem_st16(ts + 16, *reinterpret_cast<const uint32_t(*)[16]>(&raw[16]));
+                            for (int i = 0; i < HK; i += 2) {
+                                const float x = ptx::ex2(fmaf(__uint_as_float(raw[i]), sl2, -ref));
+                                const float y = ptx::ex2(fmaf(__uint_as_float(raw[i + 1]), sl2, -ref));
+                                acc[i & 2] += x, acc[(i & 2) + 1] += y;
+                                // weights as bf16: at most 2^-8 of each, independent from key to key
+                                raw[i / 2] = pack_bf16(x, y);
+                            }
+                            if (!C::P_SMEM)
+#pragma unroll
+                                for (int i = 0; i < HK / 2; i += 16) ptx::tmem_st16(ts + h / 2 + i, *reinterpret_cast<const uint32_t(*)[16]>(&raw[i]));
                         }
                         if (m != m_l) l *= ptx::ex2(m_l - ref);
                         m_l = m;
                         l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
                     }
-                    if (C::P_SMEM) {
+                    if constexpr (C::P_SMEM) {
                         if (g >= 2 && !wait_warp(&sh.pv_done[g % C::NV], (g / C::NV - 1) & 1)) return false;  // the buffer's last reader
                         if (warp_on) {  // row of 128 bytes, swizzled as the MMA reads it
                             unsigned char *p = p_bufs + (g & 1) * C::P_BYTES + row * 128;
