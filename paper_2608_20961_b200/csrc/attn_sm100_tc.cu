@@ -39,10 +39,10 @@ constexpr int ITEMS = 8;               // ring of work items between the produce
 constexpr int MAX_START = 40, MAX_TILE = 5;
 constexpr int MIN_UNITS = 8;           // of a CTA's part: below this a part is mostly start and end
 // What a tile and the start of an item cost, in quarters of a tile of few rows, by the rows of the row tile.  With up to
-// 32 rows one softmax warp in four works and a tile takes 0.47 us (0.53 where HBM bounds it); with 128 all of them share the
-// exponentials' pipe and it takes 0.63.  A start (queries into tensor memory, the pipeline's start, the output) takes 2 us,
-// 3.1 beside a shared prompt (every output is a block in fp32) and about 6 with 128 rows.  (A part's time against its tiles and
-// items, least squares over the 148 parts of the benchmark's cases.)
+// 32 rows one softmax warp in four works and a tile takes 0.47 us (0.53 where HBM bounds it); with 128 all of them do, and it
+// takes 0.6.  A start (queries into tensor memory, the pipeline's start, the output) takes 2 us, 3.1 beside a shared prompt
+// (every output is a block in fp32) and 3 to 6 with 128 rows.  (A part's time against its tiles and items, least squares over
+// the 148 parts; heads of 128, pages of 16.)
 __device__ __forceinline__ int tile_cost(long long rows) { return rows > 32 ? 5 : 4; }
 __device__ __forceinline__ int start_cost(long long rows, bool shared) { return rows > 32 ? MAX_START : shared ? 30 : 20; }
 constexpr float LAZY = 8.f;
@@ -53,6 +53,10 @@ template <int D> struct Cfg {
     // Heads of 256 leave tensor memory for two S buffers only.  With the weights in S's place the Q K^T after next would
     // wait for this tile's P V; so there P goes through shared memory and S is free as soon as it has been read.
     static constexpr bool P_SMEM = D == 256;
+    // Softmax: half a row of S in registers at a time, read twice (for the maximum and for the weights), or all of it, read
+    // once.  Halves are half the code, which the roles' shared instruction cache rewards with heads of 128 (256 sequences of
+    // 512 keys 102 us instead of 111, a shared prompt of 4096 under 64 trees 71 instead of 74); with heads of 64 the second read
+    // costs more (decoding 143 us instead of 132), with 256 S would stay taken for longer (shared prompt 161 instead of 141).
     static constexpr bool HALVES = D == 128;
     static constexpr int P_BYTES = P_SMEM ? MT * KT * 2 : 0;       // of one of the two P buffers
     // K tiles and V tiles have a ring of stages each, up to 192 KB together.  K runs further ahead: V is wanted a softmax
@@ -67,8 +71,8 @@ template <int D> struct Cfg {
 // Where the copies put a tile, and in how many pieces.  A box is rows of one page (all of it, or 64 of it) and holds the
 // chunks of its rows one after the other.  V comes so: rows are its K index, and any 16 of one page make an MMA step.  K
 // needs its 8-row groups equally far apart: whole boxes one chunk at a time, or all chunks of 8 rows, whichever makes
-// fewer copies.  (One thread issues them; a copy of 16 rows of 128 bytes takes the TMA 70 cycles, one of 64 rows 200, and
-// the kernel needs a tile in about 1400.)
+// fewer copies.  (One thread issues them; a copy of 16 rows of 128 bytes takes the TMA 70 cycles, one of 64 rows 200: a
+// tile of 64 keys with heads of 128 and pages of 16, K and V, takes about 1000 where the softmax of 128 rows takes 1100.)
 template <int D, int BOX> struct Boxes {
     static constexpr int NC = D / 64, P = KT / BOX;  // boxes of a tile
     static constexpr bool K_BY_CHUNK = P * NC <= KT / 8;
@@ -852,8 +856,10 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
 // The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys.  A warp
 // takes 8 rows and 16 STEPS columns of them: lane = row + 8 * column group, 4 groups of 4 columns a step, so that both the
 // blocks (8 rows of a group are 128 bytes) and the output (4 groups of a row are 32) move in whole sectors.  Warps share out
-// columns, not parts: nothing has to meet (with the parts over warps that met in shared memory, too few of a CTA's warps had
-// work; the trees above took 94 us).  The blocks come out of L2, where the main kernel left them.  A part of a sequence with a bad page has l = -1: the row is left.
+// columns, not parts: nothing has to meet.  (With the parts over warps that met in shared memory too few of a CTA's warps had
+// work: 32 trees of 32 nodes, heads of 256, took 94 us instead of 87.)  The blocks come out of L2, where the main kernel left
+// them; what bounds it is the chain launch, lookup, blocks, output: 3 us with few rows, 6 to 10 with 20 MB of blocks.
+// A part of a sequence with a bad page has l = -1: the row is left.
 template <int STEPS> struct Join {
     float4 acc[STEPS];
     float m = -INFINITY, l = 0.f;
@@ -1058,8 +1064,10 @@ template <int D> cudaError_t launch_d(AttnArgs a, cudaStream_t stream)
         const cuuint64_t strides[4] = {(cuuint64_t)c.stride_slot * 2, 128, c.H_kv > 1 ? (cuuint64_t)c.stride_head * 2 : 16,
                                        c.n_pages > 1 ? (cuuint64_t)c.stride_page * 2 : 16};
         const cuuint32_t bx[5] = {64, (cuuint32_t)rows, (cuuint32_t)chunks, 1, 1}, es[5] = {1, 1, 1, 1, 1};
+        // (128 bytes to L2 at a time: a row of a head of 64 is no longer, and with 256 its neighbour came along from HBM;
+        // decoding 64 x 8192 keys, 8 such heads: 132 us instead of 139, other widths the same)
         return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, bx, es,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     const uint64_t cols = (uint64_t)c.H_kv * D;

@@ -426,31 +426,6 @@ __device__ __forceinline__ bool elect_one()
         : "=r"(r));
     return r != 0;
 }
-// two fp32 operations in one instruction
-__device__ __forceinline__ uint64_t pack2(float2 x)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.x), "f"(x.y));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t x)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)), "l"(pack2(c)));
-    return unpack2(r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a)), "l"(pack2(b)));
-    return unpack2(r);
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;
