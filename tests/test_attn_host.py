@@ -79,11 +79,11 @@ def _append(at, cache=None, rope=None, B=2, T=8, off=A, k=A, ld_k=128, v=A, ld_v
 
 
 def _verify(at, cache=None, tree=None, q=A, ld_q=256, k=A, ld_k=128, v=A, ld_v=128, H_q=4, pages=None, shared=0, io=BF16,
-            O=A, ws=A, ws_bytes=1 << 40, status=None, generic=False):
+            O=A, ws=A, ws_bytes=1 << 40, status=None, generic=False, scale=0.125):
     cache, tree = _cache(at) if cache is None else cache, _tree(at) if tree is None else tree
     lib = at.load_library()
     fn = lib.treewy_attn_verify_generic if generic else lib.treewy_attn_verify
-    return fn(ctypes.byref(cache), ctypes.byref(tree), vp(q), ld_q, vp(k), ld_k, vp(v), ld_v, H_q, 0.125, vp(pages), shared, io,
+    return fn(ctypes.byref(cache), ctypes.byref(tree), vp(q), ld_q, vp(k), ld_k, vp(v), ld_v, H_q, scale, vp(pages), shared, io,
               vp(O), vp(ws), ws_bytes, vp(status), None)
 
 
@@ -134,7 +134,7 @@ def test_verify_and_commit_refusals(at):
     for generic in (False, True):
         for bad in (dict(q=None), dict(k=A + 2), dict(v=None), dict(O=None), dict(ld_q=128), dict(ld_k=132), dict(H_q=3), dict(H_q=0),
                     dict(shared=8), dict(shared=12, pages=A), dict(shared=-8, pages=A), dict(status=A + 4), dict(ws_bytes=0),
-                    dict(ws=None)):
+                    dict(ws=None), dict(scale=0.0), dict(scale=-0.5), dict(scale=float("inf")), dict(scale=float("nan"))):
             assert _verify(at, generic=generic, **bad) == INVALID, bad
         assert _verify(at, io=3, generic=generic) == UNSUPPORTED
         for bad, code in ((dict(B=-1), INVALID), (dict(T=-1), INVALID), (dict(max_nodes=-1), INVALID), (dict(max_nodes=65), UNSUPPORTED),

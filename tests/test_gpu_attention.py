@@ -554,3 +554,22 @@ def test_a_wait_that_runs_out_raises_timeout_and_leaves_the_stream_usable(D, ski
     O, status = au.run_attn(c)
     assert not any(status)
     au.assert_attn(c, O, ref, size, tensor_cores=True)
+
+
+@pytest.mark.parametrize("skip", [0, 3])
+def test_a_wait_that_runs_out_beside_a_shared_prompt(skip):
+    """The same with a shared prompt: items that were never worked on leave nothing to join, which has to be harmless, and
+    the next call on the same workspace is right."""
+    from paper_2608_20961_b200 import binding as tw
+    c = au.make_case([700, 500, 590], [3, 9, 1], Hq=8, Hkv=2, D=128, seed=13, shared=480)
+    ref, size = au.attn_reference(c)
+    try:
+        tw.treewy_debug_inject(2_000_000, skip)
+        _, status = au.run_attn(c)
+        torch.cuda.synchronize()
+    finally:
+        tw.treewy_debug_inject(0, -1)
+    assert any(s & tw.SEQ_TIMEOUT for s in status)
+    O, status = au.run_attn(c)
+    assert not any(status)
+    au.assert_attn(c, O, ref, size, tensor_cores=True)
