@@ -6,7 +6,8 @@
 // keys in tiles of 32 with the running maximum m, sum l and output o of a softmax,
 //     m' = max(m, max_j s_j),  o' = o e^{m - m'} + sum_j e^{s_j - m'} v_j,  l' likewise,
 // and parts are joined by a second kernel with the same rule.  Keys are split until the grid fills the GPU:
-// the calls that come here are small, and what bounds them is the length of one CTA's walk.
+// the calls that come here are small, and what bounds them is the length of one CTA's walk (5 trees of 3 nodes, 777 keys, 6 / 2
+// heads of 64 in fp32: 19.8 us with one 32-key step to a part, 22.6 with longer parts).
 // A masked weight is a negative number that the product skips, so what a row may not see is never multiplied.
 #include "attn_common.cuh"
 
@@ -225,7 +226,8 @@ __global__ void __launch_bounds__(THREADS) attn_generic_kernel(AttnArgs a, int p
     }
 }
 
-// Joins the parts: one warp to a row.  Grid (row warps of the longest tree, B).
+// Joins the parts: one warp to a row, a lane to each part's m and l.  Grid (row warps of the longest tree, B).  Latency of two
+// rounds of L2 reads.
 template <typename T>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, int parts, const float *part_ml, const float *part_o)
 {
