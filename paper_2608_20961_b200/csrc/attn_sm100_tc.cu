@@ -32,6 +32,7 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "attn_phases.cuh"
 #include "ptx_sm100.cuh"
 #include "tma_host.cuh"
 
@@ -71,7 +72,7 @@ template <int D> struct Cfg {
     static constexpr int NK = D == 256 ? 3 : 8, NV = D == 256 ? 2 : D == 128 ? 4 : 8;
     static constexpr int NSB = D == 256 ? 2 : 4;                   // S buffers: what 512 columns leave
     static_assert(!P_SMEM || NV == NSB, "P's two buffers go around with the V stages");
-    static constexpr int NQ = D == 256 ? 1 : 2;                    // Q buffers
+    static constexpr int NQ = q_buffers(D);                        // Q buffers, and barriers that say they are filled
     static constexpr int TM_Q = D, TM_S = D + NQ * (D / 2);
 };
 
@@ -113,7 +114,7 @@ struct Seq {
 struct Shared {
     // s_full of tile g (Q K^T done: S is there, the K stage is free) goes around with the K stages, pv_done (P V done: the V
     // stage and P's place are free) with the V stages: one commit of the MMAs says both
-    uint64_t k_full[8], s_full[8], v_full[8], pv_done[8], p_full[4], s_free[4], q_full, o_free, item_full[ITEMS], item_empty[ITEMS],
+    uint64_t k_full[8], s_full[8], v_full[8], pv_done[8], p_full[4], s_free[4], q_full[2], o_free, item_full[ITEMS], item_empty[ITEMS],
         exch[4];
     Item items[ITEMS];
     // running maximum of each row beside the number + 1 of the tile that decided it: one 64-bit word, so that a row's next
@@ -230,7 +231,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.pv_done[i], 1);
         for (int i = 0; i < C::NSB; ++i)
             ptx::mbar_init(&sh.s_free[i], 4), ptx::mbar_init(&sh.p_full[i], 4);
-        ptx::mbar_init(&sh.q_full, 8), ptx::mbar_init(&sh.o_free, 8);
+        for (int i = 0; i < C::NQ; ++i) ptx::mbar_init(&sh.q_full[i], 8);
+        ptx::mbar_init(&sh.o_free, 8);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.exch[i], 2);
         ptx::fence_barrier_init();
@@ -517,7 +519,8 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     ptx::mbar_arrive(&sh.item_empty[r]);
                     const int n = it.tiles;
                     if (warp == MMA_QK) {
-                        if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
+                        const Phase q = q_phase(ord, C::NQ);
+                        if (!ptx::mbar_wait(&sh.q_full[q.barrier], q.parity)) return false;
                         for (int j = 0; j < n; ++j) {
                             const unsigned g = tile + j, sidx = g % C::NK, buf = g % C::NSB;
                             if (g >= C::NSB && !(C::P_SMEM ? ptx::mbar_wait(&sh.s_free[buf], (g / C::NSB - 1) & 1) : wait_pv(g - C::NSB))) return false;
@@ -603,7 +606,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 ptx::tmem_wait_st();
             }
             ptx::tc_fence_before_sync();
-            ptx::mbar_arrive_warp(&sh.q_full);
+            ptx::mbar_arrive_warp(&sh.q_full[q_phase(ord, C::NQ).barrier]);
             return true;
         };
         auto run = [&]() -> bool {
