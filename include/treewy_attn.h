@@ -107,6 +107,7 @@ treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_ro
  * from 8 takes the tensor-core kernel; everything else an fp32 SIMT kernel.  Scores, softmax statistics and
  * accumulators are fp32; the tensor-core kernel rounds the softmax weights to bf16 (at most 2^-8 of each) for
  * the product with v.
+ * A bounded wait that gives up (treewy.h) flags TREEWY_SEQ_TIMEOUT on every sequence that has rows left unwritten.
  */
 size_t treewy_attn_workspace(const treewy_kv_cache_t *cache, const treewy_tree_t *tree, int32_t H_q,
                              int32_t shared_len, treewy_dtype_t io_dtype);

@@ -111,6 +111,12 @@ struct Seq {
     unsigned units;             // H_kv * groups * per, below 2^31 (the launcher has checked)
 };
 
+// A CTA's part of the line of work
+struct Part {
+    long long u0, u1, W;        // its units, and all of the line
+    int parts, group, member, R;
+};
+
 struct Shared {
     // s_full of tile g (Q K^T done: S is there, the K stage is free) goes around with the K stages, pv_done (P V done: the V
     // stage and P's place are free) with the V stages: one commit of the MMAs says both
@@ -125,7 +131,10 @@ struct Shared {
     unsigned nonfinite[4][2];   // draft rows of an item with NaN or infinity among their values
     long long scan[THREADS / 32], first_off, last_off;
     Seq first_seq;              // of sequence first_b
-    int first_b, last_b, total_fail;
+    Part part;
+    int first_b, last_b;
+    unsigned unfinished;        // first of this CTA's items whose output is not all stored, once a wait has run out; else ~0
+    unsigned copied[2];         // tiles whose copies of K and of V were issued
     uint32_t tmem;
 };
 
@@ -183,6 +192,71 @@ __device__ __forceinline__ int tiles_before(int o, int ov, int wt, int kts) { re
 // falls into and one more.
 __device__ __forceinline__ int slot_of(int g, long long begin, long long u0) { return begin <= u0 ? 2 * g : 2 * g + 1; }
 
+// A CTA's way along its part
+struct Walk {
+    int b;
+    unsigned off;               // in the units of sequence b
+    long long u;                // on the line
+    Seq s;
+};
+// The next item that has tiles here and rows for this member of the group; 0 tiles: the end.  An item that begins here beside a
+// shared prompt leaves word of where its parts are.
+template <int D> __device__ __forceinline__ void next_item(const AttnArgs &a, const Ws &ws, const Part &p, Walk &w, Item &it)
+{
+    int st;
+    it.tiles = 0;
+    while (w.u < p.u1 && it.tiles == 0) {
+        if (w.off >= w.s.units) {  // (a sequence without work has no units)
+            w.off = 0, ++w.b;
+            w.s = load_seq(a, w.b, p.R, &st);
+            continue;
+        }
+        const Seq &s = w.s;
+        const int b = w.b;
+        const unsigned i_ = w.off / s.per, o = w.off - i_ * s.per, h = i_ / s.groups, rg = i_ - h * s.groups;
+        const int span = (int)min((long long)(s.per - o), p.u1 - w.u);
+        const int kt0 = tiles_before(o, s.ov, s.wt, s.kts), kt1 = tiles_before(o + span, s.ov, s.wt, s.kts);
+        const long long begin = w.u - o;
+        const long long row0 = (long long)(rg * p.R + p.member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
+        w.off += span, w.u += span;
+        if (row0 >= rows) continue;
+        it.b = b, it.h = h, it.lo = s.lo, it.n = s.n, it.len = s.len;
+        it.row0 = (int)row0, it.rows = (int)min((long long)MT, rows - row0);
+        it.kt0 = kt0, it.tiles = kt1 - kt0, it.kts = s.kts;
+        const int own = b < 0 ? s.len : s.len - a.shared_len;
+        it.full = own / KT - kt0, it.rest = own % KT, it.draft = b < 0 ? 0x7fffffff : s.kts - 1 - kt0;
+        long long blk = 0;
+        it.blk_o = it.blk_ml = nullptr, it.cap = 0;
+        const bool cut = kt0 > 0 || kt1 < s.kts;
+        if (cut || a.shared_len > 0) {
+            const int tile = it.row0 / MT;
+            const long long i = b < 0 ? (long long)h * s.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
+            blk = cut ? (long long)slot_of(p.group, begin, p.u0) * p.R + p.member : i;
+            it.blk_o = cut ? ws.slot_o : b < 0 ? ws.shared_o : ws.own_o, it.blk_ml = cut ? ws.slot_ml : b < 0 ? ws.shared_ml : ws.own_ml;
+            it.cap = cut ? ws.slot_cap : b < 0 ? MT : ws.own_cap;
+            if (kt0 == 0 && kt1 > 0 && a.shared_len > 0)
+                (b < 0 ? ws.shared_at : ws.own_at)[i] =
+                    make_int4((int)blk, cut ? part_of(begin + s.ov + s.wt * (s.kts - 1), p.W, p.parts) - p.group + 1 : 0, p.group, 0);
+        }
+        it.blk_o += blk * it.cap * D, it.blk_ml += blk * it.cap * 2;
+    }
+}
+// l of a row whose part is not there
+constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;
+// After a wait that ran out: from item `unfinished` on, this CTA's blocks say that they are not there and the sequences are
+// flagged (for a shared prompt's items the join does that, by the rows that want them).
+template <int D> __device__ __noinline__ void mark_unfinished(const AttnArgs &a, const Ws &ws, const Part &p, Walk w, unsigned unfinished)
+{
+    Item it;
+    for (unsigned ord = 0;; ++ord) {
+        next_item<D>(a, ws, p, w, it);
+        if (it.tiles == 0) return;
+        if (ord < unfinished) continue;
+        if (it.cap > 0 && threadIdx.x < it.rows) reinterpret_cast<float2 *>(it.blk_ml)[threadIdx.x] = make_float2(0.f, NOT_DONE);
+        if (it.b >= 0 && threadIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_TIMEOUT);
+    }
+}
+
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
 // a wait with one outcome for the whole warp: what follows needs all of its lanes
@@ -213,7 +287,7 @@ __device__ __forceinline__ bool row_max(const volatile unsigned long long *p, un
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
-attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
+attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, const __grid_constant__ Ws ws, Layout lay, const __grid_constant__ CUtensorMap map_kc, const __grid_constant__ CUtensorMap map_vc,
                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using C = Cfg<D>;
@@ -236,7 +310,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], 11);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.exch[i], 2);
         ptx::fence_barrier_init();
-        sh.total_fail = 0;
+        sh.unfinished = ~0u;
         sh.first_b = sh.last_b = -2;
         ptx::prefetch_tmap(&map_kc), ptx::prefetch_tmap(&map_vc), ptx::prefetch_tmap(&map_k), ptx::prefetch_tmap(&map_v);
     }
@@ -295,27 +369,23 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
     if (tid == 0) {
         if (u1 > u0 && u0 < shared_units) sh.first_b = -1, sh.first_off = u0, sh.first_seq = load_seq(a, -1, R, &st);
         if (u1 > u0 && u1 - 1 < shared_units) sh.last_b = -1, sh.last_off = u1 - 1;
+        sh.part = {u0, u1, W, parts, group, member, R};
     }
     __syncthreads();
     const uint32_t tmem = sh.tmem;
     const float sl2 = a.scale * 1.4426950408889634f;
-    auto fail = [&](int b) {
-        sh.total_fail = 1;
-        if (a.seq_status && a.B > 0) atomicOr(&a.seq_status[b < 0 ? 0 : b], TREEWY_SEQ_TIMEOUT);
-    };
 
     if (warp == PRODUCER_K || warp == PRODUCER_V) {
         // ---------------------------------------------------------------- work items and TMA copies: one thread each
         if (ptx::elect_one()) {
             const int ps = 1 << a.log_page;
             unsigned filled = 0;    // tiles whose copies were issued
-            int cur_b = -1;
             auto mark_bad = [&](int b, unsigned ord) {
                 sh.bad_item[ord % 16] = ord + 1;
                 if (b >= 0 && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
             };
-            // 0: all done, 1: a wait ran out, 2: stopped on purpose
-            auto run = [&](auto box_, auto is_v_) -> int {
+            // (returns early when a wait runs out)
+            auto run = [&](auto box_, auto is_v_) {
                 constexpr int BOX = decltype(box_)::value;
                 constexpr bool IS_V = decltype(is_v_)::value;
                 using B = Boxes<D, BOX>;
@@ -323,60 +393,23 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 constexpr int NS = IS_V ? C::NV : C::NK;
                 uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *empties = IS_V ? sh.pv_done : sh.s_full;
                 unsigned char *ring = IS_V ? v_stages : stages;
-                int b = sh.first_b, st2;
-                unsigned off = (unsigned)sh.first_off;
-                long long u = u0;
-                Seq s = sh.first_seq;
+                Walk walk{sh.first_b, (unsigned)sh.first_off, u0, sh.first_seq};
+                const Part part{u0, u1, W, parts, group, member, R};
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
                     Item it;
                     if constexpr (!IS_V) {
-                        // the next item that has tiles here and rows for this member of the group; 0 tiles: the end
-                        it.tiles = 0;
-                        while (u < u1 && it.tiles == 0) {
-                            if (off >= s.units) {  // (a sequence without work has no units)
-                                off = 0, ++b;
-                                s = load_seq(a, b, R, &st2);
-                                continue;
-                            }
-                            const unsigned i_ = off / s.per, o = off - i_ * s.per, h = i_ / s.groups, rg = i_ - h * s.groups;
-                            const int span = (int)min((long long)(s.per - o), u1 - u);
-                            const int kt0 = tiles_before(o, s.ov, s.wt, s.kts), kt1 = tiles_before(o + span, s.ov, s.wt, s.kts);
-                            const long long begin = u - o;
-                            const long long row0 = (long long)(rg * R + member) * MT, rows = (long long)(b < 0 ? a.T : s.n) * a.G;
-                            off += span, u += span;
-                            if (row0 >= rows) continue;
-                            it.b = b, it.h = h, it.lo = s.lo, it.n = s.n, it.len = s.len;
-                            it.row0 = (int)row0, it.rows = (int)min((long long)MT, rows - row0);
-                            it.kt0 = kt0, it.tiles = kt1 - kt0, it.kts = s.kts;
-                            const int own = b < 0 ? s.len : s.len - a.shared_len;
-                            it.full = own / KT - kt0, it.rest = own % KT, it.draft = b < 0 ? 0x7fffffff : s.kts - 1 - kt0;
-                            long long blk = 0;
-                            it.blk_o = it.blk_ml = nullptr, it.cap = 0;
-                            const bool cut = kt0 > 0 || kt1 < s.kts;
-                            if (cut || a.shared_len > 0) {
-                                const int tile = it.row0 / MT;
-                                const long long i = b < 0 ? (long long)h * s.row_tiles + tile : ((long long)b * a.c.H_kv + h) * ws.own_tiles + tile;
-                                blk = cut ? (long long)slot_of(group, begin, u0) * R + member : i;
-                                it.blk_o = cut ? ws.slot_o : b < 0 ? ws.shared_o : ws.own_o, it.blk_ml = cut ? ws.slot_ml : b < 0 ? ws.shared_ml : ws.own_ml;
-                                it.cap = cut ? ws.slot_cap : b < 0 ? MT : ws.own_cap;
-                                if (kt0 == 0 && kt1 > 0 && a.shared_len > 0)
-                                    (b < 0 ? ws.shared_at : ws.own_at)[i] =
-                                        make_int4((int)blk, cut ? part_of(begin + s.ov + s.wt * (s.kts - 1), W, parts) - group + 1 : 0, group, 0);
-                            }
-                            it.blk_o += blk * it.cap * D, it.blk_ml += blk * it.cap * 2;
-                        }
-                        if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return 1;
+                        next_item<D>(a, ws, part, walk, it);
+                        if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return;
                         sh.items[r] = it;
                         ptx::mbar_arrive(&sh.item_full[r]);
                     } else {
-                        if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return 1;
+                        if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return;
                         it = sh.items[r];
                         if (it.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
                     }
-                    if (it.tiles == 0) return 0;
-                    cur_b = it.b;
-                    if (it.b >= 0 && it.b * a.c.H_kv + it.h == a.skip_item) return 2;  // (test hook)
+                    if (it.tiles == 0) return;
+                    if (it.b >= 0 && it.b * a.c.H_kv + it.h == a.skip_item) return;  // (test hook)
 
                     const int n = it.tiles, key0 = it.b < 0 ? 0 : a.shared_len;
                     const int *table = it.b < 0 ? a.shared_pages : a.c.page_table + (size_t)it.b * a.c.max_pages;
@@ -394,7 +427,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     for (int j = 0; j < n; ++j) {
                         const unsigned sidx = filled % NS;
                         const int kt = it.kt0 + j, token = key0 + kt * KT, slot0 = token & (ps - 1);
-                        if (filled >= NS && !ptx::mbar_wait(&empties[sidx], (filled / NS - 1) & 1)) return 1;
+                        if (filled >= NS && !ptx::mbar_wait(&empties[sidx], (filled / NS - 1) & 1)) return;
                         ++filled;
                         unsigned char *dst = ring + sidx * C::STAGE;
                         uint64_t *full = &fulls[sidx];
@@ -456,24 +489,17 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 }
             };
             auto run_box = [&](auto box_) { return warp == PRODUCER_V ? run(box_, std::true_type{}) : run(box_, std::false_type{}); };
-            const int rc = lay.v_rows == 8    ? run_box(std::integral_constant<int, 8>{})
-                           : lay.v_rows == 16 ? run_box(std::integral_constant<int, 16>{})
-                           : lay.v_rows == 32 ? run_box(std::integral_constant<int, 32>{})
-                                              : run_box(std::integral_constant<int, 64>{});
-            if (rc == 1) fail(cur_b);
-            if (rc != 0) {  // copies in flight have to land before the CTA may leave
-                const unsigned ns = warp == PRODUCER_V ? C::NV : C::NK;
-                uint64_t *fulls = warp == PRODUCER_V ? sh.v_full : sh.k_full;
-                for (unsigned i = filled > ns ? filled - ns : 0; i < filled; ++i)
-                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&fulls[i % ns], (i / ns) & 1); ++t) __nanosleep(20);
-            }
+            if (lay.v_rows == 64) run_box(std::integral_constant<int, 64>{});
+            else if (lay.v_rows == 32) run_box(std::integral_constant<int, 32>{});
+            else if (lay.v_rows == 8) run_box(std::integral_constant<int, 8>{});
+            else run_box(std::integral_constant<int, 16>{});
+            sh.copied[warp == PRODUCER_V] = filled;
         }
         __syncwarp();
     } else if (warp == MMA_QK || warp == MMA_PV) {
         // ---------------------------------------------------------------- MMAs: one thread for Q K^T, one for P V
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
-            int cur_b = -1;
             // Descriptors: the stage and the step only add to the address, 16 bytes a unit in the low bits.  A step of V is 16
             // rows.
             const uint64_t kd = ptx::umma_desc_k_sw128(ptx::smem_u32(stages), lay.k_group);
@@ -515,7 +541,6 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return false;
                     const Item it = sh.items[r];
                     if (it.tiles == 0) return true;
-                    cur_b = it.b;
                     ptx::mbar_arrive(&sh.item_empty[r]);
                     const int n = it.tiles;
                     if (warp == MMA_QK) {
@@ -559,28 +584,25 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                     tile += n;
                 }
             };
-            if (!run()) {
-                fail(cur_b);
-                if (newest)  // MMAs in flight have to end before the CTA may leave
-                    for (int t = 0; t < 100000 && !ptx::mbar_try_wait(newest, newest_phase); ++t) __nanosleep(20);
-            }
+            if (!run() && newest)  // MMAs in flight have to end before the CTA may leave
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(newest, newest_phase); ++t) __nanosleep(20);
         }
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax, epilogue
         const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
-        int cur_b = -1;
+        unsigned ord = ~0u;    // the item in work
         // An item and this thread's row of it: its packed row, its query head, the draft rows it sees
         struct Mine {
             const Item *it;  // (stays in its slot of the ring until this warp says that it is done)
             int t, hq;
             uint64_t tree;
         };
-        // Takes over item `ord`: finds this thread's row and brings its half of the row's query into tensor memory.
-        auto take = [&](unsigned ord, Mine &x) -> bool {
-            if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
-            const Item &it = sh.items[ord % ITEMS];
+        // Takes over item `nr`: finds this thread's row and brings its half of the row's query into tensor memory.
+        auto take = [&](unsigned nr, Mine &x) -> bool {
+            if (!wait_warp(&sh.item_full[nr % ITEMS], (nr / ITEMS) & 1)) return false;
+            const Item &it = sh.items[nr % ITEMS];
             x.it = &it, x.tree = 0;
             if (it.tiles == 0) return true;
             if (w4 * 32 < it.rows) {
@@ -590,7 +612,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + x.t * a.ld_q +
                                                                    (long long)x.hq * D + wg * (D / 2));
                 if (it.b >= 0 && on && it.kt0 + it.tiles == it.kts) x.tree = a.anc_mask[x.t] & low_bits(it.n);
-                const uint32_t dst = tmem + lane_base + C::TM_Q + (ord % C::NQ) * (D / 2) + wg * (D / 4);
+                const uint32_t dst = tmem + lane_base + C::TM_Q + (nr % C::NQ) * (D / 2) + wg * (D / 4);
                 constexpr int QC = D / 4 < 32 ? D / 4 : 32;  // columns at a time
 #pragma unroll 1
                 for (int c = 0; c < D / 4; c += QC) {
@@ -606,7 +628,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 ptx::tmem_wait_st();
             }
             ptx::tc_fence_before_sync();
-            ptx::mbar_arrive_warp(&sh.q_full[q_phase(ord, C::NQ).barrier]);
+            ptx::mbar_arrive_warp(&sh.q_full[q_phase(nr, C::NQ).barrier]);
             return true;
         };
         auto run = [&]() -> bool {
@@ -615,7 +637,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
             int n = 0;
             int full = 0, draft_at = 0, rest = 0;     // (registers: read at every tile)
             // (the round before the first item only takes that one)
-            for (unsigned ord = ~0u;; ++ord) {
+            for (;; ++ord) {
                 const Item &it = *me.it;
                 const bool warp_on = n > 0 && w4 * 32 < it.rows, on = n > 0 && row < it.rows;
                 const unsigned last = tile + n - 1;
@@ -818,7 +840,7 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                                 }
                             }
                         } else {
-                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(it.blk_ml + 2 * row) = make_float2(m, bad ? -1.f : l);
+                            if (wg == 0 && c == 0) *reinterpret_cast<float2 *>(it.blk_ml + 2 * row) = make_float2(m, bad ? PAGE_BAD : l);
                             float *po = it.blk_o + (c / 4 * cap + row) * 4;
 #pragma unroll
                             for (int i = 0; i < EC; i += 4)
@@ -849,17 +871,28 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
                 }
                 if (next.it->tiles == 0) return true;
                 tile += n;
-                me = next, n = me.it->tiles, cur_b = me.it->b;
+                me = next, n = me.it->tiles;
                 full = me.it->full, draft_at = me.it->draft, rest = me.it->rest;
             }
         };
-        const bool ok = run();
-        if (!ok && lane == 0) fail(cur_b);
+        if (!run()) {
+            ptx::tmem_wait_st();
+            if (lane == 0) atomicMin(&sh.unfinished, ord == ~0u ? 0u : ord);
+        }
         __syncwarp();
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
+    if (sh.unfinished != ~0u) {
+        if (tid < 2) {  // copies in flight have to land before the CTA may leave
+            const unsigned filled = sh.copied[tid], ns = tid ? C::NV : C::NK;
+            uint64_t *fulls = tid ? sh.v_full : sh.k_full;
+            for (unsigned i = filled > ns ? filled - ns : 0; i < filled; ++i)
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&fulls[i % ns], (i / ns) & 1); ++t) __nanosleep(20);
+        }
+        mark_unfinished<D>(a, ws, sh.part, Walk{sh.first_b, (unsigned)sh.first_off, sh.part.u0, sh.first_seq}, sh.unfinished);
+    }
     if (warp == MMA_QK) ptx::tmem_dealloc(tmem, 512);
 }
 
@@ -869,11 +902,11 @@ attn_tc_kernel(const __grid_constant__ AttnArgs a, int R, Ws ws, Layout lay, con
 // columns, not parts: nothing has to meet.  (With the parts over warps that met in shared memory too few of a CTA's warps had
 // work: 32 trees of 32 nodes, heads of 256, took 94 us instead of 87.)  The blocks come out of L2, where the main kernel left
 // them; what bounds it is the chain launch, lookup, blocks, output: 3 us with few rows, 6 to 10 with 20 MB of blocks.
-// A part of a sequence with a bad page has l = -1: the row is left.
+// A part with a bad page, or one that was not worked out, has a negative l: the row is left.
 template <int STEPS> struct Join {
     float4 acc[STEPS];
     float m = -INFINITY, l = 0.f;
-    bool bad = false;
+    int bad = 0;  // status bits
     __device__ __forceinline__ Join()
     {
 #pragma unroll
@@ -881,7 +914,7 @@ template <int STEPS> struct Join {
     }
     __device__ __forceinline__ void add(float2 x, const float4 (&y)[STEPS])
     {
-        if (x.y < 0.f) bad = true;
+        if (x.y < 0.f) bad |= x.y == PAGE_BAD ? TREEWY_SEQ_BAD_PAGE : TREEWY_SEQ_TIMEOUT;
         if (x.y == 0.f) return;  // saw nothing
         const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
         const float f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
@@ -978,7 +1011,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(const
         } else {
             x.ml = ws.slot_ml, x.o = ws.slot_o, x.cap = ws.slot_cap;
         }
-        // (a main kernel that ran into its time limit may have left out items: whatever lies there then stays within the workspace)
+        // (calls that overlap on one workspace overwrite each other's: whatever lies there stays within it)
         const unsigned most = at.y == 0 ? (is_own ? a.B : 1) * a.c.H_kv * tiles : blocks;
         const long long blk = min((unsigned)at.x, most - 1);
         x.slot = min((unsigned)((at.z + 1) * 2 * R + tile % R), (unsigned)blocks);
@@ -1006,7 +1039,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_shared_kernel(const
             load_part<STEPS>(yp, ws.slot_o + blk * D, ws.slot_cap, at[i].row, c0, cg);
             jn.add(xp, yp);
         }
-        if (i == 0 && jn.bad && a.seq_status) atomicOr(&a.seq_status[b], TREEWY_SEQ_BAD_PAGE);
+        if (i == 0 && jn.bad && a.seq_status) atomicOr(&a.seq_status[b], jn.bad);
     }
     const int node = r / a.G;
     jn.store(static_cast<__nv_bfloat16 *>(a.O) + ((long long)(lo + node) * a.H_q + h * a.G + r - node * a.G) * D + c0, cg);

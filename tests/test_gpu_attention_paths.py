@@ -20,3 +20,45 @@ def test_items_of_one_and_two_tiles(D):
         O, status = au.run_attn(c)
         assert not any(status)
         au.assert_attn(c, O, ref, size, tensor_cores=True)
+
+
+def _rows_of(c, b):
+    return slice(int(c.offsets[b]), int(c.offsets[b + 1]))
+
+
+@pytest.mark.parametrize("limit,skip", [(2_000_000, 0), (2_000_000, 7), (2_000_000, 61), (40_000, -1), (12_000, -1)])
+@pytest.mark.parametrize("D,shared", [(64, 0), (128, 0), (256, 0), (128, 192), (256, 64)])
+def test_what_a_wait_that_ran_out_left_is_flagged(D, shared, limit, skip):
+    """Waits with a short limit, with one item whose copies are never issued or with work for longer: a sequence without a
+    flag is right, and what was not worked out is not written, whatever the workspace held."""
+    from paper_2608_20961_b200 import attention as at, binding as tw
+    B, Hkv = 160, 2
+    long = 9000 if skip < 0 else 300
+    c = au.make_case([shared + (97 * b) % long for b in range(B)], [1 + b % 5 for b in range(B)], Hq=16, Hkv=Hkv, D=D, seed=21, shared=shared,
+                     poison=False)
+    g = au.on_gpu(c)
+    ws = at.attn_workspace(g["cache"], g["tree"], c.Hq, shared)
+
+    def call(fill):
+        O = torch.full((c.T, c.Hq, D), 7.25, dtype=BF16, device=DEV)
+        status = torch.zeros(B, dtype=torch.int32, device=DEV)
+        ws.view(torch.float32)[:] = fill
+        at.treewy_attn_verify(g["cache"], g["tree"], g["q"], g["k"], g["v"], c.scale, O, ws, g["shared_pages"], shared, status)
+        torch.cuda.synchronize()
+        return O.cpu(), status.cpu().tolist()
+
+    good, status = call(1.0)
+    assert not any(status)
+    try:
+        tw.treewy_debug_inject(limit, skip)
+        O, status = call(1.0)
+    finally:
+        tw.treewy_debug_inject(0, -1)
+    assert all(s in (0, tw.SEQ_TIMEOUT) for s in status) and any(status)
+    if skip >= 0:
+        assert status[skip // Hkv] == tw.SEQ_TIMEOUT and not all(status)
+    for b in range(B):
+        got, want = O[_rows_of(c, b)], good[_rows_of(c, b)]
+        assert (torch.equal(got, want) if not status[b] else ((got == want) | (got == 7.25)).all()), (b, status[b])
+    again, status = call(float("nan"))
+    assert not any(status) and torch.equal(again, good)
