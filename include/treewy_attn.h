@@ -128,8 +128,8 @@ treewy_status_t treewy_attn_verify_generic(const treewy_kv_cache_t *cache, const
  * Commit of the accepted path to the cache: for a = accepted[b] >= 0 the r-th node of a's root path (r = 0 at
  * the root; bits of anc_mask[a] in ascending order) has its packed k and v rows copied to slot
  * context_len[b] + r.  new_context_len [B] (may be NULL; must not be context_len) receives context_len[b] + the
- * path's length, for accepted = -1 context_len[b].  A flagged sequence (bad range, accepted index, length or
- * page) is skipped whole, its new_context_len untouched.
+ * path's length, for accepted = -1 context_len[b].  A flagged sequence (bad range, no node or too many, accepted
+ * index, length or page) is skipped whole, its new_context_len untouched.
  */
 treewy_status_t treewy_kv_commit(const treewy_kv_cache_t *cache, const treewy_tree_t *tree, const void *k, int64_t ld_k,
                                  const void *v, int64_t ld_v, const int32_t *accepted, treewy_dtype_t io_dtype,

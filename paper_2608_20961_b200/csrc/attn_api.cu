@@ -198,10 +198,12 @@ treewy_status_t treewy_kv_commit(const treewy_kv_cache_t *cache, const treewy_tr
     if (st != TREEWY_OK) return st;
     if (seq_status && misaligned(seq_status)) return TREEWY_ERR_INVALID_ARG;
     if (new_context_len && (misaligned(new_context_len) || new_context_len == cache->context_len)) return TREEWY_ERR_INVALID_ARG;
-    if (tree->B == 0 || tree->T == 0) return TREEWY_OK;
+    if (tree->B == 0) return TREEWY_OK;
     const int64_t kv_row = (int64_t)cache->H_kv * cache->d_head;
     const int e = elem_size(io_dtype);
-    if (bad_ptr(k) || bad_ptr(v) || bad_ptr(accepted) || bad_stride(ld_k, kv_row, e) || bad_stride(ld_v, kv_row, e))
+    if (bad_ptr(accepted)) return TREEWY_ERR_INVALID_ARG;
+    // (no rows at all: the kernel flags every sequence, as it does an empty one among others)
+    if (tree->T > 0 && (bad_ptr(k) || bad_ptr(v) || bad_stride(ld_k, kv_row, e) || bad_stride(ld_v, kv_row, e)))
         return TREEWY_ERR_INVALID_ARG;
     a.node_offsets = tree->node_offsets, a.anc_mask = tree->anc_mask;
     a.k = k, a.v = v, a.ld_k = ld_k, a.ld_v = ld_v, a.accepted = accepted;

@@ -62,3 +62,18 @@ def test_what_a_wait_that_ran_out_left_is_flagged(D, shared, limit, skip):
         assert (torch.equal(got, want) if not status[b] else ((got == want) | (got == 7.25)).all()), (b, status[b])
     again, status = call(float("nan"))
     assert not any(status) and torch.equal(again, good)
+
+
+def test_commit_without_rows_flags_every_sequence():
+    """No packed rows at all: each tree is empty, and is flagged as an empty one in a larger batch is."""
+    from paper_2608_20961_b200 import attention as at, binding as tw
+    c = au.make_case([10, 20], [2, 3], Hkv=2, Hq=2, poison=False, room=1)
+    g = au.on_gpu(c)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    before = g["cache"].k.clone()
+    for offsets, want in (((0, 0, 0), [tw.SEQ_TOO_MANY_NODES] * 2), ((0, 0, 3), [tw.SEQ_TOO_MANY_NODES, 0])):
+        tree = tw.Tree.empty(i32(*offsets), torch.full((offsets[-1],), -1, dtype=torch.int32, device=DEV), 1)
+        new, status = i32(-5, -5), i32(0, 0)
+        at.treewy_kv_commit(g["cache"], tree, g["k"][:offsets[-1]], g["v"][:offsets[-1]], i32(-1, -1), new, status)
+        assert status.tolist() == want and new.tolist() == [-5, -5 if want[1] else 20]
+    assert torch.equal(g["cache"].k, before)
