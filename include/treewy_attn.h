@@ -80,8 +80,9 @@ treewy_status_t treewy_rope(const treewy_rope_t *rope, const void *x, int64_t ld
  * context_len[b] + i of the cache: v as it is, k rotated on the way (rope NULL: as it is).  With H_q > 0 the
  * rows' queries are rotated in the same pass, q [T, H_q, d] -> q_out [T, H_q, d] (q_out may be q).
  * context_len is not advanced: every layer of a step appends at the same place.  A sequence whose rows do
- * not fit its max_pages pages is flagged TREEWY_SEQ_BAD_LENGTH and skipped; a row whose page is out
- * of range or whose position is, is skipped with its flag.
+ * not fit its max_pages pages is flagged TREEWY_SEQ_BAD_LENGTH and skipped, one whose range leaves the packed rows
+ * or runs backwards TREEWY_SEQ_BAD_OFFSETS; a row whose page is out of range or whose position is, is skipped with
+ * its flag.  (A row that two sequences claim, beside one that runs backwards, goes to one of them.)
  */
 treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_rope_t *rope, int32_t B, int32_t T,
                                  const int32_t *row_offsets, const void *k, int64_t ld_k, const void *v, int64_t ld_v,

@@ -144,22 +144,24 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 6) rows_kernel(const __grid_c
     if (a.c.H_kv > 0) {
         b = find_sequence(a.row_offsets, a.B, t);
         const int lo = a.row_offsets[b], hi = a.row_offsets[b + 1];
-        if (t < lo || t >= hi) return;                // a row of no sequence
-        if (bad_offsets(lo, hi - lo, a.T)) {
-            bad = TREEWY_SEQ_BAD_OFFSETS;
+        // Ranges outside the packed rows: no row need fall into one, so the last row's warp looks at all of them.
+        if (t == a.T - 1 && a.status) {
+#pragma unroll 4
+            for (int i = lane; i < a.B; i += 32)
+                if (bad_offsets(a.row_offsets[i], a.row_offsets[i + 1] - a.row_offsets[i], a.T)) atomicOr(&a.status[i], TREEWY_SEQ_BAD_OFFSETS);
+        }
+        if (t < lo || t >= hi || bad_offsets(lo, hi - lo, a.T)) return;  // a row of no sequence
+        const int len = a.c.context_len[b];
+        if (len < 0 || (long long)len + (hi - lo) > (long long)a.c.max_pages * a.c.page_size) {
+            bad = TREEWY_SEQ_BAD_LENGTH;
         } else {
-            const int len = a.c.context_len[b];
-            if (len < 0 || (long long)len + (hi - lo) > (long long)a.c.max_pages * a.c.page_size) {
-                bad = TREEWY_SEQ_BAD_LENGTH;
+            const int slot = len + (t - lo), pi = slot / a.c.page_size;
+            const int page = a.c.page_table[(size_t)b * a.c.max_pages + pi];
+            if (page < 0 || page >= a.c.n_pages) {
+                bad |= TREEWY_SEQ_BAD_PAGE;
             } else {
-                const int slot = len + (t - lo), pi = slot / a.c.page_size;
-                const int page = a.c.page_table[(size_t)b * a.c.max_pages + pi];
-                if (page < 0 || page >= a.c.n_pages) {
-                    bad |= TREEWY_SEQ_BAD_PAGE;
-                } else {
-                    const long long at = page * a.c.stride_page + (slot - pi * a.c.page_size) * a.c.stride_slot;
-                    kd = static_cast<T *>(a.c.k) + at, vd = static_cast<T *>(a.c.v) + at;
-                }
+                const long long at = page * a.c.stride_page + (slot - pi * a.c.page_size) * a.c.stride_slot;
+                kd = static_cast<T *>(a.c.k) + at, vd = static_cast<T *>(a.c.v) + at;
             }
         }
     }

@@ -77,3 +77,21 @@ def test_commit_without_rows_flags_every_sequence():
         at.treewy_kv_commit(g["cache"], tree, g["k"][:offsets[-1]], g["v"][:offsets[-1]], i32(-1, -1), new, status)
         assert status.tolist() == want and new.tolist() == [-5, -5 if want[1] else 20]
     assert torch.equal(g["cache"].k, before)
+
+
+@pytest.mark.parametrize("offsets,bad,written", [((0, 5, 9, 9), [1, 2], {0: 5}),          # past the rows, and none of them falls there
+                                                 ((0, 2, 1, 5), [1], {0: None, 2: None}),  # backwards
+                                                 ((-3, 0, 0, 5), [0], {2: 5}), ((0, 0, 0, 7), [2], {})])
+def test_append_flags_ranges_that_no_row_falls_into(offsets, bad, written):
+    from paper_2608_20961_b200 import attention as at, binding as tw
+    c = au.make_case([3, 4, 5], [2, 2, 1], Hkv=2, Hq=2, poison=False, room=1)
+    g = au.on_gpu(c)
+    before = g["cache"].k.clone()
+    status = torch.zeros(3, dtype=torch.int32, device=DEV)
+    at.treewy_kv_append(g["cache"], torch.tensor(offsets, dtype=torch.int32, device=DEV), g["k"], g["v"], seq_status=status)
+    assert status.tolist() == [tw.SEQ_BAD_OFFSETS if b in bad else 0 for b in range(3)]
+    changed = (g["cache"].k != before).flatten(2).any(2)
+    for b in range(3):
+        rows = [bool(changed[int(c.table[b, s // c.page]), s % c.page]) for s in range(c.L[b], c.L[b] + 5)]
+        if written.get(b, 0) is not None:
+            assert rows == [i < written.get(b, 0) for i in range(5)], (b, rows)
