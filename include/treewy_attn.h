@@ -74,6 +74,11 @@ typedef struct {
 treewy_status_t treewy_rope(const treewy_rope_t *rope, const void *x, int64_t ld_x, void *y, int64_t ld_y, int32_t T,
                             int32_t H, int32_t d_head, int32_t inverse, treewy_dtype_t io_dtype, int32_t *row_status,
                             void *cuda_stream);
+/* The same for the packed rows of sequences (row_offsets [B+1], as in treewy_kv_append): a position out of range flags
+ * seq_status[b] (may be NULL) of the row's own sequence. */
+treewy_status_t treewy_rope_rows(const treewy_rope_t *rope, int32_t B, int32_t T, const int32_t *row_offsets, const void *x,
+                                 int64_t ld_x, void *y, int64_t ld_y, int32_t H, int32_t d_head, int32_t inverse,
+                                 treewy_dtype_t io_dtype, int32_t *seq_status, void *cuda_stream);
 
 /*
  * Append: row i of sequence b (packed rows row_offsets[b] .. row_offsets[b+1]-1 of T; none is legal) goes to slot

@@ -50,12 +50,13 @@ def load_library():
     vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     cache, rope, tree = ctypes.POINTER(KVCacheStruct), ctypes.POINTER(RopeStruct), ctypes.POINTER(tw.TreeStruct)
     lib.treewy_rope.argtypes = [rope, vp, i64, vp, i64, i32, i32, i32, i32, ctypes.c_int, vp, vp]
+    lib.treewy_rope_rows.argtypes = [rope, i32, i32, vp, vp, i64, vp, i64, i32, i32, i32, ctypes.c_int, vp, vp]
     lib.treewy_kv_append.argtypes = [cache, rope, i32, i32, vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, ctypes.c_int, vp, vp]
     verify = [cache, tree, vp, i64, vp, i64, vp, i64, i32, f32, vp, i32, ctypes.c_int, vp, vp, ctypes.c_size_t, vp, vp]
     lib.treewy_attn_verify.argtypes = verify
     lib.treewy_attn_verify_generic.argtypes = verify
     lib.treewy_kv_commit.argtypes = [cache, tree, vp, i64, vp, i64, vp, ctypes.c_int, vp, vp, vp]
-    for fn in (lib.treewy_rope, lib.treewy_kv_append, lib.treewy_attn_verify, lib.treewy_attn_verify_generic,
+    for fn in (lib.treewy_rope, lib.treewy_rope_rows, lib.treewy_kv_append, lib.treewy_attn_verify, lib.treewy_attn_verify_generic,
                lib.treewy_kv_commit):
         fn.restype = ctypes.c_int
     lib.treewy_attn_workspace.argtypes = [cache, tree, i32, i32, ctypes.c_int]
@@ -166,6 +167,18 @@ def treewy_rope(rope: Rope, x: torch.Tensor, y: torch.Tensor, inverse: bool = Fa
              int(inverse), dt, _int32(row_status, 1, "row_status"), _stream(stream, x))
 
 
+def treewy_rope_rows(rope: Rope, row_offsets: torch.Tensor, x: torch.Tensor, y: torch.Tensor, inverse: bool = False,
+                     seq_status: torch.Tensor | None = None, stream=None) -> None:
+    """treewy_rope for the packed rows of the sequences at row_offsets [B + 1]: a position out of range flags its sequence."""
+    T, H, d = x.shape
+    B, dt = row_offsets.numel() - 1, tw._DTYPES.get(x.dtype)
+    if T != rope.T or dt is None or B < 0:
+        raise ValueError(f"x: bfloat16 or float32, {rope.T} tokens as rope.positions has, wanted; row_offsets: B + 1 of them")
+    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x"), _rows(y, T, H, d, x.dtype, "y")
+    tw._call("treewy_rope_rows", load_library().treewy_rope_rows, rope._ref, B, T, _int32(row_offsets, B + 1, "row_offsets"),
+             x.data_ptr(), ld_x, y.data_ptr(), ld_y, H, d, int(inverse), dt, _int32(seq_status, B, "seq_status"), _stream(stream, x))
+
+
 def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                      rope: Rope | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
                      seq_status: torch.Tensor | None = None, stream=None) -> None:
@@ -235,7 +248,11 @@ class AttentionLayer:
     """One attention layer's side of a speculative round, on the current stream: the paged cache, the rotary table and
     a workspace stay with the layer; each call takes the round's packed rows.  The cache's ``context_len`` is
     advanced by ``commit`` and ``append_and_attend``.  Layers of one model that share a context_len array have to leave
-    that to one of them: the others pass advance=False."""
+    that to one of them: the others pass advance=False.
+
+    seq_status [B], zeroed by the caller ahead of a round and passed to all of its calls, receives their flags; without it
+    the layer keeps its own.  A sequence that is flagged in it keeps its length, and its rows of the outputs mean
+    nothing."""
 
     def __init__(self, cache: KVCache, H_q: int, cos_sin: torch.Tensor, pair_axis: torch.Tensor | None = None,
                  interleaved: bool = False, scale: float | None = None):
@@ -244,7 +261,10 @@ class AttentionLayer:
         self.cache, self.H_q = cache, H_q
         self.cos_sin, self.pair_axis, self.interleaved = cos_sin, pair_axis, interleaved
         self.scale = cache.d_head ** -0.5 if scale is None else scale
-        self._new_len = torch.empty_like(cache.context_len)
+        self._len = cache.context_len.view(-1)[:cache.B]
+        self._new_len = torch.empty_like(self._len)
+        self._own = torch.zeros_like(self._len)    # status words of a round whose caller has none
+        self._round = None                         # those of the round that verify began
         self._ws, self._ws_for = None, None
 
     def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
@@ -262,25 +282,40 @@ class AttentionLayer:
     def _rope(self, positions: torch.Tensor) -> Rope:
         return Rope(self.cos_sin, positions, self.pair_axis, self.interleaved)
 
+    def _begin(self, tree: Tree, seq_status: torch.Tensor | None) -> torch.Tensor:
+        """The status words of a round that begins."""
+        if tree.B != self.cache.B:
+            raise ValueError("tree: another number of sequences than the cache's page table")
+        _int32(seq_status, self.cache.B, "seq_status")
+        self._round = self._own.zero_() if seq_status is None else seq_status.view(-1)[:self.cache.B]
+        return self._round
+
     def verify(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                seq_status: torch.Tensor | None = None, shared_pages: torch.Tensor | None = None,
                shared_len: int = 0) -> torch.Tensor:
         """Rotates q and k in place (keep k and v until commit) and returns the attention's output for every node."""
+        status = self._begin(tree, seq_status)
         rope = self._rope(positions)
-        treewy_rope(rope, q, q)
-        treewy_rope(rope, k, k)
+        offsets = tree.node_offsets[:tree.B + 1]
+        treewy_rope_rows(rope, offsets, q, q, seq_status=status)
+        treewy_rope_rows(rope, offsets, k, k, seq_status=status)
         O = self._out(q)
         treewy_attn_verify(self.cache, tree, q, k, v, self.scale, O, self._workspace(tree, shared_len), shared_pages,
-                           shared_len, seq_status)
+                           shared_len, status)
         return O
 
     def commit(self, tree: Tree, k: torch.Tensor, v: torch.Tensor, accepted: torch.Tensor,
                seq_status: torch.Tensor | None = None, advance: bool = True) -> None:
-        """The accepted path's keys and values enter the cache (flagged sequences keep their length)."""
-        self._new_len.copy_(self.cache.context_len)
-        treewy_kv_commit(self.cache, tree, k, v, accepted, self._new_len, seq_status)
+        """The accepted path's keys and values enter the cache.  Sequences that verify or this call has flagged keep their
+        length (what is written behind it does not count)."""
+        begun = self._round
+        status = self._begin(tree, seq_status) if begun is None or seq_status is not None else begun
+        if begun is not None and begun.data_ptr() != status.data_ptr():
+            status |= begun
+        self._round = None
+        treewy_kv_commit(self.cache, tree, k, v, accepted, self._new_len, status)
         if advance:
-            self.cache.context_len.copy_(self._new_len)
+            torch.where(status == 0, self._new_len, self._len, out=self._len)
 
     def append_and_attend(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                           seq_status: torch.Tensor | None = None) -> torch.Tensor:

@@ -107,6 +107,26 @@ treewy_status_t attn_common(bool force_generic, const treewy_kv_cache_t *cache, 
     return launched(launch_attn_generic(a, io, static_cast<cudaStream_t>(cuda_stream)));
 }
 
+// row_offsets NULL: one status word for all rows
+treewy_status_t rope_common(const treewy_rope_t *rope, int32_t B, int32_t T, const int32_t *row_offsets, const void *x,
+                            int64_t ld_x, void *y, int64_t ld_y, int32_t H, int32_t d_head, int32_t inverse,
+                            treewy_dtype_t io_dtype, int32_t *status, void *cuda_stream)
+{
+    if (T < 0 || H < 1 || d_head < 2) return TREEWY_ERR_INVALID_ARG;
+    if (bad_dtype(io_dtype) || d_head % 2 != 0) return TREEWY_ERR_UNSUPPORTED;
+    RowsArgs a = {};
+    treewy_status_t st = check_rope(rope, T, d_head, inverse, &a.r);
+    if (st != TREEWY_OK) return st;
+    if (status && misaligned(status)) return TREEWY_ERR_INVALID_ARG;
+    if (T == 0) return TREEWY_OK;
+    const int e = elem_size(io_dtype);
+    const int64_t row = (int64_t)H * d_head;
+    if (bad_ptr(x) || bad_ptr(y) || bad_stride(ld_x, row, e) || bad_stride(ld_y, row, e)) return TREEWY_ERR_INVALID_ARG;
+    a.q = x, a.ld_q = ld_x, a.q_out = y, a.ld_qo = ld_y;
+    a.row_offsets = row_offsets, a.B = B, a.T = T, a.H_q = H, a.d = d_head, a.status = status;
+    return launched(launch_rows(a, io_dtype, static_cast<cudaStream_t>(cuda_stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -115,19 +135,16 @@ treewy_status_t treewy_rope(const treewy_rope_t *rope, const void *x, int64_t ld
                             int32_t H, int32_t d_head, int32_t inverse, treewy_dtype_t io_dtype, int32_t *row_status,
                             void *cuda_stream)
 {
-    if (T < 0 || H < 1 || d_head < 2) return TREEWY_ERR_INVALID_ARG;
-    if (bad_dtype(io_dtype) || d_head % 2 != 0) return TREEWY_ERR_UNSUPPORTED;
-    RowsArgs a = {};
-    treewy_status_t st = check_rope(rope, T, d_head, inverse, &a.r);
-    if (st != TREEWY_OK) return st;
-    if (row_status && misaligned(row_status)) return TREEWY_ERR_INVALID_ARG;
-    if (T == 0) return TREEWY_OK;
-    const int e = elem_size(io_dtype);
-    const int64_t row = (int64_t)H * d_head;
-    if (bad_ptr(x) || bad_ptr(y) || bad_stride(ld_x, row, e) || bad_stride(ld_y, row, e)) return TREEWY_ERR_INVALID_ARG;
-    a.q = x, a.ld_q = ld_x, a.q_out = y, a.ld_qo = ld_y;
-    a.T = T, a.H_q = H, a.d = d_head, a.status = row_status;
-    return launched(launch_rows(a, io_dtype, static_cast<cudaStream_t>(cuda_stream)));
+    return rope_common(rope, 0, T, nullptr, x, ld_x, y, ld_y, H, d_head, inverse, io_dtype, row_status, cuda_stream);
+}
+
+treewy_status_t treewy_rope_rows(const treewy_rope_t *rope, int32_t B, int32_t T, const int32_t *row_offsets, const void *x,
+                                 int64_t ld_x, void *y, int64_t ld_y, int32_t H, int32_t d_head, int32_t inverse,
+                                 treewy_dtype_t io_dtype, int32_t *seq_status, void *cuda_stream)
+{
+    if (B < 0) return TREEWY_ERR_INVALID_ARG;
+    if (B > 0 && T > 0 && bad_ptr(row_offsets)) return TREEWY_ERR_INVALID_ARG;
+    return rope_common(rope, B, B > 0 ? T : 0, row_offsets, x, ld_x, y, ld_y, H, d_head, inverse, io_dtype, seq_status, cuda_stream);
 }
 
 treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_rope_t *rope, int32_t B, int32_t T,

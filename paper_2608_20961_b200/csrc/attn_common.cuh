@@ -27,7 +27,7 @@ struct RopeView {
 struct RowsArgs {
     CacheView c;
     RopeView r;
-    const int32_t *row_offsets;
+    const int32_t *row_offsets;  // (for treewy_rope NULL)
     const void *q, *k, *v;
     void *q_out;
     long long ld_q, ld_k, ld_v, ld_qo;

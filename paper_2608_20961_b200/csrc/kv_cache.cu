@@ -166,6 +166,10 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 6) rows_kernel(const __grid_c
         }
     }
     if (bad) {
+        if (a.c.H_kv == 0 && a.row_offsets) {         // rotation alone: the sequence is wanted for its flag only
+            b = find_sequence(a.row_offsets, a.B, t);
+            if (t < a.row_offsets[b] || t >= a.row_offsets[b + 1]) return;
+        }
         if (lane == 0 && a.status) atomicOr(&a.status[b], bad);
         return;
     }
