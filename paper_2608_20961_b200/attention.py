@@ -265,6 +265,9 @@ class AttentionLayer:
         self._new_len = torch.empty_like(self._len)
         self._own = torch.zeros_like(self._len)    # status words of a round whose caller has none
         self._round = None                         # those of the round that verify began
+        # the cache with the token that append_and_attend has just written
+        self._ahead = KVCache(cache.k, cache.v, cache.page_table, self._new_len)
+        self._unseen = None                        # ancestor masks of nodes that see no draft row
         self._ws, self._ws_for = None, None
 
     def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
@@ -322,9 +325,16 @@ class AttentionLayer:
         """Ordinary decoding: one token a sequence, written to the cache (rotated on the way) and attended from there."""
         if tree.T != tree.B:
             raise ValueError("tree: one node a sequence wanted")
+        status = self._begin(tree, seq_status)
+        self._round = None
         q_out, O = self._out(q), self._out(q)
-        treewy_kv_append(self.cache, tree.node_offsets, k, v, self._rope(positions), q, q_out, seq_status)
-        self.cache.context_len.add_(1)
-        alone = Tree(**{**vars(tree), "anc_mask": torch.zeros_like(tree.anc_mask)})   # the token is in the cache already
-        treewy_attn_verify(self.cache, alone, q_out, k, v, self.scale, O, self._workspace(tree, 0), seq_status=seq_status)
+        treewy_kv_append(self.cache, tree.node_offsets, k, v, self._rope(positions), q, q_out, status)
+        # The token is in the cache already: it is seen there and not as a draft row.  One node at most, so that a sequence with
+        # none or with several is flagged.
+        torch.add(self._len, 1, out=self._new_len)
+        if self._unseen is None or self._unseen.numel() < tree.T:
+            self._unseen = torch.zeros((tree.T,), dtype=torch.int64, device=q.device)
+        alone = Tree(**{**vars(tree), "anc_mask": self._unseen, "max_nodes": 1})
+        treewy_attn_verify(self._ahead, alone, q_out, k, v, self.scale, O, self._workspace(alone, 0), seq_status=status)
+        self._len.add_(status == 0)
         return O

@@ -91,3 +91,73 @@ def test_rotation_flags_the_sequence_of_the_row():
         owner = [max(b for b in range(B) if off[b] <= t and n[b]) for t in bad]
         assert torch.equal(y, want) and (y[bad] == 7.25).all()
         assert status.tolist() == [at.SEQ_BAD_POSITION if b in owner else 0 for b in range(B)]
+
+
+def decode_reference(c, pos):
+    """One token a sequence: its own case, which sees the context and itself."""
+    one = rotated(c, pos)
+    one.mask = torch.ones(c.T, dtype=torch.int64)
+    return one, *au.attn_reference(one)
+
+
+def test_decoding_leaves_flagged_sequences_where_they_are():
+    """Beside two good sequences: a position out of range, a page out of range, and a table that is full."""
+    from paper_2608_20961_b200 import attention as at
+    c = random_case([20, 33, 48, 15, 40], [1] * 5, seed=2)
+    c.table[2, 3] = -1                                  # where token 48 would go
+    c.table = c.table[:, :4].contiguous()
+    c.L[3] = 4 * PAGE                                   # no slot left (what the table holds there does not matter)
+    layer, g = layer_of(c)
+    pos = torch.tensor(c.L, dtype=I32)
+    pos[1] = -1
+    before = layer.cache.k.clone()
+    status = i32(*[0] * 5)
+    O = layer.append_and_attend(g["tree"], pos.to(DEV), g["q"], g["k"], g["v"], status)
+    assert status.tolist() == [0, at.SEQ_BAD_POSITION, at.SEQ_BAD_PAGE, at.SEQ_BAD_LENGTH, 0]
+    assert layer.cache.context_len.tolist() == [21, 33, 48, 4 * PAGE, 41]
+    changed = (layer.cache.k != before).flatten(2).any(2).nonzero().tolist()
+    assert sorted(changed) == sorted([int(c.table[b, n // PAGE]), n % PAGE] for b, n in ((0, 20), (4, 40)))
+    pos[1], c.L[3] = 0, 0
+    one, ref, size = decode_reference(c, pos)
+    au.assert_attn(one, O.cpu(), ref, size, tensor_cores=True, rows=rows_of(c, (0, 4)))
+    # the position mended, the same token again: now it counts, and nothing of the first try is seen
+    g2 = au.on_gpu(random_case([20, 33, 48, 15, 40], [1] * 5, seed=2))
+    pos[0], pos[4] = 21, 41
+    pos[1] = 33
+    status.zero_()
+    layer.append_and_attend(g2["tree"], pos.to(DEV), g2["q"], g2["k"], g2["v"], status)
+    assert status.tolist()[:2] == [0, 0] and layer.cache.context_len.tolist() == [22, 34, 48, 4 * PAGE, 42]
+
+
+def test_decoding_without_status_words_keeps_lengths_as_well():
+    c = random_case([20, 33], [1, 1], seed=3)
+    layer, g = layer_of(c)
+    layer.append_and_attend(g["tree"], i32(20, TOP), g["q"], g["k"], g["v"])
+    assert layer.cache.context_len.tolist() == [21, 33]
+    layer.append_and_attend(g["tree"], i32(21, 33), g["q"], g["k"], g["v"])
+    assert layer.cache.context_len.tolist() == [22, 34]
+
+
+@pytest.mark.parametrize("hint", [0, 2])
+def test_decoding_flags_sequences_without_exactly_one_token(hint):
+    """As many rows as sequences, but two of one and none of another."""
+    from paper_2608_20961_b200 import binding as tw
+    c = random_case([20, 33, 9], [1, 1, 1], seed=4)
+    layer, g = layer_of(c)
+    tree = tw.Tree.empty(i32(0, 2, 2, 3), i32(-1, 0, -1), 1, hint)
+    status = i32(0, 0, 0)
+    layer.append_and_attend(tree, i32(20, 21, 9), g["q"], g["k"], g["v"], status)
+    assert status.tolist() == [tw.SEQ_TOO_MANY_NODES, tw.SEQ_TOO_MANY_NODES, 0]
+    assert layer.cache.context_len.tolist() == [20, 33, 10]
+
+
+def test_a_tree_for_another_number_of_sequences_is_refused_before_anything_is_rotated():
+    from paper_2608_20961_b200 import binding as tw
+    c = random_case([20, 33], [1, 1], seed=5)
+    layer, g = layer_of(c)
+    q, k = g["q"].clone(), g["k"].clone()
+    tree = tw.Tree.empty(i32(0, 1), i32(-1), 1)
+    for call in (layer.verify, layer.append_and_attend):
+        with pytest.raises(ValueError):
+            call(tree, i32(20), q[:1], k[:1], g["v"][:1])
+    assert torch.equal(q, g["q"]) and layer.cache.context_len.tolist() == [20, 33]
