@@ -247,12 +247,12 @@ def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tenso
 class AttentionLayer:
     """One attention layer's side of a speculative round, on the current stream: the paged cache, the rotary table and
     a workspace stay with the layer; each call takes the round's packed rows.  The cache's ``context_len`` is
-    advanced by ``commit`` and ``append_and_attend``.  Layers of one model that share a context_len array have to leave
-    that to one of them: the others pass advance=False.
+    advanced by ``commit`` and ``append_and_attend``.  Layers of one model that share a context_len array leave that to the
+    last of them, since all of a round write at the same place: the others pass advance=False.
 
     seq_status [B], zeroed by the caller ahead of a round and passed to all of its calls, receives their flags; without it
-    the layer keeps its own.  A sequence that is flagged in it keeps its length, and its rows of the outputs mean
-    nothing."""
+    the layer keeps its own.  A sequence that is flagged in it, by whichever layer, keeps its length, and its rows of the
+    outputs mean nothing."""
 
     def __init__(self, cache: KVCache, H_q: int, cos_sin: torch.Tensor, pair_axis: torch.Tensor | None = None,
                  interleaved: bool = False, scale: float | None = None):
@@ -321,7 +321,7 @@ class AttentionLayer:
             torch.where(status == 0, self._new_len, self._len, out=self._len)
 
     def append_and_attend(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
-                          seq_status: torch.Tensor | None = None) -> torch.Tensor:
+                          seq_status: torch.Tensor | None = None, advance: bool = True) -> torch.Tensor:
         """Ordinary decoding: one token a sequence, written to the cache (rotated on the way) and attended from there."""
         if tree.T != tree.B:
             raise ValueError("tree: one node a sequence wanted")
@@ -336,5 +336,6 @@ class AttentionLayer:
             self._unseen = torch.zeros((tree.T,), dtype=torch.int64, device=q.device)
         alone = Tree(**{**vars(tree), "anc_mask": self._unseen, "max_nodes": 1})
         treewy_attn_verify(self._ahead, alone, q_out, k, v, self.scale, O, self._workspace(alone, 0), seq_status=status)
-        self._len.add_(status == 0)
+        if advance:
+            self._len.add_(status == 0)
         return O

@@ -161,3 +161,51 @@ def test_a_tree_for_another_number_of_sequences_is_refused_before_anything_is_ro
         with pytest.raises(ValueError):
             call(tree, i32(20), q[:1], k[:1], g["v"][:1])
     assert torch.equal(q, g["q"]) and layer.cache.context_len.tolist() == [20, 33]
+
+
+def two_layers(seed, L, N, **kw):
+    """Two cases with one context_len array."""
+    cases = [random_case(L, N, seed=seed + i, **kw) for i in range(2)]
+    cases[1].offsets, cases[1].parent, cases[1].mask = cases[0].offsets, cases[0].parent, cases[0].mask
+    context_len = i32(*L)
+    layers, gs = zip(*(layer_of(c, context_len) for c in cases))
+    return cases, layers, gs, context_len
+
+
+def test_two_layers_on_one_length_array_decode():
+    cases, layers, gs, context_len = two_layers(30, [20, 33, 64], [1, 1, 1])
+    status = i32(0, 0, 0)
+    for step in range(3):
+        pos = torch.tensor([n + step for n in (20, 33, 64)], dtype=I32)
+        gen = torch.Generator().manual_seed(step)
+        for i, (c, layer, g) in enumerate(zip(cases, layers, gs)):
+            c.q, c.k, c.v = (torch.randn(x.shape, generator=gen).to(BF16) for x in (c.q, c.k, c.v))
+            O = layer.append_and_attend(g["tree"], pos.to(DEV), c.q.to(DEV), c.k.to(DEV), c.v.to(DEV), status, advance=i == 1)
+            c.L = pos.tolist()
+            one, ref, size = decode_reference(c, pos)
+            au.assert_attn(one, O.cpu(), ref, size, tensor_cores=True)
+            for b, n in enumerate(c.L):                 # what the next step finds
+                at_ = int(c.table[b, n // PAGE]), n % PAGE
+                c.kc[at_], c.vc[at_] = layer.cache.k.cpu()[at_], c.v[b]
+                assert torch.equal(layer.cache.v.cpu()[at_], c.v[b])
+                assert (layer.cache.k.cpu()[at_].double() - c.k[b].double()).abs().max() <= 2 * au.BF16_HALF_ULP * c.k.double().abs().max()
+            assert context_len.tolist() == [n + step + i for n in (20, 33, 64)]
+    assert not status.any()
+
+
+@pytest.mark.parametrize("speculative", [False, True])
+def test_what_one_layer_flags_the_last_one_does_not_advance(speculative):
+    from paper_2608_20961_b200 import attention as at
+    cases, layers, gs, context_len = two_layers(40, [20, 32, 48], [1, 1, 1])
+    layers[0].cache.page_table[1, 2] = -1               # where token 32 goes, in the first layer alone
+    status, pos = i32(0, 0, 0), i32(20, 32, 48)
+    for i, (layer, g) in enumerate(zip(layers, gs)):
+        if speculative:
+            layer.verify(g["tree"], pos, g["q"], g["k"], g["v"], status)
+        else:
+            layer.append_and_attend(g["tree"], pos, g["q"], g["k"], g["v"], status, advance=i == 1)
+    if speculative:
+        for i, (layer, g) in enumerate(zip(layers, gs)):
+            layer.commit(g["tree"], g["k"], g["v"], i32(0, 0, 0), status, advance=i == 1)
+    assert status.tolist() == [0, at.SEQ_BAD_PAGE, 0]
+    assert context_len.tolist() == [21, 32, 49]
