@@ -321,7 +321,8 @@ class AttentionLayer:
             torch.where(status == 0, self._new_len, self._len, out=self._len)
 
     def append_and_attend(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
-                          seq_status: torch.Tensor | None = None, advance: bool = True) -> torch.Tensor:
+                          seq_status: torch.Tensor | None = None, advance: bool = True,
+                          shared_pages: torch.Tensor | None = None, shared_len: int = 0) -> torch.Tensor:
         """Ordinary decoding: one token a sequence, written to the cache (rotated on the way) and attended from there."""
         if tree.T != tree.B:
             raise ValueError("tree: one node a sequence wanted")
@@ -331,11 +332,14 @@ class AttentionLayer:
         treewy_kv_append(self.cache, tree.node_offsets, k, v, self._rope(positions), q, q_out, status)
         # The token is in the cache already: it is seen there and not as a draft row.  One node at most, so that a sequence with
         # none or with several is flagged.
+        if shared_len > 0:                         # (with the token the attention would take one that is a token short)
+            status |= (self._len < shared_len) * SEQ_BAD_LENGTH
         torch.add(self._len, 1, out=self._new_len)
         if self._unseen is None or self._unseen.numel() < tree.T:
             self._unseen = torch.zeros((tree.T,), dtype=torch.int64, device=q.device)
         alone = Tree(**{**vars(tree), "anc_mask": self._unseen, "max_nodes": 1})
-        treewy_attn_verify(self._ahead, alone, q_out, k, v, self.scale, O, self._workspace(alone, 0), seq_status=status)
+        treewy_attn_verify(self._ahead, alone, q_out, k, v, self.scale, O, self._workspace(alone, shared_len), shared_pages,
+                           shared_len, status)
         if advance:
             self._len.add_(status == 0)
         return O

@@ -209,3 +209,21 @@ def test_what_one_layer_flags_the_last_one_does_not_advance(speculative):
             layer.commit(g["tree"], g["k"], g["v"], i32(0, 0, 0), status, advance=i == 1)
     assert status.tolist() == [0, at.SEQ_BAD_PAGE, 0]
     assert context_len.tolist() == [21, 32, 49]
+
+
+def test_decoding_beside_a_shared_prompt():
+    """The page tables' entries for the prompt are not valid pages: neither call may read them."""
+    from paper_2608_20961_b200 import attention as at
+    c = random_case([70, 64, 90], [1, 1, 1], seed=6, shared=64)
+    layer, g = layer_of(c)
+    assert (c.table[:, :4] < 0).all()
+    pos, status = torch.tensor(c.L, dtype=I32), i32(0, 0, 0)
+    O = layer.append_and_attend(g["tree"], pos.to(DEV), g["q"], g["k"], g["v"], status, shared_pages=g["shared_pages"], shared_len=64)
+    assert not status.any() and layer.cache.context_len.tolist() == [71, 65, 91]
+    one, ref, size = decode_reference(c, pos)
+    au.assert_attn(one, O.cpu(), ref, size, tensor_cores=True)
+    layer.cache.context_len[1] = 63                     # shorter than the prompt, with a page of its own there
+    layer.cache.page_table[1, 3] = layer.cache.page_table[1, 4]
+    layer.append_and_attend(g["tree"], i32(71, 63, 91), g["q"], g["k"], g["v"], status, shared_pages=g["shared_pages"], shared_len=64)
+    assert status.tolist() == [0, at.SEQ_BAD_LENGTH, 0]
+    assert layer.cache.context_len.tolist() == [72, 63, 92]
