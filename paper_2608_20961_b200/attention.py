@@ -3,12 +3,13 @@ layer's speculative round.
 
 Function names and argument order follow the C header; as in ``binding``, torch tensors supply
 device memory and the stream, every computation runs in the library's CUDA kernels, and outputs are
-written in place.  Shapes, strides and types are checked here (``ValueError``), sizes and alignment by
+written in place.  Devices, shapes, strides and types are checked here (``ValueError``), sizes and alignment by
 the library (``binding.TreewyError``).
 """
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -48,7 +49,7 @@ def load_library():
         return _lib
     lib = tw.load_library()
     vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-    cache, rope, tree = ctypes.POINTER(KVCacheStruct), ctypes.POINTER(RopeStruct), ctypes.POINTER(tw.TreeStruct)
+    cache, rope, tree = ctypes.POINTER(KVCacheStruct), ctypes.POINTER(RopeStruct), vp
     lib.treewy_rope.argtypes = [rope, vp, i64, vp, i64, i32, i32, i32, i32, ctypes.c_int, vp, vp]
     lib.treewy_rope_rows.argtypes = [rope, i32, i32, vp, vp, i64, vp, i64, i32, i32, i32, ctypes.c_int, vp, vp]
     lib.treewy_kv_append.argtypes = [cache, rope, i32, i32, vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, ctypes.c_int, vp, vp]
@@ -70,23 +71,36 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _int32(t: torch.Tensor | None, n: int, what: str) -> int | None:
+def _int32(t: torch.Tensor | None, n: int, what: str, dev: int) -> int | None:
     """Checks an optional int32 array; returns its address."""
     if t is None:
         return None
     if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous int32 tensor of at least {n} elements wanted")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: on another device")
     return t.data_ptr()
 
 
-def _rows(x: torch.Tensor, T: int, H: int, d: int, dtype: torch.dtype, what: str) -> int:
+def _rows(x: torch.Tensor, T: int, H: int, d: int, dtype: torch.dtype, what: str, dev: int) -> int:
     """Checks packed rows [T, H, d] (heads contiguous, tokens at any distance); returns that distance."""
-    shape, st = x.shape, x.stride()
-    if x.dtype is not dtype or len(shape) != 3 or shape[1] != H or shape[2] != d or shape[0] < T:
-        raise ValueError(f"{what}: {dtype} [{T}, {H}, {d}] wanted, got {x.dtype} {list(shape)}")
-    if (st[2] != 1 and d > 1) or (st[1] != d and H > 1):
+    try:
+        (n, h, c), (row, head, one) = x.shape, x.stride()
+    except ValueError:
+        n = h = c = row = head = one = -1
+    if x.dtype is not dtype or h != H or c != d or n < T:
+        raise ValueError(f"{what}: {dtype} [{T}, {H}, {d}] wanted, got {x.dtype} {list(x.shape)}")
+    if (one != 1 and d > 1) or (head != d and H > 1):
         raise ValueError(f"{what}: the heads of a token have to be contiguous")
-    return st[0] if shape[0] > 1 else H * d
+    if x.get_device() != dev:
+        raise ValueError(f"{what}: on another device")
+    return row if n > 1 else H * d
+
+
+def _on_gpu(dev: int, work: int) -> None:
+    """A call that has something to do wants a GPU's memory (dev: torch's number of it, negative for the host)."""
+    if dev < 0 and work > 0:
+        raise ValueError("tensors in a GPU's memory wanted")
 
 
 # (These calls are a few microseconds of GPU work in a decoding step, so the host side is kept short: raw addresses,
@@ -102,10 +116,18 @@ def _stream(stream, x: torch.Tensor) -> int | None:
     return torch.cuda.current_stream().cuda_stream
 
 
-def _tree_ref(tree: Tree):
-    """The tree's struct.  Its arrays may be replaced between calls, so it is built for each."""
-    return ctypes.byref(tw.TreeStruct(tree.B, tree.T, tree.H_v, tree.max_nodes, tree.node_offsets.data_ptr(),
-                                      tree.parent.data_ptr(), None, tree.anc_mask.data_ptr(), None, None))
+_TREE = struct.Struct("4i6P")                         # treewy_tree_t, which takes ctypes twice as long to fill
+assert _TREE.size == ctypes.sizeof(tw.TreeStruct)
+
+
+def _tree_struct(tree: Tree, dev: int) -> bytes:
+    """The tree as the C calls take it.  Its arrays may be replaced between calls, so what is read of it is checked for each."""
+    offsets, mask = tree.node_offsets, tree.anc_mask
+    if offsets.dtype is not torch.int32 or offsets.numel() <= tree.B or not offsets.is_contiguous() or offsets.get_device() != dev:
+        raise ValueError("tree: node_offsets: contiguous int32 [B + 1] on the cache's device wanted")
+    if mask.dtype is not torch.int64 or mask.numel() < tree.T or not mask.is_contiguous() or mask.get_device() != dev:
+        raise ValueError("tree: anc_mask: contiguous int64 [T] on the cache's device wanted")
+    return _TREE.pack(tree.B, tree.T, tree.H_v, tree.max_nodes, offsets.data_ptr(), 0, 0, mask.data_ptr(), 0, 0)
 
 
 class KVCache:
@@ -119,7 +141,8 @@ class KVCache:
         _require(k.shape[3] == 1 or k.stride(3) == 1, "k, v: d_head has to be contiguous")
         _require(page_table.dim() == 2 and page_table.is_contiguous() and page_table.dtype == torch.int32,
                  "page_table: contiguous int32 [B, max_pages] wanted")
-        _int32(context_len, page_table.shape[0], "context_len")
+        self._dev = k.get_device()
+        _int32(context_len, page_table.shape[0], "context_len", self._dev)
         _require(page_table.device == k.device == v.device == context_len.device, "cache tensors on different devices")
         self.k, self.v, self.page_table, self.context_len = k, v, page_table, context_len
         self.B, self.max_pages = (int(n) for n in page_table.shape)
@@ -147,7 +170,10 @@ class Rope:
         _require(pair_axis is None or (pair_axis.dtype == torch.uint8 and pair_axis.is_contiguous()
                                        and pair_axis.numel() == cos_sin.shape[1] // 2),
                  "pair_axis: uint8 [rot_dim / 2] wanted")
+        _require(cos_sin.device == positions.device and (pair_axis is None or pair_axis.device == cos_sin.device),
+                 "rotary tensors on different devices")
         self.cos_sin, self.positions, self.pair_axis = cos_sin, positions, pair_axis
+        self._dev = cos_sin.get_device()
         self.T = int(positions.shape[1])
         self._struct = RopeStruct(cos_sin.data_ptr(), positions.data_ptr(),
                                   None if pair_axis is None else pair_axis.data_ptr(), int(positions.shape[0]),
@@ -162,9 +188,11 @@ def treewy_rope(rope: Rope, x: torch.Tensor, y: torch.Tensor, inverse: bool = Fa
     dt = tw._DTYPES.get(x.dtype)
     if T != rope.T or dt is None:
         raise ValueError(f"x: bfloat16 or float32, {rope.T} tokens as rope.positions has, wanted")
-    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x"), _rows(y, T, H, d, x.dtype, "y")
+    dev = rope._dev
+    _on_gpu(dev, T)
+    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x", dev), _rows(y, T, H, d, x.dtype, "y", dev)
     tw._call("treewy_rope", load_library().treewy_rope, rope._ref, x.data_ptr(), ld_x, y.data_ptr(), ld_y, T, H, d,
-             int(inverse), dt, _int32(row_status, 1, "row_status"), _stream(stream, x))
+             int(inverse), dt, _int32(row_status, 1, "row_status", dev), _stream(stream, x))
 
 
 def treewy_rope_rows(rope: Rope, row_offsets: torch.Tensor, x: torch.Tensor, y: torch.Tensor, inverse: bool = False,
@@ -174,9 +202,11 @@ def treewy_rope_rows(rope: Rope, row_offsets: torch.Tensor, x: torch.Tensor, y: 
     B, dt = row_offsets.numel() - 1, tw._DTYPES.get(x.dtype)
     if T != rope.T or dt is None or B < 0:
         raise ValueError(f"x: bfloat16 or float32, {rope.T} tokens as rope.positions has, wanted; row_offsets: B + 1 of them")
-    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x"), _rows(y, T, H, d, x.dtype, "y")
-    tw._call("treewy_rope_rows", load_library().treewy_rope_rows, rope._ref, B, T, _int32(row_offsets, B + 1, "row_offsets"),
-             x.data_ptr(), ld_x, y.data_ptr(), ld_y, H, d, int(inverse), dt, _int32(seq_status, B, "seq_status"), _stream(stream, x))
+    dev = rope._dev
+    _on_gpu(dev, T)
+    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x", dev), _rows(y, T, H, d, x.dtype, "y", dev)
+    tw._call("treewy_rope_rows", load_library().treewy_rope_rows, rope._ref, B, T, _int32(row_offsets, B + 1, "row_offsets", dev),
+             x.data_ptr(), ld_x, y.data_ptr(), ld_y, H, d, int(inverse), dt, _int32(seq_status, B, "seq_status", dev), _stream(stream, x))
 
 
 def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -184,26 +214,27 @@ def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor,
                      seq_status: torch.Tensor | None = None, stream=None) -> None:
     """Rows k, v [T, H_kv, d] of the sequences at row_offsets [B + 1] go behind context_len of each sequence's
     cache, k rotated on the way; q [T, H_q, d], when given, is rotated into q_out in the same pass."""
-    T, H_kv, d, dtype = k.shape[0], cache.H_kv, cache.d_head, cache.dtype
-    if rope is not None and rope.T != T:
-        raise ValueError("rope: as many positions as rows wanted")
-    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
+    T, H_kv, d, dtype, dev = k.shape[0], cache.H_kv, cache.d_head, cache.dtype, cache._dev
+    if rope is not None and (rope.T != T or rope._dev != dev):
+        raise ValueError("rope: as many positions as rows, on the cache's device, wanted")
+    _on_gpu(dev, T)
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
     H_q = ld_q = ld_qo = 0
     q_at = qo_at = None
     if q is not None:
         if q_out is None:
             raise ValueError("q_out: wanted with q")
         H_q = q.shape[1]
-        ld_q, ld_qo = _rows(q, T, H_q, d, dtype, "q"), _rows(q_out, T, H_q, d, dtype, "q_out")
+        ld_q, ld_qo = _rows(q, T, H_q, d, dtype, "q", dev), _rows(q_out, T, H_q, d, dtype, "q_out", dev)
         q_at, qo_at = q.data_ptr(), q_out.data_ptr()
     tw._call("treewy_kv_append", load_library().treewy_kv_append, cache._ref, None if rope is None else rope._ref, cache.B, T,
-             _int32(row_offsets, cache.B + 1, "row_offsets"), k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, q_at, ld_q, qo_at,
-             ld_qo, cache._dt, _int32(seq_status, cache.B, "seq_status"), _stream(stream, k))
+             _int32(row_offsets, cache.B + 1, "row_offsets", dev), k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, q_at, ld_q, qo_at,
+             ld_qo, cache._dt, _int32(seq_status, cache.B, "seq_status", dev), _stream(stream, k))
 
 
 def attn_workspace(cache: KVCache, tree: Tree, H_q: int, shared_len: int = 0) -> torch.Tensor:
     """A workspace for ``treewy_attn_verify`` calls of these sizes (one per call in flight)."""
-    n = load_library().treewy_attn_workspace(cache._ref, _tree_ref(tree), H_q, shared_len, cache._dt)
+    n = load_library().treewy_attn_workspace(cache._ref, _tree_struct(tree, cache._dev), H_q, shared_len, cache._dt)
     return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=cache.k.device)
 
 
@@ -214,19 +245,22 @@ def treewy_attn_verify(cache: KVCache, tree: Tree, q: torch.Tensor, k: torch.Ten
     """O [T, H_q, d] <- attention of every draft node (q, k, v: packed rows) over its sequence's cached tokens
     and its ancestors."""
     lib = load_library()
-    T, H_kv, d, dtype = tree.T, cache.H_kv, cache.d_head, cache.dtype
+    T, H_kv, d, dtype, dev = tree.T, cache.H_kv, cache.d_head, cache.dtype, cache._dev
+    _on_gpu(dev, T)
     H_q = q.shape[1]
     if tree.B != cache.B:
         raise ValueError("tree: another number of sequences than the cache's page table")
-    ld_q = _rows(q, T, H_q, d, dtype, "q")
-    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
-    if _rows(O, T, H_q, d, dtype, "O") != H_q * d and T > 0:
+    ld_q = _rows(q, T, H_q, d, dtype, "q", dev)
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
+    if _rows(O, T, H_q, d, dtype, "O", dev) != H_q * d and T > 0:
         raise ValueError("O: contiguous rows wanted")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous and on the cache's device wanted")
     fn = lib.treewy_attn_verify_generic if generic else lib.treewy_attn_verify
-    tw._call("treewy_attn_verify_generic" if generic else "treewy_attn_verify", fn, cache._ref, _tree_ref(tree),
+    tw._call("treewy_attn_verify_generic" if generic else "treewy_attn_verify", fn, cache._ref, _tree_struct(tree, dev),
              q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, scale,
-             _int32(shared_pages, shared_len // cache.page_size, "shared_pages"), shared_len, cache._dt, O.data_ptr(),
-             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _int32(seq_status, cache.B, "seq_status"),
+             _int32(shared_pages, shared_len // cache.page_size, "shared_pages", dev), shared_len, cache._dt, O.data_ptr(),
+             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _int32(seq_status, cache.B, "seq_status", dev),
              _stream(stream, q))
 
 
@@ -237,11 +271,12 @@ def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tenso
     lengths after it."""
     if tree.B != cache.B:
         raise ValueError("tree: another number of sequences than the cache's page table")
-    B, T, H_kv, d, dtype = cache.B, tree.T, cache.H_kv, cache.d_head, cache.dtype
-    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k"), _rows(v, T, H_kv, d, dtype, "v")
-    tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, _tree_ref(tree), k.data_ptr(), ld_k, v.data_ptr(),
-             ld_v, _int32(accepted, B, "accepted"), cache._dt, _int32(new_context_len, B, "new_context_len"),
-             _int32(seq_status, B, "seq_status"), _stream(stream, k))
+    B, T, H_kv, d, dtype, dev = cache.B, tree.T, cache.H_kv, cache.d_head, cache.dtype, cache._dev
+    _on_gpu(dev, B)
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
+    tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, _tree_struct(tree, dev), k.data_ptr(), ld_k, v.data_ptr(),
+             ld_v, _int32(accepted, B, "accepted", dev), cache._dt, _int32(new_context_len, B, "new_context_len", dev),
+             _int32(seq_status, B, "seq_status", dev), _stream(stream, k))
 
 
 class AttentionLayer:
@@ -289,7 +324,7 @@ class AttentionLayer:
         """The status words of a round that begins."""
         if tree.B != self.cache.B:
             raise ValueError("tree: another number of sequences than the cache's page table")
-        _int32(seq_status, self.cache.B, "seq_status")
+        _int32(seq_status, self.cache.B, "seq_status", self.cache._dev)
         self._round = self._own.zero_() if seq_status is None else seq_status.view(-1)[:self.cache.B]
         return self._round
 

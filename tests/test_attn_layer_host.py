@@ -40,3 +40,60 @@ def test_rope_rows_refusals(at):
     for off, x in ((i32(3), z(5, 4, 64)), (i32(3).long(), z(6, 4, 64)), (i32(0), z(6, 4, 64)), (i32(3), z(6, 4, 64, dt=torch.float16))):
         with pytest.raises(ValueError):
             at.treewy_rope_rows(handle, off, x, x)
+
+
+def calls(at, dev="cpu"):
+    """Every call of the binding as (function, keyword arguments), with something to do."""
+    t = lambda x: x.to(dev)
+    cache = at.KVCache(t(z(4, 8, 2, 64)), t(z(4, 8, 2, 64)), t(i32(2, 2)), t(i32(2)))
+    tree = at.tw.Tree.empty(t(torch.tensor([0, 3, 6], dtype=torch.int32)), t(i32(6)), 1)
+    rope = at.Rope(t(z(16, 64, dt=torch.float32)), t(i32(6)))
+    rows = lambda h: t(z(6, h, 64))
+    return cache, tree, rope, [
+        (at.treewy_rope, dict(rope=rope, x=rows(4), y=rows(4), row_status=t(i32(1)))),
+        (at.treewy_rope_rows, dict(rope=rope, row_offsets=t(torch.tensor([0, 3, 6], dtype=torch.int32)), x=rows(4), y=rows(4), seq_status=t(i32(2)))),
+        (at.treewy_kv_append, dict(cache=cache, row_offsets=t(torch.tensor([0, 3, 6], dtype=torch.int32)), k=rows(2), v=rows(2), rope=rope, q=rows(4),
+                                   q_out=rows(4), seq_status=t(i32(2)))),
+        (at.treewy_attn_verify, dict(cache=cache, tree=tree, q=rows(4), k=rows(2), v=rows(2), scale=1.0, O=rows(4), workspace=t(z(1 << 24, dt=torch.uint8)),
+                                     shared_pages=t(i32(1)), shared_len=8, seq_status=t(i32(2)))),
+        (at.treewy_kv_commit, dict(cache=cache, tree=tree, k=rows(2), v=rows(2), accepted=t(i32(2)), new_context_len=t(i32(2)), seq_status=t(i32(2))))]
+
+
+class Stream:
+    cuda_stream = 0
+
+
+def test_host_tensors_are_refused(at):
+    for fn, kw in calls(at)[3]:
+        with pytest.raises(ValueError):
+            fn(**kw, stream=Stream())
+
+
+@pytest.mark.gpu
+def test_tensors_of_two_devices_are_refused(at):
+    """One argument at a time on the host: refused before a kernel could meet its address."""
+    cache, tree, rope, all_calls = calls(at, "cuda:0")
+    for fn, kw in all_calls:
+        for name, x in kw.items():
+            if isinstance(x, torch.Tensor):
+                with pytest.raises(ValueError):
+                    fn(**{**kw, name: x.cpu()})
+        if "tree" in kw:
+            for name in ("node_offsets", "anc_mask"):
+                with pytest.raises(ValueError):
+                    fn(**{**kw, "tree": at.tw.Tree(**{**vars(tree), name: getattr(tree, name).cpu()})})
+    cpu = calls(at)
+    with pytest.raises(ValueError):
+        at.treewy_kv_append(**{**all_calls[2][1], "rope": cpu[2]})
+    for bad in (dict(positions=rope.positions.cpu()), dict(cos_sin=rope.cos_sin.cpu()), dict(pair_axis=torch.zeros(32, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            at.Rope(**{**dict(cos_sin=rope.cos_sin, positions=rope.positions), **bad})
+
+
+@pytest.mark.parametrize("bad", [dict(node_offsets=i32(2)), dict(node_offsets=i32(3).long()), dict(node_offsets=i32(6)[::2]),
+                                 dict(anc_mask=torch.zeros(5, dtype=torch.int64)), dict(anc_mask=i32(6)),
+                                 dict(anc_mask=torch.zeros(12, dtype=torch.int64)[::2])])
+def test_arrays_of_a_tree_are_checked(at, bad):
+    cache, tree, _, _ = calls(at)
+    with pytest.raises(ValueError):
+        at.attn_workspace(cache, at.tw.Tree(**{**vars(tree), **bad}), 4)
