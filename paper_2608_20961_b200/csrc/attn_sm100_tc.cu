@@ -45,7 +45,11 @@ constexpr int MAX_CTAS = 160;
 constexpr int THREADS = 384, PRODUCER_K = 8, PRODUCER_V = 9, MMA_QK = 10, MMA_PV = 11;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
 constexpr int MAX_START = 40, MAX_TILE = 5;
-constexpr int MIN_UNITS = 8;           // of a CTA's part: below this a part is mostly start and end
+// Least units of a CTA's part.  A part within an item's tiles has to hold the beginning of one of them: the joins read a block
+// from every part between an item's first and its last.  (Some parts of a small batch lie in an item's start and have no
+// tile; more and smaller parts still end earlier.  One sequence of 1023 keys with 4, 8, 12, 20: 14.1, 13.8, 13.6, 14.0 us.)
+constexpr int MIN_UNITS = 8;
+static_assert(MIN_UNITS >= MAX_TILE, "a part within an item's tiles holds the beginning of one");
 // What a tile and the start of an item cost, in quarters of a tile of few rows, by the rows of the row tile.  With up to
 // 32 rows one softmax warp in four works and a tile takes 0.47 us (0.53 where HBM bounds it); with 128 all of them do, and it
 // takes 0.6.  A start (queries into tensor memory, the pipeline's start, the output) takes 2 us, 3.1 beside a shared prompt
