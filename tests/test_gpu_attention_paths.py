@@ -95,3 +95,64 @@ def test_append_flags_ranges_that_no_row_falls_into(offsets, bad, written):
         rows = [bool(changed[int(c.table[b, s // c.page]), s % c.page]) for s in range(c.L[b], c.L[b] + 5)]
         if written.get(b, 0) is not None:
             assert rows == [i < written.get(b, 0) for i in range(5)], (b, rows)
+
+
+@pytest.mark.parametrize("D,shared", [(64, 0), (128, 48), (256, 0)])
+def test_more_sequences_than_a_cta_has_threads(D, shared):
+    """Several sequences to each thread of the plan, among them empty and malformed ones, and trees of 1, 8, 16, 32 and 64 nodes."""
+    from paper_2608_20961_b200 import attention as at, binding as tw
+    B = 520
+    c = au.make_case([shared + (29 * b) % 90 for b in range(B)], [(1, 8, 1, 16, 3, 1, 32, 2, 64, 1)[b % 10] for b in range(B)], Hq=4, Hkv=2, D=D,
+                     seed=22, shared=shared)
+    ref, size = au.attn_reference(c)
+    O, status = au.run_attn(c)
+    assert not any(status)
+    au.assert_attn(c, O, ref, size, tensor_cores=True)
+    bad = [b for b in range(B) if b % 37 == 5]
+    for b in bad:
+        c.L[b] = -1
+    good = torch.ones(c.T, dtype=torch.bool)
+    for b in bad:
+        good[_rows_of(c, b)] = False
+    O, status = au.run_attn(c, max_nodes=32)
+    for b in range(B):
+        if c.N[b] > 32:
+            good[_rows_of(c, b)] = False
+            assert status[b] == tw.SEQ_TOO_MANY_NODES
+        else:
+            assert status[b] == (at.SEQ_BAD_LENGTH if b in bad else 0)
+    au.assert_attn(c, O, ref, size, tensor_cores=True, rows=good)
+    assert (O[~good] == 7.25).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,shared", [(16, 1, 64, 0), (40, 2, 128, 0), (24, 1, 256, 64), (32, 1, 128, 32)])
+def test_more_rows_to_a_head_than_a_group_of_ctas_takes(Hq, Hkv, D, shared):
+    """Trees of up to 64 nodes with 16 to 32 query heads to a key/value head: six to sixteen row tiles, beside short trees."""
+    c = au.make_case([shared + n for n in (300, 0, 70, 1000, 64)], [64, 3, 40, 64, 1], Hq=Hq, Hkv=Hkv, D=D, seed=23, shared=shared)
+    ref, size = au.attn_reference(c)
+    for hint in (0, 64):
+        O, status = au.run_attn(c, max_nodes=hint)
+        assert not any(status)
+        au.assert_attn(c, O, ref, size, tensor_cores=True)
+
+
+@pytest.mark.parametrize("B", [33, 70, 1025, 1100])
+def test_append_to_many_sequences(B):
+    """More sequences than one and than two rounds of the search for a row's sequence tell apart, many without a row."""
+    from paper_2608_20961_b200 import attention as at
+    new = [(0, 1, 0, 0, 3)[b % 5] for b in range(B)]
+    c = au.make_case([b % 7 for b in range(B)], [1] * B, Hq=1, Hkv=1, D=64, page=8, poison=False, room=1)
+    g = au.on_gpu(c)
+    off = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).to(torch.int32)
+    T = int(off[-1])
+    k, v = (torch.randn(T, 1, 64, generator=torch.Generator().manual_seed(i)).to(BF16) for i in range(2))
+    kc, vc = c.kc.clone(), c.vc.clone()
+    for b in range(B):
+        for i in range(new[b]):
+            s, t = c.L[b] + i, int(off[b]) + i
+            at_ = int(c.table[b, s // 8]), s % 8
+            kc[at_], vc[at_] = k[t], v[t]
+    status = torch.zeros(B, dtype=torch.int32, device=DEV)
+    at.treewy_kv_append(g["cache"], off.to(DEV), k.to(DEV), v.to(DEV), seq_status=status)
+    assert not status.any()
+    assert torch.equal(g["cache"].k.cpu(), kc) and torch.equal(g["cache"].v.cpu(), vc)
