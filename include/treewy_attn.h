@@ -16,7 +16,8 @@
  * flag the sequence in seq_status (may be NULL; caller zeroes it) and skip it.  Element types are
  * TREEWY_BF16 and TREEWY_F32, one for all data of a call.  `ld_*` are the distances in elements between
  * the rows of consecutive tokens (a row is [heads, d], contiguous); they let q, k and v be column
- * ranges of one projection's output.  Row distances and the cache's strides are multiples of 16 bytes.
+ * ranges of one projection's output.  Row distances and the cache's strides are multiples of 16 bytes; a
+ * row has fewer than 2^31 elements.
  */
 #ifndef TREEWY_ATTN_H
 #define TREEWY_ATTN_H

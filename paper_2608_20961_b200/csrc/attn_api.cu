@@ -15,13 +15,15 @@ inline bool bad_dtype(int d) { return d != TREEWY_F32 && d != TREEWY_BF16; }
 inline int elem_size(treewy_dtype_t t) { return t == TREEWY_BF16 ? 2 : 4; }
 // a distance between rows: whole 16-byte vectors, rows that do not overlap
 inline bool bad_stride(int64_t ld, int64_t least, int elem) { return ld < least || ld % (16 / elem) != 0; }
+// rows whose elements 32 bits do not count (the kernels take offsets within a row in 32 bits)
+inline bool wide_row(int64_t heads, int d) { return heads * d > INT32_MAX; }
 inline treewy_status_t launched(cudaError_t e) { return e == cudaSuccess ? TREEWY_OK : TREEWY_ERR_CUDA; }
 
 treewy_status_t check_cache(const treewy_kv_cache_t *c, int B, treewy_dtype_t io, CacheView *out)
 {
     if (!c || bad_dtype(io)) return c ? TREEWY_ERR_UNSUPPORTED : TREEWY_ERR_INVALID_ARG;
     if (c->n_pages < 0 || c->page_size < 1 || c->max_pages < 0 || c->H_kv < 1 || c->d_head < 1) return TREEWY_ERR_INVALID_ARG;
-    if (c->d_head % 8 != 0 || c->d_head > 256) return TREEWY_ERR_UNSUPPORTED;
+    if (c->d_head % 8 != 0 || c->d_head > 256 || wide_row(c->H_kv, c->d_head)) return TREEWY_ERR_UNSUPPORTED;
     if ((int64_t)c->max_pages * c->page_size > INT32_MAX - TREEWY_MAX_NODES) return TREEWY_ERR_UNSUPPORTED;  // tokens are int32
     const int vec = 16 / elem_size(io);
     if (c->stride_page < 0 || c->stride_slot < 0 || c->stride_head < 0 || c->stride_page % vec || c->stride_slot % vec ||
@@ -69,6 +71,7 @@ treewy_status_t attn_args(const treewy_kv_cache_t *cache, const treewy_tree_t *t
     st = check_cache(cache, tree->B, io, &a->c);
     if (st != TREEWY_OK) return st;
     if (H_q < 1 || H_q % cache->H_kv != 0) return TREEWY_ERR_INVALID_ARG;
+    if (wide_row(H_q, cache->d_head)) return TREEWY_ERR_UNSUPPORTED;
     if (shared_len < 0 || shared_len % cache->page_size != 0) return TREEWY_ERR_INVALID_ARG;
     a->node_offsets = tree->node_offsets, a->anc_mask = tree->anc_mask;
     a->B = tree->B, a->T = tree->T, a->max_nodes = max_nodes, a->H_q = H_q, a->G = H_q / cache->H_kv;
@@ -113,7 +116,7 @@ treewy_status_t rope_common(const treewy_rope_t *rope, int32_t B, int32_t T, con
                             treewy_dtype_t io_dtype, int32_t *status, void *cuda_stream)
 {
     if (T < 0 || H < 1 || d_head < 2) return TREEWY_ERR_INVALID_ARG;
-    if (bad_dtype(io_dtype) || d_head % 2 != 0) return TREEWY_ERR_UNSUPPORTED;
+    if (bad_dtype(io_dtype) || d_head % 2 != 0 || wide_row(H, d_head)) return TREEWY_ERR_UNSUPPORTED;
     RowsArgs a = {};
     treewy_status_t st = check_rope(rope, T, d_head, inverse, &a.r);
     if (st != TREEWY_OK) return st;
@@ -156,6 +159,7 @@ treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_ro
     RowsArgs a = {};
     treewy_status_t st = check_cache(cache, B, io_dtype, &a.c);
     if (st != TREEWY_OK) return st;
+    if (wide_row(H_q, cache->d_head)) return TREEWY_ERR_UNSUPPORTED;
     if (rope) {
         st = check_rope(rope, T, cache->d_head, 0, &a.r);
         if (st != TREEWY_OK) return st;

@@ -97,3 +97,20 @@ def test_arrays_of_a_tree_are_checked(at, bad):
     cache, tree, _, _ = calls(at)
     with pytest.raises(ValueError):
         at.attn_workspace(cache, at.tw.Tree(**{**vars(tree), **bad}), 4)
+
+
+def test_rows_past_32_bits_are_refused(at):
+    """Offsets within a token's row are 32-bit in the kernels."""
+    lib, H = at.load_library(), 1 << 24                # x 128 = 2^31 elements, 4 GB of bf16
+    cache = lambda H_kv: at.KVCacheStruct(k=A, v=A, stride_page=1 << 40, stride_slot=1 << 34, stride_head=128, page_table=A, context_len=A + 16,
+                                          n_pages=4, page_size=8, max_pages=64, H_kv=H_kv, d_head=128)
+    rope = at.RopeStruct(cos_sin=A, positions=A, pair_axis=None, n_axes=1, max_positions=16, rot_dim=64, interleaved=0)
+    tree = at.tw.TreeStruct(B=1, T=1, H_v=1, max_nodes=1, node_offsets=A, parent=None, depth=None, anc_mask=A, cum_log_gate=None, level_order=None)
+    ref, ld = ctypes.byref, 1 << 34
+    assert lib.treewy_rope(ref(rope), vp(A), ld, vp(A), ld, 1, H, 128, 0, BF16, None, None) == UNSUPPORTED
+    for hk, hq in ((1, H), (H, 0)):
+        assert lib.treewy_kv_append(ref(cache(hk)), ref(rope), 1, 1, vp(A), vp(A), ld, vp(A), ld, hq, vp(A), ld, vp(A), ld, BF16, None, None) == UNSUPPORTED
+    for fn in (lib.treewy_attn_verify, lib.treewy_attn_verify_generic):
+        for hk in (1, H):
+            assert fn(ref(cache(hk)), ref(tree), vp(A), ld, vp(A), ld, vp(A), ld, H, 0.1, None, 0, BF16, vp(A), vp(A), 1 << 60, None, None) == UNSUPPORTED
+    assert lib.treewy_kv_commit(ref(cache(H)), ref(tree), vp(A), ld, vp(A), ld, vp(A), BF16, None, None, None) == UNSUPPORTED
