@@ -12,11 +12,13 @@ CONFIG = {64: (8, 8, 4, False), 128: (8, 4, 4, False), 256: (3, 2, 2, True)}
 
 
 def programs(d, items, q_phase, q_buffers, rescale):
-    """Role -> list of steps; ("wait", barrier, phase, parity), ("arrive", barrier), ("tag", tile), ("say", tile).
+    """Role -> list of steps; ("wait", barrier, phase, parity), ("arrive", barrier), ("tag", tile), ("say", tile), and
+    ("done", barrier): a copy or a product that arrives some time after it was issued, in the order of issue.
     items: key tiles of each item.  rescale: every tile moves the running maximum (a wait more), or none does."""
     NK, NV, NSB, P_SMEM = CONFIG[d]
     wait = lambda name, i, n: ("wait", (name, i % n), i // n, (i // n) & 1)
     arrive = lambda name, i, n: ("arrive", (name, i % n))
+    done = lambda name, i, n: ("done", (name, i % n))
 
     def q(kind, item):
         barrier, parity = q_phase(item, q_buffers)
@@ -73,7 +75,7 @@ def programs(d, items, q_phase, q_buffers, rescale):
             for _ in range(n):
                 if g >= NSB:
                     out.append(wait("s_free", g - NSB, NSB) if P_SMEM else wait("pv_done", g - NSB, NV))
-                out += [wait("k_full", g, NK), arrive("s_full", g, NK)]
+                out += [wait("k_full", g, NK), done("s_full", g, NK)]
                 g += 1
         return out + [wait("item_full", len(items), ITEMS)]
 
@@ -85,7 +87,7 @@ def programs(d, items, q_phase, q_buffers, rescale):
                 out.append(wait("v_full", g, NV))
                 if j == 0 and i > 0:
                     out.append(wait("o_free", i - 1, 1))
-                out += [wait("p_full", g, NSB), arrive("pv_done", g, NV)]
+                out += [wait("p_full", g, NSB), done("pv_done", g, NV)]
                 g += 1
         return out + [wait("item_full", len(items), ITEMS)]
 
@@ -104,7 +106,7 @@ def programs(d, items, q_phase, q_buffers, rescale):
             for _ in range(n):
                 if g >= ns:
                     out.append(wait(empty, g - ns, ns))
-                out.append(arrive(full, g, ns))
+                out.append(done(full, g, ns))
                 g += 1
         return out
 
@@ -127,6 +129,11 @@ def walk(progs, limit=2_000_000):
                 cur = []
             cur.append(op)
         steps.append(mine + [cur])
+    # what a role has issued completes in a role of its own
+    for r in range(len(steps)):
+        late = [[("after", r, i + 1), ("arrive", op[1])] for i, step in enumerate(steps[r]) for op in step if op[0] == "done"]
+        if late:
+            steps.append(late)
     arrivals, said = [], []                          # of each role, by the number of its steps that are done
     for s in steps:
         a, t, last = [{}], [-1], -1
@@ -158,6 +165,9 @@ def walk(progs, limit=2_000_000):
                 if done > op[2] + 1:
                     return f"role {r}: phase {op[2]} of {op[1]} has been overtaken ({done} are complete)"
                 if not passes:
+                    continue
+            elif op[0] == "after":
+                if pcs[op[1]] < op[2]:
                     continue
             elif op[0] == "tag":
                 tag = max(t[x] for t, x in zip(said, pcs))

@@ -17,7 +17,7 @@ extern "C" unsigned q_barrier(unsigned i, int n) { return treewy::q_phase(i, n).
 extern "C" unsigned q_parity(unsigned i, int n) { return treewy::q_phase(i, n).parity; }
 """
 # tiles of an item: one (a cut piece), two (up to 64 keys and the draft rows), more
-BATCHES = [[1, 1, 1, 1], [2, 2, 2], [2, 1, 2, 1], [3, 2, 2], [1, 3, 2], [5, 2, 1]]
+BATCHES = [[1, 1, 1], [2, 2, 2], [2, 1, 2], [3, 2], [5, 1]]
 
 
 @pytest.fixture(scope="module")
