@@ -15,7 +15,7 @@ namespace treewy {
 namespace {
 
 constexpr int THREADS = 256, RB = 32, KB = 32;
-constexpr int TARGET_CTAS = 592;   // four to an SM
+constexpr int TARGET_CTAS = 592;   // four to an SM, which their shared memory allows up to heads of 128 (256: two, 100 KB each)
 constexpr int MIN_KEYS = 32;       // of a part: one step
 constexpr int MAX_PARTS = 64;
 constexpr float MASKED = -1.f;

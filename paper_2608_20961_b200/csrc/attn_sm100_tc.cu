@@ -24,11 +24,11 @@
 // S = Q K^T and O += P V (a single one for both was the slowest role: its waits alone took as long as a tile).
 //
 // What it measures and what bounds it (floor at a plain copy's 6.5 TB/s in brackets), 32 query over 8 key/value heads of 128
-// unless said: decoding 64 x up to 8192 keys 172 us [146], two chains of 5 over 65537 keys 93 us [82]: HBM, in the main
-// kernel at 0.92 of the copy's rate.  32 trees of up to 32 nodes over 8192 keys, 16 over 2 heads of 256, 87 to 94 us [43]: the
-// copies out of L2, which bring each tile to two CTAs at 40 bytes a cycle.  64 trees of 8 under a prompt of 4096, 70 to 75 us
+// unless said: decoding 64 x up to 8192 keys 173 us [146], two chains of 5 over 65537 keys 93 us [82]: HBM, in the main
+// kernel at 0.92 of the copy's rate.  32 trees of up to 32 nodes over 8192 keys, 16 over 2 heads of 256, 88 to 94 us [43]: the
+// copies out of L2, which bring each tile to two CTAs at 40 bytes a cycle.  64 trees of 8 under a prompt of 4096, 69 to 75 us
 // [17]: with 128 rows the copies of a tile and the softmax step, two groups in turn, are equally long; leaving out all of the
-// softmax's arithmetic saves 5 us.  One sequence of 1023 keys 13.5 us [0.6]: latency.
+// softmax's arithmetic saves 5 us.  One sequence of 1023 keys 14 us [0.6]: latency.
 #include <type_traits>
 
 #include "attn_common.cuh"
@@ -54,7 +54,9 @@ static_assert(MIN_UNITS >= MAX_TILE, "a part within an item's tiles holds the be
 // 32 rows one softmax warp in four works and a tile takes 0.47 us (0.53 where HBM bounds it); with 128 all of them do, and it
 // takes 0.6.  A start (queries into tensor memory, the pipeline's start, the output) takes 2 us, 3.1 beside a shared prompt
 // (every output is a block in fp32) and 3 to 6 with 128 rows.  (A part's time against its tiles and items, least squares over
-// the 148 parts; heads of 128, pages of 16.)
+// the 148 parts; heads of 128, pages of 16.)  Heads of 64 and 256 have other tiles and the same figures: with starts of half /
+// twice as much decoding takes 148 / 136 us instead of 135 (64) and 97 / 99 instead of 97 (256), 32 trees of 32 with heads
+// of 256 95 / 91 instead of 89; with tiles of 4 / 7 units above 32 rows those trees take 88 / 91.
 __device__ __forceinline__ int tile_cost(long long rows) { return rows > 32 ? 5 : 4; }
 __device__ __forceinline__ int start_cost(long long rows, bool shared) { return rows > 32 ? MAX_START : shared ? 30 : 20; }
 constexpr float LAZY = 8.f;
