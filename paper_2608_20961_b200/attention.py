@@ -1,5 +1,5 @@
-"""Thin ctypes binding of the attention-layer calls (``include/treewy_attn.h``) and one attention
-layer's speculative round.
+"""Thin ctypes binding of the attention-layer calls (``include/treewy_attn.h``, ``include/treewy_prompt.h``) and one
+attention layer's steps: a speculative round, a prompt or a piece of one, single tokens.
 
 Function names and argument order follow the C header; as in ``binding``, torch tensors supply
 device memory and the stream, every computation runs in the library's CUDA kernels, and outputs are
@@ -16,7 +16,7 @@ import torch
 from . import binding as tw
 from .binding import Tree
 
-SEQ_BAD_PAGE, SEQ_BAD_LENGTH, SEQ_BAD_POSITION = 64, 128, 256
+SEQ_BAD_PAGE, SEQ_BAD_LENGTH, SEQ_BAD_POSITION, SEQ_NO_PAGES = 64, 128, 256, 512
 
 
 class KVCacheStruct(ctypes.Structure):
@@ -37,6 +37,17 @@ class RopeStruct(ctypes.Structure):
         ("n_axes", ctypes.c_int32), ("max_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
         ("interleaved", ctypes.c_int32),
     ]
+
+
+class HeadNormStruct(ctypes.Structure):
+    """Mirror of ``treewy_head_norm_t``."""
+    _fields_ = [("weight", ctypes.c_void_p), ("weight_dtype", ctypes.c_int), ("eps", ctypes.c_float), ("plus_one", ctypes.c_int32)]
+
+
+class PagePoolStruct(ctypes.Structure):
+    """Mirror of ``treewy_page_pool_t``."""
+    _fields_ = [("page_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
 
 
 _lib = None
@@ -62,6 +73,21 @@ def load_library():
         fn.restype = ctypes.c_int
     lib.treewy_attn_workspace.argtypes = [cache, tree, i32, i32, ctypes.c_int]
     lib.treewy_attn_workspace.restype = ctypes.c_size_t
+    norm, pool, size, dt = ctypes.POINTER(HeadNormStruct), ctypes.POINTER(PagePoolStruct), ctypes.c_size_t, ctypes.c_int
+    lib.treewy_norm_rope.argtypes = [norm, rope, i32, i32, vp, vp, i64, vp, i64, i32, i32, dt, vp, vp]
+    lib.treewy_norm_rope_backward.argtypes = [norm, rope, vp, i64, vp, i64, vp, i64, vp, i32, i32, i32, dt, vp, size, vp, vp]
+    lib.treewy_kv_append_norm.argtypes = [cache, rope, norm, norm, i32, i32, vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, dt, vp, vp]
+    chunk = [cache, i32, i32, vp, vp, i64, i32, f32, i32, i32, dt, vp, vp, size, vp, vp]
+    lib.treewy_attn_chunk.argtypes = chunk
+    lib.treewy_attn_chunk_generic.argtypes = chunk
+    lib.treewy_pages_reserve.argtypes = [pool, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.treewy_pages_release.argtypes = [pool, i32, vp, vp, vp, vp]
+    for fn in (lib.treewy_norm_rope, lib.treewy_norm_rope_backward, lib.treewy_kv_append_norm, lib.treewy_attn_chunk,
+               lib.treewy_attn_chunk_generic, lib.treewy_pages_reserve, lib.treewy_pages_release):
+        fn.restype = ctypes.c_int
+    lib.treewy_norm_rope_workspace.argtypes = [i32, i32, i32, dt]
+    lib.treewy_attn_chunk_workspace.argtypes = [cache, i32, i32, i32, i32, i32, dt]
+    lib.treewy_norm_rope_workspace.restype = lib.treewy_attn_chunk_workspace.restype = size
     _lib = lib
     return lib
 
@@ -277,6 +303,178 @@ def treewy_kv_commit(cache: KVCache, tree: Tree, k: torch.Tensor, v: torch.Tenso
     tw._call("treewy_kv_commit", load_library().treewy_kv_commit, cache._ref, _tree_struct(tree, dev), k.data_ptr(), ld_k, v.data_ptr(),
              ld_v, _int32(accepted, B, "accepted", dev), cache._dt, _int32(new_context_len, B, "new_context_len", dev),
              _int32(seq_status, B, "seq_status", dev), _stream(stream, k))
+
+
+class HeadNorm:
+    """Root-mean-square norm of each head (``treewy_head_norm_t``): weight [d_head] bfloat16 or float32, the same for all heads;
+    plus_one: 1 + weight is meant.  The object refers to the weight's memory."""
+
+    def __init__(self, weight: torch.Tensor, eps: float = 1e-6, plus_one: bool = False):
+        _require(weight.dtype in tw._DTYPES and weight.dim() == 1 and weight.is_contiguous(),
+                 "weight: contiguous bfloat16 or float32 [d_head] wanted")
+        self.weight, self.eps, self.plus_one, self.d = weight, eps, plus_one, int(weight.numel())
+        self._dev = weight.get_device()
+        self._struct = HeadNormStruct(weight.data_ptr(), tw._DTYPES[weight.dtype], eps, int(bool(plus_one)))
+        self._ref = ctypes.byref(self._struct)
+
+
+def _norm(norm: HeadNorm | None, d: int, what: str, dev: int):
+    if norm is None:
+        return None
+    if norm.d != d or norm._dev != dev:
+        raise ValueError(f"{what}: a weight of {d} elements on the rows' device wanted")
+    return norm._ref
+
+
+def _norm_rows(norm: HeadNorm, rope: Rope | None, x: torch.Tensor):
+    """What the norm's calls check of x [T, H, d]."""
+    if x.dim() != 3 or x.dtype not in tw._DTYPES:
+        raise ValueError("x: bfloat16 or float32 [T, H, d] wanted")
+    T, H, d = x.shape
+    dev = x.get_device()
+    if rope is not None and (rope.T != T or rope._dev != dev):
+        raise ValueError("rope: as many positions as rows, on their device, wanted")
+    return T, H, d, dev, _norm(norm, d, "norm", dev)
+
+
+def treewy_norm_rope(norm: HeadNorm, rope: Rope | None, x: torch.Tensor, y: torch.Tensor, row_offsets: torch.Tensor | None = None,
+                     seq_status: torch.Tensor | None = None, stream=None) -> None:
+    """y [T, H, d] <- x, each head normalised and then rotated (rope None: normalised only).  With row_offsets [B + 1] a
+    position out of range flags its sequence, else the one word of seq_status."""
+    T, H, d, dev, ref = _norm_rows(norm, rope, x)
+    B = 0 if row_offsets is None else row_offsets.numel() - 1
+    if B < 0:
+        raise ValueError("row_offsets: B + 1 of them wanted")
+    _on_gpu(dev, T)
+    ld_x, ld_y = _rows(x, T, H, d, x.dtype, "x", dev), _rows(y, T, H, d, x.dtype, "y", dev)
+    tw._call("treewy_norm_rope", load_library().treewy_norm_rope, ref, None if rope is None else rope._ref, B, T,
+             _int32(row_offsets, B + 1, "row_offsets", dev), x.data_ptr(), ld_x, y.data_ptr(), ld_y, H, d, tw._DTYPES[x.dtype],
+             _int32(seq_status, B or 1, "seq_status", dev), _stream(stream, x))
+
+
+def norm_rope_workspace(x: torch.Tensor) -> torch.Tensor:
+    """A workspace for ``treewy_norm_rope_backward`` calls on rows like x [T, H, d] (one per call in flight)."""
+    T, H, d = x.shape
+    n = load_library().treewy_norm_rope_workspace(T, H, d, tw._DTYPES[x.dtype])
+    return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=x.device)
+
+
+def treewy_norm_rope_backward(norm: HeadNorm, rope: Rope | None, x: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
+                              dweight: torch.Tensor, workspace: torch.Tensor, row_status: torch.Tensor | None = None,
+                              stream=None) -> None:
+    """dx [T, H, d] and dweight [d] (float32) <- the gradients of treewy_norm_rope's input and weight, given that of its
+    output.  dx may be x or dy."""
+    T, H, d, dev, ref = _norm_rows(norm, rope, x)
+    _on_gpu(dev, 1)
+    ld_x, ld_dy, ld_dx = (_rows(r, T, H, d, x.dtype, what, dev) for r, what in ((x, "x"), (dy, "dy"), (dx, "dx")))
+    if dweight.dtype is not torch.float32 or dweight.numel() != d or not dweight.is_contiguous() or dweight.get_device() != dev:
+        raise ValueError(f"dweight: contiguous float32 [{d}] on the rows' device wanted")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous and on the rows' device wanted")
+    tw._call("treewy_norm_rope_backward", load_library().treewy_norm_rope_backward, ref, None if rope is None else rope._ref,
+             x.data_ptr(), ld_x, dy.data_ptr(), ld_dy, dx.data_ptr(), ld_dx, dweight.data_ptr(), T, H, d, tw._DTYPES[x.dtype],
+             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _int32(row_status, 1, "row_status", dev),
+             _stream(stream, x))
+
+
+def treewy_kv_append_norm(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_norm: HeadNorm | None,
+                          rope: Rope | None = None, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                          q_norm: HeadNorm | None = None, seq_status: torch.Tensor | None = None, stream=None) -> None:
+    """treewy_kv_append with the keys' (and queries') heads normalised ahead of the rotation."""
+    T, H_kv, d, dtype, dev = k.shape[0], cache.H_kv, cache.d_head, cache.dtype, cache._dev
+    if rope is not None and (rope.T != T or rope._dev != dev):
+        raise ValueError("rope: as many positions as rows, on the cache's device, wanted")
+    _on_gpu(dev, T)
+    ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
+    H_q = ld_q = ld_qo = 0
+    q_at = qo_at = None
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q_out: wanted with q")
+        H_q = q.shape[1]
+        ld_q, ld_qo = _rows(q, T, H_q, d, dtype, "q", dev), _rows(q_out, T, H_q, d, dtype, "q_out", dev)
+        q_at, qo_at = q.data_ptr(), q_out.data_ptr()
+    tw._call("treewy_kv_append_norm", load_library().treewy_kv_append_norm, cache._ref, None if rope is None else rope._ref,
+             _norm(q_norm, d, "q_norm", dev), _norm(k_norm, d, "k_norm", dev), cache.B, T,
+             _int32(row_offsets, cache.B + 1, "row_offsets", dev), k.data_ptr(), ld_k, v.data_ptr(), ld_v, H_q, q_at, ld_q, qo_at,
+             ld_qo, cache._dt, _int32(seq_status, cache.B, "seq_status", dev), _stream(stream, k))
+
+
+def attn_chunk_workspace(cache: KVCache, T: int, H_q: int, window: int = 0, sinks: int = 0) -> torch.Tensor:
+    """A workspace for ``treewy_attn_chunk`` calls of up to T rows with this window (one per call in flight)."""
+    n = load_library().treewy_attn_chunk_workspace(cache._ref, cache.B, T, H_q, window, sinks, cache._dt)
+    return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=cache.k.device)
+
+
+def treewy_attn_chunk(cache: KVCache, row_offsets: torch.Tensor, q: torch.Tensor, scale: float, O: torch.Tensor,
+                      workspace: torch.Tensor, window: int = 0, sinks: int = 0, seq_status: torch.Tensor | None = None, stream=None,
+                      generic: bool = False) -> None:
+    """O [T, H_q, d] <- attention of every new row (q: packed rows of the sequences at row_offsets [B + 1]; their keys and
+    values are in the cache behind context_len) over the cached tokens up to its own: all of them, or (window > 0) the last
+    `window` and the first `sinks`."""
+    lib = load_library()
+    if q.dim() != 3:
+        raise ValueError("q: [T, H_q, d] wanted")
+    (T, H_q, d), dtype, dev = q.shape, cache.dtype, cache._dev
+    if d != cache.d_head:
+        raise ValueError("q: the cache's d_head wanted")
+    _on_gpu(dev, T)
+    ld_q = _rows(q, T, H_q, d, dtype, "q", dev)
+    if _rows(O, T, H_q, d, dtype, "O", dev) != H_q * d and T > 0:
+        raise ValueError("O: contiguous rows wanted")
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous and on the cache's device wanted")
+    tw._call("treewy_attn_chunk_generic" if generic else "treewy_attn_chunk", lib.treewy_attn_chunk_generic if generic else lib.treewy_attn_chunk,
+             cache._ref, cache.B, T, _int32(row_offsets, cache.B + 1, "row_offsets", dev), q.data_ptr(), ld_q, H_q, scale, window, sinks,
+             cache._dt, O.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+             _int32(seq_status, cache.B, "seq_status", dev), _stream(stream, q))
+
+
+class PagePool:
+    """A page table kept on the GPU and the stack of pages that nobody holds (``treewy_page_pool_t``): page_table [B, max_pages]
+    (negative: no page), free_pages [n_pages], free_count [1], all int32.  The object refers to the tensors' memory."""
+
+    def __init__(self, page_table: torch.Tensor, page_size: int, n_pages: int, free_pages: torch.Tensor, free_count: torch.Tensor):
+        _require(page_table.dim() == 2 and page_table.is_contiguous() and page_table.dtype == torch.int32,
+                 "page_table: contiguous int32 [B, max_pages] wanted")
+        self._dev = page_table.get_device()
+        _int32(free_pages, n_pages, "free_pages", self._dev)
+        _int32(free_count, 1, "free_count", self._dev)
+        self.page_table, self.free_pages, self.free_count = page_table, free_pages, free_count
+        self.page_size, self.n_pages = page_size, n_pages
+        self.B, self.max_pages = (int(n) for n in page_table.shape)
+        self._struct = PagePoolStruct(page_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), n_pages, page_size, self.max_pages)
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, B: int, max_pages: int, page_size: int, n_pages: int, device) -> "PagePool":
+        """No sequence holds a page; page 0 is taken first."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((B, max_pages), -1, **i32), page_size, n_pages, torch.arange(n_pages - 1, -1, -1, **i32),
+                   torch.full((1,), n_pages, **i32))
+
+
+def treewy_pages_reserve(pool: PagePool, context_len: torch.Tensor, row_offsets: torch.Tensor, T: int,
+                         positions: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                         seq_status: torch.Tensor | None = None, stream=None) -> None:
+    """Pages for the rows at row_offsets [B + 1] (T in all) behind context_len [B]; positions [T] int32 receives each row's token
+    number and slots [T] int64 its place in the cache."""
+    B, dev = pool.B, pool._dev
+    _on_gpu(dev, B)
+    if slots is not None and (slots.dtype is not torch.int64 or slots.numel() < T or not slots.is_contiguous() or slots.get_device() != dev):
+        raise ValueError(f"slots: contiguous int64 [{T}] on the pool's device wanted")
+    tw._call("treewy_pages_reserve", load_library().treewy_pages_reserve, pool._ref, B, T, _int32(context_len, B, "context_len", dev),
+             _int32(row_offsets, B + 1, "row_offsets", dev), _int32(positions, T, "positions", dev),
+             None if slots is None else slots.data_ptr(), _int32(seq_status, B, "seq_status", dev), _stream(stream, pool.page_table))
+
+
+def treewy_pages_release(pool: PagePool, first: torch.Tensor, end: torch.Tensor, seq_status: torch.Tensor | None = None,
+                         stream=None) -> None:
+    """The pages whose tokens all lie in first[b] .. end[b] - 1 go back to the pool."""
+    B, dev = pool.B, pool._dev
+    _on_gpu(dev, B)
+    tw._call("treewy_pages_release", load_library().treewy_pages_release, pool._ref, B, _int32(first, B, "first", dev),
+             _int32(end, B, "end", dev), _int32(seq_status, B, "seq_status", dev), _stream(stream, pool.page_table))
 
 
 class AttentionLayer:

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "../../include/treewy_attn.h"
+#include "../../include/treewy_prompt.h"
 #include "treewy_common.cuh"
 
 namespace treewy {
@@ -33,6 +34,24 @@ struct RowsArgs {
     long long ld_q, ld_k, ld_v, ld_qo;
     int B, T, H_q, d;
     int32_t *status;  // per sequence, or one word for treewy_rope
+};
+
+// A norm of each head ahead of its rotation (weight NULL: none)
+struct NormView {
+    const void *weight;
+    int bf16, plus_one;
+    float eps;
+};
+struct NormRowsArgs {
+    RowsArgs rows;
+    NormView q, k;
+};
+struct NormBackwardArgs {
+    RowsArgs rows;  // q: x, q_out: dx, no cache
+    NormView norm;
+    const void *dy;
+    long long ld_dy;
+    float *dweight, *parts;
 };
 
 struct KvCommitArgs {
@@ -72,6 +91,55 @@ size_t attn_generic_workspace(const AttnArgs &a);
 bool attn_tc_applies(const AttnArgs &a, treewy_dtype_t io);
 cudaError_t launch_attn_tc(const AttnArgs &a, cudaStream_t stream);
 size_t attn_tc_workspace(const AttnArgs &a);
+
+
+// New rows over the cache (treewy_attn_chunk): row i of sequence b is its token context_len[b] + i
+struct ChunkArgs {
+    CacheView c;
+    const int32_t *row_offsets;
+    const void *q;
+    long long ld_q;
+    void *O;
+    float scale;
+    int window, sinks;      // window 0x7fffffff: all
+    int log_page;           // page_size = 1 << log_page (tensor-core kernel only)
+    int B, T, H_q, G;
+    float *ws;
+    int32_t *seq_status;
+    long long wait_cycles;  // as in AttnArgs
+    int skip_item;
+};
+
+struct PagesArgs {
+    int32_t *page_table, *free_pages, *free_count;
+    int n_pages, page_size, max_pages;
+    int B, T;
+    const int32_t *context_len, *row_offsets;  // reserve
+    const int32_t *first, *end;                // release
+    int32_t *positions;
+    int64_t *slots;
+    int32_t *seq_status;
+};
+
+cudaError_t launch_norm_rows(const NormRowsArgs &a, treewy_dtype_t io, cudaStream_t stream);
+size_t norm_backward_workspace(int d);
+cudaError_t launch_norm_backward(const NormBackwardArgs &a, treewy_dtype_t io, cudaStream_t stream);
+cudaError_t launch_chunk_generic(const ChunkArgs &a, treewy_dtype_t io, cudaStream_t stream);
+size_t chunk_generic_workspace(const ChunkArgs &a);
+cudaError_t launch_pages_reserve(const PagesArgs &a, cudaStream_t stream);
+cudaError_t launch_pages_release(const PagesArgs &a, cudaStream_t stream);
+
+// Status bits of sequence b of new rows, and its rows and length.
+__device__ __forceinline__ int check_rows(const int32_t *row_offsets, const int32_t *context_len, int b, int T, long long capacity,
+                                          int *lo, int *n, int *len)
+{
+    *lo = row_offsets[b];
+    *n = row_offsets[b + 1] - *lo;
+    *len = context_len[b];
+    if (bad_offsets(*lo, *n, T)) return TREEWY_SEQ_BAD_OFFSETS;
+    if (*len < 0 || (long long)*len + *n > capacity) return TREEWY_SEQ_BAD_LENGTH;
+    return 0;
+}
 
 // Status bits of sequence b, and its rows and length: every kernel of the attention calls decides
 // what to skip by this one function.  The cached part is read up to context_len, so it has to fit the table.

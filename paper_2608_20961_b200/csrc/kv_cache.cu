@@ -7,71 +7,13 @@
 // A thread takes one unit: the two 16-byte vectors that hold 8 (bf16) or 4 (fp32) pairs of one head.  A
 // warp takes a slice of one token's heads with the same pairs in every lane throughout, so a lane reads its
 // cosines and sines once and keeps them in registers over the heads.
-#include "attn_common.cuh"
+#include "rows_common.cuh"
 
 namespace treewy {
 namespace {
 
 constexpr int ROWS_WARPS = 4;
 constexpr int HEAD_UNROLL = 2;  // heads a lane has in flight
-
-template <typename T, int VE> struct Vec;
-template <> struct Vec<__nv_bfloat16, 8> {
-    uint4 x;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { x = __ldcs(reinterpret_cast<const uint4 *>(p)); }
-    __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = x; }
-    __device__ __forceinline__ void get(float (&f)[8]) const { widen8(x, f); }
-    __device__ __forceinline__ void set(const float (&f)[8])
-    {
-        x = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-    }
-};
-template <> struct Vec<float, 4> {
-    float4 x;
-    __device__ __forceinline__ void load(const float *p) { x = __ldcs(reinterpret_cast<const float4 *>(p)); }
-    __device__ __forceinline__ void store(float *p) const { *reinterpret_cast<float4 *>(p) = x; }
-    __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w; }
-    __device__ __forceinline__ void set(const float (&f)[4]) { x = make_float4(f[0], f[1], f[2], f[3]); }
-};
-template <typename T> struct Vec<T, 1> {
-    T x;
-    __device__ __forceinline__ void load(const T *p) { x = *p; }
-    __device__ __forceinline__ void store(T *p) const { *p = x; }
-    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(x); }
-    __device__ __forceinline__ void set(const float (&f)[1]) { x = from_f32<T>(f[0]); }
-};
-
-// The sequence that owns packed row t (largest b with row_offsets[b] <= t among non-decreasing offsets), found
-// by a whole warp: each round narrows the range 32-fold.  Any result is checked by the caller.
-__device__ __forceinline__ int find_sequence(const int32_t *offsets, int B, int t)
-{
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = B;
-    while (n > 1) {
-        const int step = (n + 31) / 32;
-        const int at = lo + lane * step;
-        const bool le = lane * step < n && offsets[at] <= t;
-        const unsigned m = __ballot_sync(0xffffffffu, le);
-        const int last = m ? 31 - __clz(m) : 0;
-        n = min(step, n - last * step);
-        lo += last * step;
-    }
-    return lo;
-}
-
-// Four (or VE) consecutive entries of a table row
-template <int VE> __device__ __forceinline__ void load_row(const float *p, float (&f)[VE])
-{
-    if constexpr (VE == 1) {
-        f[0] = *p;
-    } else {
-#pragma unroll
-        for (int i = 0; i < VE; i += 4) {
-            const float4 x = *reinterpret_cast<const float4 *>(p + i);
-            f[i] = x.x, f[i + 1] = x.y, f[i + 2] = x.z, f[i + 3] = x.w;
-        }
-    }
-}
 
 // VE: pairs of a unit.  Grid: one warp per (token, slice of heads).  A warp's first loads of x go out before anything
 // that has to be looked up for the token (positions, then the table's rows; the sequence, then its length, then its
@@ -126,96 +68,19 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 6) rows_kernel(const __grid_c
     while (run.h0 >= run.h1 && kind < 2) run = run_of(++kind);
     load(run, run.h0, ul);
 
-    // positions: lane i keeps the one of axis i
-    int pos = 0;
-    bool bad_pos = false;
-    if (turned > 0) {
-        if (lane < a.r.n_axes) {
-            pos = a.r.positions[(size_t)lane * a.T + t];
-            bad_pos = pos < 0 || pos >= a.r.max_positions;
-        }
-        if (a.r.pair_axis)
-            for (int p = lane; p < half; p += 32) bad_pos |= a.r.pair_axis[p] >= a.r.n_axes;
-        bad_pos = __any_sync(0xffffffffu, bad_pos);
-    }
+    int pos;
+    const bool bad_pos = token_position(a, t, turned, &pos);
     // where the row goes
-    T *kd = nullptr, *vd = nullptr;
-    int bad = bad_pos ? TREEWY_SEQ_BAD_POSITION : 0, b = 0;
-    if (a.c.H_kv > 0) {
-        b = find_sequence(a.row_offsets, a.B, t);
-        const int lo = a.row_offsets[b], hi = a.row_offsets[b + 1];
-        // Ranges outside the packed rows: no row need fall into one, so the last row's warp looks at all of them.
-        if (t == a.T - 1 && a.status) {
-#pragma unroll 4
-            for (int i = lane; i < a.B; i += 32)
-                if (bad_offsets(a.row_offsets[i], a.row_offsets[i + 1] - a.row_offsets[i], a.T)) atomicOr(&a.status[i], TREEWY_SEQ_BAD_OFFSETS);
-        }
-        if (t < lo || t >= hi || bad_offsets(lo, hi - lo, a.T)) return;  // a row of no sequence
-        const int len = a.c.context_len[b];
-        if (len < 0 || (long long)len + (hi - lo) > (long long)a.c.max_pages * a.c.page_size) {
-            bad = TREEWY_SEQ_BAD_LENGTH;
-        } else {
-            const int slot = len + (t - lo), pi = slot / a.c.page_size;
-            const int page = a.c.page_table[(size_t)b * a.c.max_pages + pi];
-            if (page < 0 || page >= a.c.n_pages) {
-                bad |= TREEWY_SEQ_BAD_PAGE;
-            } else {
-                const long long at = page * a.c.stride_page + (slot - pi * a.c.page_size) * a.c.stride_slot;
-                kd = static_cast<T *>(a.c.k) + at, vd = static_cast<T *>(a.c.v) + at;
-            }
-        }
-    }
-    if (bad) {
-        if (a.c.H_kv == 0 && a.row_offsets) {         // rotation alone: the sequence is wanted for its flag only
-            b = find_sequence(a.row_offsets, a.B, t);
-            if (t < a.row_offsets[b] || t >= a.row_offsets[b + 1]) return;
-        }
-        if (lane == 0 && a.status) atomicOr(&a.status[b], bad);
-        return;
-    }
+    long long at = 0;
+    if (!place_row(a, t, bad_pos, &at)) return;
+    T *const kd = static_cast<T *>(a.c.k) + at, *const vd = static_cast<T *>(a.c.v) + at;
 
     bool first = true;
     for (int u0 = 0; u0 < units; u0 += 32) {
         const int u = u0 + ul;
         const bool turns = on && u < turned;
         float cs[VE], sn[VE];
-        if (u0 < turned) {
-            int axis[VE], p0[VE];
-            bool one = true;                          // all pairs of the unit at one position: whole vectors of the table
-#pragma unroll
-            for (int i = 0; i < VE; ++i) axis[i] = 0;
-            if (turns && a.r.pair_axis) {
-                if constexpr (VE == 8) {              // (rot is a multiple of 2 VE here: the axes of a unit are aligned)
-                    const uint2 w = *reinterpret_cast<const uint2 *>(a.r.pair_axis + u * VE);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) axis[i] = ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 255;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) axis[i] = a.r.pair_axis[u * VE + i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                p0[i] = __shfl_sync(0xffffffffu, pos, axis[i]);
-                one &= axis[i] == axis[0];
-            }
-            if (turns) {
-                if (one) {
-                    const float *row = a.r.cos_sin + (size_t)p0[0] * a.r.rot + u * VE;
-                    load_row<VE>(row, cs);
-                    load_row<VE>(row + half, sn);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        const float *row = a.r.cos_sin + (size_t)p0[i] * a.r.rot + u * VE + i;
-                        cs[i] = row[0], sn[i] = row[half];
-                    }
-                }
-                if (a.r.inverse)
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) sn[i] = -sn[i];
-            }
-        }
+        if (u0 < turned) unit_angles<VE>(a.r, u, turns, pos, cs, sn);
         for (int kd_ = kind; kd_ < 3; ++kd_) {
             run = run_of(kd_);
             const bool turn = turns && run.turn, split = turn && !a.r.interleaved;
@@ -232,26 +97,7 @@ __global__ void __launch_bounds__(ROWS_WARPS * 32, 6) rows_kernel(const __grid_c
                     if (turn) {
                         float f[VE], g[VE], rf[VE], rg[VE];
                         x[i].get(f), y[i].get(g);
-                        if (split) {
-#pragma unroll
-                            for (int e = 0; e < VE; ++e) {
-                                rf[e] = f[e] * cs[e] - g[e] * sn[e];
-                                rg[e] = g[e] * cs[e] + f[e] * sn[e];
-                            }
-                        } else {  // pairs side by side: the 2 VE elements of x, y hold pairs 0 .. VE-1 in order
-                            if constexpr (VE == 1) {
-                                rf[0] = f[0] * cs[0] - g[0] * sn[0];
-                                rg[0] = g[0] * cs[0] + f[0] * sn[0];
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < VE; e += 2) {
-                                    rf[e] = f[e] * cs[e / 2] - f[e + 1] * sn[e / 2];
-                                    rf[e + 1] = f[e + 1] * cs[e / 2] + f[e] * sn[e / 2];
-                                    rg[e] = g[e] * cs[(VE + e) / 2] - g[e + 1] * sn[(VE + e) / 2];
-                                    rg[e + 1] = g[e + 1] * cs[(VE + e) / 2] + g[e] * sn[(VE + e) / 2];
-                                }
-                            }
-                        }
+                        turn_unit<VE>(f, g, cs, sn, split, rf, rg);
                         x[i].set(rf), y[i].set(rg);
                     }
                     x[i].store(d0 + h * step), y[i].store(d1 + h * step);
