@@ -1,0 +1,953 @@
+// treewy_attn_chunk, bf16: new rows over a paged cache on the tensor cores.
+//
+// Rows.  A row tile is 128 rows of one (sequence, key/value head): the G query heads that read this head, of 128 / G tokens one
+// after the other.  A CTA works on two of them at a time (heads of 256: one), each a stream with its own S and O in
+// tensor memory and its own warpgroup for the softmax, over the same tiles of keys and values: while one stream's softmax
+// runs, the tensor cores have the other's products.  An item with one row tile (decoding, short pieces) gives the two
+// streams alternate key tiles instead, and joins their outputs at its end.
+// Keys.  Tiles of 128 (heads of 256: 64) at multiples of 128: those of the sinks, then from the first row's window to the last
+// row.  Tiles that some row does not see whole are masked, those that no row of a stream sees are left out for it.
+// One tile of a stream:  S = Q K^T, the softmax step in registers (a row to a thread), P = weights as bf16 over S's
+// own columns, O += P V (V read with its rows as the K index).  The products of a stream are issued in the order P V, Q K^T of
+// the next tile, so that S's columns are free and O is at rest whenever S is full: the running maximum may move O then, which
+// it does only when a row's new maximum exceeds it by more than 8 (in log2; weights are at most 2^8 until then).
+//
+// Work.  (sequence, head, item) in one line, an item's length being its start's cost and its keys, cut into equal parts,
+// one for each CTA: no CTA waits for a longer neighbour, whatever the lengths and windows.  A cut item leaves unnormalised
+// outputs with their m and l in the workspace; a second kernel joins them in the order of the keys.
+#include <type_traits>
+
+#include "attn_common.cuh"
+#include "ptx_sm100.cuh"
+#include "tma_host.cuh"
+
+namespace treewy {
+namespace {
+
+constexpr int MT = 128;                // rows of a tile
+constexpr int MAX_CTAS = 160;
+constexpr int ITEMS = 4;               // ring of work items between the producer and the other roles
+constexpr int START = 256;             // cost of an item's start, in keys
+constexpr int MIN_UNITS = 256;         // least units of a part; at least a tile's keys, so that a part inside an item holds the start of one
+constexpr float LAZY = 8.f;
+constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;  // l of a row whose part is not there
+
+template <int D> struct Cfg {
+    static constexpr int NC = D / 64;                    // 64-column chunks of a row
+    static constexpr int STREAMS = D == 256 ? 1 : 2;     // what 512 columns of tensor memory leave
+    static constexpr int KT = D == 256 ? 64 : 128;       // keys of a tile
+    static constexpr int STAGE = NC * KT * 128;          // bytes of a tile
+    static constexpr int NK = D == 64 ? 5 : 3, NV = D == 64 ? 5 : 2;
+    static constexpr int Q_TILE = NC * MT * 128;
+    static constexpr int TILES = STREAMS * Q_TILE + (NK + NV) * STAGE;  // bytes
+    static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 1, PRODUCER_V = MMA + 2;
+    static constexpr int THREADS = (SOFT_WARPS + 3) * 32;
+    static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer s at 256 + s * KT
+    static constexpr int CAP = STREAMS * MT;             // rows of an item at most
+};
+
+// Where the copies put a tile, and in how many pieces.  A box is rows of one page (all of it, or KT of it) and holds the
+// chunks of its rows one after the other.  V comes so: rows are its K index, and any 16 of one page make an MMA step.  K
+// needs its 8-row groups equally far apart: whole boxes one chunk at a time, or all chunks of 8 rows, whichever makes
+// fewer copies.
+template <int D, int BOX> struct Boxes {
+    static constexpr int NC = D / 64, KT = Cfg<D>::KT, P = KT / BOX;  // boxes of a tile
+    static constexpr bool K_BY_CHUNK = P * NC <= KT / 8;
+    static constexpr int K_CHUNK = K_BY_CHUNK ? KT * 128 : 1024, K_GROUP = K_BY_CHUNK ? 1024 : NC * 1024;
+};
+struct Layout {                  // the same for the roles that read the tiles
+    int k_chunk, k_group;        // bytes between K's chunks, and between its 8-row groups
+    int v_rows, log_v_rows;      // rows of a V box
+};
+
+struct Item {
+    int b, h, lo, len;          // sequence, key/value head, its first packed row, its context
+    int t0, tokens;             // first token of the item among the sequence's rows, tokens
+    int pair;                   // two row tiles (else one)
+    int j0, tiles, kts;         // first key tile here, tiles here (0: the end), tiles of the whole item
+    int sink_tiles, low_tile;   // tile j is tile j of the cache for j < sink_tiles, else low_tile + j - sink_tiles
+    int slot;                   // the block of a cut item, else -1
+};
+__device__ __forceinline__ int cache_tile(const Item &it, int j) { return j < it.sink_tiles ? j : it.low_tile + (j - it.sink_tiles); }
+
+struct Seq {
+    int lo, n, len, items;
+    unsigned long long per;     // units under one head
+};
+// A CTA's part of the line of work
+struct Part {
+    long long u0, u1, W;        // its units, and all of the line
+    int parts, group;
+};
+struct Walk {                   // a CTA's way along its part
+    int b;
+    long long off, u;           // in the units of sequence b, on the line
+    Seq s;
+};
+
+struct Shared {
+    uint64_t k_full[6], k_free[6], v_full[6], v_free[6];
+    uint64_t s_full[2], p_full[2], pv_done[2], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4];
+    Item items[ITEMS];
+    float2 ml[MT];              // of the second stream's rows, for the first
+    unsigned bad_item[8];       // ordinal + 1 of an item that met a page out of range
+    unsigned nonfinite[8];      // ordinal + 1 of an item with NaN or infinity among the values of its masked tiles
+    long long scan[12], first_off;
+    Seq first_seq;              // of sequence first_b
+    Part part;
+    int first_b;
+    unsigned unfinished;        // first of this CTA's items whose output is not all stored, once a wait has run out; else ~0
+    unsigned copied[2];         // tiles whose copies of K and of V were issued
+    unsigned q_copied;          // items whose queries' copies were
+    uint32_t tmem;
+};
+
+// The workspace.  A block holds unnormalised outputs of an item's rows, column groups of 4 first: element (row, c) at ((c / 4) *
+// cap + row) * 4 + c % 4, so that the rows of a warp are neighbours when its threads write a column group each of their own
+// row; (m, l) of the rows beside it.  A part cuts two items at most, the one its start falls into (block 2 g) and one more.
+struct Ws {
+    int *desc;                  // [MAX_CTAS][8]: the item that a CTA's part cuts at its end
+    float *ml, *o;              // [2 * CTAs] blocks
+    int cap;                    // rows of a block
+};
+
+template <int D> __device__ __forceinline__ int tile_tokens(const ChunkArgs &a) { return MT / a.G; }  // of a row tile
+
+// Units of a sequence's items before item i (under one head): of each its start and its keys, which are its tokens and what
+// the first of them sees beside itself, min(p, window + sinks - 1).
+template <int D> __device__ __forceinline__ long long units_before(const ChunkArgs &a, int len, int n, long long i)
+{
+    const long long per = (long long)Cfg<D>::STREAMS * tile_tokens<D>(a), most = (long long)a.window + a.sinks - 1;
+    // items whose first token is behind fewer than `most`
+    long long m = most <= len ? 0 : (most - len + per - 1) / per;
+    m = m < i ? m : i;
+    const long long tokens = i * per < n ? i * per : n;
+    return i * START + tokens + m * len + per * (m * (m - 1) / 2) + (i - m) * most;
+}
+template <int D> static __device__ __noinline__ Seq load_seq(const ChunkArgs &a, int b, int *status)
+{
+    Seq s;
+    *status = check_rows(a.row_offsets, a.c.context_len, b, a.T, (long long)a.c.max_pages * a.c.page_size, &s.lo, &s.n, &s.len);
+    const int per = Cfg<D>::STREAMS * tile_tokens<D>(a);
+    s.items = *status ? 0 : (s.n + per - 1) / per;
+    s.per = s.items ? units_before<D>(a, s.len, s.n, s.items) : 0;
+    return s;
+}
+// parts: CTAs that get work.  Part g has units g W / parts .. (g + 1) W / parts - 1.  Of an item of START + k units tile t of kts
+// begins at START + t k / kts: it belongs to the part that this unit is in.
+__device__ __forceinline__ long long part_begin(long long g, long long W, int parts) { return g * W / parts; }
+__device__ __forceinline__ int part_of(long long unit, long long W, int parts) { return (int)(((unit + 1) * parts - 1) / W); }
+__device__ __forceinline__ int tiles_before(long long o, long long k, int kts)
+{
+    return o <= START ? 0 : (int)min((long long)kts, ((o - START) * kts + k - 1) / k);
+}
+
+// The next item that has tiles here; 0 tiles: the end.  The part that has a cut item's first tile leaves word for the join.
+template <int D> static __device__ __noinline__ void next_item(const ChunkArgs &a, const Ws &ws, const Part &p, Walk &w, Item &it, bool describe)
+{
+    constexpr int KT = Cfg<D>::KT;
+    int st;
+    it.tiles = 0;
+    while (w.u < p.u1 && it.tiles == 0) {
+        const Seq &s = w.s;
+        if ((unsigned long long)w.off >= s.per * a.c.H_kv) {  // (a sequence without work has no units)
+            w.off = 0, ++w.b;
+            w.s = load_seq<D>(a, w.b, &st);
+            continue;
+        }
+        const int h = (int)(w.off / (long long)s.per);
+        const long long in_head = w.off - h * (long long)s.per;
+        int i = 0, hi = s.items;           // the item that unit in_head is in
+        while (hi - i > 1) {
+            const int mid = (i + hi) >> 1;
+            if (units_before<D>(a, s.len, s.n, mid) <= in_head) i = mid;
+            else hi = mid;
+        }
+        const long long at = units_before<D>(a, s.len, s.n, i), cost = units_before<D>(a, s.len, s.n, i + 1) - at, o = in_head - at;
+        const int tt = tile_tokens<D>(a), per = Cfg<D>::STREAMS * tt;
+        it.b = w.b, it.h = h, it.lo = s.lo, it.len = s.len;
+        it.t0 = i * per, it.tokens = min(per, s.n - it.t0);
+        it.pair = it.tokens > tt;
+        const int p0 = s.len + it.t0, p1 = p0 + it.tokens - 1;
+        const int low = a.window > p0 ? 0 : p0 - a.window + 1;
+        it.low_tile = low / KT;
+        it.sink_tiles = min((int)(((long long)min(a.sinks, low) + KT - 1) / KT), it.low_tile);
+        it.kts = it.sink_tiles + p1 / KT - it.low_tile + 1;
+        const long long span = min(cost - o, p.u1 - w.u), begin = w.u - o;
+        it.j0 = tiles_before(o, cost - START, it.kts);
+        const int j1 = tiles_before(o + span, cost - START, it.kts);
+        it.tiles = j1 - it.j0;
+        const bool cut = it.j0 > 0 || j1 < it.kts;
+        it.slot = !cut ? -1 : begin <= p.u0 ? 2 * p.group : 2 * p.group + 1;
+        if (describe && cut && it.j0 == 0 && it.tiles > 0) {
+            int *d = ws.desc + 8 * p.group;
+            const long long last = begin + START + (long long)(it.kts - 1) * (cost - START) / it.kts;
+            d[1] = it.slot, d[2] = it.lo + it.t0, d[3] = h, d[4] = it.tokens, d[5] = it.b, d[6] = p.group;
+            d[0] = part_of(last, p.W, p.parts) - p.group + 1;
+        }
+        w.off += span, w.u += span;
+    }
+}
+
+// After a wait that ran out: from item `unfinished` on, this CTA's blocks say that they are not there and the sequences are
+// flagged.
+template <int D> static __device__ __noinline__ void mark_unfinished(const ChunkArgs &a, const Ws &ws, const Part &p, Walk w, unsigned unfinished)
+{
+    Item it;
+    for (unsigned ord = 0;; ++ord) {
+        next_item<D>(a, ws, p, w, it, false);
+        if (it.tiles == 0) return;
+        if (ord < unfinished) continue;
+        if (it.slot >= 0)
+            for (int r = threadIdx.x; r < ws.cap; r += Cfg<D>::THREADS)
+                reinterpret_cast<float2 *>(ws.ml)[(long long)it.slot * ws.cap + r] = make_float2(0.f, NOT_DONE);
+        if (threadIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_TIMEOUT);
+    }
+}
+
+// What one stream sees of an item: positions of its first and last row.
+struct View {
+    int p0, p1;
+};
+__device__ __forceinline__ View view_of(const Item &it, int tt, int s)
+{
+    const int first = it.pair ? s * tt : 0, last = it.pair && s == 0 ? tt : it.tokens;
+    return {it.len + it.t0 + first, it.len + it.t0 + last - 1};
+}
+// Whether some row of the view sees some token of tokens x0 .. x0 + n - 1
+__device__ __forceinline__ bool sees_some(const ChunkArgs &a, const View &v, int x0, int n)
+{
+    return x0 <= v.p1 && ((long long)x0 + n - 1 > (long long)v.p0 - a.window || x0 < a.sinks);
+}
+// Whether every row sees all of them
+__device__ __forceinline__ bool sees_all(const ChunkArgs &a, const View &v, int x0, int n)
+{
+    return x0 + n - 1 <= v.p0 && ((long long)x0 > (long long)v.p1 - a.window || x0 + n <= a.sinks);
+}
+__device__ __forceinline__ bool sees(const ChunkArgs &a, int p, int x) { return x <= p && (p - x < a.window || x < a.sinks); }
+
+__device__ __forceinline__ uint32_t low32(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+__device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// a wait with one outcome for the whole warp: what follows needs all of its lanes
+__device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)); }
+
+template <int D>
+__global__ void __launch_bounds__(Cfg<D>::THREADS, 1)
+chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws ws, Layout lay, int smem_bytes, const __grid_constant__ CUtensorMap map_q,
+                const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
+{
+    using C = Cfg<D>;
+    constexpr int KT = C::KT;
+    // barriers and the like first, tiles behind them: the bytes that aligning the tiles takes are used so
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem_raw);
+    unsigned char *q_tiles = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw + sizeof(Shared)) + 1023) & ~uintptr_t(1023));
+    unsigned char *k_ring = q_tiles + C::STREAMS * C::Q_TILE, *v_ring = k_ring + C::NK * C::STAGE;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        ptx::wait_deadline_init(a.wait_cycles);
+        for (int i = 0; i < 6; ++i)
+            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], 1);
+        for (int i = 0; i < 2; ++i)
+            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1), ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
+        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
+        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], C::SOFT_WARPS + 2);
+        ptx::fence_barrier_init();
+        sh.unfinished = ~0u, sh.first_b = -1;
+        sh.copied[0] = sh.copied[1] = sh.q_copied = 0;
+        ptx::prefetch_tmap(&map_q), ptx::prefetch_tmap(&map_k), ptx::prefetch_tmap(&map_v);
+    }
+    if (tid < 8) sh.bad_item[tid] = 0, sh.nonfinite[tid] = 0;
+    // (the tiles' end has been allowed for; were the base of shared memory aligned otherwise, nothing may run)
+    const bool fits = q_tiles + C::TILES <= smem_raw + smem_bytes;
+    if (warp == C::MMA) {
+        ptx::tmem_alloc(&sh.tmem, 512);
+        ptx::tmem_relinquish();
+    }
+    grid_dependency_wait();
+    grid_dependency_trigger();
+
+    // ---- the line of work and this CTA's part of it
+    int st;
+    const int chunk = (a.B + C::THREADS - 1) / C::THREADS, b_begin = min(a.B, tid * chunk), b_end = min(a.B, b_begin + chunk);
+    long long sum = 0;
+    Seq only;                    // a thread's one sequence is not read again
+#pragma unroll 1
+    for (int b = b_begin; b < b_end; ++b) {
+        only = load_seq<D>(a, b, &st);
+        sum += (long long)only.per * a.c.H_kv;
+        if (!fits && only.items) st |= TREEWY_SEQ_TIMEOUT;
+        if (st && blockIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[b], st);
+    }
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) sh.scan[warp] = incl;
+    if (tid == 0) ws.desc[8 * blockIdx.x] = 0;
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    long long before = 0, W = 0;
+#pragma unroll
+    for (int i = 0; i < C::THREADS / 32; ++i) {
+        if (i < warp) before += sh.scan[i];
+        W += sh.scan[i];
+    }
+    before += incl - sum;
+    if (!fits) W = 0;
+    const int group = blockIdx.x, parts = (int)max(1ll, min((long long)gridDim.x, W / MIN_UNITS));
+    const long long u0 = group < parts && W > 0 ? part_begin(group, W, parts) : 0;
+    const long long u1 = group < parts && W > 0 ? part_begin(group + 1, W, parts) : 0;
+#pragma unroll 1
+    for (int b = b_begin; b < b_end; ++b) {
+        if (chunk > 1) only = load_seq<D>(a, b, &st);
+        const long long units = (long long)only.per * a.c.H_kv;
+        if (u1 > u0 && u0 >= before && u0 < before + units) sh.first_b = b, sh.first_off = u0 - before, sh.first_seq = only;
+        before += units;
+    }
+    if (tid == 0) sh.part = {u0, u1, W, parts, group};
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+    const int tt = tile_tokens<D>(a);
+
+    if (warp == C::PRODUCER_K || warp == C::PRODUCER_V) {
+        // ---------------------------------------------------------------- work items and TMA copies: one thread each
+        if (ptx::elect_one()) {
+            const int ps = 1 << a.log_page;
+            unsigned filled = 0;    // tiles whose copies were issued
+            // (returns early when a wait runs out)
+            auto run = [&](auto box_, auto is_v_) {
+                constexpr int BOX = decltype(box_)::value;
+                constexpr bool IS_V = decltype(is_v_)::value;
+                using B = Boxes<D, BOX>;
+                const CUtensorMap *map = IS_V ? &map_v : &map_k;
+                constexpr int NS = IS_V ? C::NV : C::NK;
+                uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *frees = IS_V ? sh.v_free : sh.k_free;
+                unsigned char *ring = IS_V ? v_ring : k_ring;
+                Walk walk{sh.first_b, sh.first_off, u0, sh.first_seq};
+                const Part part{u0, u1, W, parts, group};
+                for (unsigned ord = 0;; ++ord) {
+                    const unsigned r = ord % ITEMS;
+                    Item it;
+                    if constexpr (!IS_V) {
+                        next_item<D>(a, ws, part, walk, it, true);
+                        if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return;
+                        sh.items[r] = it;
+                        ptx::mbar_arrive(&sh.item_full[r]);
+                    } else {
+                        if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return;
+                        it = sh.items[r];
+                        if (it.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
+                    }
+                    if (it.tiles == 0) return;
+                    if (it.b * a.c.H_kv + it.h == a.skip_item) return;  // (test hook)
+                    if constexpr (!IS_V) {  // the queries of the item
+                        if (ord > 0 && !ptx::mbar_wait(&sh.q_free, (ord - 1) & 1)) return;
+                        const int streams = C::STREAMS == 2 && it.pair ? 2 : 1;
+                        sh.q_copied = ord + 1;
+                        ptx::mbar_arrive_expect_tx(&sh.q_full, (uint32_t)(streams * C::NC * tt * a.G * 128));
+                        for (int s = 0; s < streams; ++s)
+#pragma unroll
+                            for (int c = 0; c < C::NC; ++c)
+                                ptx::tma_load_5d(q_tiles + s * C::Q_TILE + c * MT * 128, &map_q, 0, 0, it.lo + it.t0 + s * tt, c, it.h, &sh.q_full);
+                    }
+                    const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
+                    const View all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
+                    bool bad = false;
+                    // pages of the next tile, looked up one tile ahead
+                    constexpr int UNSEEN = -1;  // (a negative entry becomes a large one)
+                    int pages[B::P], next[B::P];
+                    auto look = [&](int j, int (&to)[B::P]) {
+                        const int x0 = cache_tile(it, j) * KT;
+#pragma unroll
+                        for (int i = 0; i < B::P; ++i)
+                            to[i] = j < it.j0 + it.tiles && sees_some(a, all, x0 + i * BOX, BOX) ? table[(x0 + i * BOX) >> a.log_page] & 0x7fffffff : UNSEEN;
+                    };
+                    look(it.j0, next);
+                    for (int j = it.j0; j < it.j0 + it.tiles; ++j) {
+                        const unsigned sidx = filled % NS;
+                        const int x0 = cache_tile(it, j) * KT, slot0 = x0 & (ps - 1);
+                        int boxes = 0;
+#pragma unroll
+                        for (int i = 0; i < B::P; ++i) {
+                            pages[i] = next[i];
+                            if (pages[i] != UNSEEN) {
+                                ++boxes;
+                                if (pages[i] >= a.c.n_pages) bad = true, pages[i] = a.c.n_pages;  // (one past the pool reads as zeros)
+                            }
+                        }
+                        look(j + 1, next);
+                        if (bad && !IS_V) {
+                            sh.bad_item[ord % 8] = ord + 1;
+                            if (a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
+                        }
+                        if (filled >= NS && !ptx::mbar_wait(&frees[sidx], (filled / NS - 1) & 1)) return;
+                        ++filled;
+                        unsigned char *dst = ring + sidx * C::STAGE;
+                        uint64_t *full = &fulls[sidx];
+                        ptx::mbar_arrive_expect_tx(full, (uint32_t)boxes * (BOX * C::NC * 128));
+#pragma unroll
+                        for (int i = 0; i < B::P; ++i) {
+                            if (pages[i] == UNSEEN) continue;  // (no row sees it: left as it is, never used)
+                            const int slot = BOX < KT ? (x0 + i * BOX) & (ps - 1) : slot0;
+                            if constexpr (IS_V) {
+                                ptx::tma_load_5d(dst + i * (BOX * C::NC * 128), map, 0, slot, 0, it.h, pages[i], full);
+                            } else if constexpr (B::K_BY_CHUNK) {
+#pragma unroll
+                                for (int c = 0; c < C::NC; ++c)
+                                    ptx::tma_load_5d(dst + i * (BOX * 128) + c * B::K_CHUNK, map, 0, slot, c, it.h, pages[i], full);
+                            } else {
+#pragma unroll
+                                for (int g = 0; g < BOX / 8; ++g)
+                                    ptx::tma_load_5d(dst + (i * (BOX / 8) + g) * B::K_GROUP, map, 0, slot + 8 * g, 0, it.h, pages[i], full);
+                            }
+                        }
+                    }
+                }
+            };
+            auto run_box = [&](auto box_) { return warp == C::PRODUCER_V ? run(box_, std::true_type{}) : run(box_, std::false_type{}); };
+            if (KT == 128 && lay.v_rows == 128) run_box(std::integral_constant<int, KT>{});
+            else if (lay.v_rows == 64) run_box(std::integral_constant<int, 64>{});
+            else if (lay.v_rows == 32) run_box(std::integral_constant<int, 32>{});
+            else if (lay.v_rows == 8) run_box(std::integral_constant<int, 8>{});
+            else run_box(std::integral_constant<int, 16>{});
+            sh.copied[warp == C::PRODUCER_V] = filled;
+        }
+        __syncwarp();
+    } else if (warp == C::MMA) {
+        // ---------------------------------------------------------------- MMAs: one thread
+        if (ptx::elect_one()) {
+            constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
+            // Descriptors: stages, streams and steps only add to the address, 16 bytes a unit in the low bits
+            const uint64_t qd = ptx::umma_desc_k_sw128(ptx::smem_u32(q_tiles)), kd = ptx::umma_desc_k_sw128(ptx::smem_u32(k_ring), lay.k_group);
+            const uint64_t q_hi = qd & ~0xffffffffull, k_hi = kd & ~0xffffffffull;
+            const uint32_t q_lo = (uint32_t)qd, k_lo = (uint32_t)kd, k_chunk = lay.k_chunk / 16;
+            uint64_t v_hi = 0;
+            uint32_t v_lo[KT / 16];
+#pragma unroll
+            for (int s = 0; s < KT / 16; ++s) {  // a step of V is 16 rows
+                const uint32_t off = ((16 * s) >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) + ((16 * s) & (lay.v_rows - 1)) * 128;
+                const uint64_t vd = ptx::umma_desc_mn_sw128(ptx::smem_u32(v_ring) + off, lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
+                v_hi = vd & ~0xffffffffull, v_lo[s] = (uint32_t)vd;
+            }
+            unsigned g0 = 0;              // tiles of the items before
+            unsigned made[2] = {0, 0}, used[2] = {0, 0};  // S buffers filled, P buffers consumed
+            // scores of tile g into buffer s; q: which row tile
+            auto scores = [&](unsigned g, int s, int q) -> bool {
+                if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
+                ptx::tc_fence_after_sync();
+                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16), ql = q_lo + q * (C::Q_TILE / 16);
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+                    ptx::umma_bf16(tmem + C::TM_S + s * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2),
+                                   k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk, c > 0);
+                ptx::umma_commit(&sh.s_full[s]);
+                ++made[s];
+                return true;
+            };
+            // output of tile g from buffer s onto O of stream os
+            auto product = [&](unsigned g, int s, int os, bool onto) -> bool {
+                if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
+                if (!ptx::mbar_wait(&sh.p_full[s], used[s] & 1)) return false;
+                ++used[s];
+                ptx::tc_fence_after_sync();
+#pragma unroll
+                for (int c = 0; c < KT / 16; ++c)
+                    ptx::umma_bf16_ts(tmem + os * D, tmem + C::TM_S + s * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
+                return true;
+            };
+            auto run = [&]() -> bool {
+                for (unsigned ord = 0;; ++ord) {
+                    const unsigned r = ord % ITEMS;
+                    if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return false;
+                    const Item it = sh.items[r];
+                    if (it.tiles == 0) return true;
+                    ptx::mbar_arrive(&sh.item_empty[r]);
+                    if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
+                    const int n = it.tiles;
+                    if (C::STREAMS == 2 && it.pair) {
+                        // which tiles (from j0 on) each stream takes part in
+                        View v[2] = {view_of(it, tt, 0), view_of(it, tt, 1)};
+                        auto on = [&](int j, int s) { return sees_some(a, v[s], cache_tile(it, it.j0 + j) * KT, KT); };
+                        bool onto[2] = {false, false};
+                        for (int s = 0; s < 2; ++s)
+                            if (on(0, s) && !scores(g0, s, s)) return false;
+                        ptx::umma_commit(&sh.k_free[g0 % C::NK]);
+                        if (n == 1) ptx::umma_commit(&sh.q_free);
+                        for (int j = 0; j < n; ++j) {
+                            const unsigned g = g0 + j;
+                            for (int s = 0; s < 2; ++s) {
+                                if (on(j, s)) {
+                                    if (!onto[s] && ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
+                                    if (!product(g, s, s, onto[s])) return false;
+                                    onto[s] = true;
+                                }
+                                if (s == 1) ptx::umma_commit(&sh.v_free[g % C::NV]);
+                                if (j + 1 < n && on(j + 1, s) && !scores(g + 1, s, s)) return false;
+                                if (j + 1 == n) ptx::umma_commit(&sh.pv_done[s]);
+                            }
+                            if (j + 1 < n) ptx::umma_commit(&sh.k_free[(g + 1) % C::NK]);
+                            if (j + 2 == n) ptx::umma_commit(&sh.q_free);
+                        }
+                        // (a stream without a tile here has not waited yet)
+                        for (int s = 0; s < 2; ++s)
+                            if (!onto[s] && ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
+                    } else {
+                        // tiles alternate between the S buffers; with two streams each has its own O
+                        for (int j = 0; j < 2 && j < n; ++j) {
+                            if (!scores(g0 + j, j, 0)) return false;
+                            ptx::umma_commit(&sh.k_free[(g0 + j) % C::NK]);
+                        }
+                        if (n <= 2) ptx::umma_commit(&sh.q_free);
+                        for (int s = 0; s < C::STREAMS; ++s)
+                            if (ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
+                        for (int j = 0; j < n; ++j) {
+                            const unsigned g = g0 + j;
+                            if (!product(g, j & 1, C::STREAMS == 2 ? j & 1 : 0, C::STREAMS == 2 ? j >= 2 : j >= 1)) return false;
+                            ptx::umma_commit(&sh.v_free[g % C::NV]);
+                            if (C::STREAMS == 1) ptx::umma_commit(&sh.pv_done[g & 1]);
+                            if (j + 2 < n) {
+                                if (!scores(g + 2, j & 1, 0)) return false;
+                                ptx::umma_commit(&sh.k_free[(g + 2) % C::NK]);
+                                if (j + 3 == n) ptx::umma_commit(&sh.q_free);
+                            }
+                        }
+                        if (C::STREAMS == 2) ptx::umma_commit(&sh.pv_done[0]), ptx::umma_commit(&sh.pv_done[1]);
+                    }
+                    g0 += n;
+                }
+            };
+            if (!run()) {  // MMAs in flight have to end before the CTA may leave: a commit behind all of them, on a barrier of its own
+                uint64_t *end = &sh.k_full[5];
+                ptx::umma_commit(end);
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(end, 0); ++t) __nanosleep(20);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- softmax, epilogue
+        const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
+        const float sl2 = a.scale * 1.4426950408889634f;
+        unsigned seen_s[2] = {0, 0};  // S buffers taken
+        unsigned g0 = 0, ord = 0, singles = 0;
+        auto run = [&]() -> bool {
+            for (;; ++ord) {
+                if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
+                const Item &it = sh.items[ord % ITEMS];
+                const int n = it.tiles;
+                if (n == 0) return true;
+                const bool pair = C::STREAMS == 2 && it.pair;
+                const View v = view_of(it, tt, pair ? wg : 0), all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
+                const int rows = (v.p1 - v.p0 + 1) * a.G;
+                const bool warp_on = w4 * 32 < rows, on = row < rows;
+                const int tok = row / a.G, p = v.p0 + (on ? tok : 0);  // this row's position
+                float m = -INFINITY, l = 0.f;
+                int taken = 0;             // tiles of this stream
+                for (int j = pair || C::STREAMS == 1 ? 0 : wg; j < n; j += pair || C::STREAMS == 1 ? 1 : 2) {
+                    const unsigned g = g0 + j;
+                    const int buf = C::STREAMS == 1 ? j & 1 : wg;
+                    const int x0 = cache_tile(it, it.j0 + j) * KT;
+                    if (pair && !sees_some(a, v, x0, KT)) continue;
+                    if (!wait_warp(&sh.s_full[buf], seen_s[buf] & 1)) return false;
+                    ++seen_s[buf];
+                    ptx::tc_fence_after_sync();
+                    const bool masked = !sees_all(a, v, x0, KT);
+                    const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
+                    if (warp_on) {
+                        uint32_t x[KT];
+#pragma unroll
+                        for (int c = 0; c < KT; c += 32) ptx::tmem_ld32(ts + c, *reinterpret_cast<uint32_t(*)[32]>(&x[c]));
+                        ptx::tmem_wait_ld();
+                        if (masked) {
+                            const int hi = min(p - x0, KT) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
+#pragma unroll
+                            for (int c = 0; c < KT; c += 32) {
+                                const uint32_t bits = low32(hi - c) & (~low32(from - c) | low32(sk - c));
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (!(bits & (1u << i))) x[c + i] = 0xff800000u;
+                            }
+                        }
+                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                        for (int i = 0; i < KT; i += 2) t[(i >> 1) & 3] = ptx::max3(t[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
+                        const float m0 = m;
+                        const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
+                        m = grow ? top : m0;
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < KT; i += 2) {
+                            const float y = ptx::ex2(fmaf(__uint_as_float(x[i]), sl2, -ref)), z = ptx::ex2(fmaf(__uint_as_float(x[i + 1]), sl2, -ref));
+                            acc[i & 2] += y, acc[(i & 2) + 1] += z;
+                            // weights as bf16: at most 2^-8 of each, independent from key to key
+                            x[i / 2] = pack_bf16(y, z);
+                        }
+#pragma unroll
+                        for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&x[c]));
+                        if (grow) l *= ptx::ex2(m0 - m);
+                        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+                        if (taken > 0 && __any_sync(0xffffffffu, grow)) {
+                            // (with one stream the product before this one need not be done yet)
+                            if (C::STREAMS == 1 && !wait_warp(&sh.pv_done[(g - 1) & 1], ((g - 1) >> 1) & 1)) return false;
+                            if (C::STREAMS == 1) ptx::tc_fence_after_sync();
+                            const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                const uint32_t to = tmem + lane_base + (C::STREAMS == 1 ? 0 : wg) * D + c;
+                                ptx::tmem_ld32(to, o);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                ptx::tmem_st16(to, *reinterpret_cast<const uint32_t(*)[16]>(&o[0]));
+                                ptx::tmem_st16(to + 16, *reinterpret_cast<const uint32_t(*)[16]>(&o[16]));
+                            }
+                        }
+                        ptx::tmem_wait_st();
+                    }
+                    if (masked) {
+                        // Values that a zero weight may not meet: tokens that no row of the item sees (not copied, or the page's unused
+                        // slots) become zeros, and NaN and infinity in those that only some rows see are taken out; the
+                        // epilogue adds them where they are seen.
+                        const unsigned sidx = g % C::NV;
+                        if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
+                        unsigned char *vt = v_ring + sidx * C::STAGE;
+                        constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
+                        for (int i = w4 * 32 + lane; i < KT * VR; i += 128) {
+                            const int key = i / VR, c = i - key * VR;
+                            if (sees_all(a, v, x0 + key, 1)) continue;
+                            uint4 *at = reinterpret_cast<uint4 *>(vt + (key >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) +
+                                                                  ((c >> 3) * lay.v_rows + (key & (lay.v_rows - 1))) * 128 + (c & 7) * 16);
+                            if (!sees_some(a, all, x0 + key, 1)) {
+                                *at = make_uint4(0, 0, 0, 0);
+                                continue;
+                            }
+                            uint4 y = *at;
+                            if (nonfinite2(y.x) || nonfinite2(y.y) || nonfinite2(y.z) || nonfinite2(y.w)) {
+                                sh.nonfinite[ord % 8] = ord + 1;  // (ahead of the value's going: who finds it gone finds this)
+                                __threadfence_block();
+                                uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    if ((yw[e] & 0x7f80u) == 0x7f80u) yw[e] &= 0xffff0000u;
+                                    if ((yw[e] & 0x7f800000u) == 0x7f800000u) yw[e] &= 0x0000ffffu;
+                                }
+                                *at = y;
+                            }
+                        }
+                        ptx::fence_proxy_async();
+                        __syncwarp();
+                    }
+                    // every warp's part of the values has to be clean before any of them is used: p_full counts all four
+                    ptx::tc_fence_before_sync();
+                    ptx::mbar_arrive_warp(&sh.p_full[buf]);
+                    ++taken;
+                }
+                // ---- end of the item
+                const unsigned last = g0 + n - 1;
+                if (C::STREAMS == 1) {
+                    if (!wait_warp(&sh.pv_done[last & 1], (last >> 1) & 1)) return false;
+                } else {
+                    if (!pair || wg == 0)
+                        if (!wait_warp(&sh.pv_done[0], ord & 1)) return false;
+                    if (!pair || wg == 1)
+                        if (!wait_warp(&sh.pv_done[1], ord & 1)) return false;
+                }
+                ptx::tc_fence_after_sync();
+                const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
+                const int slot = it.slot;
+                const long long orow = ((long long)it.lo + it.t0 + (p - all.p0)) * a.H_q + it.h * a.G + (row - tok * a.G);
+                const int brow = (pair ? wg * MT : 0) + row;  // in the block
+                // Alone in an item with one row tile, the first warpgroup joins both streams' outputs.
+                bool second = false;       // the second stream's O counts
+                float f0 = 1.f, f1 = 0.f;
+                if (C::STREAMS == 2 && !pair) {
+                    // (the next item's are written behind its last product, and that behind this one's o_free)
+                    second = n > 1;
+                    if (wg == 1) {
+                        sh.ml[row] = make_float2(m, l);
+                        ptx::mbar_arrive_warp(&sh.ml_full[w4]);
+                    } else if (!wait_warp(&sh.ml_full[w4], singles & 1)) {
+                        return false;
+                    }
+                    ++singles;
+                    if (wg == 0 && second) {
+                        const float2 x = sh.ml[row];
+                        const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
+                        f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
+                        l = l * f0 + x.y * f1, m = mn;
+                    }
+                }
+                const bool writes = C::STREAMS == 1 || pair || wg == 0;
+                if (writes && taken == 0 && !second) l = 0.f;
+                const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
+                __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
+                if (writes && warp_on) {
+                    float *const blk = ws.o + (long long)slot * ws.cap * D;
+                    if (slot >= 0 && on) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t o[32];
+                        if (taken > 0) {
+                            ptx::tmem_ld32(tmem + lane_base + (pair ? wg : 0) * D + c, o);
+                            ptx::tmem_wait_ld();
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = 0;
+                        }
+                        if (second) {
+                            uint32_t o1[32];
+                            ptx::tmem_ld32(tmem + lane_base + D + c, o1);
+                            ptx::tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                        }
+                        if (!on) continue;
+                        if (slot < 0) {
+                            if (!bad)
+#pragma unroll
+                                for (int i = 0; i < 32; i += 8) {
+                                    uint4 y;
+                                    uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        yw[e] = pack_bf16(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
+                                    *reinterpret_cast<uint4 *>(out_row + c + i) = y;
+                                }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                *reinterpret_cast<uint4 *>(blk + ((long long)((c + i) / 4) * ws.cap + brow) * 4) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        }
+                    }
+                    __syncwarp();
+                    if (fix && on && !bad) {  // values with NaN or infinity in masked tiles: those elements, onto what was stored
+                        // (of two streams either may have taken them out: what not every row of both sees)
+                        const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
+#pragma unroll 1
+                        for (int j = 0; j < n; ++j) {
+                            const int x0 = cache_tile(it, it.j0 + j) * KT;
+                            if (sees_all(a, all, x0, KT)) continue;
+#pragma unroll 1
+                            for (int x = x0; x < x0 + KT; ++x) {
+                                if (!sees(a, p, x) || sees_all(a, all, x, 1)) continue;
+                                const __nv_bfloat16 *vr = static_cast<const __nv_bfloat16 *>(a.c.v) + table[x >> a.log_page] * a.c.stride_page +
+                                                          (x & ((1 << a.log_page) - 1)) * a.c.stride_slot + it.h * a.c.stride_head;
+#pragma unroll 1
+                                for (int c = 0; c < D; ++c) {
+                                    const float y = to_f32(vr[c]);
+                                    if (isfinite(y)) continue;
+                                    if (slot < 0) out_row[c] = __float2bfloat16_rn(to_f32(out_row[c]) + y);
+                                    else blk[((long long)(c / 4) * ws.cap + brow) * 4 + c % 4] += y;
+                                }
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {  // all read: the next item's products may overwrite it
+                    if (C::STREAMS == 1) {
+                        ptx::mbar_arrive(&sh.o_free[0]);
+                    } else if (pair) {
+                        ptx::mbar_arrive(&sh.o_free[wg]), ptx::mbar_arrive(&sh.o_free[wg]);
+                    } else {
+                        ptx::mbar_arrive(&sh.o_free[0]), ptx::mbar_arrive(&sh.o_free[1]);
+                    }
+                    ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
+                }
+                g0 += n;
+            }
+        };
+        if (!run()) {
+            ptx::tmem_wait_st();
+            if (lane == 0) atomicMin(&sh.unfinished, ord);
+        }
+        __syncwarp();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    if (sh.unfinished != ~0u) {
+        if (tid < 2) {  // copies in flight have to land before the CTA may leave
+            const unsigned filled = sh.copied[tid], ns = tid ? C::NV : C::NK;
+            uint64_t *fulls = tid ? sh.v_full : sh.k_full;
+            for (unsigned i = filled > ns ? filled - ns : 0; i < filled; ++i)
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&fulls[i % ns], (i / ns) & 1); ++t) __nanosleep(20);
+            if (tid == 0 && sh.q_copied > 0)
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.q_full, (sh.q_copied - 1) & 1); ++t) __nanosleep(20);
+        }
+        mark_unfinished<D>(a, ws, sh.part, Walk{sh.first_b, sh.first_off, sh.part.u0, sh.first_seq}, sh.unfinished);
+    }
+    __syncthreads();
+    if (warp == C::MMA) ptx::tmem_dealloc(tmem, 512);
+}
+
+// The join: o = sum_p 2^{m_p - m} o_p / sum_p 2^{m_p - m} l_p over the parts p of an item in the order of its keys.  A warp
+// takes 8 rows and 16 STEPS columns of them: lane = row + 8 * column group, 4 groups of 4 columns a step, so that both the
+// blocks (8 rows of a group are 128 bytes) and the output (4 groups of a row are 32) move in whole sectors.  UN parts are loaded
+// at a time.  A part with a bad page, or one that was not worked out, has a negative l: the row is left.
+constexpr int JOIN_WARPS = 8;
+template <int D, int STEPS, int UN>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) chunk_tc_join_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws ws)
+{
+    constexpr int CW = D / (16 * STEPS);         // warps that share a row
+    const int w = blockIdx.y * JOIN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31, cg = lane >> 3;
+    const int row = w / CW * 8 + (lane & 7), c0 = w % CW * (16 * STEPS);
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    const int4 d0 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x), d1 = *reinterpret_cast<const int4 *>(ws.desc + 8 * blockIdx.x + 4);
+    const int pieces = min(d0.x, MAX_CTAS), tt = MT / a.G;  // (calls that overlap on one workspace overwrite each other's: whatever lies there stays within it)
+    const int first = row / MT * tt, in_tile = row % MT, token = first + in_tile / a.G;
+    if (pieces <= 0 || token >= d1.x || in_tile >= tt * a.G || d1.z != (int)blockIdx.x || (unsigned)d0.y >= 2u * gridDim.x || d1.z + pieces > (int)gridDim.x) return;
+    float m = -INFINITY, l = 0.f;
+    int bad = 0;
+    float4 acc[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int p0 = 0; p0 < pieces; p0 += UN) {
+        float2 x[UN];
+        float4 y[UN][STEPS];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int p = min(p0 + i, pieces - 1);
+            const long long blk = (long long)(p == 0 ? d0.y : 2 * (d1.z + p)) * ws.cap;
+            x[i] = __ldcs(reinterpret_cast<const float2 *>(ws.ml) + blk + row);
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) y[i][e] = __ldcs(reinterpret_cast<const float4 *>(ws.o + blk * D + ((long long)(c0 / 4 + 4 * e + cg) * ws.cap + row) * 4));
+        }
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            if (p0 + i >= pieces) continue;
+            if (x[i].y < 0.f) bad = 1;
+            if (x[i].y == 0.f) continue;  // saw nothing
+            const float mn = fmaxf(m, x[i].x), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x[i].x - ref);
+            m = mn, l = l * f0 + x[i].y * f1;
+#pragma unroll
+            for (int e = 0; e < STEPS; ++e) {
+                acc[e].x = acc[e].x * f0 + y[i][e].x * f1, acc[e].y = acc[e].y * f0 + y[i][e].y * f1;
+                acc[e].z = acc[e].z * f0 + y[i][e].z * f1, acc[e].w = acc[e].w * f0 + y[i][e].w * f1;
+            }
+        }
+    }
+    if (bad) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const long long orow = ((long long)d0.z + token) * a.H_q + (long long)d0.w * a.G + in_tile % a.G;
+    __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.O) + orow * D + c0;
+#pragma unroll
+    for (int e = 0; e < STEPS; ++e)
+        *reinterpret_cast<uint2 *>(out + 16 * e + 4 * cg) =
+            make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
+}
+
+// rows of a block: an item's, as far as the batch can have them
+template <int D> int cap_of(const ChunkArgs &a)
+{
+    const long long rows = ((long long)a.T * a.G + 7) / 8 * 8;
+    // (a second row tile starts at row 128 of the block whatever the first one holds)
+    return (int)(a.T <= MT / a.G ? (rows < MT ? rows : MT) : Cfg<D>::CAP);
+}
+size_t desc_bytes() { return (size_t)MAX_CTAS * 8 * sizeof(int); }
+template <int D> size_t workspace_of(const ChunkArgs &a) { return desc_bytes() + 2ull * MAX_CTAS * cap_of<D>(a) * (D + 2) * sizeof(float); }
+
+template <int D> cudaError_t launch_d(ChunkArgs a, cudaStream_t stream)
+{
+    using C = Cfg<D>;
+    int dev = 0, sms = 0;
+    cudaError_t e = current_device_sms(&dev, &sms);
+    if (e != cudaSuccess) return e;
+    const int ctas = sms < MAX_CTAS ? sms : MAX_CTAS;
+    Ws ws;
+    ws.cap = cap_of<D>(a);
+    ws.desc = reinterpret_cast<int *>(a.ws);
+    ws.o = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(a.ws) + desc_bytes());
+    ws.ml = ws.o + 2ull * MAX_CTAS * ws.cap * D;
+    a.log_page = 0;
+    while ((1 << a.log_page) < a.c.page_size) ++a.log_page;
+
+    EncodeTiledFn enc = tma_encode_fn();
+    if (!enc) return cudaErrorNotSupported;
+    CUtensorMap q, k, v;
+    const CacheView &c = a.c;
+    const int box = c.page_size < C::KT ? c.page_size : C::KT;
+    Layout lay;
+    lay.v_rows = box;
+    for (lay.log_v_rows = 3; (1 << lay.log_v_rows) < box; ++lay.log_v_rows) {}
+    bool by_chunk = false;
+    auto lay_k = [&](auto b) { by_chunk = decltype(b)::K_BY_CHUNK, lay.k_chunk = decltype(b)::K_CHUNK, lay.k_group = decltype(b)::K_GROUP; };
+    if (box == 8) lay_k(Boxes<D, 8>{});
+    else if (box == 16) lay_k(Boxes<D, 16>{});
+    else if (box == 32) lay_k(Boxes<D, 32>{});
+    else if (box == 64) lay_k(Boxes<D, 64>{});
+    else lay_k(Boxes<D, C::KT>{});
+    auto map5 = [&](CUtensorMap *m, const void *base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&bx)[5]) {
+        const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+        return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    // (the stride of a dimension of one does not count, but has to be a legal one)
+    const cuuint64_t cache_dims[5] = {64, (cuuint64_t)c.page_size, (cuuint64_t)C::NC, (cuuint64_t)c.H_kv, (cuuint64_t)c.n_pages};
+    const cuuint64_t cache_strides[4] = {(cuuint64_t)c.stride_slot * 2, 128, c.H_kv > 1 ? (cuuint64_t)c.stride_head * 2 : 16,
+                                         c.n_pages > 1 ? (cuuint64_t)c.stride_page * 2 : 16};
+    const cuuint32_t k_box[5] = {64, (cuuint32_t)(by_chunk ? box : 8), (cuuint32_t)(by_chunk ? 1 : C::NC), 1, 1};
+    const cuuint32_t v_box[5] = {64, (cuuint32_t)box, (cuuint32_t)C::NC, 1, 1};
+    const cuuint64_t q_dims[5] = {64, (cuuint64_t)a.G, (cuuint64_t)a.T, (cuuint64_t)C::NC, (cuuint64_t)c.H_kv};
+    const cuuint64_t q_strides[4] = {D * 2, (cuuint64_t)a.ld_q * 2, 128, (cuuint64_t)a.G * D * 2};
+    const cuuint32_t q_box[5] = {64, (cuuint32_t)a.G, (cuuint32_t)(MT / a.G), 1, 1};
+    if (!map5(&k, c.k, cache_dims, cache_strides, k_box) || !map5(&v, c.v, cache_dims, cache_strides, v_box) || !map5(&q, a.q, q_dims, q_strides, q_box))
+        return cudaErrorInvalidValue;
+    // (the kernel's static shared memory, a deadline, comes first; the tiles start at the next multiple of 1024 behind `Shared`)
+    const int smem = (16 + (int)sizeof(Shared) + 1023) / 1024 * 1024 - 16 + C::TILES;
+    static_assert((16 + sizeof(Shared) + 1023) / 1024 * 1024 + C::TILES <= 227 * 1024, "shared memory of a CTA");
+    e = ensure_dynamic_smem(reinterpret_cast<const void *>(chunk_tc_kernel<D>), smem, dev);
+    if (e != cudaSuccess) return e;
+    e = launch_dependent(chunk_tc_kernel<D>, dim3(ctas), dim3(C::THREADS), smem, stream, a, ws, lay, smem, q, k, v);
+    if (e != cudaSuccess) return e;
+    auto join = [&](auto steps, auto un) {
+        constexpr int STEPS = decltype(steps)::value;
+        const int warps = (ws.cap + 7) / 8 * (D / (16 * STEPS));
+        return launch_dependent(chunk_tc_join_kernel<D, STEPS, decltype(un)::value>, dim3(ctas, (warps + JOIN_WARPS - 1) / JOIN_WARPS), dim3(JOIN_WARPS * 32),
+                                0, stream, a, ws);
+    };
+    return join(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+}
+
+}  // namespace
+
+// The line's units times the parts stay within 63 bits.
+static bool units_fit(const ChunkArgs &a)
+{
+    const double items = (double)a.T * a.G / 64 + a.B, keys = (double)a.c.max_pages * a.c.page_size + START;
+    return items * keys * a.c.H_kv * MAX_CTAS < 4e18;
+}
+
+bool chunk_tc_applies(const ChunkArgs &a, treewy_dtype_t io)
+{
+    const CacheView &c = a.c;
+    const bool pow2 = (c.page_size & (c.page_size - 1)) == 0;
+    // 8-row groups of the swizzle have to stay whole within a page; the tensor maps want a pool that exists and real strides
+    return io == TREEWY_BF16 && (c.d == 64 || c.d == 128 || c.d == 256) && pow2 && c.page_size >= 8 && c.n_pages > 0 && c.max_pages > 0 &&
+           c.stride_slot > 0 && (c.H_kv == 1 || c.stride_head > 0) && (c.n_pages == 1 || c.stride_page > 0) && a.G <= MT && units_fit(a);
+}
+
+size_t chunk_tc_workspace(const ChunkArgs &a) { return a.c.d == 256 ? workspace_of<256>(a) : a.c.d == 128 ? workspace_of<128>(a) : workspace_of<64>(a); }
+
+cudaError_t launch_chunk_tc(const ChunkArgs &a, cudaStream_t stream)
+{
+    if (a.c.d == 256) return launch_d<256>(a, stream);
+    if (a.c.d == 128) return launch_d<128>(a, stream);
+    return launch_d<64>(a, stream);
+}
+
+}  // namespace treewy

@@ -58,10 +58,13 @@ treewy_status_t chunk_common(bool force_generic, const treewy_kv_cache_t *cache,
     if (B == 0 || T == 0) return TREEWY_OK;
     if (bad_ptr(row_offsets) || bad_ptr(q) || bad_ptr(O) || bad_stride(ld_q, (int64_t)H_q * cache->d_head, elem_size(io)))
         return TREEWY_ERR_INVALID_ARG;
-    const size_t need = chunk_generic_workspace(a);
+    const bool tc = !force_generic && chunk_tc_applies(a, io);
+    const size_t need = tc ? chunk_tc_workspace(a) : chunk_generic_workspace(a);
     if (workspace_bytes < need || (need > 0 && bad_ptr(workspace))) return TREEWY_ERR_INVALID_ARG;
     a.row_offsets = row_offsets, a.q = q, a.ld_q = ld_q, a.O = O, a.scale = scale;
     a.ws = static_cast<float *>(workspace), a.seq_status = seq_status;
+    a.wait_cycles = debug_inject().wait_cycles, a.skip_item = debug_inject().skip_item;
+    if (tc) return launched(launch_chunk_tc(a, static_cast<cudaStream_t>(cuda_stream)));
     return launched(launch_chunk_generic(a, io, static_cast<cudaStream_t>(cuda_stream)));
 }
 
@@ -165,7 +168,8 @@ size_t treewy_attn_chunk_workspace(const treewy_kv_cache_t *cache, int32_t B, in
 {
     ChunkArgs a;
     if (chunk_args(cache, B, T, H_q, window, sinks, io_dtype, &a) != TREEWY_OK || B == 0 || T == 0) return 0;
-    return chunk_generic_workspace(a);
+    const size_t g = chunk_generic_workspace(a), t = chunk_tc_applies(a, io_dtype) ? chunk_tc_workspace(a) : 0;
+    return g > t ? g : t;
 }
 
 treewy_status_t treewy_attn_chunk(const treewy_kv_cache_t *cache, int32_t B, int32_t T, const int32_t *row_offsets, const void *q,
