@@ -5,12 +5,13 @@
 // tensor memory and its own warpgroup for the softmax, over the same tiles of keys and values: while one stream's softmax
 // runs, the tensor cores have the other's products.  An item with one row tile (decoding, short pieces) gives the two
 // streams alternate key tiles instead, and joins their outputs at its end.
-// Keys.  Tiles of 128 (heads of 256: 64) at multiples of 128: those of the sinks, then from the first row's window to the last
+// Keys.  Tiles of 64 at multiples of 64: those of the sinks, then from the first row's window to the last
 // row.  Tiles that some row does not see whole are masked, those that no row of a stream sees are left out for it.
 // One tile of a stream:  S = Q K^T, the softmax step in registers (a row to a thread), P = weights as bf16 over S's
-// own columns, O += P V (V read with its rows as the K index).  The products of a stream are issued in the order P V, Q K^T of
-// the next tile, so that S's columns are free and O is at rest whenever S is full: the running maximum may move O then, which
-// it does only when a row's new maximum exceeds it by more than 8 (in log2; weights are at most 2^8 until then).
+// own columns, O += P V (V read with its rows as the K index).  A stream has two S buffers or more, and its scores are issued as many tiles
+// ahead of its products: the next S is there when a softmax step ends.  The running maximum m moves only when a row's new maximum
+// exceeds it by more than 8 (in log2): until then weights are at most 2^8 and nothing overflows, and the pass over O
+// that a new m costs is rare after a row's first tiles.
 //
 // Work.  (sequence, head, item) in one line, an item's length being its start's cost and its keys, cut into equal parts,
 // one for each CTA: no CTA waits for a longer neighbour, whatever the lengths and windows.  A cut item leaves unnormalised
@@ -25,6 +26,8 @@ namespace treewy {
 namespace {
 
 constexpr int MT = 128;                // rows of a tile
+constexpr int KT = 64;                 // keys of a tile
+constexpr int MAX_STAGES = 10;         // of a ring
 constexpr int MAX_CTAS = 160;
 constexpr int ITEMS = 4;               // ring of work items between the producer and the other roles
 constexpr int START = 256;             // cost of an item's start, in keys
@@ -35,14 +38,14 @@ constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;  // l of a row whose part is n
 template <int D> struct Cfg {
     static constexpr int NC = D / 64;                    // 64-column chunks of a row
     static constexpr int STREAMS = D == 256 ? 1 : 2;     // what 512 columns of tensor memory leave
-    static constexpr int KT = D == 256 ? 64 : 128;       // keys of a tile
     static constexpr int STAGE = NC * KT * 128;          // bytes of a tile
-    static constexpr int NK = D == 64 ? 5 : 3, NV = D == 64 ? 5 : 2;
+    static constexpr int NB = D == 256 ? 4 : 2;          // S buffers of a stream
+    static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 5 : 2;
     static constexpr int Q_TILE = NC * MT * 128;
     static constexpr int TILES = STREAMS * Q_TILE + (NK + NV) * STAGE;  // bytes
     static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 1, PRODUCER_V = MMA + 2;
     static constexpr int THREADS = (SOFT_WARPS + 3) * 32;
-    static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer s at 256 + s * KT
+    static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer b of it at 256 + (s * NB + b) * KT
     static constexpr int CAP = STREAMS * MT;             // rows of an item at most
 };
 
@@ -51,7 +54,7 @@ template <int D> struct Cfg {
 // needs its 8-row groups equally far apart: whole boxes one chunk at a time, or all chunks of 8 rows, whichever makes
 // fewer copies.
 template <int D, int BOX> struct Boxes {
-    static constexpr int NC = D / 64, KT = Cfg<D>::KT, P = KT / BOX;  // boxes of a tile
+    static constexpr int NC = D / 64, P = KT / BOX;  // boxes of a tile
     static constexpr bool K_BY_CHUNK = P * NC <= KT / 8;
     static constexpr int K_CHUNK = K_BY_CHUNK ? KT * 128 : 1024, K_GROUP = K_BY_CHUNK ? 1024 : NC * 1024;
 };
@@ -86,8 +89,10 @@ struct Walk {                   // a CTA's way along its part
 };
 
 struct Shared {
-    uint64_t k_full[6], k_free[6], v_full[6], v_free[6];
-    uint64_t s_full[2], p_full[2], pv_done[2], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4];
+    uint64_t k_full[MAX_STAGES], k_free[MAX_STAGES], v_full[MAX_STAGES], v_free[MAX_STAGES];
+    // Of an S buffer: filled, its weights stored, its product done.  (One to a buffer: a parity names a phase only to who has seen
+    // the one before it, and a full S says that the buffer's last product is done.)
+    uint64_t s_full[4], p_full[4], pv_done[4], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4], end;
     Item items[ITEMS];
     float2 ml[MT];              // of the second stream's rows, for the first
     unsigned bad_item[8];       // ordinal + 1 of an item that met a page out of range
@@ -145,7 +150,6 @@ __device__ __forceinline__ int tiles_before(long long o, long long k, int kts)
 // The next item that has tiles here; 0 tiles: the end.  The part that has a cut item's first tile leaves word for the join.
 template <int D> static __device__ __noinline__ void next_item(const ChunkArgs &a, const Ws &ws, const Part &p, Walk &w, Item &it, bool describe)
 {
-    constexpr int KT = Cfg<D>::KT;
     int st;
     it.tiles = 0;
     while (w.u < p.u1 && it.tiles == 0) {
@@ -237,7 +241,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v)
 {
     using C = Cfg<D>;
-    constexpr int KT = C::KT;
     // barriers and the like first, tiles behind them: the bytes that aligning the tiles takes are used so
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Shared &sh = *reinterpret_cast<Shared *>(smem_raw);
@@ -247,11 +250,12 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
 
     if (tid == 0) {
         ptx::wait_deadline_init(a.wait_cycles);
-        for (int i = 0; i < 6; ++i)
+#pragma unroll 1
+        for (int i = 0; i < MAX_STAGES; ++i)
             ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], 1);
-        for (int i = 0; i < 2; ++i)
-            ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1), ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
-        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
+        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, 1), ptx::mbar_init(&sh.end, 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], C::SOFT_WARPS + 2);
         ptx::fence_barrier_init();
@@ -411,8 +415,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 }
             };
             auto run_box = [&](auto box_) { return warp == C::PRODUCER_V ? run(box_, std::true_type{}) : run(box_, std::false_type{}); };
-            if (KT == 128 && lay.v_rows == 128) run_box(std::integral_constant<int, KT>{});
-            else if (lay.v_rows == 64) run_box(std::integral_constant<int, 64>{});
+            if (lay.v_rows == 64) run_box(std::integral_constant<int, 64>{});
             else if (lay.v_rows == 32) run_box(std::integral_constant<int, 32>{});
             else if (lay.v_rows == 8) run_box(std::integral_constant<int, 8>{});
             else run_box(std::integral_constant<int, 16>{});
@@ -436,29 +439,31 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 v_hi = vd & ~0xffffffffull, v_lo[s] = (uint32_t)vd;
             }
             unsigned g0 = 0;              // tiles of the items before
-            unsigned made[2] = {0, 0}, used[2] = {0, 0};  // S buffers filled, P buffers consumed
-            // scores of tile g into buffer s; q: which row tile
+            unsigned made[2] = {0, 0}, used[2] = {0, 0};  // tiles of a stream whose scores, whose products were issued
+            // scores of tile g for stream s; q: which row tile
             auto scores = [&](unsigned g, int s, int q) -> bool {
                 if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
                 ptx::tc_fence_after_sync();
-                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16), ql = q_lo + q * (C::Q_TILE / 16);
+                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16), ql = q_lo + q * (C::Q_TILE / 16), buf = s * C::NB + made[s] % C::NB;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c)
-                    ptx::umma_bf16(tmem + C::TM_S + s * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2),
+                    ptx::umma_bf16(tmem + C::TM_S + buf * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2),
                                    k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk, c > 0);
-                ptx::umma_commit(&sh.s_full[s]);
+                ptx::umma_commit(&sh.s_full[buf]);
                 ++made[s];
                 return true;
             };
-            // output of tile g from buffer s onto O of stream os
-            auto product = [&](unsigned g, int s, int os, bool onto) -> bool {
+            // output of tile g onto O of stream s
+            auto product = [&](unsigned g, int s, bool onto) -> bool {
+                const uint32_t buf = s * C::NB + used[s] % C::NB;
                 if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
-                if (!ptx::mbar_wait(&sh.p_full[s], used[s] & 1)) return false;
-                ++used[s];
+                if (!ptx::mbar_wait(&sh.p_full[buf], (used[s] / C::NB) & 1)) return false;
                 ptx::tc_fence_after_sync();
 #pragma unroll
                 for (int c = 0; c < KT / 16; ++c)
-                    ptx::umma_bf16_ts(tmem + os * D, tmem + C::TM_S + s * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
+                    ptx::umma_bf16_ts(tmem + s * D, tmem + C::TM_S + buf * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
+                ptx::umma_commit(&sh.pv_done[buf]);
+                ++used[s];
                 return true;
             };
             auto run = [&]() -> bool {
@@ -470,62 +475,47 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     ptx::mbar_arrive(&sh.item_empty[r]);
                     if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                     const int n = it.tiles;
-                    if (C::STREAMS == 2 && it.pair) {
-                        // which tiles (from j0 on) each stream takes part in
-                        View v[2] = {view_of(it, tt, 0), view_of(it, tt, 1)};
-                        auto on = [&](int j, int s) { return sees_some(a, v[s], cache_tile(it, it.j0 + j) * KT, KT); };
-                        bool onto[2] = {false, false};
-                        for (int s = 0; s < 2; ++s)
-                            if (on(0, s) && !scores(g0, s, s)) return false;
-                        ptx::umma_commit(&sh.k_free[g0 % C::NK]);
-                        if (n == 1) ptx::umma_commit(&sh.q_free);
-                        for (int j = 0; j < n; ++j) {
-                            const unsigned g = g0 + j;
-                            for (int s = 0; s < 2; ++s) {
-                                if (on(j, s)) {
-                                    if (!onto[s] && ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
-                                    if (!product(g, s, s, onto[s])) return false;
-                                    onto[s] = true;
-                                }
-                                if (s == 1) ptx::umma_commit(&sh.v_free[g % C::NV]);
-                                if (j + 1 < n && on(j + 1, s) && !scores(g + 1, s, s)) return false;
-                                if (j + 1 == n) ptx::umma_commit(&sh.pv_done[s]);
-                            }
-                            if (j + 1 < n) ptx::umma_commit(&sh.k_free[(g + 1) % C::NK]);
-                            if (j + 2 == n) ptx::umma_commit(&sh.q_free);
-                        }
-                        // (a stream without a tile here has not waited yet)
-                        for (int s = 0; s < 2; ++s)
-                            if (!onto[s] && ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
-                    } else {
-                        // tiles alternate between the S buffers; with two streams each has its own O
-                        for (int j = 0; j < 2 && j < n; ++j) {
-                            if (!scores(g0 + j, j, 0)) return false;
-                            ptx::umma_commit(&sh.k_free[(g0 + j) % C::NK]);
-                        }
-                        if (n <= 2) ptx::umma_commit(&sh.q_free);
+                    // Scores run `ahead` tiles ahead of the products: as many as there are S buffers for.
+                    const bool pair = C::STREAMS == 2 && it.pair;
+                    const int ahead = pair || C::STREAMS == 1 ? C::NB : 2 * C::NB;
+                    const View v[2] = {view_of(it, tt, 0), view_of(it, tt, 1)};
+                    // whether stream s takes part in tile j (from j0 on): with two row tiles as far as it sees some of it, else in turn
+                    auto on = [&](int j, int s) {
+                        if (!pair) return C::STREAMS == 1 || (j & 1) == s;
+                        return sees_some(a, v[s], cache_tile(it, it.j0 + j) * KT, KT);
+                    };
+                    auto scores_of = [&](int j) -> bool {
                         for (int s = 0; s < C::STREAMS; ++s)
-                            if (ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
-                        for (int j = 0; j < n; ++j) {
-                            const unsigned g = g0 + j;
-                            if (!product(g, j & 1, C::STREAMS == 2 ? j & 1 : 0, C::STREAMS == 2 ? j >= 2 : j >= 1)) return false;
-                            ptx::umma_commit(&sh.v_free[g % C::NV]);
-                            if (C::STREAMS == 1) ptx::umma_commit(&sh.pv_done[g & 1]);
-                            if (j + 2 < n) {
-                                if (!scores(g + 2, j & 1, 0)) return false;
-                                ptx::umma_commit(&sh.k_free[(g + 2) % C::NK]);
-                                if (j + 3 == n) ptx::umma_commit(&sh.q_free);
+                            if (on(j, s) && !scores(g0 + j, s, pair ? s : 0)) return false;
+                        ptx::umma_commit(&sh.k_free[(g0 + j) % C::NK]);
+                        if (j + 1 == n) ptx::umma_commit(&sh.q_free);
+                        return true;
+                    };
+                    bool onto[2] = {false, false};
+                    for (int j = 0; j < ahead && j < n; ++j)
+                        if (!scores_of(j)) return false;
+                    for (int s = 0; s < C::STREAMS; ++s)
+                        if (ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
+                    for (int j = 0; j < n; ++j) {
+                        const bool more = j + ahead < n;
+                        for (int s = 0; s < C::STREAMS; ++s) {
+                            if (on(j, s)) {
+                                if (!product(g0 + j, s, onto[s])) return false;
+                                onto[s] = true;
                             }
+                            // (each stream's next scores right behind its product: the other's wait for its weights must not hold them up)
+                            if (more && on(j + ahead, s) && !scores(g0 + j + ahead, s, pair ? s : 0)) return false;
                         }
-                        if (C::STREAMS == 2) ptx::umma_commit(&sh.pv_done[0]), ptx::umma_commit(&sh.pv_done[1]);
+                        ptx::umma_commit(&sh.v_free[(g0 + j) % C::NV]);
+                        if (more) ptx::umma_commit(&sh.k_free[(g0 + j + ahead) % C::NK]);
+                        if (j + ahead + 1 == n) ptx::umma_commit(&sh.q_free);
                     }
                     g0 += n;
                 }
             };
             if (!run()) {  // MMAs in flight have to end before the CTA may leave: a commit behind all of them, on a barrier of its own
-                uint64_t *end = &sh.k_full[5];
-                ptx::umma_commit(end);
-                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(end, 0); ++t) __nanosleep(20);
+                ptx::umma_commit(&sh.end);
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.end, 0); ++t) __nanosleep(20);
             }
         }
         __syncwarp();
@@ -534,8 +524,10 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
         const float sl2 = a.scale * 1.4426950408889634f;
-        unsigned seen_s[2] = {0, 0};  // S buffers taken
+        const int strm = C::STREAMS == 1 ? 0 : wg;  // this warpgroup's stream
+        unsigned count = 0;           // its tiles so far
         unsigned g0 = 0, ord = 0, singles = 0;
+        auto wait_product = [&](unsigned i) { return wait_warp(&sh.pv_done[strm * C::NB + i % C::NB], (i / C::NB) & 1); };  // of this stream's tile i
         auto run = [&]() -> bool {
             for (;; ++ord) {
                 if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
@@ -551,11 +543,10 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 int taken = 0;             // tiles of this stream
                 for (int j = pair || C::STREAMS == 1 ? 0 : wg; j < n; j += pair || C::STREAMS == 1 ? 1 : 2) {
                     const unsigned g = g0 + j;
-                    const int buf = C::STREAMS == 1 ? j & 1 : wg;
+                    const int buf = strm * C::NB + count % C::NB;
                     const int x0 = cache_tile(it, it.j0 + j) * KT;
                     if (pair && !sees_some(a, v, x0, KT)) continue;
-                    if (!wait_warp(&sh.s_full[buf], seen_s[buf] & 1)) return false;
-                    ++seen_s[buf];
+                    if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
                     ptx::tc_fence_after_sync();
                     const bool masked = !sees_all(a, v, x0, KT);
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
@@ -582,27 +573,29 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
                         m = grow ? top : m0;
                         const float ref = m == -INFINITY ? 0.f : m;
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                        const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-ref, -ref);
+                        float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                         for (int i = 0; i < KT; i += 2) {
-                            const float y = ptx::ex2(fmaf(__uint_as_float(x[i]), sl2, -ref)), z = ptx::ex2(fmaf(__uint_as_float(x[i + 1]), sl2, -ref));
-                            acc[i & 2] += y, acc[(i & 2) + 1] += z;
+                            float2 y = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
+                            y.x = ptx::ex2(y.x), y.y = ptx::ex2(y.y);
+                            acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
                             // weights as bf16: at most 2^-8 of each, independent from key to key
-                            x[i / 2] = pack_bf16(y, z);
+                            x[i / 2] = pack_bf16(y.x, y.y);
                         }
 #pragma unroll
                         for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&x[c]));
                         if (grow) l *= ptx::ex2(m0 - m);
-                        l += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+                        l += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
                         if (taken > 0 && __any_sync(0xffffffffu, grow)) {
-                            // (with one stream the product before this one need not be done yet)
-                            if (C::STREAMS == 1 && !wait_warp(&sh.pv_done[(g - 1) & 1], ((g - 1) >> 1) & 1)) return false;
-                            if (C::STREAMS == 1) ptx::tc_fence_after_sync();
+                            // O at rest: the stream's product before this one is done, and the next one waits for these weights
+                            if (!wait_product(count - 1)) return false;
+                            ptx::tc_fence_after_sync();
                             const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
 #pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 uint32_t o[32];
-                                const uint32_t to = tmem + lane_base + (C::STREAMS == 1 ? 0 : wg) * D + c;
+                                const uint32_t to = tmem + lane_base + strm * D + c;
                                 ptx::tmem_ld32(to, o);
                                 ptx::tmem_wait_ld();
 #pragma unroll
@@ -618,6 +611,8 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         // slots) become zeros, and NaN and infinity in those that only some rows see are taken out; the
                         // epilogue adds them where they are seen.
                         const unsigned sidx = g % C::NV;
+                        // (where S runs further ahead than V's ring, the stage's last tile has to be done for its phase to mean this one)
+                        if (C::NV < C::NB && count >= C::NV && !wait_product(count - C::NV)) return false;
                         if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
                         unsigned char *vt = v_ring + sidx * C::STAGE;
                         constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
@@ -649,17 +644,16 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     // every warp's part of the values has to be clean before any of them is used: p_full counts all four
                     ptx::tc_fence_before_sync();
                     ptx::mbar_arrive_warp(&sh.p_full[buf]);
-                    ++taken;
+                    ++taken, ++count;
                 }
                 // ---- end of the item
-                const unsigned last = g0 + n - 1;
-                if (C::STREAMS == 1) {
-                    if (!wait_warp(&sh.pv_done[last & 1], (last >> 1) & 1)) return false;
-                } else {
-                    if (!pair || wg == 0)
-                        if (!wait_warp(&sh.pv_done[0], ord & 1)) return false;
-                    if (!pair || wg == 1)
-                        if (!wait_warp(&sh.pv_done[1], ord & 1)) return false;
+                if (taken > 0) {
+                    if (!wait_product(count - 1)) return false;
+                } else if (ord > 0) {
+                    // A stream without a tile here has no product to wait for, which would be behind the release of the last item's
+                    // outputs.  So that it does not count twice towards that, and does not overwrite what is still read of that item:
+                    for (int s = 0; s < C::STREAMS; ++s)
+                        if (!wait_warp(&sh.o_free[s], (ord - 1) & 1)) return false;
                 }
                 ptx::tc_fence_after_sync();
                 const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
@@ -670,13 +664,15 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 bool second = false;       // the second stream's O counts
                 float f0 = 1.f, f1 = 0.f;
                 if (C::STREAMS == 2 && !pair) {
-                    // (the next item's are written behind its last product, and that behind this one's o_free)
+                    // (the next item's are written behind this one's o_free)
                     second = n > 1;
-                    if (wg == 1) {
+                    if (wg == 1) {  // (its products are done, then)
                         sh.ml[row] = make_float2(m, l);
+                        ptx::tc_fence_before_sync();
                         ptx::mbar_arrive_warp(&sh.ml_full[w4]);
-                    } else if (!wait_warp(&sh.ml_full[w4], singles & 1)) {
-                        return false;
+                    } else {
+                        if (!wait_warp(&sh.ml_full[w4], singles & 1)) return false;
+                        ptx::tc_fence_after_sync();
                     }
                     ++singles;
                     if (wg == 0 && second) {
@@ -880,7 +876,7 @@ template <int D> cudaError_t launch_d(ChunkArgs a, cudaStream_t stream)
     if (!enc) return cudaErrorNotSupported;
     CUtensorMap q, k, v;
     const CacheView &c = a.c;
-    const int box = c.page_size < C::KT ? c.page_size : C::KT;
+    const int box = c.page_size < KT ? c.page_size : KT;
     Layout lay;
     lay.v_rows = box;
     for (lay.log_v_rows = 3; (1 << lay.log_v_rows) < box; ++lay.log_v_rows) {}
@@ -889,8 +885,7 @@ template <int D> cudaError_t launch_d(ChunkArgs a, cudaStream_t stream)
     if (box == 8) lay_k(Boxes<D, 8>{});
     else if (box == 16) lay_k(Boxes<D, 16>{});
     else if (box == 32) lay_k(Boxes<D, 32>{});
-    else if (box == 64) lay_k(Boxes<D, 64>{});
-    else lay_k(Boxes<D, C::KT>{});
+    else lay_k(Boxes<D, 64>{});
     auto map5 = [&](CUtensorMap *m, const void *base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&bx)[5]) {
         const cuuint32_t es[5] = {1, 1, 1, 1, 1};
         return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
