@@ -29,7 +29,7 @@ constexpr int MT = 128;                // rows of a tile
 constexpr int KT = 64;                 // keys of a tile
 constexpr int MAX_STAGES = 10;         // of a ring
 constexpr int MAX_CTAS = 160;
-constexpr int ITEMS = 4;               // ring of work items between the producer and the other roles
+constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
 constexpr int START = 256;             // cost of an item's start, in keys
 constexpr int MIN_UNITS = 256;         // least units of a part; at least a tile's keys, so that a part inside an item holds the start of one
 constexpr float LAZY = 8.f;
@@ -43,8 +43,10 @@ template <int D> struct Cfg {
     static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 5 : 2;
     static constexpr int Q_TILE = NC * MT * 128;
     static constexpr int TILES = STREAMS * Q_TILE + (NK + NV) * STAGE;  // bytes
-    static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 1, PRODUCER_V = MMA + 2;
-    static constexpr int THREADS = (SOFT_WARPS + 3) * 32;
+    static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 2, PRODUCER_V = MMA + 3;  // (two of MMA)
+    static constexpr int THREADS = (SOFT_WARPS + 4) * 32;
+    // Of POLY_OF pairs of weights POLY are worked out on the FMA pipes, the others by the special-function unit.
+    static constexpr int POLY = 0, POLY_OF = 4;
     static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer b of it at 256 + (s * NB + b) * KT
     static constexpr int CAP = STREAMS * MT;             // rows of an item at most
 };
@@ -71,7 +73,6 @@ struct Item {
     int sink_tiles, low_tile;   // tile j is tile j of the cache for j < sink_tiles, else low_tile + j - sink_tiles
     int slot;                   // the block of a cut item, else -1
 };
-__device__ __forceinline__ int cache_tile(const Item &it, int j) { return j < it.sink_tiles ? j : it.low_tile + (j - it.sink_tiles); }
 
 struct Seq {
     int lo, n, len, items;
@@ -83,8 +84,8 @@ struct Part {
     int parts, group;
 };
 struct Walk {                   // a CTA's way along its part
-    int b;
-    long long off, u;           // in the units of sequence b, on the line
+    int b, h, i;                // the item it is in: sequence, head, item under it
+    long long o, u;             // units into the item, and on the line
     Seq s;
 };
 
@@ -92,7 +93,7 @@ struct Shared {
     uint64_t k_full[MAX_STAGES], k_free[MAX_STAGES], v_full[MAX_STAGES], v_free[MAX_STAGES];
     // Of an S buffer: filled, its weights stored, its product done.  (One to a buffer: a parity names a phase only to who has seen
     // the one before it, and a full S says that the buffer's last product is done.)
-    uint64_t s_full[4], p_full[4], pv_done[4], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4], end;
+    uint64_t s_full[4], p_full[4], pv_done[4], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4], end[2];
     Item items[ITEMS];
     float2 ml[MT];              // of the second stream's rows, for the first
     unsigned bad_item[8];       // ordinal + 1 of an item that met a page out of range
@@ -147,55 +148,70 @@ __device__ __forceinline__ int tiles_before(long long o, long long k, int kts)
     return o <= START ? 0 : (int)min((long long)kts, ((o - START) * kts + k - 1) / k);
 }
 
-// The next item that has tiles here; 0 tiles: the end.  The part that has a cut item's first tile leaves word for the join.
+// Where a CTA's part begins: unit `off` of sequence b
+template <int D> static __device__ __noinline__ Walk walk_from(const ChunkArgs &a, int b, long long off, long long u, const Seq &s)
+{
+    Walk w{b, 0, 0, 0, u, s};
+    if (b < 0) return w;               // (no work)
+    w.h = (int)(off / (long long)s.per);
+    const long long in_head = off - w.h * (long long)s.per;
+    int hi = s.items;
+    while (hi - w.i > 1) {
+        const int mid = (w.i + hi) >> 1;
+        if (units_before<D>(a, s.len, s.n, mid) <= in_head) w.i = mid;
+        else hi = mid;
+    }
+    w.o = in_head - units_before<D>(a, s.len, s.n, w.i);
+    return w;
+}
+
+// The next item that has tiles here; 0 tiles: the end.  The part that has a cut item's first tile leaves word for the join.  (One thread
+// walks while tiles are copied and worked on: divisions only for items that are cut.)
 template <int D> static __device__ __noinline__ void next_item(const ChunkArgs &a, const Ws &ws, const Part &p, Walk &w, Item &it, bool describe)
 {
-    int st;
+    const int tt = tile_tokens<D>(a), per = Cfg<D>::STREAMS * tt;
     it.tiles = 0;
     while (w.u < p.u1 && it.tiles == 0) {
         const Seq &s = w.s;
-        if ((unsigned long long)w.off >= s.per * a.c.H_kv) {  // (a sequence without work has no units)
-            w.off = 0, ++w.b;
-            w.s = load_seq<D>(a, w.b, &st);
+        if (w.i >= s.items) {          // (a sequence without work has no items)
+            w.i = 0;
+            if (s.items == 0 || ++w.h >= a.c.H_kv) {
+                int st;
+                w.h = 0, ++w.b;
+                w.s = load_seq<D>(a, w.b, &st);
+            }
             continue;
         }
-        const int h = (int)(w.off / (long long)s.per);
-        const long long in_head = w.off - h * (long long)s.per;
-        int i = 0, hi = s.items;           // the item that unit in_head is in
-        while (hi - i > 1) {
-            const int mid = (i + hi) >> 1;
-            if (units_before<D>(a, s.len, s.n, mid) <= in_head) i = mid;
-            else hi = mid;
-        }
-        const long long at = units_before<D>(a, s.len, s.n, i), cost = units_before<D>(a, s.len, s.n, i + 1) - at, o = in_head - at;
-        const int tt = tile_tokens<D>(a), per = Cfg<D>::STREAMS * tt;
-        it.b = w.b, it.h = h, it.lo = s.lo, it.len = s.len;
-        it.t0 = i * per, it.tokens = min(per, s.n - it.t0);
+        it.b = w.b, it.h = w.h, it.lo = s.lo, it.len = s.len;
+        it.t0 = w.i * per, it.tokens = min(per, s.n - it.t0);
         it.pair = it.tokens > tt;
         const int p0 = s.len + it.t0, p1 = p0 + it.tokens - 1;
         const int low = a.window > p0 ? 0 : p0 - a.window + 1;
         it.low_tile = low / KT;
-        it.sink_tiles = min((int)(((long long)min(a.sinks, low) + KT - 1) / KT), it.low_tile);
+        it.sink_tiles = min((min(a.sinks, low) + (KT - 1)) / KT, it.low_tile);
         it.kts = it.sink_tiles + p1 / KT - it.low_tile + 1;
-        const long long span = min(cost - o, p.u1 - w.u), begin = w.u - o;
-        it.j0 = tiles_before(o, cost - START, it.kts);
-        const int j1 = tiles_before(o + span, cost - START, it.kts);
+        const long long keys = it.tokens + min((long long)p0, (long long)a.window + a.sinks - 1);
+        const long long span = min(START + keys - w.o, p.u1 - w.u), begin = w.u - w.o;
+        const bool to_end = w.o + span == START + keys;
+        it.j0 = w.o <= START ? 0 : tiles_before(w.o, keys, it.kts);
+        const int j1 = to_end ? it.kts : tiles_before(w.o + span, keys, it.kts);
         it.tiles = j1 - it.j0;
         const bool cut = it.j0 > 0 || j1 < it.kts;
         it.slot = !cut ? -1 : begin <= p.u0 ? 2 * p.group : 2 * p.group + 1;
         if (describe && cut && it.j0 == 0 && it.tiles > 0) {
             int *d = ws.desc + 8 * p.group;
-            const long long last = begin + START + (long long)(it.kts - 1) * (cost - START) / it.kts;
-            d[1] = it.slot, d[2] = it.lo + it.t0, d[3] = h, d[4] = it.tokens, d[5] = it.b, d[6] = p.group;
+            const long long last = begin + START + (long long)(it.kts - 1) * keys / it.kts;
+            d[1] = it.slot, d[2] = it.lo + it.t0, d[3] = it.h, d[4] = it.tokens, d[5] = it.b, d[6] = p.group;
             d[0] = part_of(last, p.W, p.parts) - p.group + 1;
         }
-        w.off += span, w.u += span;
+        w.u += span, w.o += span;
+        if (to_end) w.o = 0, ++w.i;
     }
 }
 
 // After a wait that ran out: from item `unfinished` on, this CTA's blocks say that they are not there and the sequences are
 // flagged.
-template <int D> static __device__ __noinline__ void mark_unfinished(const ChunkArgs &a, const Ws &ws, const Part &p, Walk w, unsigned unfinished)
+template <int D> static __device__ __noinline__ void mark_unfinished(const ChunkArgs &a, const Ws &ws, const Part &p, Walk w, unsigned unfinished, int tid, int threads)
 {
     Item it;
     for (unsigned ord = 0;; ++ord) {
@@ -203,9 +219,9 @@ template <int D> static __device__ __noinline__ void mark_unfinished(const Chunk
         if (it.tiles == 0) return;
         if (ord < unfinished) continue;
         if (it.slot >= 0)
-            for (int r = threadIdx.x; r < ws.cap; r += Cfg<D>::THREADS)
+            for (int r = tid; r < ws.cap; r += threads)
                 reinterpret_cast<float2 *>(ws.ml)[(long long)it.slot * ws.cap + r] = make_float2(0.f, NOT_DONE);
-        if (threadIdx.x == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_TIMEOUT);
+        if (tid == 0 && a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_TIMEOUT);
     }
 }
 
@@ -218,6 +234,23 @@ __device__ __forceinline__ View view_of(const Item &it, int tt, int s)
     const int first = it.pair ? s * tt : 0, last = it.pair && s == 0 ? tt : it.tokens;
     return {it.len + it.t0 + first, it.len + it.t0 + last - 1};
 }
+// The same for whole tiles, worked out once: tile kt is seen by some row of the view, or whole by every row.
+struct Span {
+    int sink_some, low_some, high_some, sink_all, low_all, high_all;
+    __device__ __forceinline__ bool some(int kt) const { return kt <= high_some && (kt >= low_some || kt < sink_some); }
+    __device__ __forceinline__ bool all(int kt) const { return kt < high_all && (kt >= low_all || kt < sink_all); }
+};
+__device__ __forceinline__ Span span_of(const ChunkArgs &a, const View &v)
+{
+    const int from0 = a.window > v.p0 ? 0 : v.p0 - a.window + 1, from1 = a.window > v.p1 ? 0 : v.p1 - a.window + 1;
+    return {a.sinks > 0 ? (a.sinks - 1) / KT + 1 : 0, from0 / KT, v.p1 / KT, a.sinks / KT, from1 > 0 ? (from1 - 1) / KT + 1 : 0, (v.p0 + 1) / KT};
+}
+// The cache's tile for tile j of an item's tiles here
+struct Tiles {
+    int sinks, first, then;
+    __device__ __forceinline__ explicit Tiles(const Item &it) : sinks(it.sink_tiles - it.j0), first(it.j0), then(it.low_tile - it.sink_tiles + it.j0) {}
+    __device__ __forceinline__ int operator()(int j) const { return j + (j < sinks ? first : then); }
+};
 // Whether some row of the view sees some token of tokens x0 .. x0 + n - 1
 __device__ __forceinline__ bool sees_some(const ChunkArgs &a, const View &v, int x0, int n)
 {
@@ -252,12 +285,12 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         ptx::wait_deadline_init(a.wait_cycles);
 #pragma unroll 1
         for (int i = 0; i < MAX_STAGES; ++i)
-            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], 1), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], 1);
+            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], C::STREAMS), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], C::STREAMS);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
         for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
-        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, 1), ptx::mbar_init(&sh.end, 1);
+        ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, C::STREAMS), ptx::mbar_init(&sh.end[0], 1), ptx::mbar_init(&sh.end[1], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
-        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], C::SOFT_WARPS + 2);
+        for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], C::SOFT_WARPS + 3);
         ptx::fence_barrier_init();
         sh.unfinished = ~0u, sh.first_b = -1;
         sh.copied[0] = sh.copied[1] = sh.q_copied = 0;
@@ -318,9 +351,8 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
     __syncthreads();
     const uint32_t tmem = sh.tmem;
     const int tt = tile_tokens<D>(a);
-
     if (warp == C::PRODUCER_K || warp == C::PRODUCER_V) {
-        // ---------------------------------------------------------------- work items and TMA copies: one thread each
+        // ---------------------------------------------------------------- TMA copies: one thread each; that of V also finds the items
         if (ptx::elect_one()) {
             const int ps = 1 << a.log_page;
             unsigned filled = 0;    // tiles whose copies were issued
@@ -333,22 +365,29 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 constexpr int NS = IS_V ? C::NV : C::NK;
                 uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *frees = IS_V ? sh.v_free : sh.k_free;
                 unsigned char *ring = IS_V ? v_ring : k_ring;
-                Walk walk{sh.first_b, sh.first_off, u0, sh.first_seq};
+                Walk walk = walk_from<D>(a, IS_V ? sh.first_b : -1, sh.first_off, u0, sh.first_seq);
                 const Part part{u0, u1, W, parts, group};
+                unsigned found = 0;     // items
+                auto find = [&]() -> bool {
+                    Item it;
+                    next_item<D>(a, ws, part, walk, it, true);
+                    if (found >= ITEMS && !ptx::mbar_wait(&sh.item_empty[found % ITEMS], (found / ITEMS - 1) & 1)) return false;
+                    sh.items[found % ITEMS] = it;
+                    ptx::mbar_arrive(&sh.item_full[found % ITEMS]);
+                    ++found;
+                    return true;
+                };
+                if (IS_V && !find()) return;
                 for (unsigned ord = 0;; ++ord) {
                     const unsigned r = ord % ITEMS;
-                    Item it;
-                    if constexpr (!IS_V) {
-                        next_item<D>(a, ws, part, walk, it, true);
-                        if (ord >= ITEMS && !ptx::mbar_wait(&sh.item_empty[r], (ord / ITEMS - 1) & 1)) return;
-                        sh.items[r] = it;
-                        ptx::mbar_arrive(&sh.item_full[r]);
-                    } else {
-                        if (!ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return;
-                        it = sh.items[r];
-                        if (it.tiles > 0) ptx::mbar_arrive(&sh.item_empty[r]);
-                    }
+                    if (!IS_V && !ptx::mbar_wait(&sh.item_full[r], (ord / ITEMS) & 1)) return;
+                    const Item it = sh.items[r];
                     if (it.tiles == 0) return;
+                    if (IS_V) {             // the next item, ahead of this one's copies
+                        if (!find()) return;
+                    } else {
+                        ptx::mbar_arrive(&sh.item_empty[r]);
+                    }
                     if (it.b * a.c.H_kv + it.h == a.skip_item) return;  // (test hook)
                     if constexpr (!IS_V) {  // the queries of the item
                         if (ord > 0 && !ptx::mbar_wait(&sh.q_free, (ord - 1) & 1)) return;
@@ -362,28 +401,30 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     }
                     const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
                     const View all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
+                    const Tiles tiles(it);
+                    const int n = it.tiles;
                     bool bad = false;
                     // pages of the next tile, looked up one tile ahead
                     constexpr int UNSEEN = -1;  // (a negative entry becomes a large one)
                     int pages[B::P], next[B::P];
                     auto look = [&](int j, int (&to)[B::P]) {
-                        const int x0 = cache_tile(it, j) * KT;
+                        const int x0 = tiles(j) * KT;
 #pragma unroll
                         for (int i = 0; i < B::P; ++i)
-                            to[i] = j < it.j0 + it.tiles && sees_some(a, all, x0 + i * BOX, BOX) ? table[(x0 + i * BOX) >> a.log_page] & 0x7fffffff : UNSEEN;
+                            to[i] = j < n && sees_some(a, all, x0 + i * BOX, BOX) ? table[(x0 + i * BOX) >> a.log_page] & 0x7fffffff : UNSEEN;
                     };
-                    look(it.j0, next);
-                    for (int j = it.j0; j < it.j0 + it.tiles; ++j) {
+                    look(0, next);
+#pragma unroll 1
+                    for (int j = 0; j < n; ++j) {
                         const unsigned sidx = filled % NS;
-                        const int x0 = cache_tile(it, j) * KT, slot0 = x0 & (ps - 1);
+                        const int slot = BOX < KT ? 0 : tiles(j) * KT & (ps - 1);
                         int boxes = 0;
 #pragma unroll
                         for (int i = 0; i < B::P; ++i) {
                             pages[i] = next[i];
-                            if (pages[i] != UNSEEN) {
-                                ++boxes;
-                                if (pages[i] >= a.c.n_pages) bad = true, pages[i] = a.c.n_pages;  // (one past the pool reads as zeros)
-                            }
+                            if (pages[i] == UNSEEN) continue;
+                            ++boxes;
+                            if (pages[i] >= a.c.n_pages) bad = true, pages[i] = a.c.n_pages;  // (one past the pool reads as zeros)
                         }
                         look(j + 1, next);
                         if (bad && !IS_V) {
@@ -398,7 +439,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
 #pragma unroll
                         for (int i = 0; i < B::P; ++i) {
                             if (pages[i] == UNSEEN) continue;  // (no row sees it: left as it is, never used)
-                            const int slot = BOX < KT ? (x0 + i * BOX) & (ps - 1) : slot0;
                             if constexpr (IS_V) {
                                 ptx::tma_load_5d(dst + i * (BOX * C::NC * 128), map, 0, slot, 0, it.h, pages[i], full);
                             } else if constexpr (B::K_BY_CHUNK) {
@@ -422,10 +462,12 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
             sh.copied[warp == C::PRODUCER_V] = filled;
         }
         __syncwarp();
-    } else if (warp == C::MMA) {
-        // ---------------------------------------------------------------- MMAs: one thread
+    } else if (warp >= C::MMA) {
+        // ---------------------------------------------------------------- MMAs: a thread to each stream; of one stream, one to Q K^T and
+        // one to P V (a single thread for all was the slowest role: what it does between two MMAs alone took as long as a tile)
         if (ptx::elect_one()) {
             constexpr uint32_t idesc_qk = ptx::umma_idesc_bf16_f32(MT, KT), idesc_pv = ptx::umma_idesc_bf16_f32_bmn(MT, D);
+            const int me = warp - C::MMA, strm = C::STREAMS == 2 ? me : 0;
             // Descriptors: stages, streams and steps only add to the address, 16 bytes a unit in the low bits
             const uint64_t qd = ptx::umma_desc_k_sw128(ptx::smem_u32(q_tiles)), kd = ptx::umma_desc_k_sw128(ptx::smem_u32(k_ring), lay.k_group);
             const uint64_t q_hi = qd & ~0xffffffffull, k_hi = kd & ~0xffffffffull;
@@ -438,32 +480,51 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 const uint64_t vd = ptx::umma_desc_mn_sw128(ptx::smem_u32(v_ring) + off, lay.v_rows * 128, lay.v_rows == 8 ? C::NC * 1024 : 1024);
                 v_hi = vd & ~0xffffffffull, v_lo[s] = (uint32_t)vd;
             }
+            const uint32_t tm_o = tmem + strm * D, tm_s = tmem + C::TM_S + strm * C::NB * KT;
+            uint64_t *const s_full = sh.s_full + strm * C::NB, *const p_full = sh.p_full + strm * C::NB, *const pv_done = sh.pv_done + strm * C::NB;
             unsigned g0 = 0;              // tiles of the items before
-            unsigned made[2] = {0, 0}, used[2] = {0, 0};  // tiles of a stream whose scores, whose products were issued
-            // scores of tile g for stream s; q: which row tile
-            auto scores = [&](unsigned g, int s, int q) -> bool {
+            unsigned made = 0, used = 0;  // tiles of this stream whose scores, whose products were issued
+            // scores of tile g; q: low word of the queries' descriptor
+            auto scores = [&](unsigned g, uint32_t ql) -> bool {
+                const uint32_t buf = made % C::NB;
+                // (in the other case the same thread has issued that product before)
+                if (C::STREAMS == 1 && made >= C::NB && !ptx::mbar_wait(&pv_done[buf], (made / C::NB - 1) & 1)) return false;
                 if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
                 ptx::tc_fence_after_sync();
-                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16), ql = q_lo + q * (C::Q_TILE / 16), buf = s * C::NB + made[s] % C::NB;
+                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16);
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c)
-                    ptx::umma_bf16(tmem + C::TM_S + buf * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2),
-                                   k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk, c > 0);
-                ptx::umma_commit(&sh.s_full[buf]);
-                ++made[s];
+                    ptx::umma_bf16(tm_s + buf * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2), k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk,
+                                   c > 0);
+                ptx::umma_commit(&s_full[buf]);
+                ptx::umma_commit(&sh.k_free[g % C::NK]);
+                ++made;
                 return true;
             };
-            // output of tile g onto O of stream s
-            auto product = [&](unsigned g, int s, bool onto) -> bool {
-                const uint32_t buf = s * C::NB + used[s] % C::NB;
+            // output of tile g
+            auto product = [&](unsigned g, bool onto) -> bool {
+                const uint32_t buf = used % C::NB;
                 if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
-                if (!ptx::mbar_wait(&sh.p_full[buf], (used[s] / C::NB) & 1)) return false;
+                if (!ptx::mbar_wait(&p_full[buf], (used / C::NB) & 1)) return false;
                 ptx::tc_fence_after_sync();
 #pragma unroll
                 for (int c = 0; c < KT / 16; ++c)
-                    ptx::umma_bf16_ts(tmem + s * D, tmem + C::TM_S + buf * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
-                ptx::umma_commit(&sh.pv_done[buf]);
-                ++used[s];
+                    ptx::umma_bf16_ts(tm_o, tm_s + buf * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
+                ptx::umma_commit(&pv_done[buf]);
+                ptx::umma_commit(&sh.v_free[g % C::NV]);
+                ++used;
+                return true;
+            };
+            // a tile that this stream takes no part in: its stages are free as far as this thread goes (once they are filled: an
+            // arrival ahead of that would count for the tile before)
+            auto pass_k = [&](unsigned g) -> bool {
+                if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
+                ptx::mbar_arrive(&sh.k_free[g % C::NK]);
+                return true;
+            };
+            auto pass_v = [&](unsigned g) -> bool {
+                if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
+                ptx::mbar_arrive(&sh.v_free[g % C::NV]);
                 return true;
             };
             auto run = [&]() -> bool {
@@ -473,49 +534,46 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     const Item it = sh.items[r];
                     if (it.tiles == 0) return true;
                     ptx::mbar_arrive(&sh.item_empty[r]);
-                    if (!ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
                     const int n = it.tiles;
-                    // Scores run `ahead` tiles ahead of the products: as many as there are S buffers for.
                     const bool pair = C::STREAMS == 2 && it.pair;
+                    // Scores run `ahead` tiles ahead of the products: as many as there are S buffers for.
                     const int ahead = pair || C::STREAMS == 1 ? C::NB : 2 * C::NB;
-                    const View v[2] = {view_of(it, tt, 0), view_of(it, tt, 1)};
-                    // whether stream s takes part in tile j (from j0 on): with two row tiles as far as it sees some of it, else in turn
-                    auto on = [&](int j, int s) {
-                        if (!pair) return C::STREAMS == 1 || (j & 1) == s;
-                        return sees_some(a, v[s], cache_tile(it, it.j0 + j) * KT, KT);
-                    };
-                    auto scores_of = [&](int j) -> bool {
-                        for (int s = 0; s < C::STREAMS; ++s)
-                            if (on(j, s) && !scores(g0 + j, s, pair ? s : 0)) return false;
-                        ptx::umma_commit(&sh.k_free[(g0 + j) % C::NK]);
-                        if (j + 1 == n) ptx::umma_commit(&sh.q_free);
-                        return true;
-                    };
-                    bool onto[2] = {false, false};
-                    for (int j = 0; j < ahead && j < n; ++j)
-                        if (!scores_of(j)) return false;
-                    for (int s = 0; s < C::STREAMS; ++s)
-                        if (ord > 0 && !ptx::mbar_wait(&sh.o_free[s], (ord - 1) & 1)) return false;
-                    for (int j = 0; j < n; ++j) {
-                        const bool more = j + ahead < n;
-                        for (int s = 0; s < C::STREAMS; ++s) {
-                            if (on(j, s)) {
-                                if (!product(g0 + j, s, onto[s])) return false;
-                                onto[s] = true;
+                    const Span span = span_of(a, view_of(it, tt, strm));
+                    const Tiles tiles(it);
+                    // whether this stream takes part in tile j: with two row tiles as far as it sees some of it, else in turn
+                    auto on = [&](int j) { return C::STREAMS == 1 || (pair ? span.some(tiles(j)) : (j & 1) == strm); };
+                    const uint32_t ql = q_lo + (pair ? strm : 0) * (C::Q_TILE / 16);
+                    const bool does_qk = C::STREAMS == 2 || me == 0, does_pv = C::STREAMS == 2 || me == 1;
+                    if (does_qk && !ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
+                    if (does_pv && ord > 0 && C::STREAMS == 1 && !ptx::mbar_wait(&sh.o_free[0], (ord - 1) & 1)) return false;
+                    bool onto = false;
+#pragma unroll 1
+                    for (int t = 0; t < n + ahead; ++t) {  // scores of tile t, products of tile j
+                        const int j = t - ahead;
+                        if (C::STREAMS == 2 && j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free[strm], (ord - 1) & 1)) return false;
+                        if (does_pv && j >= 0) {
+                            if (on(j)) {
+                                if (!product(g0 + j, onto)) return false;
+                                onto = true;
+                            } else if (!pass_v(g0 + j)) {
+                                return false;
                             }
-                            // (each stream's next scores right behind its product: the other's wait for its weights must not hold them up)
-                            if (more && on(j + ahead, s) && !scores(g0 + j + ahead, s, pair ? s : 0)) return false;
                         }
-                        ptx::umma_commit(&sh.v_free[(g0 + j) % C::NV]);
-                        if (more) ptx::umma_commit(&sh.k_free[(g0 + j + ahead) % C::NK]);
-                        if (j + ahead + 1 == n) ptx::umma_commit(&sh.q_free);
+                        if (does_qk && t < n) {
+                            if (on(t)) {
+                                if (!scores(g0 + t, ql)) return false;
+                            } else if (!pass_k(g0 + t)) {
+                                return false;
+                            }
+                            if (t + 1 == n) ptx::umma_commit(&sh.q_free);
+                        }
                     }
                     g0 += n;
                 }
             };
             if (!run()) {  // MMAs in flight have to end before the CTA may leave: a commit behind all of them, on a barrier of its own
-                ptx::umma_commit(&sh.end);
-                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.end, 0); ++t) __nanosleep(20);
+                ptx::umma_commit(&sh.end[me]);
+                for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.end[me], 0); ++t) __nanosleep(20);
             }
         }
         __syncwarp();
@@ -525,9 +583,11 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
         const float sl2 = a.scale * 1.4426950408889634f;
         const int strm = C::STREAMS == 1 ? 0 : wg;  // this warpgroup's stream
+        const int tok = row / a.G;    // this row's token in a row tile
         unsigned count = 0;           // its tiles so far
-        unsigned g0 = 0, ord = 0, singles = 0;
+        unsigned g0 = 0, ord = 0;
         auto wait_product = [&](unsigned i) { return wait_warp(&sh.pv_done[strm * C::NB + i % C::NB], (i / C::NB) & 1); };  // of this stream's tile i
+        unsigned singles = 0;
         auto run = [&]() -> bool {
             for (;; ++ord) {
                 if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
@@ -536,24 +596,38 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 if (n == 0) return true;
                 const bool pair = C::STREAMS == 2 && it.pair;
                 const View v = view_of(it, tt, pair ? wg : 0), all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
+                const Span span = span_of(a, v);
+                const Tiles tiles(it);
                 const int rows = (v.p1 - v.p0 + 1) * a.G;
                 const bool warp_on = w4 * 32 < rows, on = row < rows;
-                const int tok = row / a.G, p = v.p0 + (on ? tok : 0);  // this row's position
+                const int p = v.p0 + (on ? tok : 0);  // this row's position
+                const int step = pair || C::STREAMS == 1 ? 1 : 2;
+                // this stream's next tile from j on
+                auto at_or_after = [&](int j) {
+                    while (j < n && pair && !span.some(tiles(j))) ++j;
+                    return j;
+                };
                 float m = -INFINITY, l = 0.f;
                 int taken = 0;             // tiles of this stream
-                for (int j = pair || C::STREAMS == 1 ? 0 : wg; j < n; j += pair || C::STREAMS == 1 ? 1 : 2) {
+                uint32_t x[KT];            // a row of S
+                bool loaded = false;       // (its next tile's is on its way there)
+                for (int j = at_or_after(step == 1 ? 0 : wg), next; j < n; j = next) {
                     const unsigned g = g0 + j;
-                    const int buf = strm * C::NB + count % C::NB;
-                    const int x0 = cache_tile(it, it.j0 + j) * KT;
-                    if (pair && !sees_some(a, v, x0, KT)) continue;
-                    if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
-                    ptx::tc_fence_after_sync();
-                    const bool masked = !sees_all(a, v, x0, KT);
+                    const int buf = strm * C::NB + count % C::NB, kt = tiles(j), x0 = kt * KT;
+                    const bool masked = !span.all(kt);
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
-                    if (warp_on) {
-                        uint32_t x[KT];
+                    auto load = [&](uint32_t from) {
 #pragma unroll
-                        for (int c = 0; c < KT; c += 32) ptx::tmem_ld32(ts + c, *reinterpret_cast<uint32_t(*)[32]>(&x[c]));
+                        for (int c = 0; c < KT; c += 32) ptx::tmem_ld32(from + c, *reinterpret_cast<uint32_t(*)[32]>(&x[c]));
+                    };
+                    if (!loaded) {
+                        if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
+                        ptx::tc_fence_after_sync();
+                        if (warp_on) load(ts);
+                    }
+                    next = at_or_after(j + step);
+                    loaded = false;
+                    if (warp_on) {
                         ptx::tmem_wait_ld();
                         if (masked) {
                             const int hi = min(p - x0, KT) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
@@ -567,41 +641,58 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         }
                         float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                        for (int i = 0; i < KT; i += 2) t[(i >> 1) & 3] = ptx::max3(t[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-                        const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * sl2;
+                        for (int i = 0; i < KT; i += 2) t[(i >> 1) & 3] = ptx::max3_nan(t[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                        const float top = ptx::max3_nan(ptx::max3_nan(t[0], t[1], t[2]), t[3], t[3]) * sl2;
                         const float m0 = m;
                         const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
                         m = grow ? top : m0;
                         const float ref = m == -INFINITY ? 0.f : m;
+                        const unsigned nc = count + 1, nbuf = strm * C::NB + nc % C::NB;
+                        const bool ready = next < n && ptx::mbar_try_wait(&sh.s_full[nbuf], (nc / C::NB) & 1);
                         const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-ref, -ref);
                         float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                        uint32_t w[KT / 2];
+                        auto weights = [&](auto whole_) {
 #pragma unroll
-                        for (int i = 0; i < KT; i += 2) {
-                            float2 y = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
-                            y.x = ptx::ex2(y.x), y.y = ptx::ex2(y.y);
-                            acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
-                            // weights as bf16: at most 2^-8 of each, independent from key to key
-                            x[i / 2] = pack_bf16(y.x, y.y);
+                            for (int i = 0; i < KT; i += 2) {
+                                const float2 z = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
+                                float2 y;
+                                if (decltype(whole_)::value && (i / 2) % C::POLY_OF < C::POLY) y = ptx::ex2_poly(z);
+                                else y = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
+                                acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
+                                // weights as bf16: at most 2^-8 of each, independent from key to key
+                                w[i / 2] = pack_bf16(y.x, y.y);
+                            }
+                        };
+                        // (the polynomial does not give 0 for minus infinity, so masked tiles go without it)
+                        if (masked) weights(std::false_type{});
+                        else weights(std::true_type{});
+                        // S of the next tile while these weights are stored
+                        loaded = __all_sync(0xffffffffu, ready);
+                        if (loaded) {
+                            ptx::tc_fence_after_sync();
+                            load(tmem + lane_base + C::TM_S + nbuf * KT);
                         }
 #pragma unroll
-                        for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&x[c]));
+                        for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&w[c]));
                         if (grow) l *= ptx::ex2(m0 - m);
                         l += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
+                        // A score of NaN or plus infinity makes the row NaN, by its sum: the polynomial lets neither through.
+                        if (!(top < INFINITY)) l = __uint_as_float(0x7fffffffu);
                         if (taken > 0 && __any_sync(0xffffffffu, grow)) {
                             // O at rest: the stream's product before this one is done, and the next one waits for these weights
                             if (!wait_product(count - 1)) return false;
                             ptx::tc_fence_after_sync();
                             const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
                                 const uint32_t to = tmem + lane_base + strm * D + c;
-                                ptx::tmem_ld32(to, o);
+                                ptx::tmem_ld16(to, o);
                                 ptx::tmem_wait_ld();
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                ptx::tmem_st16(to, *reinterpret_cast<const uint32_t(*)[16]>(&o[0]));
-                                ptx::tmem_st16(to + 16, *reinterpret_cast<const uint32_t(*)[16]>(&o[16]));
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                ptx::tmem_st16(to, o);
                             }
                         }
                         ptx::tmem_wait_st();
@@ -639,7 +730,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                             }
                         }
                         ptx::fence_proxy_async();
-                        __syncwarp();
                     }
                     // every warp's part of the values has to be clean before any of them is used: p_full counts all four
                     ptx::tc_fence_before_sync();
@@ -730,7 +820,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
 #pragma unroll 1
                         for (int j = 0; j < n; ++j) {
-                            const int x0 = cache_tile(it, it.j0 + j) * KT;
+                            const int x0 = tiles(j) * KT;
                             if (sees_all(a, all, x0, KT)) continue;
 #pragma unroll 1
                             for (int x = x0; x < x0 + KT; ++x) {
@@ -769,22 +859,27 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
             if (lane == 0) atomicMin(&sh.unfinished, ord);
         }
         __syncwarp();
+        ptx::tc_fence_before_sync();
+        ptx::named_arrive(1, C::THREADS);
+        return;
     }
+    // ---- what is left when all have come to their end: the other warpgroup's work
     ptx::tc_fence_before_sync();
-    __syncthreads();
+    ptx::named_sync(1, C::THREADS);
     ptx::tc_fence_after_sync();
+    const int rest = tid - C::SOFT_WARPS * 32;
     if (sh.unfinished != ~0u) {
-        if (tid < 2) {  // copies in flight have to land before the CTA may leave
-            const unsigned filled = sh.copied[tid], ns = tid ? C::NV : C::NK;
-            uint64_t *fulls = tid ? sh.v_full : sh.k_full;
+        if (rest < 2) {  // copies in flight have to land before the CTA may leave
+            const unsigned filled = sh.copied[rest], ns = rest ? C::NV : C::NK;
+            uint64_t *fulls = rest ? sh.v_full : sh.k_full;
             for (unsigned i = filled > ns ? filled - ns : 0; i < filled; ++i)
                 for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&fulls[i % ns], (i / ns) & 1); ++t) __nanosleep(20);
-            if (tid == 0 && sh.q_copied > 0)
+            if (rest == 0 && sh.q_copied > 0)
                 for (int t = 0; t < 100000 && !ptx::mbar_try_wait(&sh.q_full, (sh.q_copied - 1) & 1); ++t) __nanosleep(20);
         }
-        mark_unfinished<D>(a, ws, sh.part, Walk{sh.first_b, sh.first_off, sh.part.u0, sh.first_seq}, sh.unfinished);
+        mark_unfinished<D>(a, ws, sh.part, walk_from<D>(a, sh.first_b, sh.first_off, sh.part.u0, sh.first_seq), sh.unfinished, rest, 128);
     }
-    __syncthreads();
+    ptx::named_sync(2, 128);
     if (warp == C::MMA) ptx::tmem_dealloc(tmem, 512);
 }
 

@@ -377,7 +377,6 @@ __device__ __forceinline__ float tf32_hi(float x) { return __uint_as_float(__flo
 // x to the nearest bf16, as a float (the hi part of a two-term bf16 split; lo = bf16(x - hi) leaves 2^-18 |x|)
 __device__ __forceinline__ float bf16_hi(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
 
-
 }  // namespace ptx
 }  // namespace treewy
 
@@ -432,6 +431,13 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// ... and NaN where one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // two fp32 operations in one instruction, each rounded as the single ones
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
@@ -458,6 +464,23 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// 2^x of two values on the FMA pipes: x = i + f with i the nearest integer (its two's complement is left in the low bits by
+// the addition of 1.5 * 2^23) and 2^f by a polynomial, i added to its exponent.  The coefficients are the minimax ones of degree
+// 3 for the relative error on [-1/2, 1/2] (Remez exchange on p(f) 2^-f - 1): 7.5e-5 = 2^-13.7.  Below -126 the result
+// stays 2^-126; NaN and +infinity give no meaningful result.
+__device__ __forceinline__ float2 ex2_poly(float2 x)
+{
+    x.x = fmaxf(x.x, -126.f), x.y = fmaxf(x.y, -126.f);
+    const float magic = 12582912.f;
+    const float2 t = add2(x, make_float2(magic, magic)), i = add2(t, make_float2(-magic, -magic));
+    const float2 f = fma2(i, make_float2(-1.f, -1.f), x);
+    float2 p = fma2(f, make_float2(0.0551716685295105f, 0.0551716685295105f), make_float2(0.2426111251115799f, 0.2426111251115799f));
+    p = fma2(p, f, make_float2(0.6932609677314758f, 0.6932609677314758f));
+    p = fma2(p, f, make_float2(0.9999280571937561f, 0.9999280571937561f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
 }  // namespace ptx
