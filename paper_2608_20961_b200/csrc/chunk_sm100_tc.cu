@@ -27,12 +27,14 @@ namespace {
 
 constexpr int MT = 128;                // rows of a tile
 constexpr int KT = 64;                 // keys of a tile
-constexpr int MAX_STAGES = 10;         // of a ring
 constexpr int MAX_CTAS = 160;
 constexpr int ITEMS = 8;               // ring of work items between the producer and the other roles
 constexpr int START = 256;             // cost of an item's start, in keys
 constexpr int MIN_UNITS = 256;         // least units of a part; at least a tile's keys, so that a part inside an item holds the start of one
+constexpr int UNSEEN = -0x7fffffff;    // for a page that is not looked up
 constexpr float LAZY = 8.f;
+constexpr float LOWEST = -3e38f;
+constexpr int HK = KT / 2;             // keys of a tile that a softmax thread has
 constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;  // l of a row whose part is not there
 
 template <int D> struct Cfg {
@@ -40,13 +42,11 @@ template <int D> struct Cfg {
     static constexpr int STREAMS = D == 256 ? 1 : 2;     // what 512 columns of tensor memory leave
     static constexpr int STAGE = NC * KT * 128;          // bytes of a tile
     static constexpr int NB = D == 256 ? 4 : 2;          // S buffers of a stream
-    static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 5 : 2;
+    static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 4 : 2;
     static constexpr int Q_TILE = NC * MT * 128;
     static constexpr int TILES = STREAMS * Q_TILE + (NK + NV) * STAGE;  // bytes
-    static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 2, PRODUCER_V = MMA + 3;  // (two of MMA)
+    static constexpr int SOFT_WARPS = 8 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 2, PRODUCER_V = MMA + 3;  // (two of MMA)
     static constexpr int THREADS = (SOFT_WARPS + 4) * 32;
-    // Of POLY_OF pairs of weights POLY are worked out on the FMA pipes, the others by the special-function unit.
-    static constexpr int POLY = 0, POLY_OF = 4;
     static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer b of it at 256 + (s * NB + b) * KT
     static constexpr int CAP = STREAMS * MT;             // rows of an item at most
 };
@@ -89,16 +89,21 @@ struct Walk {                   // a CTA's way along its part
     Seq s;
 };
 
-struct Shared {
-    uint64_t k_full[MAX_STAGES], k_free[MAX_STAGES], v_full[MAX_STAGES], v_free[MAX_STAGES];
+template <int D> struct Shared {
+    using C = Cfg<D>;
+    uint64_t k_full[C::NK], k_free[C::NK], v_full[C::NV], v_free[C::NV];
     // Of an S buffer: filled, its weights stored, its product done.  (One to a buffer: a parity names a phase only to who has seen
     // the one before it, and a full S says that the buffer's last product is done.)
     uint64_t s_full[4], p_full[4], pv_done[4], o_free[2], q_full, q_free, item_full[ITEMS], item_empty[ITEMS], ml_full[4], end[2];
     Item items[ITEMS];
-    float2 ml[MT];              // of the second stream's rows, for the first
+    float2 ml[C::STREAMS == 2 ? MT : 1];  // of the second stream's rows, for the first
     unsigned bad_item[8];       // ordinal + 1 of an item that met a page out of range
     unsigned nonfinite[8];      // ordinal + 1 of an item with NaN or infinity among the values of its masked tiles
-    long long scan[12], first_off;
+    union {
+        uint32_t swap[C::STREAMS][2][2][MT];  // between the threads of a row
+        long long scan[C::THREADS / 32];      // (before any of that)
+    };
+    long long first_off;
     Seq first_seq;              // of sequence first_b
     Part part;
     int first_b;
@@ -234,11 +239,10 @@ __device__ __forceinline__ View view_of(const Item &it, int tt, int s)
     const int first = it.pair ? s * tt : 0, last = it.pair && s == 0 ? tt : it.tokens;
     return {it.len + it.t0 + first, it.len + it.t0 + last - 1};
 }
-// The same for whole tiles, worked out once: tile kt is seen by some row of the view, or whole by every row.
+// The same for whole tiles kt: some row sees some of one if kt <= high_some and kt >= low_some or kt < sink_some, every row all of it if
+// kt < high_all and kt >= low_all or kt < sink_all.
 struct Span {
     int sink_some, low_some, high_some, sink_all, low_all, high_all;
-    __device__ __forceinline__ bool some(int kt) const { return kt <= high_some && (kt >= low_some || kt < sink_some); }
-    __device__ __forceinline__ bool all(int kt) const { return kt < high_all && (kt >= low_all || kt < sink_all); }
 };
 __device__ __forceinline__ Span span_of(const ChunkArgs &a, const View &v)
 {
@@ -251,6 +255,28 @@ struct Tiles {
     __device__ __forceinline__ explicit Tiles(const Item &it) : sinks(it.sink_tiles - it.j0), first(it.j0), then(it.low_tile - it.sink_tiles + it.j0) {}
     __device__ __forceinline__ int operator()(int j) const { return j + (j < sinks ? first : then); }
 };
+// A stream's part in an item's tiles here.  With two row tiles: j < hole (the sinks') and from `on_again` to `end`, else (as far as
+// this goes) all.  Those that every row sees whole: j < sinks_whole, and from `whole` to `whole_end`.  (Tiles of the window may be the
+// sinks' too.)
+struct Turns {
+    int hole, on_again, end, sinks_whole, whole, whole_end;
+    __device__ __forceinline__ bool some(int j) const { return j < end && (j < hole || j >= on_again); }
+    __device__ __forceinline__ bool all(int j) const { return j < sinks_whole || (j >= whole && j < whole_end); }
+    __device__ __forceinline__ int at_or_after(int j) const { return j >= hole && j < on_again ? on_again : j; }
+};
+__device__ __forceinline__ Turns turns_of(const Item &it, const Span &s, bool pair)
+{
+    const Tiles tiles(it);
+    const int n = it.tiles, sink_part = max(min(tiles.sinks, n), 0);
+    auto below = [&](int kt) { return kt - tiles.first <= sink_part ? kt - tiles.first : max(sink_part, kt - tiles.then); };  // tiles j before the cache's kt
+    Turns t;
+    t.end = pair ? min(n, max(sink_part, s.high_some - tiles.then + 1)) : n;
+    t.hole = pair ? min(t.end, below(max(s.sink_some, tiles.first + sink_part))) : n;
+    t.on_again = pair ? max(t.hole, s.low_some - tiles.then) : n;
+    t.sinks_whole = below(min(s.sink_all, s.high_all));
+    t.whole = max(sink_part, s.low_all - tiles.then), t.whole_end = s.high_all - tiles.then;
+    return t;
+}
 // Whether some row of the view sees some token of tokens x0 .. x0 + n - 1
 __device__ __forceinline__ bool sees_some(const ChunkArgs &a, const View &v, int x0, int n)
 {
@@ -265,6 +291,14 @@ __device__ __forceinline__ bool sees(const ChunkArgs &a, int p, int x) { return 
 
 __device__ __forceinline__ uint32_t low32(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// Waits until the word's lowest bit is `tag` for every lane, each with its own word.
+static __device__ __noinline__ bool swap_slow(const volatile uint32_t *word, uint32_t tag)
+{
+    for (;;) {
+        if (__all_sync(0xffffffffu, (*word & 1) == tag)) return true;
+        if (__any_sync(0xffffffffu, ptx::wait_deadline_passed())) return false;
+    }
+}
 // a wait with one outcome for the whole warp: what follows needs all of its lanes
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)); }
 
@@ -276,17 +310,18 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
     using C = Cfg<D>;
     // barriers and the like first, tiles behind them: the bytes that aligning the tiles takes are used so
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    Shared &sh = *reinterpret_cast<Shared *>(smem_raw);
-    unsigned char *q_tiles = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw + sizeof(Shared)) + 1023) & ~uintptr_t(1023));
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(smem_raw);
+    unsigned char *q_tiles = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw + sizeof(Shared<D>)) + 1023) & ~uintptr_t(1023));
     unsigned char *k_ring = q_tiles + C::STREAMS * C::Q_TILE, *v_ring = k_ring + C::NK * C::STAGE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
         ptx::wait_deadline_init(a.wait_cycles);
 #pragma unroll 1
-        for (int i = 0; i < MAX_STAGES; ++i)
-            ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], C::STREAMS), ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], C::STREAMS);
-        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
+        for (int i = 0; i < C::NK; ++i) ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], C::STREAMS);
+#pragma unroll 1
+        for (int i = 0; i < C::NV; ++i) ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], C::STREAMS);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 8), ptx::mbar_init(&sh.pv_done[i], 1);
         for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
         ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, C::STREAMS), ptx::mbar_init(&sh.end[0], 1), ptx::mbar_init(&sh.end[1], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
@@ -349,10 +384,13 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
     }
     if (tid == 0) sh.part = {u0, u1, W, parts, group};
     __syncthreads();
+    for (int i = tid; i < C::STREAMS * 4 * MT; i += C::THREADS) (&sh.swap[0][0][0][0])[i] = 1;  // (neither of the first two uses')
+    __syncthreads();
     const uint32_t tmem = sh.tmem;
     const int tt = tile_tokens<D>(a);
     if (warp == C::PRODUCER_K || warp == C::PRODUCER_V) {
         // ---------------------------------------------------------------- TMA copies: one thread each; that of V also finds the items
+        // (A thread alone takes some 6 cycles for an instruction: what it does for a tile is kept short.)
         if (ptx::elect_one()) {
             const int ps = 1 << a.log_page;
             unsigned filled = 0;    // tiles whose copies were issued
@@ -363,8 +401,9 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 using B = Boxes<D, BOX>;
                 const CUtensorMap *map = IS_V ? &map_v : &map_k;
                 constexpr int NS = IS_V ? C::NV : C::NK;
-                uint64_t *fulls = IS_V ? sh.v_full : sh.k_full, *frees = IS_V ? sh.v_free : sh.k_free;
-                unsigned char *ring = IS_V ? v_ring : k_ring;
+                uint64_t *const fulls = IS_V ? sh.v_full : sh.k_full, *const frees = IS_V ? sh.v_free : sh.k_free;
+                const uint32_t ring = ptx::smem_u32(IS_V ? v_ring : k_ring);
+                unsigned stage = 0, phase = 0;  // of the next tile
                 Walk walk = walk_from<D>(a, IS_V ? sh.first_b : -1, sh.first_off, u0, sh.first_seq);
                 const Part part{u0, u1, W, parts, group};
                 unsigned found = 0;     // items
@@ -402,55 +441,69 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
                     const View all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
                     const Tiles tiles(it);
-                    const int n = it.tiles;
-                    bool bad = false;
-                    // pages of the next tile, looked up one tile ahead
-                    constexpr int UNSEEN = -1;  // (a negative entry becomes a large one)
-                    int pages[B::P], next[B::P];
+                    const int n = it.tiles, h = it.h;
+                    // tiles of the cache of which every page is seen: what is needed of others is looked at page by page
+                    const int low = a.window > all.p0 ? 0 : all.p0 - a.window + 1;
+                    const int low_whole = low > 0 ? (low - 1) / KT + 1 : 0, high_whole = (all.p1 + 1) / KT, sinks_whole = a.sinks / KT;
                     auto look = [&](int j, int (&to)[B::P]) {
-                        const int x0 = tiles(j) * KT;
+                        const int kt = tiles(j), x0 = kt * KT;
+                        const int32_t *t = table + (x0 >> a.log_page);
+                        if (kt < high_whole && (kt >= low_whole || kt < sinks_whole)) {
 #pragma unroll
-                        for (int i = 0; i < B::P; ++i)
-                            to[i] = j < n && sees_some(a, all, x0 + i * BOX, BOX) ? table[(x0 + i * BOX) >> a.log_page] & 0x7fffffff : UNSEEN;
+                            for (int i = 0; i < B::P; ++i) to[i] = t[i];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < B::P; ++i) {
+                                to[i] = UNSEEN;
+                                if (sees_some(a, all, x0 + i * BOX, BOX)) {
+                                    to[i] = t[i];
+                                    if (to[i] == UNSEEN) to[i] = -1;
+                                }
+                            }
+                        }
                     };
+                    bool bad = false;
+                    int next[B::P];
                     look(0, next);
 #pragma unroll 1
                     for (int j = 0; j < n; ++j) {
-                        const unsigned sidx = filled % NS;
+                        int pages[B::P];
+                        uint32_t bytes = BOX * C::NC * 128 * B::P;
+                        bool odd = false;
+#pragma unroll
+                        for (int i = 0; i < B::P; ++i) pages[i] = next[i], odd |= (unsigned)pages[i] >= (unsigned)a.c.n_pages;
+                        if (odd) {          // pages that no row sees, and such as there are not
+#pragma unroll
+                            for (int i = 0; i < B::P; ++i) {
+                                if (pages[i] == UNSEEN) bytes -= BOX * C::NC * 128;
+                                else if ((unsigned)pages[i] >= (unsigned)a.c.n_pages) bad = true, pages[i] = a.c.n_pages;  // (one past the pool reads as zeros)
+                            }
+                            if (bad && !IS_V) {
+                                sh.bad_item[ord % 8] = ord + 1;
+                                if (a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
+                            }
+                        }
                         const int slot = BOX < KT ? 0 : tiles(j) * KT & (ps - 1);
-                        int boxes = 0;
-#pragma unroll
-                        for (int i = 0; i < B::P; ++i) {
-                            pages[i] = next[i];
-                            if (pages[i] == UNSEEN) continue;
-                            ++boxes;
-                            if (pages[i] >= a.c.n_pages) bad = true, pages[i] = a.c.n_pages;  // (one past the pool reads as zeros)
-                        }
-                        look(j + 1, next);
-                        if (bad && !IS_V) {
-                            sh.bad_item[ord % 8] = ord + 1;
-                            if (a.seq_status) atomicOr(&a.seq_status[it.b], TREEWY_SEQ_BAD_PAGE);
-                        }
-                        if (filled >= NS && !ptx::mbar_wait(&frees[sidx], (filled / NS - 1) & 1)) return;
+                        if (j + 1 < n) look(j + 1, next);
+                        if (!ptx::mbar_wait(&frees[stage], phase ^ 1)) return;  // (the first time round: the phase before the first)
                         ++filled;
-                        unsigned char *dst = ring + sidx * C::STAGE;
-                        uint64_t *full = &fulls[sidx];
-                        ptx::mbar_arrive_expect_tx(full, (uint32_t)boxes * (BOX * C::NC * 128));
+                        const uint32_t dst = ring + stage * C::STAGE, full = ptx::smem_u32(&fulls[stage]);
+                        ptx::mbar_arrive_expect_tx(full, bytes);
 #pragma unroll
                         for (int i = 0; i < B::P; ++i) {
-                            if (pages[i] == UNSEEN) continue;  // (no row sees it: left as it is, never used)
+                            if (pages[i] == UNSEEN) continue;  // (left as it is, never used)
                             if constexpr (IS_V) {
-                                ptx::tma_load_5d(dst + i * (BOX * C::NC * 128), map, 0, slot, 0, it.h, pages[i], full);
+                                ptx::tma_load_5d(dst + i * (BOX * C::NC * 128), map, 0, slot, 0, h, pages[i], full);
                             } else if constexpr (B::K_BY_CHUNK) {
 #pragma unroll
-                                for (int c = 0; c < C::NC; ++c)
-                                    ptx::tma_load_5d(dst + i * (BOX * 128) + c * B::K_CHUNK, map, 0, slot, c, it.h, pages[i], full);
+                                for (int c = 0; c < C::NC; ++c) ptx::tma_load_5d(dst + i * (BOX * 128) + c * B::K_CHUNK, map, 0, slot, c, h, pages[i], full);
                             } else {
 #pragma unroll
                                 for (int g = 0; g < BOX / 8; ++g)
-                                    ptx::tma_load_5d(dst + (i * (BOX / 8) + g) * B::K_GROUP, map, 0, slot + 8 * g, 0, it.h, pages[i], full);
+                                    ptx::tma_load_5d(dst + (i * (BOX / 8) + g) * B::K_GROUP, map, 0, slot + 8 * g, 0, h, pages[i], full);
                             }
                         }
+                        if (++stage == NS) stage = 0, phase ^= 1;
                     }
                 }
             };
@@ -482,49 +535,52 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
             }
             const uint32_t tm_o = tmem + strm * D, tm_s = tmem + C::TM_S + strm * C::NB * KT;
             uint64_t *const s_full = sh.s_full + strm * C::NB, *const p_full = sh.p_full + strm * C::NB, *const pv_done = sh.pv_done + strm * C::NB;
-            unsigned g0 = 0;              // tiles of the items before
-            unsigned made = 0, used = 0;  // tiles of this stream whose scores, whose products were issued
-            // scores of tile g; q: low word of the queries' descriptor
-            auto scores = [&](unsigned g, uint32_t ql) -> bool {
-                const uint32_t buf = made % C::NB;
-                // (in the other case the same thread has issued that product before)
-                if (C::STREAMS == 1 && made >= C::NB && !ptx::mbar_wait(&pv_done[buf], (made / C::NB - 1) & 1)) return false;
-                if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
+            // stages of the rings and S buffers, and their phases
+            unsigned k_stage = 0, k_phase = 0, v_stage = 0, v_phase = 0, made = 0, made_phase = 0, used = 0, used_phase = 0;
+            auto next_k = [&]() { if (++k_stage == C::NK) k_stage = 0, k_phase ^= 1; };
+            auto next_v = [&]() { if (++v_stage == C::NV) v_stage = 0, v_phase ^= 1; };
+            // scores of the next tile; ql: low word of the queries' descriptor
+            auto scores = [&](uint32_t ql) -> bool {
+                // (the buffer's last product is done; in the other case the same thread has issued it before)
+                if (C::STREAMS == 1 && !ptx::mbar_wait(&pv_done[made], made_phase ^ 1)) return false;
+                if (!ptx::mbar_wait(&sh.k_full[k_stage], k_phase)) return false;
                 ptx::tc_fence_after_sync();
-                const uint32_t lo = k_lo + g % C::NK * (C::STAGE / 16);
+                const uint32_t lo = k_lo + k_stage * (C::STAGE / 16), to = tm_s + made * KT;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c)
-                    ptx::umma_bf16(tm_s + buf * KT, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2), k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk,
-                                   c > 0);
-                ptx::umma_commit(&s_full[buf]);
-                ptx::umma_commit(&sh.k_free[g % C::NK]);
-                ++made;
+                    ptx::umma_bf16(to, q_hi | (ql + (c / 4) * (MT * 128 / 16) + (c % 4) * 2), k_hi | (lo + (c / 4) * k_chunk + (c % 4) * 2), idesc_qk, c > 0);
+                ptx::umma_commit(&s_full[made]);
+                ptx::umma_commit(&sh.k_free[k_stage]);
+                if (++made == C::NB) made = 0, made_phase ^= 1;
+                next_k();
                 return true;
             };
-            // output of tile g
-            auto product = [&](unsigned g, bool onto) -> bool {
-                const uint32_t buf = used % C::NB;
-                if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
-                if (!ptx::mbar_wait(&p_full[buf], (used / C::NB) & 1)) return false;
+            // output of the next tile
+            auto product = [&](bool onto) -> bool {
+                if (!ptx::mbar_wait(&sh.v_full[v_stage], v_phase)) return false;
+                if (!ptx::mbar_wait(&p_full[used], used_phase)) return false;
                 ptx::tc_fence_after_sync();
+                const uint32_t at = v_stage * (C::STAGE / 16), from = tm_s + used * KT;
 #pragma unroll
-                for (int c = 0; c < KT / 16; ++c)
-                    ptx::umma_bf16_ts(tm_o, tm_s + buf * KT + c * 8, v_hi | (v_lo[c] + g % C::NV * (C::STAGE / 16)), idesc_pv, onto || c > 0);
-                ptx::umma_commit(&pv_done[buf]);
-                ptx::umma_commit(&sh.v_free[g % C::NV]);
-                ++used;
+                for (int c = 0; c < KT / 16; ++c) ptx::umma_bf16_ts(tm_o, from + c * 8, v_hi | (v_lo[c] + at), idesc_pv, onto || c > 0);
+                ptx::umma_commit(&pv_done[used]);
+                ptx::umma_commit(&sh.v_free[v_stage]);
+                if (++used == C::NB) used = 0, used_phase ^= 1;
+                next_v();
                 return true;
             };
             // a tile that this stream takes no part in: its stages are free as far as this thread goes (once they are filled: an
             // arrival ahead of that would count for the tile before)
-            auto pass_k = [&](unsigned g) -> bool {
-                if (!ptx::mbar_wait(&sh.k_full[g % C::NK], (g / C::NK) & 1)) return false;
-                ptx::mbar_arrive(&sh.k_free[g % C::NK]);
+            auto pass_k = [&]() -> bool {
+                if (!ptx::mbar_wait(&sh.k_full[k_stage], k_phase)) return false;
+                ptx::mbar_arrive(&sh.k_free[k_stage]);
+                next_k();
                 return true;
             };
-            auto pass_v = [&](unsigned g) -> bool {
-                if (!ptx::mbar_wait(&sh.v_full[g % C::NV], (g / C::NV) & 1)) return false;
-                ptx::mbar_arrive(&sh.v_free[g % C::NV]);
+            auto pass_v = [&]() -> bool {
+                if (!ptx::mbar_wait(&sh.v_full[v_stage], v_phase)) return false;
+                ptx::mbar_arrive(&sh.v_free[v_stage]);
+                next_v();
                 return true;
             };
             auto run = [&]() -> bool {
@@ -538,10 +594,9 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     const bool pair = C::STREAMS == 2 && it.pair;
                     // Scores run `ahead` tiles ahead of the products: as many as there are S buffers for.
                     const int ahead = pair || C::STREAMS == 1 ? C::NB : 2 * C::NB;
-                    const Span span = span_of(a, view_of(it, tt, strm));
-                    const Tiles tiles(it);
+                    const Turns turns = turns_of(it, span_of(a, view_of(it, tt, strm)), pair);
                     // whether this stream takes part in tile j: with two row tiles as far as it sees some of it, else in turn
-                    auto on = [&](int j) { return C::STREAMS == 1 || (pair ? span.some(tiles(j)) : (j & 1) == strm); };
+                    auto on = [&](int j) { return C::STREAMS == 1 || (pair ? turns.some(j) : (j & 1) == strm); };
                     const uint32_t ql = q_lo + (pair ? strm : 0) * (C::Q_TILE / 16);
                     const bool does_qk = C::STREAMS == 2 || me == 0, does_pv = C::STREAMS == 2 || me == 1;
                     if (does_qk && !ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
@@ -553,22 +608,21 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         if (C::STREAMS == 2 && j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free[strm], (ord - 1) & 1)) return false;
                         if (does_pv && j >= 0) {
                             if (on(j)) {
-                                if (!product(g0 + j, onto)) return false;
+                                if (!product(onto)) return false;
                                 onto = true;
-                            } else if (!pass_v(g0 + j)) {
+                            } else if (!pass_v()) {
                                 return false;
                             }
                         }
                         if (does_qk && t < n) {
                             if (on(t)) {
-                                if (!scores(g0 + t, ql)) return false;
-                            } else if (!pass_k(g0 + t)) {
+                                if (!scores(ql)) return false;
+                            } else if (!pass_k()) {
                                 return false;
                             }
                             if (t + 1 == n) ptx::umma_commit(&sh.q_free);
                         }
                     }
-                    g0 += n;
                 }
             };
             if (!run()) {  // MMAs in flight have to end before the CTA may leave: a commit behind all of them, on a barrier of its own
@@ -579,15 +633,34 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax, epilogue
-        const int wg = warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;
+        // A row is two threads', of warps that reach the same lanes of tensor memory: each has half of a tile's keys, and half of O's
+        // columns.  (A step of one warp is mostly latency, three or four times what its exponentials take; four warps to a
+        // scheduler fill that.)
+        const int w4 = warp & 3, half = (warp >> 2) & 1, row = w4 * 32 + lane;
+        const int strm = warp >> 3;   // this warp's stream
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
         const float sl2 = a.scale * 1.4426950408889634f;
-        const int strm = C::STREAMS == 1 ? 0 : wg;  // this warpgroup's stream
         const int tok = row / a.G;    // this row's token in a row tile
-        unsigned count = 0;           // its tiles so far
-        unsigned g0 = 0, ord = 0;
+        unsigned count = 0;           // the stream's tiles so far
+        unsigned g0 = 0, ord = 0, singles = 0, swaps = 0;
         auto wait_product = [&](unsigned i) { return wait_warp(&sh.pv_done[strm * C::NB + i % C::NB], (i / C::NB) & 1); };  // of this stream's tile i
-        unsigned singles = 0;
+        // Both threads of a row give a number and get the other's.  Two words each, in turn, whose lowest bit says which use of them it
+        // is: a thread that has seen the other's word of one swap has been seen with its own of the swap before.  The lowest bit is lost;
+        // infinities become NaN by it.
+        auto swap = [&](float &mine, float &other) -> bool {
+            volatile uint32_t *const word = &sh.swap[strm][swaps & 1][0][row];
+            const uint32_t tag = (swaps >> 1) & 1, bits = (__float_as_uint(mine) & ~1u) | tag;
+            word[half * MT] = bits;
+            mine = __uint_as_float(bits);
+            uint32_t got = word[(half ^ 1) * MT];
+            if (!__all_sync(0xffffffffu, (got & 1) == tag)) {
+                if (!swap_slow(&word[(half ^ 1) * MT], tag)) return false;
+                got = word[(half ^ 1) * MT];
+            }
+            other = __uint_as_float(got);
+            ++swaps;
+            return true;
+        };
         auto run = [&]() -> bool {
             for (;; ++ord) {
                 if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
@@ -595,97 +668,68 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 const int n = it.tiles;
                 if (n == 0) return true;
                 const bool pair = C::STREAMS == 2 && it.pair;
-                const View v = view_of(it, tt, pair ? wg : 0), all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
+                const View v = view_of(it, tt, pair ? strm : 0), all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
                 const Span span = span_of(a, v);
                 const Tiles tiles(it);
                 const int rows = (v.p1 - v.p0 + 1) * a.G;
                 const bool warp_on = w4 * 32 < rows, on = row < rows;
                 const int p = v.p0 + (on ? tok : 0);  // this row's position
                 const int step = pair || C::STREAMS == 1 ? 1 : 2;
-                // this stream's next tile from j on
-                auto at_or_after = [&](int j) {
-                    while (j < n && pair && !span.some(tiles(j))) ++j;
-                    return j;
-                };
-                float m = -INFINITY, l = 0.f;
+                const Turns turns = turns_of(it, span, pair);
+                // (a row that has seen nothing has LOWEST for its maximum: finite, so that weights of minus infinity are 0 beside it)
+                float m = LOWEST, l = 0.f, worst = LOWEST;
                 int taken = 0;             // tiles of this stream
-                uint32_t x[KT];            // a row of S
-                bool loaded = false;       // (its next tile's is on its way there)
-                for (int j = at_or_after(step == 1 ? 0 : wg), next; j < n; j = next) {
-                    const unsigned g = g0 + j;
-                    const int buf = strm * C::NB + count % C::NB, kt = tiles(j), x0 = kt * KT;
-                    const bool masked = !span.all(kt);
+                for (int j = turns.at_or_after(step == 1 ? 0 : strm); j < turns.end; j = turns.at_or_after(j + step)) {
+                    const int buf = strm * C::NB + count % C::NB;
+                    const bool masked = !turns.all(j);
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
-                    auto load = [&](uint32_t from) {
-#pragma unroll
-                        for (int c = 0; c < KT; c += 32) ptx::tmem_ld32(from + c, *reinterpret_cast<uint32_t(*)[32]>(&x[c]));
-                    };
-                    if (!loaded) {
-                        if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
-                        ptx::tc_fence_after_sync();
-                        if (warp_on) load(ts);
-                    }
-                    next = at_or_after(j + step);
-                    loaded = false;
+                    if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
+                    ptx::tc_fence_after_sync();
                     if (warp_on) {
+                        uint32_t x[HK];
+                        ptx::tmem_ld32(ts + half * HK, x);
                         ptx::tmem_wait_ld();
                         if (masked) {
-                            const int hi = min(p - x0, KT) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
+                            __syncwarp();  // (a branch, not predicated instructions for every tile)
+                            const int x0 = tiles(j) * KT + half * HK;
+                            const int hi = min(p - x0, HK) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
+                            const uint32_t bits = low32(hi) & (~low32(from) | low32(sk));
 #pragma unroll
-                            for (int c = 0; c < KT; c += 32) {
-                                const uint32_t bits = low32(hi - c) & (~low32(from - c) | low32(sk - c));
-#pragma unroll
-                                for (int i = 0; i < 32; ++i)
-                                    if (!(bits & (1u << i))) x[c + i] = 0xff800000u;
-                            }
+                            for (int i = 0; i < HK; ++i)
+                                if (!(bits & (1u << i))) x[i] = 0xff800000u;
                         }
-                        float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        float t[2] = {LOWEST, LOWEST};
 #pragma unroll
-                        for (int i = 0; i < KT; i += 2) t[(i >> 1) & 3] = ptx::max3_nan(t[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-                        const float top = ptx::max3_nan(ptx::max3_nan(t[0], t[1], t[2]), t[3], t[3]) * sl2;
+                        for (int i = 0; i < HK; i += 2) t[(i >> 1) & 1] = ptx::max3_nan(t[(i >> 1) & 1], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                        float top = ptx::max3_nan(t[0], t[1], t[1]), other;
+                        if (!swap(top, other)) return false;
+                        top = ptx::max3_nan(top, other, other) * sl2;
+                        worst = ptx::max3_nan(worst, top, top);
                         const float m0 = m;
-                        const bool grow = top > m0 + LAZY || (m0 == -INFINITY && top > m0);
+                        const bool grow = top > m0 + LAZY;
                         m = grow ? top : m0;
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        const unsigned nc = count + 1, nbuf = strm * C::NB + nc % C::NB;
-                        const bool ready = next < n && ptx::mbar_try_wait(&sh.s_full[nbuf], (nc / C::NB) & 1);
-                        const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-ref, -ref);
+                        const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-m, -m);
                         float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                        uint32_t w[KT / 2];
-                        auto weights = [&](auto whole_) {
+                        uint32_t w[HK / 2];
 #pragma unroll
-                            for (int i = 0; i < KT; i += 2) {
-                                const float2 z = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
-                                float2 y;
-                                if (decltype(whole_)::value && (i / 2) % C::POLY_OF < C::POLY) y = ptx::ex2_poly(z);
-                                else y = make_float2(ptx::ex2(z.x), ptx::ex2(z.y));
-                                acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
-                                // weights as bf16: at most 2^-8 of each, independent from key to key
-                                w[i / 2] = pack_bf16(y.x, y.y);
-                            }
-                        };
-                        // (the polynomial does not give 0 for minus infinity, so masked tiles go without it)
-                        if (masked) weights(std::false_type{});
-                        else weights(std::true_type{});
-                        // S of the next tile while these weights are stored
-                        loaded = __all_sync(0xffffffffu, ready);
-                        if (loaded) {
-                            ptx::tc_fence_after_sync();
-                            load(tmem + lane_base + C::TM_S + nbuf * KT);
+                        for (int i = 0; i < HK; i += 2) {
+                            float2 y = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
+                            y.x = ptx::ex2(y.x), y.y = ptx::ex2(y.y);
+                            acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
+                            // weights as bf16: at most 2^-8 of each, independent from key to key
+                            w[i / 2] = pack_bf16(y.x, y.y);
                         }
-#pragma unroll
-                        for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&w[c]));
+                        // (over columns of S that the other thread has read before it gave its maximum)
+                        ptx::tmem_st16(ts + half * (HK / 2), w);
                         if (grow) l *= ptx::ex2(m0 - m);
                         l += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
-                        // A score of NaN or plus infinity makes the row NaN, by its sum: the polynomial lets neither through.
-                        if (!(top < INFINITY)) l = __uint_as_float(0x7fffffffu);
                         if (taken > 0 && __any_sync(0xffffffffu, grow)) {
                             // O at rest: the stream's product before this one is done, and the next one waits for these weights
                             if (!wait_product(count - 1)) return false;
                             ptx::tc_fence_after_sync();
-                            const float f = grow ? ptx::ex2(m0 - m) : 1.f;  // (grow: m is finite or +infinity)
+                            const float f = grow ? ptx::ex2(m0 - m) : 1.f;
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 16) {
+                            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
                                 uint32_t o[16];
                                 const uint32_t to = tmem + lane_base + strm * D + c;
                                 ptx::tmem_ld16(to, o);
@@ -701,13 +745,14 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         // Values that a zero weight may not meet: tokens that no row of the item sees (not copied, or the page's unused
                         // slots) become zeros, and NaN and infinity in those that only some rows see are taken out; the
                         // epilogue adds them where they are seen.
-                        const unsigned sidx = g % C::NV;
+                        const unsigned g = g0 + j, sidx = g % C::NV;
+                        const int x0 = tiles(j) * KT;
                         // (where S runs further ahead than V's ring, the stage's last tile has to be done for its phase to mean this one)
                         if (C::NV < C::NB && count >= C::NV && !wait_product(count - C::NV)) return false;
                         if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
                         unsigned char *vt = v_ring + sidx * C::STAGE;
                         constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
-                        for (int i = w4 * 32 + lane; i < KT * VR; i += 128) {
+                        for (int i = (warp & 7) * 32 + lane; i < KT * VR; i += 256) {
                             const int key = i / VR, c = i - key * VR;
                             if (sees_all(a, v, x0 + key, 1)) continue;
                             uint4 *at = reinterpret_cast<uint4 *>(vt + (key >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) +
@@ -731,7 +776,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         }
                         ptx::fence_proxy_async();
                     }
-                    // every warp's part of the values has to be clean before any of them is used: p_full counts all four
+                    // every warp's part of the values has to be clean before any of them is used: p_full counts all eight
                     ptx::tc_fence_before_sync();
                     ptx::mbar_arrive_warp(&sh.p_full[buf]);
                     ++taken, ++count;
@@ -746,55 +791,65 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         if (!wait_warp(&sh.o_free[s], (ord - 1) & 1)) return false;
                 }
                 ptx::tc_fence_after_sync();
+                if (warp_on) {             // the row's sum is both threads'
+                    float mine = l, other;
+                    if (!swap(mine, other)) return false;
+                    l = mine + other;
+                }
+                if (!(worst < INFINITY)) l = __uint_as_float(0x7fffffffu);  // a score of NaN or plus infinity makes the row NaN
                 const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
                 const int slot = it.slot;
                 const long long orow = ((long long)it.lo + it.t0 + (p - all.p0)) * a.H_q + it.h * a.G + (row - tok * a.G);
-                const int brow = (pair ? wg * MT : 0) + row;  // in the block
-                // Alone in an item with one row tile, the first warpgroup joins both streams' outputs.
+                const int brow = (pair ? strm * MT : 0) + row;  // in the block
+                // Alone in an item with one row tile, the first stream's warps join both streams' outputs.
                 bool second = false;       // the second stream's O counts
                 float f0 = 1.f, f1 = 0.f;
                 if (C::STREAMS == 2 && !pair) {
                     // (the next item's are written behind this one's o_free)
                     second = n > 1;
-                    if (wg == 1) {  // (its products are done, then)
-                        sh.ml[row] = make_float2(m, l);
-                        ptx::tc_fence_before_sync();
-                        ptx::mbar_arrive_warp(&sh.ml_full[w4]);
+                    if (strm == 1) {  // (its products are done, then)
+                        if (half == 0) {
+                            sh.ml[row] = make_float2(m, l);
+                            ptx::tc_fence_before_sync();
+                            ptx::mbar_arrive_warp(&sh.ml_full[w4]);
+                        }
                     } else {
                         if (!wait_warp(&sh.ml_full[w4], singles & 1)) return false;
                         ptx::tc_fence_after_sync();
                     }
                     ++singles;
-                    if (wg == 0 && second) {
+                    if (strm == 0 && second) {
                         const float2 x = sh.ml[row];
-                        const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
-                        f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
+                        const float mn = fmaxf(m, x.x);
+                        f0 = ptx::ex2(m - mn), f1 = ptx::ex2(x.x - mn);
                         l = l * f0 + x.y * f1, m = mn;
                     }
                 }
-                const bool writes = C::STREAMS == 1 || pair || wg == 0;
-                if (writes && taken == 0 && !second) l = 0.f;
+                const bool writes = C::STREAMS == 1 || pair || strm == 0;
                 const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
                 __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
+                float *const blk = ws.o + (long long)slot * ws.cap * D;
                 if (writes && warp_on) {
-                    float *const blk = ws.o + (long long)slot * ws.cap * D;
-                    if (slot >= 0 && on) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
+                    if (slot >= 0 && on && half == 0) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
+                    for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
                         uint32_t o[32];
                         if (taken > 0) {
-                            ptx::tmem_ld32(tmem + lane_base + (pair ? wg : 0) * D + c, o);
+                            ptx::tmem_ld32(tmem + lane_base + (pair ? strm : 0) * D + c, o);
                             ptx::tmem_wait_ld();
                         } else {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0;
                         }
                         if (second) {
-                            uint32_t o1[32];
-                            ptx::tmem_ld32(tmem + lane_base + D + c, o1);
-                            ptx::tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                            for (int e = 0; e < 32; e += 16) {
+                                uint32_t o1[16];
+                                ptx::tmem_ld16(tmem + lane_base + D + c + e, o1);
+                                ptx::tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[e + i] = __float_as_uint(__uint_as_float(o[e + i]) * f0 + __uint_as_float(o1[i]) * f1);
+                            }
                         }
                         if (!on) continue;
                         if (slot < 0) {
@@ -815,29 +870,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         }
                     }
                     __syncwarp();
-                    if (fix && on && !bad) {  // values with NaN or infinity in masked tiles: those elements, onto what was stored
-                        // (of two streams either may have taken them out: what not every row of both sees)
-                        const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
-#pragma unroll 1
-                        for (int j = 0; j < n; ++j) {
-                            const int x0 = tiles(j) * KT;
-                            if (sees_all(a, all, x0, KT)) continue;
-#pragma unroll 1
-                            for (int x = x0; x < x0 + KT; ++x) {
-                                if (!sees(a, p, x) || sees_all(a, all, x, 1)) continue;
-                                const __nv_bfloat16 *vr = static_cast<const __nv_bfloat16 *>(a.c.v) + table[x >> a.log_page] * a.c.stride_page +
-                                                          (x & ((1 << a.log_page) - 1)) * a.c.stride_slot + it.h * a.c.stride_head;
-#pragma unroll 1
-                                for (int c = 0; c < D; ++c) {
-                                    const float y = to_f32(vr[c]);
-                                    if (isfinite(y)) continue;
-                                    if (slot < 0) out_row[c] = __float2bfloat16_rn(to_f32(out_row[c]) + y);
-                                    else blk[((long long)(c / 4) * ws.cap + brow) * 4 + c % 4] += y;
-                                }
-                            }
-                        }
-                    }
-                    __syncwarp();
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
@@ -845,12 +877,36 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     if (C::STREAMS == 1) {
                         ptx::mbar_arrive(&sh.o_free[0]);
                     } else if (pair) {
-                        ptx::mbar_arrive(&sh.o_free[wg]), ptx::mbar_arrive(&sh.o_free[wg]);
+                        ptx::mbar_arrive(&sh.o_free[strm]), ptx::mbar_arrive(&sh.o_free[strm]);
                     } else {
                         ptx::mbar_arrive(&sh.o_free[0]), ptx::mbar_arrive(&sh.o_free[1]);
                     }
-                    ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
                 }
+                if (writes && warp_on && fix && on && !bad) {
+                    // Values with NaN or infinity in masked tiles: those elements, onto what was stored.  (Of two streams either may have
+                    // taken them out: what not every row of both sees.)
+                    const int32_t *table = a.c.page_table + (size_t)it.b * a.c.max_pages;
+#pragma unroll 1
+                    for (int j = 0; j < n; ++j) {
+                        const int x0 = tiles(j) * KT;
+                        if (sees_all(a, all, x0, KT)) continue;
+#pragma unroll 1
+                        for (int x = x0; x < x0 + KT; ++x) {
+                            if (!sees(a, p, x) || sees_all(a, all, x, 1)) continue;
+                            const __nv_bfloat16 *vr = static_cast<const __nv_bfloat16 *>(a.c.v) + table[x >> a.log_page] * a.c.stride_page +
+                                                      (x & ((1 << a.log_page) - 1)) * a.c.stride_slot + it.h * a.c.stride_head;
+#pragma unroll 1
+                            for (int c = half * (D / 2); c < (half + 1) * (D / 2); ++c) {
+                                const float y = to_f32(vr[c]);
+                                if (isfinite(y)) continue;
+                                if (slot < 0) out_row[c] = __float2bfloat16_rn(to_f32(out_row[c]) + y);
+                                else blk[((long long)(c / 4) * ws.cap + brow) * 4 + c % 4] += y;
+                            }
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(&sh.item_empty[ord % ITEMS]);
                 g0 += n;
             }
         };
@@ -998,8 +1054,8 @@ template <int D> cudaError_t launch_d(ChunkArgs a, cudaStream_t stream)
     if (!map5(&k, c.k, cache_dims, cache_strides, k_box) || !map5(&v, c.v, cache_dims, cache_strides, v_box) || !map5(&q, a.q, q_dims, q_strides, q_box))
         return cudaErrorInvalidValue;
     // (the kernel's static shared memory, a deadline, comes first; the tiles start at the next multiple of 1024 behind `Shared`)
-    const int smem = (16 + (int)sizeof(Shared) + 1023) / 1024 * 1024 - 16 + C::TILES;
-    static_assert((16 + sizeof(Shared) + 1023) / 1024 * 1024 + C::TILES <= 227 * 1024, "shared memory of a CTA");
+    const int smem = (16 + (int)sizeof(Shared<D>) + 1023) / 1024 * 1024 - 16 + C::TILES;
+    static_assert((16 + sizeof(Shared<D>) + 1023) / 1024 * 1024 + C::TILES <= 227 * 1024, "shared memory of a CTA");
     e = ensure_dynamic_smem(reinterpret_cast<const void *>(chunk_tc_kernel<D>), smem, dev);
     if (e != cudaSuccess) return e;
     e = launch_dependent(chunk_tc_kernel<D>, dim3(ctas), dim3(C::THREADS), smem, stream, a, ws, lay, smem, q, k, v);

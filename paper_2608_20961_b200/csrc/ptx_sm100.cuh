@@ -394,6 +394,19 @@ __device__ __forceinline__ void tma_load_5d(void *dst_smem, const void *tmap, in
         "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(smem_u32(bar))
         : "memory");
 }
+// The same, and mbar_arrive_expect_tx, by their shared-memory addresses
+__device__ __forceinline__ void tma_load_5d(uint32_t dst_smem, const void *tmap, int x, int y, int z, int w, int v, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+        "[%7];" ::"r"(dst_smem),
+        "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 // umma_desc_k_sw128 with 8-row groups `group` bytes apart
 __device__ __forceinline__ uint64_t umma_desc_k_sw128(uint32_t addr, uint32_t group)
 {
@@ -464,23 +477,6 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-
-// 2^x of two values on the FMA pipes: x = i + f with i the nearest integer (its two's complement is left in the low bits by
-// the addition of 1.5 * 2^23) and 2^f by a polynomial, i added to its exponent.  The coefficients are the minimax ones of degree
-// 3 for the relative error on [-1/2, 1/2] (Remez exchange on p(f) 2^-f - 1): 7.5e-5 = 2^-13.7.  Below -126 the result
-// stays 2^-126; NaN and +infinity give no meaningful result.
-__device__ __forceinline__ float2 ex2_poly(float2 x)
-{
-    x.x = fmaxf(x.x, -126.f), x.y = fmaxf(x.y, -126.f);
-    const float magic = 12582912.f;
-    const float2 t = add2(x, make_float2(magic, magic)), i = add2(t, make_float2(-magic, -magic));
-    const float2 f = fma2(i, make_float2(-1.f, -1.f), x);
-    float2 p = fma2(f, make_float2(0.0551716685295105f, 0.0551716685295105f), make_float2(0.2426111251115799f, 0.2426111251115799f));
-    p = fma2(p, f, make_float2(0.6932609677314758f, 0.6932609677314758f));
-    p = fma2(p, f, make_float2(0.9999280571937561f, 0.9999280571937561f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
 }  // namespace ptx
