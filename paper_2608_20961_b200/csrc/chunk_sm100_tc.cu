@@ -32,9 +32,7 @@ constexpr int ITEMS = 8;               // ring of work items between the produce
 constexpr int START = 256;             // cost of an item's start, in keys
 constexpr int MIN_UNITS = 256;         // least units of a part; at least a tile's keys, so that a part inside an item holds the start of one
 constexpr int UNSEEN = -0x7fffffff;    // for a page that is not looked up
-constexpr float LAZY = 8.f;
-constexpr float LOWEST = -3e38f;
-constexpr int HK = KT / 2;             // keys of a tile that a softmax thread has
+constexpr float LARGE = 1099511627776.f;  // 2^40: a row's weights of one tile do not add up to more
 constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;  // l of a row whose part is not there
 
 template <int D> struct Cfg {
@@ -42,10 +40,10 @@ template <int D> struct Cfg {
     static constexpr int STREAMS = D == 256 ? 1 : 2;     // what 512 columns of tensor memory leave
     static constexpr int STAGE = NC * KT * 128;          // bytes of a tile
     static constexpr int NB = D == 256 ? 4 : 2;          // S buffers of a stream
-    static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 4 : 2;
+    static constexpr int NK = D == 64 ? 10 : D == 128 ? 5 : 3, NV = D == 64 ? 10 : D == 128 ? 5 : 2;
     static constexpr int Q_TILE = NC * MT * 128;
     static constexpr int TILES = STREAMS * Q_TILE + (NK + NV) * STAGE;  // bytes
-    static constexpr int SOFT_WARPS = 8 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 2, PRODUCER_V = MMA + 3;  // (two of MMA)
+    static constexpr int SOFT_WARPS = 4 * STREAMS, MMA = SOFT_WARPS, PRODUCER_K = MMA + 2, PRODUCER_V = MMA + 3;  // (two of MMA)
     static constexpr int THREADS = (SOFT_WARPS + 4) * 32;
     static constexpr int TM_S = 256;                     // columns: O of stream s at s * D, S buffer b of it at 256 + (s * NB + b) * KT
     static constexpr int CAP = STREAMS * MT;             // rows of an item at most
@@ -99,10 +97,7 @@ template <int D> struct Shared {
     float2 ml[C::STREAMS == 2 ? MT : 1];  // of the second stream's rows, for the first
     unsigned bad_item[8];       // ordinal + 1 of an item that met a page out of range
     unsigned nonfinite[8];      // ordinal + 1 of an item with NaN or infinity among the values of its masked tiles
-    union {
-        uint32_t swap[C::STREAMS][2][2][MT];  // between the threads of a row
-        long long scan[C::THREADS / 32];      // (before any of that)
-    };
+    long long scan[C::THREADS / 32];
     long long first_off;
     Seq first_seq;              // of sequence first_b
     Part part;
@@ -291,14 +286,6 @@ __device__ __forceinline__ bool sees(const ChunkArgs &a, int p, int x) { return 
 
 __device__ __forceinline__ uint32_t low32(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 __device__ __forceinline__ bool nonfinite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-// Waits until the word's lowest bit is `tag` for every lane, each with its own word.
-static __device__ __noinline__ bool swap_slow(const volatile uint32_t *word, uint32_t tag)
-{
-    for (;;) {
-        if (__all_sync(0xffffffffu, (*word & 1) == tag)) return true;
-        if (__any_sync(0xffffffffu, ptx::wait_deadline_passed())) return false;
-    }
-}
 // a wait with one outcome for the whole warp: what follows needs all of its lanes
 __device__ __forceinline__ bool wait_warp(uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity)); }
 
@@ -321,7 +308,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         for (int i = 0; i < C::NK; ++i) ptx::mbar_init(&sh.k_full[i], 1), ptx::mbar_init(&sh.k_free[i], C::STREAMS);
 #pragma unroll 1
         for (int i = 0; i < C::NV; ++i) ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], C::STREAMS);
-        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 8), ptx::mbar_init(&sh.pv_done[i], 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
         for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
         ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, C::STREAMS), ptx::mbar_init(&sh.end[0], 1), ptx::mbar_init(&sh.end[1], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
@@ -383,8 +370,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         before += units;
     }
     if (tid == 0) sh.part = {u0, u1, W, parts, group};
-    __syncthreads();
-    for (int i = tid; i < C::STREAMS * 4 * MT; i += C::THREADS) (&sh.swap[0][0][0][0])[i] = 1;  // (neither of the first two uses')
     __syncthreads();
     const uint32_t tmem = sh.tmem;
     const int tt = tile_tokens<D>(a);
@@ -633,34 +618,13 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax, epilogue
-        // A row is two threads', of warps that reach the same lanes of tensor memory: each has half of a tile's keys, and half of O's
-        // columns.  (A step of one warp is mostly latency, three or four times what its exponentials take; four warps to a
-        // scheduler fill that.)
-        const int w4 = warp & 3, half = (warp >> 2) & 1, row = w4 * 32 + lane;
-        const int strm = warp >> 3;   // this warp's stream
+        const int strm = C::STREAMS == 1 ? 0 : warp >> 2, w4 = warp & 3, row = w4 * 32 + lane;  // this warpgroup's stream; a row to a thread
         const uint32_t lane_base = (uint32_t)(w4 * 32) << 16;
         const float sl2 = a.scale * 1.4426950408889634f;
         const int tok = row / a.G;    // this row's token in a row tile
         unsigned count = 0;           // the stream's tiles so far
-        unsigned g0 = 0, ord = 0, singles = 0, swaps = 0;
+        unsigned g0 = 0, ord = 0, singles = 0;
         auto wait_product = [&](unsigned i) { return wait_warp(&sh.pv_done[strm * C::NB + i % C::NB], (i / C::NB) & 1); };  // of this stream's tile i
-        // Both threads of a row give a number and get the other's.  Two words each, in turn, whose lowest bit says which use of them it
-        // is: a thread that has seen the other's word of one swap has been seen with its own of the swap before.  The lowest bit is lost;
-        // infinities become NaN by it.
-        auto swap = [&](float &mine, float &other) -> bool {
-            volatile uint32_t *const word = &sh.swap[strm][swaps & 1][0][row];
-            const uint32_t tag = (swaps >> 1) & 1, bits = (__float_as_uint(mine) & ~1u) | tag;
-            word[half * MT] = bits;
-            mine = __uint_as_float(bits);
-            uint32_t got = word[(half ^ 1) * MT];
-            if (!__all_sync(0xffffffffu, (got & 1) == tag)) {
-                if (!swap_slow(&word[(half ^ 1) * MT], tag)) return false;
-                got = word[(half ^ 1) * MT];
-            }
-            other = __uint_as_float(got);
-            ++swaps;
-            return true;
-        };
         auto run = [&]() -> bool {
             for (;; ++ord) {
                 if (!wait_warp(&sh.item_full[ord % ITEMS], (ord / ITEMS) & 1)) return false;
@@ -669,76 +633,99 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 if (n == 0) return true;
                 const bool pair = C::STREAMS == 2 && it.pair;
                 const View v = view_of(it, tt, pair ? strm : 0), all{it.len + it.t0, it.len + it.t0 + it.tokens - 1};
-                const Span span = span_of(a, v);
                 const Tiles tiles(it);
                 const int rows = (v.p1 - v.p0 + 1) * a.G;
                 const bool warp_on = w4 * 32 < rows, on = row < rows;
                 const int p = v.p0 + (on ? tok : 0);  // this row's position
                 const int step = pair || C::STREAMS == 1 ? 1 : 2;
-                const Turns turns = turns_of(it, span, pair);
-                // (a row that has seen nothing has LOWEST for its maximum: finite, so that weights of minus infinity are 0 beside it)
-                float m = LOWEST, l = 0.f, worst = LOWEST;
+                const Turns turns = turns_of(it, span_of(a, v), pair);
+                float m = -INFINITY, l = 0.f;
                 int taken = 0;             // tiles of this stream
-                for (int j = turns.at_or_after(step == 1 ? 0 : strm); j < turns.end; j = turns.at_or_after(j + step)) {
+                uint32_t x[KT];            // a row of S
+                bool loaded = false;       // (its next tile's is on its way there)
+                for (int j = turns.at_or_after(step == 1 ? 0 : strm), next; j < turns.end; j = next) {
                     const int buf = strm * C::NB + count % C::NB;
                     const bool masked = !turns.all(j);
                     const uint32_t ts = tmem + lane_base + C::TM_S + buf * KT;
-                    if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
-                    ptx::tc_fence_after_sync();
+                    auto load = [&](uint32_t from) {
+#pragma unroll
+                        for (int c = 0; c < KT; c += 32) ptx::tmem_ld32(from + c, *reinterpret_cast<uint32_t(*)[32]>(&x[c]));
+                    };
+                    if (!loaded) {
+                        if (!wait_warp(&sh.s_full[buf], (count / C::NB) & 1)) return false;
+                        ptx::tc_fence_after_sync();
+                        if (warp_on) load(ts);
+                    }
+                    next = turns.at_or_after(j + step);
+                    loaded = false;
+                    bool ready = false;
                     if (warp_on) {
-                        uint32_t x[HK];
-                        ptx::tmem_ld32(ts + half * HK, x);
                         ptx::tmem_wait_ld();
                         if (masked) {
                             __syncwarp();  // (a branch, not predicated instructions for every tile)
-                            const int x0 = tiles(j) * KT + half * HK;
-                            const int hi = min(p - x0, HK) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
-                            const uint32_t bits = low32(hi) & (~low32(from) | low32(sk));
+                            const int x0 = tiles(j) * KT;
+                            const int hi = min(p - x0, KT) + 1, from = (int)max((long long)p - a.window + 1 - x0, -1ll), sk = (int)max((long long)a.sinks - x0, -1ll);
 #pragma unroll
-                            for (int i = 0; i < HK; ++i)
-                                if (!(bits & (1u << i))) x[i] = 0xff800000u;
-                        }
-                        float t[2] = {LOWEST, LOWEST};
+                            for (int c = 0; c < KT; c += 32) {
+                                const uint32_t bits = low32(hi - c) & (~low32(from - c) | low32(sk - c));
 #pragma unroll
-                        for (int i = 0; i < HK; i += 2) t[(i >> 1) & 1] = ptx::max3_nan(t[(i >> 1) & 1], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-                        float top = ptx::max3_nan(t[0], t[1], t[1]), other;
-                        if (!swap(top, other)) return false;
-                        top = ptx::max3_nan(top, other, other) * sl2;
-                        worst = ptx::max3_nan(worst, top, top);
-                        const float m0 = m;
-                        const bool grow = top > m0 + LAZY;
-                        m = grow ? top : m0;
-                        const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-m, -m);
-                        float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                        uint32_t w[HK / 2];
-#pragma unroll
-                        for (int i = 0; i < HK; i += 2) {
-                            float2 y = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
-                            y.x = ptx::ex2(y.x), y.y = ptx::ex2(y.y);
-                            acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
-                            // weights as bf16: at most 2^-8 of each, independent from key to key
-                            w[i / 2] = pack_bf16(y.x, y.y);
-                        }
-                        // (over columns of S that the other thread has read before it gave its maximum)
-                        ptx::tmem_st16(ts + half * (HK / 2), w);
-                        if (grow) l *= ptx::ex2(m0 - m);
-                        l += (acc[0].x + acc[0].y) + (acc[1].x + acc[1].y);
-                        if (taken > 0 && __any_sync(0xffffffffu, grow)) {
-                            // O at rest: the stream's product before this one is done, and the next one waits for these weights
-                            if (!wait_product(count - 1)) return false;
-                            ptx::tc_fence_after_sync();
-                            const float f = grow ? ptx::ex2(m0 - m) : 1.f;
-#pragma unroll 1
-                            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 16) {
-                                uint32_t o[16];
-                                const uint32_t to = tmem + lane_base + strm * D + c;
-                                ptx::tmem_ld16(to, o);
-                                ptx::tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                ptx::tmem_st16(to, o);
+                                for (int i = 0; i < 32; ++i)
+                                    if (!(bits & (1u << i))) x[c + i] = 0xff800000u;
                             }
                         }
+                        // Weights against the reference as it is; if they come out too large, or there is none yet, it becomes the maximum.
+                        bool anew = __any_sync(0xffffffffu, on && m == -INFINITY);
+                        float2 acc[2];
+                        uint32_t w[KT / 2];
+#pragma unroll 1
+                        for (;;) {
+                            if (anew) {
+                                float t[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                                for (int i = 0; i < KT; i += 2) t[(i >> 1) & 1] = ptx::max3_nan(t[(i >> 1) & 1], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                                const float top = ptx::max3_nan(t[0], t[1], t[1]) * sl2, m0 = m;
+                                // (a NaN or plus infinity there makes the row NaN, by its sum)
+                                m = top > m0 || top != top ? top : m0;
+                                const float f = m == m0 ? 1.f : ptx::ex2(m0 - m);
+                                l *= f;
+                                if (taken > 0) {
+                                    // O at rest: the stream's product before this one is done, and the next one waits for these weights
+                                    if (!wait_product(count - 1)) return false;
+                                    ptx::tc_fence_after_sync();
+#pragma unroll 1
+                                    for (int c = 0; c < D; c += 16) {
+                                        uint32_t o[16];
+                                        const uint32_t to = tmem + lane_base + strm * D + c;
+                                        ptx::tmem_ld16(to, o);
+                                        ptx::tmem_wait_ld();
+#pragma unroll
+                                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                        ptx::tmem_st16(to, o);
+                                    }
+                                }
+                            }
+                            const float ref = m == -INFINITY ? 0.f : m;
+                            const float2 scale2 = make_float2(sl2, sl2), ref2 = make_float2(-ref, -ref);
+                            acc[0] = acc[1] = make_float2(0.f, 0.f);
+#pragma unroll
+                            for (int i = 0; i < KT; i += 2) {
+                                float2 y = ptx::fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), scale2, ref2);
+                                y.x = ptx::ex2(y.x), y.y = ptx::ex2(y.y);
+                                acc[(i >> 1) & 1] = ptx::add2(acc[(i >> 1) & 1], y);
+                                // weights as bf16: at most 2^-8 of each, independent from key to key
+                                w[i / 2] = pack_bf16(y.x, y.y);
+                            }
+                            acc[0] = ptx::add2(acc[0], acc[1]);
+                            acc[0].x += acc[0].y;
+                            if (anew || !__any_sync(0xffffffffu, on && !(acc[0].x < LARGE))) break;
+                            anew = true;
+                        }
+#pragma unroll
+                        for (int c = 0; c < KT / 2; c += 16) ptx::tmem_st16(ts + c, *reinterpret_cast<const uint32_t(*)[16]>(&w[c]));
+                        l += acc[0].x;
+                        const unsigned nc = count + 1;
+                        ready = next < turns.end && ptx::mbar_try_wait(&sh.s_full[strm * C::NB + nc % C::NB], (nc / C::NB) & 1);
+                        ready = __all_sync(0xffffffffu, ready);
                         ptx::tmem_wait_st();
                     }
                     if (masked) {
@@ -752,11 +739,12 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
                         unsigned char *vt = v_ring + sidx * C::STAGE;
                         constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
-                        for (int i = (warp & 7) * 32 + lane; i < KT * VR; i += 256) {
-                            const int key = i / VR, c = i - key * VR;
+#pragma unroll 1
+                        for (int i = w4 * 32 + lane; i < KT * VR; i += 128) {
+                            const int key = i / VR, cc = i - key * VR;
                             if (sees_all(a, v, x0 + key, 1)) continue;
                             uint4 *at = reinterpret_cast<uint4 *>(vt + (key >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) +
-                                                                  ((c >> 3) * lay.v_rows + (key & (lay.v_rows - 1))) * 128 + (c & 7) * 16);
+                                                                  ((cc >> 3) * lay.v_rows + (key & (lay.v_rows - 1))) * 128 + (cc & 7) * 16);
                             if (!sees_some(a, all, x0 + key, 1)) {
                                 *at = make_uint4(0, 0, 0, 0);
                                 continue;
@@ -776,10 +764,15 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         }
                         ptx::fence_proxy_async();
                     }
-                    // every warp's part of the values has to be clean before any of them is used: p_full counts all eight
+                    // every warp's part of the values has to be clean before any of them is used: p_full counts all four
                     ptx::tc_fence_before_sync();
                     ptx::mbar_arrive_warp(&sh.p_full[buf]);
                     ++taken, ++count;
+                    if (ready) {           // (behind the store: ahead of it the load holds that up)
+                        loaded = true;
+                        ptx::tc_fence_after_sync();
+                        load(tmem + lane_base + C::TM_S + (strm * C::NB + count % C::NB) * KT);
+                    }
                 }
                 // ---- end of the item
                 if (taken > 0) {
@@ -791,28 +784,20 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         if (!wait_warp(&sh.o_free[s], (ord - 1) & 1)) return false;
                 }
                 ptx::tc_fence_after_sync();
-                if (warp_on) {             // the row's sum is both threads'
-                    float mine = l, other;
-                    if (!swap(mine, other)) return false;
-                    l = mine + other;
-                }
-                if (!(worst < INFINITY)) l = __uint_as_float(0x7fffffffu);  // a score of NaN or plus infinity makes the row NaN
                 const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
                 const int slot = it.slot;
                 const long long orow = ((long long)it.lo + it.t0 + (p - all.p0)) * a.H_q + it.h * a.G + (row - tok * a.G);
                 const int brow = (pair ? strm * MT : 0) + row;  // in the block
-                // Alone in an item with one row tile, the first stream's warps join both streams' outputs.
+                // Alone in an item with one row tile, the first warpgroup joins both streams' outputs.
                 bool second = false;       // the second stream's O counts
                 float f0 = 1.f, f1 = 0.f;
                 if (C::STREAMS == 2 && !pair) {
                     // (the next item's are written behind this one's o_free)
                     second = n > 1;
-                    if (strm == 1) {  // (its products are done, then)
-                        if (half == 0) {
-                            sh.ml[row] = make_float2(m, l);
-                            ptx::tc_fence_before_sync();
-                            ptx::mbar_arrive_warp(&sh.ml_full[w4]);
-                        }
+                    if (strm == 1) {       // (its products are done, then)
+                        sh.ml[row] = make_float2(m, l);
+                        ptx::tc_fence_before_sync();
+                        ptx::mbar_arrive_warp(&sh.ml_full[w4]);
                     } else {
                         if (!wait_warp(&sh.ml_full[w4], singles & 1)) return false;
                         ptx::tc_fence_after_sync();
@@ -820,8 +805,8 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     ++singles;
                     if (strm == 0 && second) {
                         const float2 x = sh.ml[row];
-                        const float mn = fmaxf(m, x.x);
-                        f0 = ptx::ex2(m - mn), f1 = ptx::ex2(x.x - mn);
+                        const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
+                        f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
                         l = l * f0 + x.y * f1, m = mn;
                     }
                 }
@@ -830,9 +815,9 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
                 float *const blk = ws.o + (long long)slot * ws.cap * D;
                 if (writes && warp_on) {
-                    if (slot >= 0 && on && half == 0) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
+                    if (slot >= 0 && on) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
 #pragma unroll 1
-                    for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+                    for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
                         if (taken > 0) {
                             ptx::tmem_ld32(tmem + lane_base + (pair ? strm : 0) * D + c, o);
@@ -842,14 +827,11 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                             for (int i = 0; i < 32; ++i) o[i] = 0;
                         }
                         if (second) {
+                            uint32_t o1[32];
+                            ptx::tmem_ld32(tmem + lane_base + D + c, o1);
+                            ptx::tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; e += 16) {
-                                uint32_t o1[16];
-                                ptx::tmem_ld16(tmem + lane_base + D + c + e, o1);
-                                ptx::tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[e + i] = __float_as_uint(__uint_as_float(o[e + i]) * f0 + __uint_as_float(o1[i]) * f1);
-                            }
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
                         }
                         if (!on) continue;
                         if (slot < 0) {
@@ -896,7 +878,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                             const __nv_bfloat16 *vr = static_cast<const __nv_bfloat16 *>(a.c.v) + table[x >> a.log_page] * a.c.stride_page +
                                                       (x & ((1 << a.log_page) - 1)) * a.c.stride_slot + it.h * a.c.stride_head;
 #pragma unroll 1
-                            for (int c = half * (D / 2); c < (half + 1) * (D / 2); ++c) {
+                            for (int c = 0; c < D; ++c) {
                                 const float y = to_f32(vr[c]);
                                 if (isfinite(y)) continue;
                                 if (slot < 0) out_row[c] = __float2bfloat16_rn(to_f32(out_row[c]) + y);
