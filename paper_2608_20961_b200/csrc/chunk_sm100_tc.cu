@@ -124,9 +124,9 @@ template <int D> __device__ __forceinline__ int tile_tokens(const ChunkArgs &a) 
 template <int D> __device__ __forceinline__ long long units_before(const ChunkArgs &a, int len, int n, long long i)
 {
     const long long per = (long long)Cfg<D>::STREAMS * tile_tokens<D>(a), most = (long long)a.window + a.sinks - 1;
-    // items whose first token is behind fewer than `most`
-    long long m = most <= len ? 0 : (most - len + per - 1) / per;
-    m = m < i ? m : i;
+    // items whose first token is behind fewer than `most` (all of them where there is no window: no division)
+    const long long far = most - len;
+    const long long m = far >= i * per ? i : far <= 0 ? 0 : (long long)(((unsigned)far + (unsigned)per - 1) / (unsigned)per);
     const long long tokens = i * per < n ? i * per : n;
     return i * START + tokens + m * len + per * (m * (m - 1) / 2) + (i - m) * most;
 }
@@ -739,13 +739,17 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         if (!wait_warp(&sh.v_full[sidx], (g / C::NV) & 1)) return false;
                         unsigned char *vt = v_ring + sidx * C::STAGE;
                         constexpr int VR = C::NC * 8;  // 16-byte vectors of a row
+                        // of the tile's keys: every row of this stream sees those up to `up` from `from` on or below `sk`, some row of the item
+                        // those up to `up_any` from `from_any` on or below `sk`
+                        const int up = v.p0 - x0, up_any = all.p1 - x0, sk = (int)max((long long)a.sinks - x0, -1ll);
+                        const int from = (int)max((long long)v.p1 - a.window + 1 - x0, -1ll), from_any = (int)max((long long)all.p0 - a.window + 1 - x0, -1ll);
 #pragma unroll 1
                         for (int i = w4 * 32 + lane; i < KT * VR; i += 128) {
                             const int key = i / VR, cc = i - key * VR;
-                            if (sees_all(a, v, x0 + key, 1)) continue;
+                            if (key <= up && (key >= from || key < sk)) continue;
                             uint4 *at = reinterpret_cast<uint4 *>(vt + (key >> lay.log_v_rows) * (lay.v_rows * C::NC * 128) +
                                                                   ((cc >> 3) * lay.v_rows + (key & (lay.v_rows - 1))) * 128 + (cc & 7) * 16);
-                            if (!sees_some(a, all, x0 + key, 1)) {
+                            if (key > up_any || (key < from_any && key >= sk)) {
                                 *at = make_uint4(0, 0, 0, 0);
                                 continue;
                             }
@@ -814,6 +818,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
                 __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;
                 float *const blk = ws.o + (long long)slot * ws.cap * D;
+                const bool wide = (reinterpret_cast<uintptr_t>(a.O) & 31) == 0;
                 if (writes && warp_on) {
                     if (slot >= 0 && on) reinterpret_cast<float2 *>(ws.ml)[(long long)slot * ws.cap + brow] = make_float2(m, bad ? PAGE_BAD : l);
 #pragma unroll 1
@@ -835,16 +840,17 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         }
                         if (!on) continue;
                         if (slot < 0) {
-                            if (!bad)
+                            if (!bad) {
 #pragma unroll
-                                for (int i = 0; i < 32; i += 8) {
-                                    uint4 y;
-                                    uint32_t *yw = reinterpret_cast<uint32_t *>(&y);
+                                for (int i = 0; i < 32; i += 2) o[i / 2] = pack_bf16(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                                if (wide) {  // whole sectors
+                                    ptx::st_global_32(out_row + c, *reinterpret_cast<const uint32_t(*)[8]>(&o[0]));
+                                    ptx::st_global_32(out_row + c + 16, *reinterpret_cast<const uint32_t(*)[8]>(&o[8]));
+                                } else {
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e)
-                                        yw[e] = pack_bf16(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
-                                    *reinterpret_cast<uint4 *>(out_row + c + i) = y;
+                                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(out_row + c + 2 * i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                                 }
+                            }
                         } else {
 #pragma unroll
                             for (int i = 0; i < 32; i += 4)

@@ -426,6 +426,13 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16_f32_bmn(int M, int N)
 {
     return umma_idesc_bf16_f32(M, N) | (1u << 16);
 }
+// 32 bytes to a 32-byte boundary
+__device__ __forceinline__ void st_global_32(void *p, const uint32_t (&r)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+                 "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 // One thread of a converged warp, chosen by the hardware: the compiler then knows that a tcgen05 or TMA
 // instruction behind it is issued once, and takes its operands straight from uniform registers.
 __device__ __forceinline__ bool elect_one()
