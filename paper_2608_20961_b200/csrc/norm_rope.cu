@@ -6,6 +6,7 @@
 // with UPL units: the vectors that hold VE pairs.  As in the rotation alone a warp takes heads of one token with the same pairs
 // in every lane, so cosines, sines, weights and dw's partial sums stay in registers over the heads.  Every row is read once and
 // written once; HBM bounds a prompt, one launch and its lookups a decoding step.
+#include "ptx_sm100.cuh"
 #include "rows_common.cuh"
 
 namespace treewy {
@@ -22,14 +23,99 @@ __device__ __forceinline__ float group_sum(float x, int lanes)
     for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
+// Elementwise operations on VE numbers, two to an instruction: these kernels issue about as long as they wait for memory.
+template <int VE> __device__ __forceinline__ void mul_each(const float (&a)[VE], const float (&b)[VE], float (&r)[VE])
+{
+    if constexpr (VE == 1) {
+        r[0] = a[0] * b[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float2 y = ptx::mul2(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]));
+            r[e] = y.x, r[e + 1] = y.y;
+        }
+    }
+}
+template <int VE> __device__ __forceinline__ void mul_all(const float (&a)[VE], float b, float (&r)[VE])
+{
+    if constexpr (VE == 1) {
+        r[0] = a[0] * b;
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float2 y = ptx::mul2(make_float2(a[e], a[e + 1]), make_float2(b, b));
+            r[e] = y.x, r[e + 1] = y.y;
+        }
+    }
+}
+// r = a b + c
+template <int VE> __device__ __forceinline__ void fma_each(const float (&a)[VE], const float (&b)[VE], const float (&c)[VE], float (&r)[VE])
+{
+    if constexpr (VE == 1) {
+        r[0] = fmaf(a[0], b[0], c[0]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float2 y = ptx::fma2(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]), make_float2(c[e], c[e + 1]));
+            r[e] = y.x, r[e + 1] = y.y;
+        }
+    }
+}
+template <int VE> __device__ __forceinline__ void fma_all(const float (&a)[VE], float b, const float (&c)[VE], float (&r)[VE])
+{
+    if constexpr (VE == 1) {
+        r[0] = fmaf(a[0], b, c[0]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            const float2 y = ptx::fma2(make_float2(a[e], a[e + 1]), make_float2(b, b), make_float2(c[e], c[e + 1]));
+            r[e] = y.x, r[e + 1] = y.y;
+        }
+    }
+}
+// sum of a b over the VE numbers, onto two running sums
+template <int VE> __device__ __forceinline__ void dot_onto(const float (&a)[VE], const float (&b)[VE], float2 &sum)
+{
+    if constexpr (VE == 1) {
+        sum.x = fmaf(a[0], b[0], sum.x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) sum = ptx::fma2(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]), sum);
+    }
+}
+// A unit's pairs turned in place (split pairs: two numbers to an instruction)
+template <int VE> __device__ __forceinline__ void turn_pairs(float (&f)[VE], float (&g)[VE], const float (&cs)[VE], const float (&sn)[VE], bool split)
+{
+    float rf[VE], rg[VE];
+    if (VE > 1 && split) {
+        mul_each<VE>(g, cs, rg), mul_each<VE>(g, sn, rf);
+        fma_each<VE>(f, sn, rg, rg), mul_each<VE>(f, cs, f);
+        fma_all<VE>(rf, -1.f, f, f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) g[e] = rg[e];
+    } else {
+        turn_unit<VE>(f, g, cs, sn, split, rf, rg);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) f[e] = rf[e], g[e] = rg[e];
+    }
+}
 // `VE` weights from element e on
 template <int VE> __device__ __forceinline__ void load_weight(const NormView &n, int e, float (&w)[VE])
 {
+    if (VE == 1) {
+        w[0] = n.bf16 ? to_f32(static_cast<const __nv_bfloat16 *>(n.weight)[e]) : static_cast<const float *>(n.weight)[e];
+    } else if (n.bf16) {  // (e is a multiple of VE)
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-        const float x = n.bf16 ? to_f32(static_cast<const __nv_bfloat16 *>(n.weight)[e + i]) : static_cast<const float *>(n.weight)[e + i];
-        w[i] = n.plus_one ? 1.f + x : x;
+        for (int i = 0; i < VE; i += 4) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(n.weight) + e + i);
+            w[i] = bf16lo(x.x), w[i + 1] = bf16hi(x.x), w[i + 2] = bf16lo(x.y), w[i + 3] = bf16hi(x.y);
+        }
+    } else {
+        load_row<VE>(static_cast<const float *>(n.weight) + e, w);
     }
+    if (n.plus_one)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) w[i] += 1.f;
 }
 
 // Grid: one warp per (token, slice of heads): heads 0 .. H_q-1 of q, then those of k, then those of v.
@@ -82,6 +168,7 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, UPL == 1 ? 5 : 4) norm_rows_k
     const bool bad_pos = token_position(a, t, turned, &pos);
     long long at = 0;
     if (!place_row(a, t, bad_pos, &at)) return;
+    const bool split = !a.r.interleaved;
     float cs[UPL][VE], sn[UPL][VE];
     if (turned > 0)
 #pragma unroll
@@ -120,10 +207,9 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, UPL == 1 ? 5 : 4) norm_rows_k
                     for (int j = 0; j < UPL; ++j) {
                         float f[VE], g[VE];
                         x[i][j].get(f), y[i][j].get(g);
-                        float s = 0.f;
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) s += f[e] * f[e] + g[e] * g[e];
-                        if (ul + j * 32 < units && h0 + i * hpi + hl < run.h1) ss += s;
+                        float2 s = make_float2(0.f, 0.f);
+                        dot_onto<VE>(f, f, s), dot_onto<VE>(g, g, s);
+                        if (ul + j * 32 < units && h0 + i * hpi + hl < run.h1) ss += s.x + s.y;
                     }
                     r[i] = ss;
                 }
@@ -141,16 +227,13 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, UPL == 1 ? 5 : 4) norm_rows_k
                     if (turn) {
                         float f[VE], g[VE];
                         x[i][j].get(f), y[i][j].get(g);
-                        if (normed)
-#pragma unroll
-                            for (int e = 0; e < VE; ++e) f[e] *= r[i] * w0[j][e], g[e] *= r[i] * w1[j][e];
-                        if (u < turned) {
-                            float rf[VE], rg[VE];
-                            turn_unit<VE>(f, g, cs[j], sn[j], !a.r.interleaved, rf, rg);
-                            x[i][j].set(rf), y[i][j].set(rg);
-                        } else {
-                            x[i][j].set(f), y[i][j].set(g);
+                        if (normed) {
+                            float wr[VE];
+                            mul_all<VE>(w0[j], r[i], wr), mul_each<VE>(f, wr, f);
+                            mul_all<VE>(w1[j], r[i], wr), mul_each<VE>(g, wr, g);
                         }
+                        if (u < turned) turn_pairs<VE>(f, g, cs[j], sn[j], split);
+                        x[i][j].set(f), y[i][j].set(g);
                     }
                     x[i][j].store(dst + h * step + off0(u, turn)), y[i][j].store(dst + h * step + off1(u, turn));
                 }
@@ -207,6 +290,7 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
             if (lane == 0 && a.status) atomicOr(a.status, TREEWY_SEQ_BAD_POSITION);
             continue;
         }
+        const bool split = !a.r.interleaved;
         float cs[UPL][VE], sn[UPL][VE];
         if (turned > 0)
 #pragma unroll
@@ -218,39 +302,32 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
             for (int i = 0; i < HU; ++i) {
                 const int h = h0 + i * hpi + hl;
                 float f[UPL][VE], g[UPL][VE], gf[UPL][VE], gg[UPL][VE];
-                float ss = 0.f, sg = 0.f;
+                float2 ss = make_float2(0.f, 0.f), sg = ss;
 #pragma unroll
                 for (int j = 0; j < UPL; ++j) {
                     const int u = ul + j * 32;
                     if (u >= units || h >= h_end) continue;
-                    float p[VE], q[VE];
-                    x0[i][j].get(f[j]), x1[i][j].get(g[j]), y0[i][j].get(p), y1[i][j].get(q);
-                    if (u < turned) {
-                        turn_unit<VE>(p, q, cs[j], sn[j], !a.r.interleaved, gf[j], gg[j]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VE; ++e) gf[j][e] = p[e], gg[j][e] = q[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        ss += f[j][e] * f[j][e] + g[j][e] * g[j][e];
-                        sg += w0[j][e] * gf[j][e] * f[j][e] + w1[j][e] * gg[j][e] * g[j][e];
-                    }
+                    x0[i][j].get(f[j]), x1[i][j].get(g[j]), y0[i][j].get(gf[j]), y1[i][j].get(gg[j]);
+                    if (u < turned) turn_pairs<VE>(gf[j], gg[j], cs[j], sn[j], split);
+                    dot_onto<VE>(f[j], f[j], ss), dot_onto<VE>(g[j], g[j], ss);
+                    float p[VE];
+                    mul_each<VE>(w0[j], gf[j], p), dot_onto<VE>(p, f[j], sg);
+                    mul_each<VE>(w1[j], gg[j], p), dot_onto<VE>(p, g[j], sg);
                 }
-                const float r = rsqrtf(group_sum(ss, lph) * inv_d + na.norm.eps);
+                const float r = rsqrtf(group_sum(ss.x + ss.y, lph) * inv_d + na.norm.eps);
                 // dx = r w g - x r^3 mean(w g x)
-                const float c = group_sum(sg, lph) * inv_d * r * r * r;
+                const float c = -(group_sum(sg.x + sg.y, lph) * inv_d * r * r * r);
                 if (h >= h_end) continue;
 #pragma unroll
                 for (int j = 0; j < UPL; ++j) {
                     const int u = ul + j * 32;
                     if (u >= units) continue;
                     float p[VE], q[VE];
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        dw0[j][e] += gf[j][e] * (f[j][e] * r), dw1[j][e] += gg[j][e] * (g[j][e] * r);
-                        p[e] = r * w0[j][e] * gf[j][e] - c * f[j][e], q[e] = r * w1[j][e] * gg[j][e] - c * g[j][e];
-                    }
+                    // (g r, and of it dw += (g r) x and dx = w (g r) + c x)
+                    mul_all<VE>(gf[j], r, gf[j]), mul_all<VE>(gg[j], r, gg[j]);
+                    fma_each<VE>(gf[j], f[j], dw0[j], dw0[j]), fma_each<VE>(gg[j], g[j], dw1[j], dw1[j]);
+                    mul_all<VE>(f[j], c, p), mul_all<VE>(g[j], c, q);
+                    fma_each<VE>(w0[j], gf[j], p, p), fma_each<VE>(w1[j], gg[j], q, q);
                     x0[i][j].set(p), x1[i][j].set(q);
                     x0[i][j].store(dst + h * a.d + off0(u)), x1[i][j].store(dst + h * a.d + off1(u));
                 }

@@ -10,6 +10,7 @@ namespace treewy {
 namespace {
 
 constexpr int PT = 1024, PW = PT / 32;
+constexpr int MOST = 8;              // entries of a thread at a time
 constexpr int ROWS_IN_PLACE = 8192;  // rows up to which the one CTA writes positions and slots too
 
 struct PagesShared {
@@ -102,38 +103,55 @@ __global__ void __launch_bounds__(PT, 1) pages_reserve_kernel(const __grid_const
         __syncthreads();
         // pass 0 assigns where there is enough for every entry; else it only counts and pass 1 assigns
         const bool enough = used + (long long)E <= count;
-        int wants = 0;
+        int wants = 0, most = 0;
+        const int each = E <= PT ? 1 : E >= PT * MOST ? MOST : (E + PT - 1) / PT;
         for (int pass = 0; pass < (enough ? 1 : 2); ++pass) {
             int carry = used;
-            for (int x0 = 0; x0 < E; x0 += PT) {
-                const int x = x0 + tid;
-                int i = 0, e = 0, want = 0;
-                if (x < E) {
-                    i = owner(sh.off, nb, x);
-                    e = sh.first[i] + x - sh.off[i];
-                    const int p = a.page_table[(size_t)(c0 + i) * a.max_pages + e];
-                    want = p < 0;
-                    if (p >= a.n_pages && pass == 0) flag(a.seq_status, c0 + i, TREEWY_SEQ_BAD_PAGE);
+            for (int x0 = 0; x0 < E; x0 += PT * each) {
+                const int x1 = x0 + tid * each, here = min(each, E - x1);  // (none: negative)
+                const int i0 = here > 0 ? owner(sh.off, nb, x1) : 0;
+                int page[MOST], wanted = 0;
+                int i = i0;
+#pragma unroll
+                for (int q = 0; q < MOST; ++q) {
+                    page[q] = 0;
+                    if (q >= here) continue;
+                    while (x1 + q >= sh.off[i + 1]) ++i;
+                    page[q] = a.page_table[(size_t)(c0 + i) * a.max_pages + sh.first[i] + x1 + q - sh.off[i]];
                 }
+#pragma unroll
+                for (int q = 0; q < MOST; ++q) wanted += page[q] < 0;
                 int total;
-                const int rank = carry + block_scan(want, sh.warp_sum[0], &total);
-                if (pass == 0 && !enough && want) atomicMax(&sh.end_rank[i], rank + 1);
-                if ((enough || pass == 1) && want) {
-                    const int end = enough ? rank + 1 : sh.end_rank[i];
-                    if (end <= count) {
-                        const int p = a.free_pages[count - 1 - rank];
-                        if (p >= 0 && p < a.n_pages) a.page_table[(size_t)(c0 + i) * a.max_pages + e] = p;
-                        else flag(a.seq_status, c0 + i, TREEWY_SEQ_BAD_PAGE);
-                        atomicMax(&sh.taken, end);
+                int rank = carry + block_scan(wanted, sh.warp_sum[0], &total);
+                i = i0;
+#pragma unroll
+                for (int q = 0; q < MOST; ++q) {
+                    if (q >= here) continue;
+                    while (x1 + q >= sh.off[i + 1]) ++i;
+                    const int b = c0 + i;
+                    if (page[q] >= a.n_pages && pass == 0) flag(a.seq_status, b, TREEWY_SEQ_BAD_PAGE);
+                    if (page[q] >= 0) continue;
+                    if (pass == 0 && !enough) {
+                        atomicMax(&sh.end_rank[i], rank + 1);
                     } else {
-                        flag(a.seq_status, c0 + i, TREEWY_SEQ_NO_PAGES);
+                        const int end = enough ? rank + 1 : sh.end_rank[i];
+                        if (end <= count) {
+                            const int p = a.free_pages[count - 1 - rank];
+                            if (p >= 0 && p < a.n_pages) a.page_table[(size_t)b * a.max_pages + sh.first[i] + x1 + q - sh.off[i]] = p;
+                            else flag(a.seq_status, b, TREEWY_SEQ_BAD_PAGE);
+                            most = max(most, end);
+                        } else {
+                            flag(a.seq_status, b, TREEWY_SEQ_NO_PAGES);
+                        }
                     }
+                    ++rank;
                 }
                 carry += total;
             }
             wants = carry - used;
             __syncthreads();
         }
+        if (most > 0) atomicMax(&sh.taken, most);
         used += wants;
         if (rows_here) {
             for (int x = tid; x < R; x += PT) {
@@ -193,22 +211,35 @@ __global__ void __launch_bounds__(PT, 1) pages_release_kernel(const __grid_const
         sh.off[tid] = at;
         if (tid == 0) sh.off[nb] = E;
         __syncthreads();
-        for (int x0 = 0; x0 < E; x0 += PT) {
-            const int x = x0 + tid;
-            int i = 0, p = -1;
-            int32_t *entry = nullptr;
-            if (x < E) {
-                i = owner(sh.off, nb, x);
-                entry = &a.page_table[(size_t)(a.B - 1 - c0 - i) * a.max_pages + sh.first[i] - (x - sh.off[i])];
-                p = *entry;
+        const int each = E <= PT ? 1 : E >= PT * MOST ? MOST : (E + PT - 1) / PT;
+        for (int x0 = 0; x0 < E; x0 += PT * each) {
+            const int x1 = x0 + tid * each, here = min(each, E - x1);  // (none: negative)
+            const int i0 = here > 0 ? owner(sh.off, nb, x1) : 0;
+            auto entry = [&](int i, int q) { return &a.page_table[(size_t)(a.B - 1 - c0 - i) * a.max_pages + sh.first[i] - (x1 + q - sh.off[i])]; };
+            int page[MOST], back = 0;
+            int i = i0;
+#pragma unroll
+            for (int q = 0; q < MOST; ++q) {
+                page[q] = -1;
+                if (q >= here) continue;
+                while (x1 + q >= sh.off[i + 1]) ++i;
+                page[q] = *entry(i, q);
             }
-            const int back = p >= 0 && p < a.n_pages;
+#pragma unroll
+            for (int q = 0; q < MOST; ++q) back += page[q] >= 0 && page[q] < a.n_pages;
             int total;
-            const int to = count + block_scan(back, sh.warp_sum[0], &total);
-            if (p >= 0) {
-                *entry = -1;
-                if (back && to < a.n_pages) a.free_pages[to] = p;
+            int to = count + block_scan(back, sh.warp_sum[0], &total);
+            i = i0;
+#pragma unroll
+            for (int q = 0; q < MOST; ++q) {
+                if (q >= here) continue;
+                while (x1 + q >= sh.off[i + 1]) ++i;
+                if (page[q] < 0) continue;
+                *entry(i, q) = -1;
+                const bool is_page = page[q] < a.n_pages;
+                if (is_page && to < a.n_pages) a.free_pages[to] = page[q];
                 else flag(a.seq_status, a.B - 1 - c0 - i, TREEWY_SEQ_BAD_PAGE);
+                to += is_page;
             }
             count = (int)min((long long)a.n_pages, (long long)count + total);
         }

@@ -160,6 +160,7 @@ treewy_status_t treewy_kv_append_norm(const treewy_kv_cache_t *cache, const tree
     a.row_offsets = row_offsets, a.q = q, a.k = k, a.v = v, a.q_out = q_out;
     a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v, a.ld_qo = ld_qo;
     a.B = B, a.T = T, a.H_q = H_q, a.d = cache->d_head, a.status = seq_status;
+    if (!q_norm && !k_norm) return launched(launch_rows(a, io_dtype, static_cast<cudaStream_t>(cuda_stream)));
     return launched(launch_norm_rows(na, io_dtype, static_cast<cudaStream_t>(cuda_stream)));
 }
 
