@@ -72,8 +72,8 @@ treewy_status_t treewy_kv_append_norm(const treewy_kv_cache_t *cache, const tree
  * window 0: all x <= p.  scale is positive and finite.  What a row may not see is never multiplied; page table entries
  * whose tokens no row sees are not read (a window's old pages may be gone).
  *   q [T,H_q,d]   rotated already;  O [T,H_q,d] contiguous, io_dtype.  Rows of no sequence are left as they are.
- *   workspace     treewy_attn_chunk_workspace bytes; no initial contents, nothing kept between calls; calls that may
- *                 overlap in time need one each
+ *   workspace     treewy_attn_chunk_workspace bytes, which are enough for calls of fewer rows too; no initial contents,
+ *                 nothing kept between calls; calls that may overlap in time need one each
  * d_head is a multiple of 8, up to 256.  BF16 with d_head 64, 128 or 256, page_size a power of two from 8 and at most
  * 128 query heads to a key/value head takes the tensor-core kernel; everything else an fp32 SIMT kernel.  Scores, softmax
  * statistics and accumulators are fp32; the tensor-core kernel rounds the softmax weights to bf16 (at most 2^-8 of

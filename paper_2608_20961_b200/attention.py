@@ -478,19 +478,29 @@ def treewy_pages_release(pool: PagePool, first: torch.Tensor, end: torch.Tensor,
 
 
 class AttentionLayer:
-    """One attention layer's side of a speculative round, on the current stream: the paged cache, the rotary table and
-    a workspace stay with the layer; each call takes the round's packed rows.  The cache's ``context_len`` is
-    advanced by ``commit`` and ``append_and_attend``.  Layers of one model that share a context_len array leave that to the
-    last of them, since all of a round write at the same place: the others pass advance=False.
+    """One attention layer's side of a step -- a prompt or a piece of one, single tokens, a speculative round -- on the current
+    stream: the paged cache, the rotary table, the norms and workspaces stay with the layer; each call takes the step's packed
+    rows.  The cache's ``context_len`` is advanced by ``prefill``, ``commit`` and ``append_and_attend``.  Layers of one model that share
+    a context_len array leave that to the last of them, since all of a step write at the same place: the others pass
+    advance=False.
+
+    q_norm, k_norm: norms of the queries' and keys' heads ahead of the rotation.  window: a token sees the last `window` tokens,
+    its own among them, and the first `sinks` (0: all); pages that no later token sees may go back to a pool.  Draft trees see
+    everything, so a layer with a window has no ``verify``.
 
     seq_status [B], zeroed by the caller ahead of a round and passed to all of its calls, receives their flags; without it
     the layer keeps its own.  A sequence that is flagged in it, by whichever layer, keeps its length, and its rows of the
     outputs mean nothing."""
 
     def __init__(self, cache: KVCache, H_q: int, cos_sin: torch.Tensor, pair_axis: torch.Tensor | None = None,
-                 interleaved: bool = False, scale: float | None = None):
+                 interleaved: bool = False, scale: float | None = None, q_norm: HeadNorm | None = None,
+                 k_norm: HeadNorm | None = None, window: int = 0, sinks: int = 0):
         if H_q < 1 or H_q % cache.H_kv != 0:
             raise ValueError("H_q: a multiple of the cache's heads wanted")
+        if window < 0 or sinks < 0:
+            raise ValueError("window, sinks: not negative")
+        _norm(q_norm, cache.d_head, "q_norm", cache._dev), _norm(k_norm, cache.d_head, "k_norm", cache._dev)
+        self.q_norm, self.k_norm, self.window, self.sinks = q_norm, k_norm, window, sinks
         self.cache, self.H_q = cache, H_q
         self.cos_sin, self.pair_axis, self.interleaved = cos_sin, pair_axis, interleaved
         self.scale = cache.d_head ** -0.5 if scale is None else scale
@@ -502,6 +512,7 @@ class AttentionLayer:
         self._ahead = KVCache(cache.k, cache.v, cache.page_table, self._new_len)
         self._unseen = None                        # ancestor masks of nodes that see no draft row
         self._ws, self._ws_for = None, None
+        self._rows_ws, self._rows_for = None, 0    # workspace of prefill, and the rows it is for
 
     def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
         sizes = (tree.B, tree.T, tree.max_nodes, shared_len)
@@ -529,12 +540,18 @@ class AttentionLayer:
     def verify(self, tree: Tree, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                seq_status: torch.Tensor | None = None, shared_pages: torch.Tensor | None = None,
                shared_len: int = 0) -> torch.Tensor:
-        """Rotates q and k in place (keep k and v until commit) and returns the attention's output for every node."""
+        """Normalises and rotates q and k in place (keep k and v until commit) and returns the attention's output for every
+        node."""
+        if self.window > 0:
+            raise ValueError("a layer with a window verifies no trees")
         status = self._begin(tree, seq_status)
         rope = self._rope(positions)
         offsets = tree.node_offsets[:tree.B + 1]
-        treewy_rope_rows(rope, offsets, q, q, seq_status=status)
-        treewy_rope_rows(rope, offsets, k, k, seq_status=status)
+        for x, norm in ((q, self.q_norm), (k, self.k_norm)):
+            if norm is None:
+                treewy_rope_rows(rope, offsets, x, x, seq_status=status)
+            else:
+                treewy_norm_rope(norm, rope, x, x, offsets, status)
         O = self._out(q)
         treewy_attn_verify(self.cache, tree, q, k, v, self.scale, O, self._workspace(tree, shared_len), shared_pages,
                            shared_len, status)
@@ -559,10 +576,14 @@ class AttentionLayer:
         """Ordinary decoding: one token a sequence, written to the cache (rotated on the way) and attended from there."""
         if tree.T != tree.B:
             raise ValueError("tree: one node a sequence wanted")
+        if self.window > 0:
+            if shared_len > 0:
+                raise ValueError("shared_len: not beside a window")
+            return self._rows(tree.node_offsets, positions, q, k, v, self._begin(tree, seq_status), advance, one=True)
         status = self._begin(tree, seq_status)
         self._round = None
         q_out, O = self._out(q), self._out(q)
-        treewy_kv_append(self.cache, tree.node_offsets, k, v, self._rope(positions), q, q_out, status)
+        self._append(tree.node_offsets, positions, q, k, v, q_out, status)
         # The token is in the cache already: it is seen there and not as a draft row.  One node at most, so that a sequence with
         # none or with several is flagged.
         if shared_len > 0:                         # (with the token the attention would take one that is a token short)
@@ -576,3 +597,35 @@ class AttentionLayer:
         if advance:
             self._len.add_(status == 0)
         return O
+
+    def _append(self, offsets: torch.Tensor, positions: torch.Tensor, q, k, v, q_out, status) -> None:
+        rope = self._rope(positions)
+        if self.q_norm is None and self.k_norm is None:
+            treewy_kv_append(self.cache, offsets, k, v, rope, q, q_out, status)
+        else:
+            treewy_kv_append_norm(self.cache, offsets, k, v, self.k_norm, rope, q, q_out, self.q_norm, status)
+
+    def _rows(self, offsets: torch.Tensor, positions: torch.Tensor, q, k, v, status: torch.Tensor, advance: bool, one: bool) -> torch.Tensor:
+        """New rows enter the cache and attend to it.  one: a sequence with no row or with several is flagged."""
+        self._round = None
+        T, B = q.shape[0], self.cache.B
+        q_out, O = self._out(q), self._out(q)
+        counts = offsets[1:B + 1] - offsets[:B]
+        if one:
+            status |= (counts != 1) * tw.SEQ_TOO_MANY_NODES
+        self._append(offsets, positions, q, k, v, q_out, status)
+        if self._rows_ws is None or self._rows_for < T:
+            self._rows_ws, self._rows_for = attn_chunk_workspace(self.cache, T, self.H_q, self.window, self.sinks), T
+        treewy_attn_chunk(self.cache, offsets, q_out, self.scale, O, self._rows_ws, self.window, self.sinks, status)
+        if advance:
+            self._len.add_(counts * (status == 0))
+        return O
+
+    def prefill(self, row_offsets: torch.Tensor, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                seq_status: torch.Tensor | None = None, advance: bool = True) -> torch.Tensor:
+        """New tokens -- a prompt, a piece of one, or one each; any number a sequence, none among them -- at row_offsets [B + 1]:
+        normalised, rotated, written to the cache, and attended from there, each up to its own."""
+        _int32(row_offsets, self.cache.B + 1, "row_offsets", self.cache._dev)
+        _int32(seq_status, self.cache.B, "seq_status", self.cache._dev)
+        status = self._own.zero_() if seq_status is None else seq_status.view(-1)[:self.cache.B]
+        return self._rows(row_offsets.view(-1), positions, q, k, v, status, advance, one=False)

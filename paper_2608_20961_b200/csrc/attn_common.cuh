@@ -126,9 +126,10 @@ size_t norm_backward_workspace(int d);
 cudaError_t launch_norm_backward(const NormBackwardArgs &a, treewy_dtype_t io, cudaStream_t stream);
 cudaError_t launch_chunk_generic(const ChunkArgs &a, treewy_dtype_t io, cudaStream_t stream);
 size_t chunk_generic_workspace(const ChunkArgs &a);
+size_t chunk_generic_workspace_most(const ChunkArgs &a);
 bool chunk_tc_applies(const ChunkArgs &a, treewy_dtype_t io);
 cudaError_t launch_chunk_tc(const ChunkArgs &a, cudaStream_t stream);
-size_t chunk_tc_workspace(const ChunkArgs &a);
+size_t chunk_tc_workspace(const ChunkArgs &a);  // (grows with a.T; 0 for widths of heads without a tensor-core kernel)
 cudaError_t launch_pages_reserve(const PagesArgs &a, cudaStream_t stream);
 cudaError_t launch_pages_release(const PagesArgs &a, cudaStream_t stream);
 

@@ -366,6 +366,15 @@ size_t chunk_generic_workspace(const ChunkArgs &a)
     return p.parts > 1 ? (size_t)p.parts * p.rows * (a.c.d + 2) * sizeof(float) : 0;
 }
 
+// What calls of up to a.T rows need.  With more than one part there are fewer than TARGET_CTAS row blocks, T H_q / RB at least, and
+// parts <= TARGET_CTAS / blocks + 1: parts * rows is at most TARGET_CTAS * RB + rows (and MAX_PARTS * rows).
+size_t chunk_generic_workspace_most(const ChunkArgs &a)
+{
+    const long long all = TARGET_CTAS * RB, rows = (long long)a.T * a.H_q < all ? (long long)a.T * a.H_q : all;
+    const long long n = MAX_PARTS * rows < all + rows ? MAX_PARTS * rows : all + rows;
+    return (size_t)n * (a.c.d + 2) * sizeof(float);
+}
+
 cudaError_t launch_chunk_generic(const ChunkArgs &a, treewy_dtype_t io, cudaStream_t stream)
 {
     return io == TREEWY_BF16 ? launch_typed<__nv_bfloat16>(a, stream) : launch_typed<float>(a, stream);

@@ -1075,7 +1075,11 @@ bool chunk_tc_applies(const ChunkArgs &a, treewy_dtype_t io)
            c.stride_slot > 0 && (c.H_kv == 1 || c.stride_head > 0) && (c.n_pages == 1 || c.stride_page > 0) && a.G <= MT && units_fit(a);
 }
 
-size_t chunk_tc_workspace(const ChunkArgs &a) { return a.c.d == 256 ? workspace_of<256>(a) : a.c.d == 128 ? workspace_of<128>(a) : workspace_of<64>(a); }
+size_t chunk_tc_workspace(const ChunkArgs &a)
+{
+    if (a.G > MT) return 0;
+    return a.c.d == 256 ? workspace_of<256>(a) : a.c.d == 128 ? workspace_of<128>(a) : a.c.d == 64 ? workspace_of<64>(a) : 0;
+}
 
 cudaError_t launch_chunk_tc(const ChunkArgs &a, cudaStream_t stream)
 {

@@ -169,7 +169,7 @@ size_t treewy_attn_chunk_workspace(const treewy_kv_cache_t *cache, int32_t B, in
 {
     ChunkArgs a;
     if (chunk_args(cache, B, T, H_q, window, sinks, io_dtype, &a) != TREEWY_OK || B == 0 || T == 0) return 0;
-    const size_t g = chunk_generic_workspace(a), t = chunk_tc_applies(a, io_dtype) ? chunk_tc_workspace(a) : 0;
+    const size_t g = chunk_generic_workspace_most(a), t = io_dtype == TREEWY_BF16 ? chunk_tc_workspace(a) : 0;
     return g > t ? g : t;
 }
 

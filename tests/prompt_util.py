@@ -98,6 +98,30 @@ def chunk_reference(c: Case):
     return out, size
 
 
+def chunk_reference_gpu(c: Case):
+    """The same for larger cases without NaN, whole rows at a time on the GPU."""
+    out = torch.zeros(c.T, c.Hq, c.D, dtype=F64)
+    size, G = torch.zeros_like(out), c.Hq // c.Hkv
+    kc, vc, q = c.kc.cuda(), c.vc.cuda(), c.q.cuda()
+    for b in range(c.B):
+        if c.N[b] == 0:
+            continue
+        lo, L, n = int(c.offsets[b]), c.L[b], c.N[b]
+        pages = c.table[b, :-(-(L + n) // c.page)].long().clamp(min=0).cuda()
+        p, x = torch.arange(L, L + n, device="cuda")[:, None], torch.arange(L + n, device="cuda")
+        hidden = x > p
+        if c.window:
+            hidden |= (p - x >= c.window) & (x >= c.sinks)
+        for h in range(c.Hq):
+            k, v = (s[pages, :, h // G].reshape(-1, c.D)[:L + n].to(F64) for s in (kc, vc))
+            v = torch.where(hidden.all(0)[:, None], 0.0, v)
+            s = ((q[lo:lo + n, h].to(F64) @ k.T) * c.scale).masked_fill_(hidden, -math.inf)
+            w = torch.exp(s - s.amax(1, keepdim=True))
+            total = w.sum(1, keepdim=True)
+            out[lo:lo + n, h], size[lo:lo + n, h] = ((w @ y / total).cpu() for y in (v, v.abs()))
+    return out, size
+
+
 def assert_chunk(c: Case, O, ref, size, tensor_cores, rows=None):
     """The bounds of tests/attn_util.py: the same arithmetic."""
     au.assert_attn(c, O, ref, size, tensor_cores, rows)

@@ -204,3 +204,42 @@ def test_empty_calls_need_no_gpu(at):
     pool = at.PagePool(i32(0, 4), 8, 4, i32(4), i32(1))
     at.treewy_pages_reserve(pool, i32(0), i32(1), 0, stream=FakeStream())
     at.treewy_pages_release(pool, i32(0), i32(0), stream=FakeStream())
+
+
+def test_the_norms_gradient_against_differences():
+    """The formulas that the kernels are tested against, against differences of the forward formula in 64 bits."""
+    from tests import attn_util as au, prompt_util as pu
+    gen = torch.Generator().manual_seed(1)
+    x, w, dy = torch.randn(3, 2, 12, generator=gen, dtype=torch.float64), torch.rand(12, generator=gen, dtype=torch.float64) + 0.5, None
+    dy = torch.randn(3, 2, 12, generator=gen, dtype=torch.float64)
+    rope = (au.rope_table(8, 50), torch.randint(50, (2, 3), generator=gen, dtype=torch.int32), torch.tensor([0, 1, 1, 0], dtype=torch.uint8), False)
+    for plus_one in (False, True):
+        f = lambda x, w: float((pu.norm_reference(x, w, 0.01, rope, plus_one) * dy).sum())
+        dx, dw = pu.norm_backward_reference(x, w, 0.01, dy, rope, plus_one)
+        h = 1e-5
+        for t, grad in ((x, dx), (w, dw)):
+            for i in range(t.numel()):
+                d = torch.zeros_like(t)
+                d.view(-1)[i] = h
+                args = lambda s: (x + s * d, w) if t is x else (x, w + s * d)
+                diff = (f(*args(1)) - f(*args(-1))) / (2 * h)
+                assert abs(diff - float(grad.view(-1)[i])) < 1e-7
+
+
+def test_layer_refusals(at):
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    cache = at.KVCache(z(4, 8, 2, 64), z(4, 8, 2, 64), i32(2, 2), i32(2))
+    table = z(16, 64, dt=torch.float32)
+    for bad in (dict(window=-1), dict(sinks=-2), dict(q_norm=at.HeadNorm(z(32))), dict(k_norm=at.HeadNorm(z(32)))):
+        with pytest.raises(ValueError):
+            at.AttentionLayer(cache, 4, table, **bad)
+    layer = at.AttentionLayer(cache, 4, table, window=8, sinks=1)
+    tree = at.tw.Tree.empty(torch.tensor([0, 1, 2], dtype=torch.int32), i32(2), 1)
+    rows = (z(2, 4, 64), z(2, 2, 64), z(2, 2, 64))
+    with pytest.raises(ValueError):
+        layer.verify(tree, i32(2), *rows)
+    with pytest.raises(ValueError):
+        layer.append_and_attend(tree, i32(2), *rows, shared_pages=i32(1), shared_len=8)
+    with pytest.raises(ValueError):
+        layer.prefill(i32(2), i32(2), *rows)
