@@ -1,7 +1,11 @@
 """Speculative decoding of a small hybrid -- one Gated DeltaNet layer and one attention layer -- with every step of both
 layers in the library:
 
-    python examples/hybrid_decode.py [--sequences 4] [--tokens 24] [--nodes 12]
+    python examples/hybrid_decode.py [--sequences 4] [--tokens 24] [--nodes 12] [--prompt 0] [--head-norms]
+
+With --prompt, each sequence starts with up to that many tokens, a different number each: the GDN layer takes them as a chain, the
+attention layer as new rows.  Pages of the cache come from a pool on the GPU.  --head-norms: queries and keys are
+normalised ahead of the rotation.
 
 Each sequence is decoded twice.  First token by token: the attention layer appends the token's key and value to its paged
 cache (rotated on the way) and attends to it.  Then with draft trees: rotate, verify the tree through both layers, accept
@@ -28,7 +32,7 @@ HIDDEN, VOCAB, H_GDN, HQ, HKV, D, PAGE, PAGES = 256, 211, 2, 4, 2, 128, 16, 8
 class Hybrid:
     """hidden -> GDN layer -> attention layer -> logits, for the rows of a batch of draft trees."""
 
-    def __init__(self, B, dev, seed=0):
+    def __init__(self, B, dev, seed=0, head_norms=False):
         gen = torch.Generator().manual_seed(seed)
         w = lambda i, o: (torch.randn((i, o), generator=gen) / math.sqrt(i)).to(BF16).to(dev)
         self.B, self.dev = B, dev
@@ -38,24 +42,26 @@ class Hybrid:
         freq = 10000.0 ** (-torch.arange(D // 2, dtype=torch.float64) / (D // 2))
         angle = torch.arange(PAGES * PAGE, dtype=torch.float64)[:, None] * freq
         self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().to(dev)
+        norm = lambda: at.HeadNorm((1 + 0.1 * torch.randn(D, generator=gen)).to(BF16).to(dev)) if head_norms else None
+        self.q_norm, self.k_norm = norm(), norm()
         self.reset()
 
     def reset(self):
         B, dev = self.B, self.dev
         self.state = torch.zeros((B, H_GDN, 128, 128), dtype=BF16, device=dev)
         kv = lambda: torch.zeros((B * PAGES, PAGE, HKV, D), dtype=BF16, device=dev)
-        table = torch.randperm(B * PAGES, generator=torch.Generator().manual_seed(1)).to(I32).view(B, PAGES).to(dev)
-        self.cache = at.KVCache(kv(), kv(), table, torch.zeros(B, dtype=I32, device=dev))
-        self.layer = at.AttentionLayer(self.cache, HQ, self.cos_sin)
+        self.pool = at.PagePool.empty(B, PAGES, PAGE, B * PAGES, dev)
+        self.cache = at.KVCache(kv(), kv(), self.pool.page_table, torch.zeros(B, dtype=I32, device=dev))
+        self.layer = at.AttentionLayer(self.cache, HQ, self.cos_sin, q_norm=self.q_norm, k_norm=self.k_norm)
         self.status = torch.zeros(B, dtype=I32, device=dev)
 
     @staticmethod
     def _norm(x):
         return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
 
-    def verify(self, tokens, parent, offsets, append=False):
-        """Logits [T, VOCAB] of every node; keeps what commit needs.  append: trees of one node, whose key and value
-        go to the cache at once."""
+    def verify(self, tokens, parent, offsets, step="tree"):
+        """Logits [T, VOCAB] of every node; keeps what commit needs.  step: "token" (trees of one node) or "prompt" (chains), whose
+        keys and values go to the cache at once."""
         dev, T = self.dev, tokens.numel()
         tree = tw.Tree.empty(offsets, parent, H_GDN, int((offsets[1:] - offsets[:-1]).max()))
         x = self.embed[tokens]
@@ -74,38 +80,63 @@ class Hybrid:
         q = qkv[:, :HQ * D].unflatten(1, (HQ, D))
         k = qkv[:, HQ * D:(HQ + HKV) * D].unflatten(1, (HKV, D))
         v = qkv[:, (HQ + HKV) * D:].unflatten(1, (HKV, D))
-        seq = torch.repeat_interleave(torch.arange(self.B, device=dev), offsets[1:] - offsets[:-1])
-        positions = (self.cache.context_len[seq] + tree.depth[:T]).to(I32)
-        if append:
+        positions = torch.empty(T, dtype=I32, device=dev)
+        at.treewy_pages_reserve(self.pool, self.cache.context_len, offsets, T, positions, seq_status=self.status)
+        if step == "token":
             O = self.layer.append_and_attend(tree, positions, q, k, v, self.status)
-        else:
+        elif step == "prompt":
+            O = self.layer.prefill(offsets, positions, q, k, v, self.status)
+        else:                                       # pages for every node are enough for any path
+            seq = torch.repeat_interleave(torch.arange(self.B, device=dev), offsets[1:] - offsets[:-1])
+            positions = (self.cache.context_len[seq] + tree.depth[:T]).to(I32)
             O = self.layer.verify(tree, positions, q, k, v, self.status)
         self.tree, self.attn_k, self.attn_v = tree, k, v
         x = x + O.view(T, -1) @ self.attn_out
         assert not self.status.any(), self.status.tolist()
         return self._norm(x).float() @ self.embed.float().T
 
-    def commit(self, accepted):
+    def commit_state(self, accepted):
         tw.treewy_commit(self.state, self.gdn_U, self.gdn_k, self.tree, H_GDN, accepted, None, self.status)
+
+    def prompt(self, tokens):
+        """Takes the sequences' prompts (lists of tokens) and returns the token after each."""
+        self.reset()
+        count = torch.tensor([len(t) for t in tokens])
+        offsets = torch.cat([torch.zeros(1, dtype=torch.int64), count.cumsum(0)]).to(I32)
+        parent = torch.cat([torch.arange(-1, n - 1) for n in count.tolist()]).to(I32).to(self.dev)
+        logits = self.verify(torch.tensor(sum(tokens, []), device=self.dev), parent, offsets.to(self.dev), "prompt")
+        self.commit_state((count - 1).to(I32).to(self.dev))
+        return logits[(offsets[1:] - 1).long().to(self.dev)].argmax(-1)
+
+    def commit(self, accepted):
+        self.commit_state(accepted)
         self.layer.commit(self.tree, self.attn_k, self.attn_v, accepted, self.status)
 
 
-def one_by_one(model, first, n):
+def start(model, prompts):
+    """The first token of each sequence: what follows its prompt, or the only token of one that has no other."""
+    if max(len(p) for p in prompts) > 1:
+        return model.prompt(prompts)
     model.reset()
+    return torch.tensor([p[0] for p in prompts], device=model.dev)
+
+
+def one_by_one(model, prompts, n):
+    first = start(model, prompts)
     B, dev = model.B, model.dev
     offsets, parent = torch.arange(B + 1, dtype=I32, device=dev), torch.full((B,), -1, dtype=I32, device=dev)
     tokens, out = first, []
     for _ in range(n):
-        logits = model.verify(tokens, parent, offsets, append=True)
-        tw.treewy_commit(model.state, model.gdn_U, model.gdn_k, model.tree, H_GDN, torch.zeros(B, dtype=I32, device=dev), None, model.status)
+        logits = model.verify(tokens, parent, offsets, "token")
+        model.commit_state(torch.zeros(B, dtype=I32, device=dev))
         tokens = logits.argmax(-1)
         out.append(tokens)
     return torch.stack(out, 1).tolist()
 
 
-def speculative(model, first, n, nodes, known, seed=0):
+def speculative(model, prompts, n, nodes, known, seed=0):
     """known: the drafts' source (what a good draft model would propose)."""
-    model.reset()
+    first = start(model, prompts)
     gen = torch.Generator().manual_seed(seed)
     rand = lambda hi: int(torch.randint(hi, (1,), generator=gen))
     dev = model.dev
@@ -145,12 +176,14 @@ def main(argv=None):
     ap.add_argument("--sequences", type=int, default=4)
     ap.add_argument("--tokens", type=int, default=24)
     ap.add_argument("--nodes", type=int, default=12)
+    ap.add_argument("--prompt", type=int, default=0)
+    ap.add_argument("--head-norms", action="store_true")
     args = ap.parse_args(argv)
-    assert args.tokens + args.nodes <= PAGE * PAGES
-    model = Hybrid(args.sequences, torch.device("cuda:0"))
-    first = torch.arange(args.sequences, device=model.dev) + 1
-    plain = one_by_one(model, first, args.tokens)
-    spec, rounds = speculative(model, first, args.tokens, args.nodes, plain)
+    assert args.prompt <= tw.MAX_NODES and args.prompt + args.tokens + args.nodes <= PAGE * PAGES
+    model = Hybrid(args.sequences, torch.device("cuda:0"), head_norms=args.head_norms)
+    prompts = [[(b + 1 + 7 * i) % VOCAB for i in range(max(1, args.prompt - 3 * b))] for b in range(args.sequences)]
+    plain = one_by_one(model, prompts, args.tokens)
+    spec, rounds = speculative(model, prompts, args.tokens, args.nodes, plain)
     same = plain == spec
     print(f"{args.tokens} tokens of {args.sequences} sequences: {args.tokens} steps one by one, {rounds} rounds of trees of "
           f"{args.nodes} nodes; the same tokens: {same}")
