@@ -90,6 +90,32 @@ def test_a_cache_past_2_31_elements():
         pu.assert_chunk(small, O.cpu(), ref, size, tensor_cores=not generic)
 
 
+# ------------------------------------------------------------------------------------------ many pages
+
+@pytest.mark.parametrize("short", [0, 1, 70001])
+def test_pages_of_more_entries_than_are_taken_at_a_time(short):
+    """Lines of 2^17 entries and more: one long sequence among short ones, more sequences than threads; and a pool that ends within."""
+    from tests.test_gpu_prompt import _pool, _release, _reserve
+    rng = np.random.default_rng(short)
+    N = [3, 140000, 0, 1, 20000, 5, 5]
+    n_pages = sum(N) - short
+    p = pu.Pages([[-1] * 140010 for _ in N], rng.permutation(n_pages).tolist(), n_pages, 1, n_pages)
+    pool, off = _pool(p), np.concatenate([[0], np.cumsum(N)]).tolist()
+    _reserve(pool, p, [0] * len(N), off, off[-1])
+    _release(pool, p, [1, 7, 0, 0, 3, 0, 0], [3, 139990, 5, 0, 20000, 5, 1 << 30])
+    _reserve(pool, p, [1, 7, 0, 1, 3, 0, 0], off, off[-1])
+    many = 3000
+    p = pu.Pages([[-1] * 9 for _ in range(many)], rng.permutation(many * 4).tolist(), many * 4, 8, many * 4)
+    pool = _pool(p)
+    for most in (10, 60):                               # (the second time the pool ends)
+        N = rng.integers(0, most, many).tolist()
+        off = np.concatenate([[0], np.cumsum(N)]).tolist()
+        L = [8 * sum(x >= 0 for x in r) for r in p.table]
+        L = [l if l + n <= 72 else 0 for l, n in zip(L, N)]
+        _reserve(pool, p, L, off, off[-1])
+    _release(pool, p, [8] * many, [40] * many)
+
+
 # ------------------------------------------------------------------------------------------ a layer's steps
 
 def _layer(dtype, window, sinks, normed, B=3, Hq=8, Hkv=2, D=128, page=16, max_pages=40, seed=0):
