@@ -192,7 +192,7 @@ template <int CL> __global__ void __launch_bounds__(PT, 1) pages_reserve_kernel(
                     entry[q] = -1, page[q] = 0;
                     const unsigned x = x0 + (warp * each + q) * 32 + lane;
                     if (q >= each || x >= (unsigned)E) continue;
-                    if (q == 0 || (int)x >= sh.off[i + 1]) i = owner(sh.off, nb, x, i);
+                    if (q == 0 || ((int)x >= sh.off[i + 1] && (int)x >= sh.off[++i + 1])) i = owner(sh.off, nb, x, i);  // (often the next one)
                     entry[q] = (c0 + i) * a.max_pages + sh.first[i] + (int)x - sh.off[i];
                     page[q] = a.page_table[entry[q]];
                 }
@@ -313,7 +313,7 @@ template <int CL> __global__ void __launch_bounds__(PT, 1) pages_release_kernel(
                 entry[q] = -1, page[q] = -1;
                 const unsigned x = x0 + (warp * each + q) * 32 + lane;
                 if (q >= each || x >= (unsigned)E) continue;
-                if (q == 0 || (int)x >= sh.off[i + 1]) i = owner(sh.off, nb, x, i);
+                if (q == 0 || ((int)x >= sh.off[i + 1] && (int)x >= sh.off[++i + 1])) i = owner(sh.off, nb, x, i);  // (often the next one)
                 entry[q] = (a.B - 1 - c0 - i) * a.max_pages + sh.first[i] - ((int)x - sh.off[i]);
                 page[q] = a.page_table[entry[q]];
             }
