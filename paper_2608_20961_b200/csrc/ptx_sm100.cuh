@@ -489,6 +489,11 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
+// asks for `bytes` (a multiple of 16) from an address of 16 bytes on to be brought to L2
+__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
