@@ -303,7 +303,12 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
             for (int j = 0; j < UPL; ++j) unit_angles<VE>(a.r, ul + j * 32, ul + j * 32 < turned, pos, cs[j], sn[j]);
 #pragma unroll 1
         for (int h0 = h_begin; h0 < h_end; h0 += hpi * HU) {
-            if (h0 > h_begin) load(h0);
+            Vec<T, VE> p0[HU][UPL], p1[HU][UPL], q0[HU][UPL], q1[HU][UPL];
+#pragma unroll
+            for (int i = 0; i < HU; ++i)
+#pragma unroll
+                for (int j = 0; j < UPL; ++j) p0[i][j] = x0[i][j], p1[i][j] = x1[i][j], q0[i][j] = y0[i][j], q1[i][j] = y1[i][j];
+            if (h0 + hpi * HU < h_end) load(h0 + hpi * HU);  // (on their way while these are worked on: 8199 rows of 32 heads of 128 54 -> 45 us)
 #pragma unroll
             for (int i = 0; i < HU; ++i) {
                 const int h = h0 + i * hpi + hl;
@@ -313,7 +318,7 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
                 for (int j = 0; j < UPL; ++j) {
                     const int u = ul + j * 32;
                     if (u >= units || h >= h_end) continue;
-                    x0[i][j].get(f[j]), x1[i][j].get(g[j]), y0[i][j].get(gf[j]), y1[i][j].get(gg[j]);
+                    p0[i][j].get(f[j]), p1[i][j].get(g[j]), q0[i][j].get(gf[j]), q1[i][j].get(gg[j]);
                     if (u < turned) turn_pairs<VE>(gf[j], gg[j], cs[j], sn[j], split);
                     dot_onto<VE>(f[j], f[j], ss), dot_onto<VE>(g[j], g[j], ss);
                     float p[VE];
@@ -334,8 +339,8 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
                     fma_each<VE>(gf[j], f[j], dw0[j], dw0[j]), fma_each<VE>(gg[j], g[j], dw1[j], dw1[j]);
                     mul_all<VE>(f[j], c, p), mul_all<VE>(g[j], c, q);
                     fma_each<VE>(w0[j], gf[j], p, p), fma_each<VE>(w1[j], gg[j], q, q);
-                    x0[i][j].set(p), x1[i][j].set(q);
-                    x0[i][j].store(dst + h * a.d + off0(u)), x1[i][j].store(dst + h * a.d + off1(u));
+                    p0[i][j].set(p), p1[i][j].set(q);
+                    p0[i][j].store(dst + h * a.d + off0(u)), p1[i][j].store(dst + h * a.d + off1(u));
                 }
             }
         }
