@@ -6,7 +6,8 @@
 // the last row, as one line.  It walks them in tiles of 64 with the running maximum, sum and output of a softmax; parts
 // are joined by a second kernel with the same rule.  Only tiles that some row does not see whole are masked: a masked weight is
 // a negative number that the product skips, so what a row may not see is never multiplied.
-// It is bound by the fp32 units and by shared memory (4 x 4 scores to a thread, four keys of a row's weights at a time).
+// It is bound by shared memory (4 x 4 scores to a thread, four keys of a row's weights at a time), small calls by the chain of one step and
+// the join: fp32, a prompt of 2048 with 32 / 8 heads of 128 2.09 ms, 16 TFLOP/s; four pieces of up to 77 rows with heads of 80 28 us.
 #include <type_traits>
 
 #include "attn_common.cuh"

@@ -9,9 +9,24 @@
 // row.  Tiles that some row does not see whole are masked, those that no row of a stream sees are left out for it.
 // One tile of a stream:  S = Q K^T, the softmax step in registers (a row to a thread), P = weights as bf16 over S's
 // own columns, O += P V (V read with its rows as the K index).  A stream has two S buffers or more, and its scores are issued as many tiles
-// ahead of its products: the next S is there when a softmax step ends.  The running maximum m moves only when a row's new maximum
-// exceeds it by more than 8 (in log2): until then weights are at most 2^8 and nothing overflows, and the pass over O
-// that a new m costs is rare after a row's first tiles.
+// ahead of its products: the next S is there when a softmax step ends.
+// Softmax.  o = sum_x 2^{s_x - m} v_x / sum_x 2^{s_x - m} (s in log2) for any reference m.  A row's m is the maximum of its first tile and
+// stays: weights are exponents of fp32 and, in P, of bf16, which has its range, so nothing is lost until they come near overflow.  Only when a
+// row's weights of one tile add up to more than 2^40 (or to NaN) its m becomes the maximum so far and O and l are scaled.  So an ordinary tile
+// has no maximum, no exchange between threads and no pass over O: an fma and an exponential a weight, an addition, half a packing.
+//
+// What bounds it.  Heads of 128, a prompt of 8192 over 32 / 8 heads (550 GFLOP), 520-540 us, 1040 TFLOP/s or 0.61 of the measured GEMM rate.
+// Without the exponentials it takes 446, without half of Q K^T 502, without both 380: three things are about equally long.  The
+// tensor cores: an MMA of Q K^T with both operands in shared memory takes 50 cycles for 64 keys where its arithmetic takes 32, since the
+// operands are 6 kB at 128 bytes a cycle; with P in tensor memory P V runs at its arithmetic.  The exponentials: 16 a cycle and SM, 1024 of some 2100 cycles a
+// tile of both streams.  And the softmax warps' own latency, 2 of them to a scheduler that issues 0.37 a cycle.  Heads of 64: 490 us (562
+// TFLOP/s), without exponentials 322.  Heads of 256 (one stream, four S buffers): 510-520 us (1060).  Decoding, 64 sequences
+// of 8192: 218 us, 6 TB/s, HBM.
+//
+// Why so.  What else was built and measured on the prompt of 8192, heads of 128 (and 64), against this: a row split over two threads
+// 585; key tiles of 128 with one S buffer 773; two warpgroups a stream on alternate tiles, the reference passed between them, 1120 (1080); three S buffers for
+// heads of 64 (504 there, window 253 -> 239); one MMA thread for both streams 719; exponentials partly on the FMA pipes 653
+// where this form had 606; the next S loaded ahead of the weights' store 714 where this form had 540.
 //
 // Work.  (sequence, head, item) in one line, an item's length being its start's cost and its keys, cut into equal parts,
 // one for each CTA: no CTA waits for a longer neighbour, whatever the lengths and windows.  A cut item leaves unnormalised
