@@ -513,6 +513,7 @@ class AttentionLayer:
         self._unseen = None                        # ancestor masks of nodes that see no draft row
         self._ws, self._ws_for = None, None
         self._rows_ws, self._rows_for = None, 0    # workspace of prefill, and the rows it is for
+        self._captured = []                        # those that graphs refer to stay
 
     def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
         sizes = (tree.B, tree.T, tree.max_nodes, shared_len)
@@ -616,6 +617,8 @@ class AttentionLayer:
         self._append(offsets, positions, q, k, v, q_out, status)
         if self._rows_ws is None or self._rows_for < T:
             self._rows_ws, self._rows_for = attn_chunk_workspace(self.cache, T, self.H_q, self.window, self.sinks), T
+        if q.is_cuda and torch.cuda.is_current_stream_capturing() and not any(ws is self._rows_ws for ws in self._captured):
+            self._captured.append(self._rows_ws)
         treewy_attn_chunk(self.cache, offsets, q_out, self.scale, O, self._rows_ws, self.window, self.sinks, status)
         if advance:
             self._len.add_(counts * (status == 0))

@@ -36,6 +36,7 @@ Parts parts_of(const ChunkArgs &a)
     const long long ctas = p.blocks * a.c.H_kv;
     long long n = ctas > 0 ? (TARGET_CTAS + ctas - 1) / ctas : 1;
     if (n > most / MIN_KEYS) n = most / MIN_KEYS;
+    if (a.B > 65535) n = 1;            // (the join's grid has a sequence a row)
     p.parts = (int)(n < 1 ? 1 : n > MAX_PARTS ? MAX_PARTS : n);
     return p;
 }
@@ -341,7 +342,7 @@ template <typename T, int RPT> cudaError_t launch_rpt(const ChunkArgs &a, const 
     if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void *>(chunk_generic_kernel<T, RPT>), smem_of(256), dev);
     if (e != cudaSuccess) return e;
     const long long x = p.blocks < 1 ? 1 : p.blocks > 0x7fffffffll ? 0x7fffffffll : p.blocks;
-    if (a.c.H_kv > 65535 || (p.parts > 1 && a.B > 65535)) return cudaErrorInvalidValue;
+    if (a.c.H_kv > 65535) return cudaErrorInvalidValue;
     e = launch_dependent(chunk_generic_kernel<T, RPT>, dim3((unsigned)x, p.parts, a.c.H_kv), dim3(THREADS), smem_of(a.c.d), stream, a, p.parts, part_ml,
                          part_o);
     if (e != cudaSuccess || p.parts == 1) return e;

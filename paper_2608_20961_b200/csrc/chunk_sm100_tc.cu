@@ -409,6 +409,8 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 unsigned found = 0;     // items
                 auto find = [&]() -> bool {
                     Item it;
+                    // (the limit is an item's: a long call's items may take seconds in all)
+                    ptx::wait_deadline_init(a.wait_cycles);
                     next_item<D>(a, ws, part, walk, it, true);
                     if (found >= ITEMS && !ptx::mbar_wait(&sh.item_empty[found % ITEMS], (found / ITEMS - 1) & 1)) return false;
                     sh.items[found % ITEMS] = it;

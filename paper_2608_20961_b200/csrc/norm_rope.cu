@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, UPL == 1 ? 5 : 4) norm_rows_k
     if (VE > 1 && lane < 3 && h_end - h_begin > hpi * HU) {
         const Run rest = run_of(lane);
         const int h0 = lane == kind ? min(rest.h0 + hpi * HU, rest.h1) : rest.h0;
-        if (h0 < rest.h1) ptx::prefetch_l2(rest.src + h0 * a.d, (uint32_t)((rest.h1 - h0) * a.d * (int)sizeof(T)));
+        if (h0 < rest.h1) ptx::prefetch_l2(rest.src + h0 * a.d, (uint32_t)min((long long)(rest.h1 - h0) * a.d * (int)sizeof(T), 65536ll));
     }
 
     int pos;

@@ -364,6 +364,112 @@ def test_a_step_captured_and_on_another_stream_is_the_eager_one(dtype):
     _same(want, got)
 
 
+def test_a_captured_prefill_keeps_its_workspace():
+    """A longer prompt makes the layer take a larger workspace; a graph that was captured ahead of that still has its own."""
+    from paper_2608_20961_b200 import attention as at
+    layer, pool = _layer(BF16, 0, 0, True, B=1, max_pages=400, seed=4)
+    gen = torch.Generator().manual_seed(4)
+    first = _qkv(layer, 5000, gen)
+    first = [x.contiguous() for x in first]
+    pos, off = torch.empty(5000, dtype=I32, device=DEV), _int(0, 5000)
+    at.treewy_pages_reserve(pool, layer.cache.context_len, off, 5000, pos)
+    layer.prefill(off, pos, *first)
+    layer._rows_ws, layer._rows_for = None, 0
+    q, k, v = (x.contiguous() for x in _qkv(layer, 3, gen))
+    pos, off = torch.empty(3, dtype=I32, device=DEV), _int(0, 3)
+    at.treewy_pages_reserve(pool, layer.cache.context_len, off, 3, pos)
+    want = layer.prefill(off, pos, q, k, v, advance=False).clone()     # (sizes the workspace outside the graph)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = layer.prefill(off, pos, q, k, v, advance=False)
+    small = layer._rows_ws.numel()
+    layer.prefill(_int(0, 700), torch.arange(5000, 5700, dtype=I32, device=DEV), *_qkv(layer, 700, gen), advance=False)
+    assert layer._rows_ws.numel() > small
+    held = [torch.full((small,), 0x5a, dtype=torch.uint8, device=DEV) for _ in range(4)]    # whoever is given freed memory
+    layer.prefill(off, pos, q, k, v, advance=False)                    # (the rows that the graph writes are there again)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(bool((h == 0x5a).all()) for h in held)
+
+
+def test_a_long_call_does_not_run_out_of_time():
+    """The limit of the waits is for an item's work: a call of many items may take longer (here: a limit of a millisecond, a call of two)."""
+    from paper_2608_20961_b200 import binding as tw
+    c = pu.make_case([0], [16384], Hq=32, Hkv=8, D=128, seed=13, poison=False)
+    want, status = pu.run_chunk(c)
+    assert not any(status)
+    try:
+        tw.treewy_debug_inject(2_000_000, -1)
+        O, status = pu.run_chunk(c)
+    finally:
+        tw.treewy_debug_inject(0, -1)
+    assert not any(status) and torch.equal(O, want)
+
+
+def test_nothing_to_do():
+    from paper_2608_20961_b200 import attention as at
+    layer, pool = _layer(BF16, 30, 2, True)
+    off, none = _int(0, 0, 0, 0), torch.empty(0, dtype=I32, device=DEV)
+    at.treewy_pages_reserve(pool, layer.cache.context_len, off, 0, none)
+    O = layer.prefill(off, none, *_qkv(layer, 0, torch.Generator().manual_seed(0)))
+    assert O.shape == (0, 8, 128) and not layer.cache.context_len.any() and int(pool.free_count) == pool.n_pages
+
+
+@pytest.mark.parametrize("Hq,D", [(127, 64), (128, 128), (128, 256), (129, 64), (200, 128)])
+def test_many_query_heads_to_one(Hq, D):
+    """Up to a whole row tile to a token, and beyond it (the SIMT kernel)."""
+    c = pu.make_case([300, 0], [3, 20], Hq=Hq, Hkv=1, D=D, page=16, window=90, sinks=5, seed=14)
+    ref, size = pu.chunk_reference(c)
+    O, status = pu.run_chunk(c)
+    assert not any(status)
+    pu.assert_chunk(c, O, ref, size, tensor_cores=Hq <= 128)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_outputs_on_any_16_bytes(D):
+    from paper_2608_20961_b200 import attention as at
+    c = pu.make_case([100, 3000], [200, 2], Hq=4, Hkv=2, D=D, seed=15, poison=False)
+    want, g = pu.run_chunk(c)[0].to(DEV), pu.on_gpu(c)
+    ws = at.attn_chunk_workspace(g["cache"], c.T, c.Hq)
+    wide = torch.full((want.numel() + 24,), 7.0, dtype=BF16, device=DEV)
+    O = wide[8:8 + want.numel()].view_as(want)                    # 16 bytes past a boundary of 32
+    at.treewy_attn_chunk(g["cache"], g["offsets"], g["q"], c.scale, O, ws)
+    assert torch.equal(O, want) and (wide[:8] == 7).all() and (wide[8 + want.numel():] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_more_sequences_than_a_grid_has_rows(dtype):
+    from paper_2608_20961_b200 import attention as at
+    B, D, page = 70000, 64, 16
+    gen = torch.Generator().manual_seed(16)
+    where = {3: 2, 65536: 1, 69999: 4}
+    N = torch.zeros(B, dtype=I32)
+    for b, n in where.items():
+        N[b] = n
+    off = torch.cat([torch.zeros(1, dtype=I32), N.cumsum(0).to(I32)]).to(DEV)
+    T, L = 7, 1000
+    pages = -(-(L + 4) // page)
+    table = torch.arange(pages, dtype=I32, device=DEV).repeat(B, 1)              # all read the same tokens
+    k, v = (torch.randn(pages, page, 1, D, generator=gen).to(dtype).to(DEV) for _ in range(2))
+    q = torch.randn(T, 2, D, generator=gen).to(dtype).to(DEV)
+    lens = torch.full((B,), L, dtype=I32, device=DEV)
+    cache = at.KVCache(k, v, table, lens)
+    O, status = torch.empty_like(q), torch.zeros(B, dtype=I32, device=DEV)
+    at.treewy_attn_chunk(cache, off, q, 0.125, O, at.attn_chunk_workspace(cache, T, 2), seq_status=status)
+    assert not status.any()
+    one = at.KVCache(k, v, table[:1], lens[:1])
+    lo = 0
+    for n in where.values():
+        P = torch.empty_like(q[lo:lo + n])
+        at.treewy_attn_chunk(one, _int(0, n), q[lo:lo + n], 0.125, P, at.attn_chunk_workspace(one, n, 2))
+        # (cut in other places: each is within its bound of the sum, |v| at most 5)
+        assert (O[lo:lo + n].to(F64) - P.to(F64)).abs().max() <= (2 * 2.0 ** -7 if dtype == BF16 else 2.0 ** -17) * 5
+        lo += n
+    x, y = torch.randn(T, 1, D, generator=gen).to(dtype).to(DEV), torch.randn(T, 1, D, generator=gen).to(dtype).to(DEV)
+    at.treewy_kv_append_norm(cache, off, x, y, at.HeadNorm(torch.ones(D, device=DEV)), seq_status=status)
+    assert not status.any()
+
+
 def test_two_graphs_on_one_workspace():
     """One after the other; what a call leaves there is nothing that the other reads."""
     from paper_2608_20961_b200 import attention as at
