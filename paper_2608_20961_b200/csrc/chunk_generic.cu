@@ -1,13 +1,14 @@
 // treewy_attn_chunk on the CUDA cores, fp32 throughout: the path of F32 inputs and of sizes the tensor-core kernel does
 // not take, and its cross-check.
 //
-// A CTA takes 64 query rows of one (sequence, key/value head) -- a row is a token and one of the G query heads that
+// A CTA takes 64 query rows (in small calls and decoding 32 or 16) of one (sequence, key/value head) -- a row is a token and one of the G query heads that
 // read this head -- and one part of the keys that some of them see: the sinks, then the window of the first row up to
 // the last row, as one line.  It walks them in tiles of 64 with the running maximum, sum and output of a softmax; parts
 // are joined by a second kernel with the same rule.  Only tiles that some row does not see whole are masked: a masked weight is
 // a negative number that the product skips, so what a row may not see is never multiplied.
 // It is bound by shared memory (4 x 4 scores to a thread, four keys of a row's weights at a time), small calls by the chain of one step and
-// the join: fp32, a prompt of 2048 with 32 / 8 heads of 128 2.09 ms, 16 TFLOP/s; four pieces of up to 77 rows with heads of 80 28 us.
+// the join: fp32, a prompt of 2048 with 32 / 8 heads of 128 2.06 ms, 17 TFLOP/s; one token over 8192 keys 68 us (157 in blocks of 64 rows); four pieces of up
+// to 77 rows with heads of 80 16.6.
 #include <type_traits>
 
 #include "attn_common.cuh"
@@ -15,29 +16,44 @@
 namespace treewy {
 namespace {
 
-constexpr int THREADS = 256, RB = 64, KB = 64, PS = KB + 4;
+constexpr int THREADS = 256, RB_MOST = 64, RB_LEAST = 16, KB_MOST = 64;
 constexpr int TARGET_CTAS = 296;   // two to an SM (heads of 256: one, 220 KB)
-constexpr int MIN_KEYS = 64;       // of a part: one step
 constexpr int MAX_PARTS = 32;
 constexpr float MASKED = -1.f, PAGE_BAD = -1.f;
 
 struct Parts {
+    int rb, kb;              // rows of a block, keys of a step (and of a part at least)
     int parts;
     long long blocks, rows;  // row blocks under one head (at most, of ranges that do not overlap); T * H_q
 };
-Parts parts_of(const ChunkArgs &a)
+Parts parts_of(const ChunkArgs &a, int rb, int kb)
 {
     Parts p;
-    p.blocks = (long long)a.T * a.G / RB + (a.B < a.T ? a.B : a.T);
+    p.rb = rb, p.kb = kb;
+    p.blocks = (long long)a.T * a.G / rb + (a.B < a.T ? a.B : a.T);
     p.rows = (long long)a.T * a.H_q;
     long long most = (long long)a.c.max_pages * a.c.page_size;
-    const long long seen = (long long)a.window + a.sinks + RB;
+    const long long seen = (long long)a.window + a.sinks + rb;
     if (most > seen) most = seen;
     const long long ctas = p.blocks * a.c.H_kv;
     long long n = ctas > 0 ? (TARGET_CTAS + ctas - 1) / ctas : 1;
-    if (n > most / MIN_KEYS) n = most / MIN_KEYS;
+    if (n > most / kb) n = most / kb;
     if (a.B > 65535) n = 1;            // (the join's grid has a sequence a row)
     p.parts = (int)(n < 1 ? 1 : n > MAX_PARTS ? MAX_PARTS : n);
+    return p;
+}
+// Blocks of 64 rows, of 32 or 16 where that many are a sequence's on average (decoding); and steps of 64 keys.  Where those would leave SMs without work blocks
+// of half as many rows, and steps of 32 as well if they still do: a step is shorter then (four pieces of up to 77 rows behind a window of 100, heads
+// of 80: 28 us, 19.6, 16.6).
+Parts parts_of(const ChunkArgs &a)
+{
+    const long long sequences = a.B < a.T ? a.B : a.T, rows = (long long)a.T * a.G;
+    int rb = RB_MOST;
+    while (rb > RB_LEAST && rows <= rb / 2 * sequences) rb /= 2;
+    Parts p = parts_of(a, rb, KB_MOST);
+    auto few = [&]() { return p.blocks * a.c.H_kv * p.parts < TARGET_CTAS / 2; };
+    if (few() && rb > RB_LEAST) p = parts_of(a, rb / 2, KB_MOST);
+    if (few()) p = parts_of(a, p.rb, KB_MOST / 2);
     return p;
 }
 
@@ -67,7 +83,7 @@ struct ScanShared {
 };
 // Row block `x` of the batch (all sequences' blocks in one line), for the whole CTA.  Sequences that are flagged have none.
 // total: row blocks of all.
-__device__ Where find_block(const ChunkArgs &a, long long x, ScanShared &sh, long long *total, bool set_flags)
+template <int RB> __device__ Where find_block(const ChunkArgs &a, long long x, ScanShared &sh, long long *total, bool set_flags)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     long long before = 0;
@@ -103,10 +119,11 @@ __device__ Where find_block(const ChunkArgs &a, long long x, ScanShared &sh, lon
     return sh.found;
 }
 
-// RPT: rows of a thread in the product with v, (RB / RPT) * (d / 4) <= THREADS.
-template <typename T, int RPT>
+// RB: rows of a block, KB: keys of a step, RPT: rows of a thread in the product with v, (RB / RPT) * (d / 4) <= THREADS.
+template <typename T, int RB, int KB, int RPT>
 __global__ void __launch_bounds__(THREADS) chunk_generic_kernel(const __grid_constant__ ChunkArgs a, int parts, float *part_ml, float *part_o)
 {
+    constexpr int PS = KB + 4, NE = KB / 32;       // a row of weights; keys of a lane
     extern __shared__ float4 smem4[];
     __shared__ ScanShared scan;
     __shared__ float s_alpha[RB], s_m[RB], s_l[RB];
@@ -122,7 +139,7 @@ __global__ void __launch_bounds__(THREADS) chunk_generic_kernel(const __grid_con
 
     long long total = 0x7fffffffffffffffll;        // (known after the first look)
     for (long long x = blockIdx.x; x < total; x += gridDim.x) {
-        const Where w = find_block(a, x, scan, &total, x == blockIdx.x && blockIdx.x == 0 && part == 0 && h == 0);
+        const Where w = find_block<RB>(a, x, scan, &total, x == blockIdx.x && blockIdx.x == 0 && part == 0 && h == 0);
         if (w.b < 0) break;                        // (the same in every thread)
         const long long rows = (long long)w.n * a.G, r0 = (long long)w.r0 * RB;
         const int b = w.b, lo = w.lo, len = w.len;
@@ -196,48 +213,53 @@ __global__ void __launch_bounds__(THREADS) chunk_generic_kernel(const __grid_con
             if (warp == THREADS / 32 - 1 && t0 + KB < k1) locate(t0 + KB, buf ^ 1);
             __syncthreads();
             {   // scores: rows ty + 16 i, keys tx + 16 j of a thread
+                constexpr int RI = RB / 16;
                 const int tx = tid & 15, ty = tid >> 4;
-                float s[4][4] = {};
+                float s[RI][KB / 16] = {};
 #pragma unroll 2
                 for (int c = 0; c < D4; ++c) {
-                    float4 u[4], y[4];
+                    float4 u[RI], y[KB / 16];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) u[i] = sQ[(ty + 16 * i) * LD4 + c], y[i] = sK[(tx + 16 * i) * LD4 + c];
+                    for (int i = 0; i < KB / 16; ++i) y[i] = sK[(tx + 16 * i) * LD4 + c];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < RI; ++i) u[i] = sQ[(ty + 16 * i) * LD4 + c];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[i][j] += u[i].x * y[j].x + u[i].y * y[j].y + u[i].z * y[j].z + u[i].w * y[j].w;
+                    for (int i = 0; i < RI; ++i)
+#pragma unroll
+                        for (int j = 0; j < KB / 16; ++j) s[i][j] += u[i].x * y[j].x + u[i].y * y[j].y + u[i].z * y[j].z + u[i].w * y[j].w;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < RI; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sP[(ty + 16 * i) * PS + tx + 16 * j] = s[i][j];
+                    for (int j = 0; j < KB / 16; ++j) sP[(ty + 16 * i) * PS + tx + 16 * j] = s[i][j];
             }
             __syncthreads();
             // whole tiles: seen by the first row up to their end, and by the last row's window from their start
             const int x0 = token_of(t0), x1 = t0 + KB <= k1 ? token_of(t0 + KB - 1) : 0x7fffffff;
             const bool masked = x1 > p_first || !(x1 < a.sinks || (x0 >= from && p_last - x0 < a.window));
-            for (int r = warp; r < RB; r += THREADS / 32) {  // softmax step of one row, lane = two keys
-                float s[2], p[2];
-                bool seen[2];
+            for (int r = warp; r < RB; r += THREADS / 32) {  // softmax step of one row, lane = one key or two
+                float s[NE], p[NE];
+                bool seen[NE];
                 const int pr = len + (int)((r0 + r) / a.G);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < NE; ++e) {
                     const int pos = s_pos[buf][lane + 32 * e];
                     seen[e] = !masked || (pos <= pr && (pos < a.sinks || pr - pos < a.window));
                     s[e] = sP[r * PS + lane + 32 * e] * a.scale;
                 }
-                float top = fmaxf(seen[0] ? s[0] : -INFINITY, seen[1] ? s[1] : -INFINITY);
+                float top = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < NE; ++e) top = fmaxf(top, seen[e] ? s[e] : -INFINITY);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const float m0 = s_m[r], m1 = fmaxf(m0, top);
                 const float ref = m1 == -INFINITY ? 0.f : m1;  // nothing seen so far: no difference of infinities
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
+                for (int e = 0; e < NE; ++e) {
                     p[e] = seen[e] ? expf(s[e] - ref) : 0.f;
                     sP[r * PS + lane + 32 * e] = seen[e] ? p[e] : MASKED;
                 }
-                const float sum = warp_sum(p[0] + p[1]);
+                const float sum = warp_sum(NE == 2 ? p[0] + p[NE - 1] : p[0]);
                 if (lane == 0) {
                     const float alpha = expf(m0 - ref);
                     s_alpha[r] = alpha, s_m[r] = m1, s_l[r] = s_l[r] * alpha + sum;
@@ -332,18 +354,18 @@ __global__ void __launch_bounds__(256) chunk_join_kernel(const __grid_constant__
     }
 }
 
-int smem_of(int d) { return ((RB + 2 * KB) * (d + 4) + RB * PS) * (int)sizeof(float); }
+int smem_of(int rb, int kb, int d) { return ((rb + 2 * kb) * (d + 4) + rb * (kb + 4)) * (int)sizeof(float); }
 
-template <typename T, int RPT> cudaError_t launch_rpt(const ChunkArgs &a, const Parts &p, cudaStream_t stream)
+template <typename T, int RB, int KB, int RPT> cudaError_t launch_rpt(const ChunkArgs &a, const Parts &p, cudaStream_t stream)
 {
     float *part_o = a.ws, *part_ml = a.ws + (p.parts > 1 ? p.parts * p.rows * a.c.d : 0);
     int dev = 0, sms = 0;
     cudaError_t e = current_device_sms(&dev, &sms);
-    if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void *>(chunk_generic_kernel<T, RPT>), smem_of(256), dev);
+    if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void *>(chunk_generic_kernel<T, RB, KB, RPT>), smem_of(RB, KB, 256), dev);
     if (e != cudaSuccess) return e;
     const long long x = p.blocks < 1 ? 1 : p.blocks > 0x7fffffffll ? 0x7fffffffll : p.blocks;
     if (a.c.H_kv > 65535) return cudaErrorInvalidValue;
-    e = launch_dependent(chunk_generic_kernel<T, RPT>, dim3((unsigned)x, p.parts, a.c.H_kv), dim3(THREADS), smem_of(a.c.d), stream, a, p.parts, part_ml,
+    e = launch_dependent(chunk_generic_kernel<T, RB, KB, RPT>, dim3((unsigned)x, p.parts, a.c.H_kv), dim3(THREADS), smem_of(RB, KB, a.c.d), stream, a, p.parts, part_ml,
                          part_o);
     if (e != cudaSuccess || p.parts == 1) return e;
     long long join = (p.rows + 7) / 8;
@@ -355,9 +377,14 @@ template <typename T, int RPT> cudaError_t launch_rpt(const ChunkArgs &a, const 
 template <typename T> cudaError_t launch_typed(const ChunkArgs &a, cudaStream_t stream)
 {
     const Parts p = parts_of(a);
-    if (a.c.d > 128) return launch_rpt<T, 16>(a, p, stream);
-    if (a.c.d > 64) return launch_rpt<T, 8>(a, p, stream);
-    return launch_rpt<T, 4>(a, p, stream);
+    auto launch = [&](auto rb, auto kb) {
+        constexpr int RB = decltype(rb)::value, KB = decltype(kb)::value;
+        return a.c.d > 128 ? launch_rpt<T, RB, KB, RB / 4>(a, p, stream) : a.c.d > 64 ? launch_rpt<T, RB, KB, RB / 8>(a, p, stream) : launch_rpt<T, RB, KB, RB / 16>(a, p, stream);
+    };
+    auto rows = [&](auto kb) {
+        return p.rb == 16 ? launch(std::integral_constant<int, 16>{}, kb) : p.rb == 32 ? launch(std::integral_constant<int, 32>{}, kb) : launch(std::integral_constant<int, 64>{}, kb);
+    };
+    return p.kb == KB_MOST ? rows(std::integral_constant<int, 64>{}) : rows(std::integral_constant<int, 32>{});
 }
 
 }  // namespace
@@ -368,11 +395,11 @@ size_t chunk_generic_workspace(const ChunkArgs &a)
     return p.parts > 1 ? (size_t)p.parts * p.rows * (a.c.d + 2) * sizeof(float) : 0;
 }
 
-// What calls of up to a.T rows need.  With more than one part there are fewer than TARGET_CTAS row blocks, T H_q / RB at least, and
-// parts <= TARGET_CTAS / blocks + 1: parts * rows is at most TARGET_CTAS * RB + rows (and MAX_PARTS * rows).
+// What calls of up to a.T rows need.  With more than one part there are fewer than TARGET_CTAS row blocks, T H_q / RB_MOST at least, and
+// parts <= TARGET_CTAS / blocks + 1: parts * rows is at most TARGET_CTAS * RB_MOST + rows (and MAX_PARTS * rows).
 size_t chunk_generic_workspace_most(const ChunkArgs &a)
 {
-    const long long all = TARGET_CTAS * RB, rows = (long long)a.T * a.H_q < all ? (long long)a.T * a.H_q : all;
+    const long long all = TARGET_CTAS * RB_MOST, rows = (long long)a.T * a.H_q < all ? (long long)a.T * a.H_q : all;
     const long long n = MAX_PARTS * rows < all + rows ? MAX_PARTS * rows : all + rows;
     return (size_t)n * (a.c.d + 2) * sizeof(float);
 }
