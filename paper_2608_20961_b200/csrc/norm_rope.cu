@@ -16,6 +16,9 @@ namespace {
 
 constexpr int NORM_WARPS = 4;
 constexpr int BACKWARD_CTAS = 592;  // four to an SM; each leaves one partial sum of dw
+// Few rows: one cluster, whose CTAs join their sums among themselves, instead of a second launch.  61 rows of 5 heads of 80: one call after
+// another 7.5 us for 9.6, in a graph 5.2 for 4.5; at four items a warp (64 rows of 32 heads of 128) 9.1 for 4.7 in a graph, so two at most.
+constexpr int CLUSTER = 8, CLUSTER_WARPS = 16, CLUSTER_ITEMS = CLUSTER * CLUSTER_WARPS * 2;
 constexpr int JOIN_COLS = 32, JOIN_ROWS = 16;
 
 // lanes of a head: units rounded up to a power of two, at most a warp
@@ -251,10 +254,10 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, UPL == 1 ? 5 : 4) norm_rows_k
 }
 
 // Warps walk (token, slice of heads) in strides of the grid, so that the grid's size alone decides the order of dw's sums.
-template <typename T, int VE, int UPL, int HU>
-__global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const __grid_constant__ NormBackwardArgs na, int slices, int heads_per_slice)
+template <typename T, int VE, int UPL, int HU, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 16 / WARPS) norm_backward_kernel(const __grid_constant__ NormBackwardArgs na, int slices, int heads_per_slice)
 {
-    __shared__ float s_dw[NORM_WARPS][256];
+    __shared__ float s_dw[WARPS][256];
     const RowsArgs &a = na.rows;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_wait();
@@ -274,7 +277,7 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
     const float inv_d = 1.f / a.d;
     const long long work = (long long)a.T * slices;
 #pragma unroll 1
-    for (long long wi = (long long)blockIdx.x * NORM_WARPS + warp; wi < work; wi += (long long)gridDim.x * NORM_WARPS) {
+    for (long long wi = (long long)blockIdx.x * WARPS + warp; wi < work; wi += (long long)gridDim.x * WARPS) {
         const int t = (int)(wi / slices), h_begin = (int)(wi - (long long)t * slices) * heads_per_slice, h_end = min(a.H_q, h_begin + heads_per_slice);
         const T *xs = static_cast<const T *>(a.q) + t * a.ld_q, *ys = static_cast<const T *>(na.dy) + t * na.ld_dy;
         T *dst = static_cast<T *>(a.q_out) + t * a.ld_qo;
@@ -361,11 +364,25 @@ __global__ void __launch_bounds__(NORM_WARPS * 32, 4) norm_backward_kernel(const
         }
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < a.d; c += NORM_WARPS * 32) {
+    constexpr bool IN_CLUSTER = WARPS == CLUSTER_WARPS;
+    __shared__ float s_sum[IN_CLUSTER ? 256 : 1];
+    for (int c = threadIdx.x; c < a.d; c += WARPS * 32) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < NORM_WARPS; ++i) s += s_dw[i][c];
-        na.parts[(long long)blockIdx.x * a.d + c] = s;
+        for (int i = 0; i < WARPS; ++i) s += s_dw[i][c];
+        if constexpr (IN_CLUSTER) s_sum[c] = s;
+        else na.parts[(long long)blockIdx.x * a.d + c] = s;
+    }
+    if constexpr (IN_CLUSTER) {
+        ptx::cluster_sync();
+        const int c = blockIdx.x * (256 / CLUSTER) + threadIdx.x;  // (the grid is the cluster)
+        if (threadIdx.x < 256 / CLUSTER && c < a.d) {
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < CLUSTER; ++i) s += ptx::load_shared_of(&s_sum[c], i);
+            na.dweight[c] = s;
+        }
+        ptx::cluster_sync();           // (none leaves before its sums are read)
     }
 }
 
@@ -429,9 +446,20 @@ template <typename T, int VE, int UPL, int HU> cudaError_t launch_backward_of(co
     Slices s;
     cudaError_t e = slices_of(a.rows.T, a.rows.H_q, heads_of_a_step(a.rows.d, VE) * HU, &s);
     if (e != cudaSuccess) return e;
+    if ((long long)a.rows.T * s.n <= CLUSTER_ITEMS) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(CLUSTER), cfg.blockDim = dim3(CLUSTER_WARPS * 32), cfg.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = CLUSTER, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr, cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, norm_backward_kernel<T, VE, UPL, HU, CLUSTER_WARPS>, a, s.n, s.heads);
+    }
     const long long ctas = ((long long)a.rows.T * s.n + NORM_WARPS - 1) / NORM_WARPS;
     const int grid = (int)(ctas < 1 ? 1 : ctas > BACKWARD_CTAS ? BACKWARD_CTAS : ctas);
-    e = launch_dependent(norm_backward_kernel<T, VE, UPL, HU>, dim3(grid), dim3(NORM_WARPS * 32), 0, stream, a, s.n, s.heads);
+    e = launch_dependent(norm_backward_kernel<T, VE, UPL, HU, NORM_WARPS>, dim3(grid), dim3(NORM_WARPS * 32), 0, stream, a, s.n, s.heads);
     if (e != cudaSuccess) return e;
     return launch_dependent(norm_join_kernel, dim3((a.rows.d + JOIN_COLS - 1) / JOIN_COLS), dim3(JOIN_COLS * JOIN_ROWS), 0, stream, a.parts, grid,
                             a.rows.d, a.dweight);

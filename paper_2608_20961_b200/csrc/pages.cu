@@ -10,6 +10,7 @@
 // 16384 21, 13.7; 65536 68, 18.9.  How many a release has the host does not know, only how many there may be: that
 // call, most often for a few rejected drafts, takes eight CTAs from four times as many on.
 #include "attn_common.cuh"
+#include "ptx_sm100.cuh"
 
 namespace treewy {
 namespace {
@@ -31,24 +32,12 @@ struct PagesShared {
     int taken;
 };
 
-__device__ __forceinline__ int cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return (int)r;
-}
-// all threads of the cluster; what they wrote before is seen after
+using ptx::address_in;
+using ptx::cluster_rank;
 template <int CL> __device__ __forceinline__ void sync_all()
 {
     if constexpr (CL == 1) __syncthreads();
-    else asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-// the same variable of another CTA of the cluster
-__device__ __forceinline__ uint32_t address_in(const int *x, int rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(x)), "r"(rank));
-    return a;
+    else ptx::cluster_sync();
 }
 __device__ __forceinline__ void store_in(const int *x, int rank, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(address_in(x, rank)), "r"(v) : "memory"); }
 __device__ __forceinline__ void max_in(const int *x, int rank, int v)

@@ -489,6 +489,28 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
+// ----------------------------------------------------------------------------- clusters
+// all threads of the cluster; what they wrote before is seen after
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ int cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return (int)r;
+}
+// the same variable of another CTA of the cluster
+__device__ __forceinline__ uint32_t address_in(const void *x, int rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(x)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float load_shared_of(const float *x, int rank)
+{
+    float y;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(y) : "r"(address_in(x, rank)) : "memory");
+    return y;
+}
 // asks for `bytes` (a multiple of 16) from an address of 16 bytes on to be brought to L2
 __device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
 {
