@@ -120,7 +120,7 @@ def _rows(x: torch.Tensor, T: int, H: int, d: int, dtype: torch.dtype, what: str
         raise ValueError(f"{what}: the heads of a token have to be contiguous")
     if x.get_device() != dev:
         raise ValueError(f"{what}: on another device")
-    return row if n > 1 else H * d
+    return row if n > 1 else -(-H * d * x.element_size() // 16) * 16 // x.element_size()  # (one row's does not count, but has to be a legal one)
 
 
 def _on_gpu(dev: int, work: int) -> None:

@@ -406,6 +406,20 @@ def test_a_long_call_does_not_run_out_of_time():
     assert not any(status) and torch.equal(O, want)
 
 
+def test_one_row_of_an_odd_size():
+    """Its distance to the next is nobody's business."""
+    from paper_2608_20961_b200 import attention as at
+    norm, gen = at.HeadNorm(torch.ones(30, device=DEV)), torch.Generator().manual_seed(1)
+    x = torch.randn(1, 3, 30, generator=gen).to(BF16)
+    xs, y, dw = x.to(DEV), torch.empty((1, 3, 30), dtype=BF16, device=DEV), torch.empty(30, device=DEV)
+    at.treewy_norm_rope(norm, None, xs, y)
+    ref = pu.norm_reference(x, torch.ones(30), 1e-6)
+    assert ((y.cpu().to(F64) - ref).abs() <= (2.0 ** -19 + pu.HALF_STEP[BF16] * 1.01) * ref.abs()).all()
+    at.treewy_norm_rope_backward(norm, None, xs, y, y, dw, at.norm_rope_workspace(xs))
+    with pytest.raises(ValueError):
+        at.treewy_norm_rope(norm, None, xs[:, :2], y)
+
+
 def test_nothing_to_do():
     from paper_2608_20961_b200 import attention as at
     layer, pool = _layer(BF16, 30, 2, True)
