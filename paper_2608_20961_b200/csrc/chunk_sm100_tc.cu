@@ -34,6 +34,7 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "chunk_phases.cuh"
 #include "ptx_sm100.cuh"
 #include "tma_host.cuh"
 
@@ -324,7 +325,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
 #pragma unroll 1
         for (int i = 0; i < C::NV; ++i) ptx::mbar_init(&sh.v_full[i], 1), ptx::mbar_init(&sh.v_free[i], C::STREAMS);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.s_full[i], 1), ptx::mbar_init(&sh.p_full[i], 4), ptx::mbar_init(&sh.pv_done[i], 1);
-        for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], C::SOFT_WARPS);
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(&sh.o_free[i], O_FREE_ARRIVALS);
         ptx::mbar_init(&sh.q_full, 1), ptx::mbar_init(&sh.q_free, C::STREAMS), ptx::mbar_init(&sh.end[0], 1), ptx::mbar_init(&sh.end[1], 1);
         for (int i = 0; i < 4; ++i) ptx::mbar_init(&sh.ml_full[i], 1);
         for (int i = 0; i < ITEMS; ++i) ptx::mbar_init(&sh.item_full[i], 1), ptx::mbar_init(&sh.item_empty[i], C::SOFT_WARPS + 3);
@@ -539,6 +540,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
             uint64_t *const s_full = sh.s_full + strm * C::NB, *const p_full = sh.p_full + strm * C::NB, *const pv_done = sh.pv_done + strm * C::NB;
             // stages of the rings and S buffers, and their phases
             unsigned k_stage = 0, k_phase = 0, v_stage = 0, v_phase = 0, made = 0, made_phase = 0, used = 0, used_phase = 0;
+            unsigned uses = 0;             // items with products here: phases of o_free
             auto next_k = [&]() { if (++k_stage == C::NK) k_stage = 0, k_phase ^= 1; };
             auto next_v = [&]() { if (++v_stage == C::NV) v_stage = 0, v_phase ^= 1; };
             // scores of the next tile; ql: low word of the queries' descriptor
@@ -559,6 +561,10 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
             };
             // output of the next tile
             auto product = [&](bool onto) -> bool {
+                if (!onto) {               // the output of the use before this one has been read
+                    if (uses > 0 && !ptx::mbar_wait(&sh.o_free[strm], (uses - 1) & 1)) return false;
+                    ++uses;
+                }
                 if (!ptx::mbar_wait(&sh.v_full[v_stage], v_phase)) return false;
                 if (!ptx::mbar_wait(&p_full[used], used_phase)) return false;
                 ptx::tc_fence_after_sync();
@@ -602,12 +608,10 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     const uint32_t ql = q_lo + (pair ? strm : 0) * (C::Q_TILE / 16);
                     const bool does_qk = C::STREAMS == 2 || me == 0, does_pv = C::STREAMS == 2 || me == 1;
                     if (does_qk && !ptx::mbar_wait(&sh.q_full, ord & 1)) return false;
-                    if (does_pv && ord > 0 && C::STREAMS == 1 && !ptx::mbar_wait(&sh.o_free[0], (ord - 1) & 1)) return false;
                     bool onto = false;
 #pragma unroll 1
                     for (int t = 0; t < n + ahead; ++t) {  // scores of tile t, products of tile j
                         const int j = t - ahead;
-                        if (C::STREAMS == 2 && j == 0 && ord > 0 && !ptx::mbar_wait(&sh.o_free[strm], (ord - 1) & 1)) return false;
                         if (does_pv && j >= 0) {
                             if (on(j)) {
                                 if (!product(onto)) return false;
@@ -796,14 +800,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                     }
                 }
                 // ---- end of the item
-                if (taken > 0) {
-                    if (!wait_product(count - 1)) return false;
-                } else if (ord > 0) {
-                    // A stream without a tile here has no product to wait for, which would be behind the release of the last item's
-                    // outputs.  So that it does not count twice towards that, and does not overwrite what is still read of that item:
-                    for (int s = 0; s < C::STREAMS; ++s)
-                        if (!wait_warp(&sh.o_free[s], (ord - 1) & 1)) return false;
-                }
+                if (taken > 0 && !wait_product(count - 1)) return false;
                 ptx::tc_fence_after_sync();
                 const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
                 const int slot = it.slot;
@@ -812,9 +809,9 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 // Alone in an item with one row tile, the first warpgroup joins both streams' outputs.
                 bool second = false;       // the second stream's O counts
                 float f0 = 1.f, f1 = 0.f;
-                if (C::STREAMS == 2 && !pair) {
-                    // (the next item's are written behind this one's o_free)
-                    second = n > 1;
+                if (C::STREAMS == 2 && !pair && n > 1) {
+                    // (the next item's m and l are written behind a product of that item, and so behind this use's o_free)
+                    second = true;
                     if (strm == 1) {       // (its products are done, then)
                         sh.ml[row] = make_float2(m, l);
                         ptx::tc_fence_before_sync();
@@ -824,7 +821,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         ptx::tc_fence_after_sync();
                     }
                     ++singles;
-                    if (strm == 0 && second) {
+                    if (strm == 0) {
                         const float2 x = sh.ml[row];
                         const float mn = fmaxf(m, x.x), ref = mn == -INFINITY ? 0.f : mn;
                         f0 = ptx::ex2(m - ref), f1 = ptx::ex2(x.x - ref);
@@ -878,14 +875,11 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 }
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) {  // all read: the next item's products may overwrite it
-                    if (C::STREAMS == 1) {
-                        ptx::mbar_arrive(&sh.o_free[0]);
-                    } else if (pair) {
-                        ptx::mbar_arrive(&sh.o_free[strm]), ptx::mbar_arrive(&sh.o_free[strm]);
-                    } else {
-                        ptx::mbar_arrive(&sh.o_free[0]), ptx::mbar_arrive(&sh.o_free[1]);
-                    }
+                if (lane == 0) {  // all read: the next products may overwrite it
+                    const bool apart = C::STREAMS == 1 || pair;
+#pragma unroll
+                    for (int s = 0; s < C::STREAMS; ++s)
+                        if (frees_output(apart, strm, s, apart ? taken > 0 : s < n)) ptx::mbar_arrive(&sh.o_free[s]);
                 }
                 if (writes && warp_on && fix && on && !bad) {
                     // Values with NaN or infinity in masked tiles: those elements, onto what was stored.  (Of two streams either may have

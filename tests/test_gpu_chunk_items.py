@@ -1,0 +1,46 @@
+"""treewy_attn_chunk on batches in which every CTA has a run of short items of all kinds: two row tiles and one, one key tile and several,
+streams without a tile.  What the roles hand to each other between items is what these are about."""
+import numpy as np
+import pytest
+import torch
+
+from tests import prompt_util as pu
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+
+
+def _batch(kind, D, seed):
+    """L, N of many sequences; a row tile has 128 / 2 rows here."""
+    r = np.random.default_rng(seed)
+    B = 160
+    if kind == "pairs and tails":            # two row tiles and then one of few rows, little before them
+        N = r.choice([65, 128, 129, 130, 160, 191, 200], B)
+        L = r.choice([0, 0, 1, 30, 63, 64, 200], B)
+    elif kind == "one key tile":             # decoding of contexts within the first tile, prompts of a tile among them
+        N = r.choice([1, 1, 1, 1, 2, 60, 64], B)
+        L = np.where(N == 1, r.integers(0, 63, B), 0)
+    else:                                    # everything
+        N = r.choice([0, 1, 1, 2, 50, 64, 65, 100, 129, 150], B)
+        L = r.choice([0, 5, 62, 63, 64, 65, 127, 130, 300, 500], B)
+    window, sinks = (70, 3) if kind == "all, window" else (0, 0)
+    return dict(L=L.tolist(), N=N.tolist(), Hq=16, Hkv=8, D=D, page=16, window=window, sinks=sinks, seed=seed)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("kind", ["pairs and tails", "one key tile", "all", "all, window"])
+def test_runs_of_short_items(kind, D):
+    from paper_2608_20961_b200 import attention as at
+    c = pu.make_case(poison=False, **_batch(kind, D, seed=41))
+    ref, size = pu.chunk_reference_gpu(c)
+    want, status = pu.run_chunk(c)
+    assert not any(status)
+    pu.assert_chunk(c, want, ref, size, tensor_cores=True)
+    g, want = pu.on_gpu(c), want.cuda()
+    ws, O, words = at.attn_chunk_workspace(g["cache"], c.T, c.Hq, c.window, c.sinks), torch.empty_like(want), torch.zeros(c.B, dtype=torch.int32, device="cuda")
+    for _ in range(30):
+        O.fill_(7.25)
+        at.treewy_attn_chunk(g["cache"], g["offsets"], g["q"], c.scale, O, ws, c.window, c.sinks, words)
+        assert torch.equal(O, want)
+    assert not words.any()
