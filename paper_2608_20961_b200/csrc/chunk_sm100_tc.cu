@@ -802,7 +802,6 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                 // ---- end of the item
                 if (taken > 0 && !wait_product(count - 1)) return false;
                 ptx::tc_fence_after_sync();
-                const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
                 const int slot = it.slot;
                 const long long orow = ((long long)it.lo + it.t0 + (p - all.p0)) * a.H_q + it.h * a.G + (row - tok * a.G);
                 const int brow = (pair ? strm * MT : 0) + row;  // in the block
@@ -828,6 +827,8 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                         l = l * f0 + x.y * f1, m = mn;
                     }
                 }
+                // (behind the wait for the other stream, whose tiles may be the ones that met something)
+                const bool bad = sh.bad_item[ord % 8] == ord + 1, fix = sh.nonfinite[ord % 8] == ord + 1;
                 const bool writes = C::STREAMS == 1 || pair || strm == 0;
                 const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that saw nothing has 0 everywhere)
                 __nv_bfloat16 *const out_row = static_cast<__nv_bfloat16 *>(a.O) + orow * D;

@@ -61,6 +61,18 @@ def test_no_order_goes_wrong(rule, d, name):
     assert model.find(d, BATCHES[name](d), rule, masked=False, rescale=True) is None
 
 
+@pytest.mark.parametrize("name", ["pair, short single", "singles", "a stream without a tile"])
+def test_what_a_tile_met_is_known_when_it_is_looked_for(rule, name):
+    """NaN and infinity that a stream has taken out of the values, and pages out of range: the stream that writes the outputs of both knows
+    of the other's too."""
+    text = _kernel()
+    wait, look = text.index("wait_warp(&sh.ml_full[w4]"), text.index("sh.nonfinite[ord % 8] == ord + 1")
+    flags = "late" if wait < look < text.index("const bool writes = ") else "early"
+    assert text.count("sh.nonfinite[ord % 8] == ") == 1 and text.count("sh.bad_item[ord % 8] == ") == 1
+    assert model.find(128, BATCHES[name](128), rule, flags=flags) is None
+    assert "is looked for before it is known" in model.find(128, BATCHES[name](128), rule, flags="early")
+
+
 @pytest.mark.parametrize("tiles", [[3, 1, 6], [1] * 4, [5, 2] * 5], ids=str)
 @pytest.mark.parametrize("rescale", [False, True])
 def test_no_order_goes_wrong_with_one_stream(rule, tiles, rescale):

@@ -1,5 +1,7 @@
 """treewy_attn_chunk on batches in which every CTA has a run of short items of all kinds: two row tiles and one, one key tile and several,
 streams without a tile.  What the roles hand to each other between items is what these are about."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -44,3 +46,25 @@ def test_runs_of_short_items(kind, D):
         at.treewy_attn_chunk(g["cache"], g["offsets"], g["q"], c.scale, O, ws, c.window, c.sinks, words)
         assert torch.equal(O, want)
     assert not words.any()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("L", [70, 200])     # of one row tile: two key tiles, four
+def test_infinity_that_some_rows_of_one_row_tile_see(D, L):
+    """Infinity among the values alone, in the last key tile and in the first one that the window leaves: taken out of the tile, and in the outputs of
+    exactly the rows that see it, whichever stream has the tile and however far ahead the other is."""
+    n, window = 20, 50
+    many = 40                                # sequences, all of them alike: many items to a CTA
+    c = pu.make_case([L] * many, [n] * many, Hq=4, Hkv=2, D=D, page=16, window=window, seed=42, poison=False)
+    want = torch.zeros(c.T, c.Hq, c.D)
+    for b in range(many):
+        early, late = L - window + 5, L + 8 + b % 8
+        for x, h, col, y in ((late, 1, 7, math.inf), (late, 0, 9, -math.inf), (early, 0, 3, math.inf)):
+            c.vc[int(c.table[b, x // c.page]), x % c.page, h, col] = y
+            rows = [b * n + i for i in range(n) if x in c.seen(L + i)]
+            want[rows, 2 * h:2 * h + 2, col] = y
+    inf = ~torch.isfinite(want)
+    for _ in range(10):
+        O, status = pu.run_chunk(c)
+        assert not any(status)
+        assert torch.equal(O[inf].float(), want[inf]) and torch.isfinite(O[~inf]).all()
