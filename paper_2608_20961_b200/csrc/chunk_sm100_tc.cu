@@ -10,10 +10,12 @@
 // One tile of a stream:  S = Q K^T, the softmax step in registers (a row to a thread), P = weights as bf16 over S's
 // own columns, O += P V (V read with its rows as the K index).  A stream has two S buffers or more, and its scores are issued as many tiles
 // ahead of its products: the next S is there when a softmax step ends.
-// Softmax.  o = sum_x 2^{s_x - m} v_x / sum_x 2^{s_x - m} (s in log2) for any reference m.  A row's m is the maximum of its first tile and
-// stays: weights are exponents of fp32 and, in P, of bf16, which has its range, so nothing is lost until they come near overflow.  Only when a
-// row's weights of one tile add up to more than 2^40 (or to NaN) its m becomes the maximum so far and O and l are scaled.  So an ordinary tile
-// has no maximum, no exchange between threads and no pass over O: an fma and an exponential a weight, an addition, half a packing.
+// Softmax.  o = sum_x 2^{s_x - m} v_x / sum_x 2^{s_x - m} (s in log2) for any reference m.  A row's m is 14 above the maximum of its first
+// tile and stays until the weights of one tile add up to 1 (or to NaN); then m becomes 14 above the maximum so far and O and l are scaled.  So
+// an ordinary tile has no maximum, no exchange between threads and no pass over O: an fma and an exponential a weight, an addition, half a
+// packing.  With weights of less than 1 a tile, rounded to bf16 or not, O overflows nowhere where weights against the true maximum would not make it,
+// whatever the values.  (Without the 14 and with a limit of 2^40 m moves less often still, but values from 2^88 on came out infinite.)  And the
+// roundings of O among fp32's last numbers, 2^-149, are 2^-135 in the output: less than bf16 tells apart.
 //
 // What bounds it.  Heads of 128, a prompt of 8192 over 32 / 8 heads (550 GFLOP), 520-540 us, 1040 TFLOP/s or 0.61 of the measured GEMM rate.
 // Without the exponentials it takes 446, without half of Q K^T 502, without both 380: three things are about equally long.  The
@@ -48,7 +50,10 @@ constexpr int ITEMS = 8;               // ring of work items between the produce
 constexpr int START = 256;             // cost of an item's start, in keys (128 and 512 cost long prompts 2 %, and 2048 rows 4)
 constexpr int MIN_UNITS = 256;         // least units of a part; at least a tile's keys, so that a part inside an item holds the start of one
 constexpr int UNSEEN = -0x7fffffff;    // for a page that is not looked up
-constexpr float LARGE = 1099511627776.f;  // 2^40: a row's weights of one tile do not add up to more
+constexpr float ABOVE = 14.f;          // the reference above the maximum that it was taken from, in log2 (7: prompts behind a window of 256, where a row
+                                       // sees little of its first tile, 162 us for 154; 20 loses what bf16 holds of values below 2^-110)
+constexpr float LARGE = 1.f;           // a row's weights of one tile add up to less
+static_assert(KT < 1 << 14, "a tile's weights add up to less than LARGE behind a new reference");
 constexpr float PAGE_BAD = -1.f, NOT_DONE = -2.f;  // l of a row whose part is not there
 
 template <int D> struct Cfg {
@@ -704,7 +709,7 @@ chunk_tc_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ Ws 
                                 float t[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                                 for (int i = 0; i < KT; i += 2) t[(i >> 1) & 1] = ptx::max3_nan(t[(i >> 1) & 1], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-                                const float top = ptx::max3_nan(t[0], t[1], t[1]) * sl2, m0 = m;
+                                const float top = ptx::max3_nan(t[0], t[1], t[1]) * sl2 + ABOVE, m0 = m;
                                 // (a NaN or plus infinity there makes the row NaN, by its sum)
                                 m = top > m0 || top != top ? top : m0;
                                 const float f = m == m0 ? 1.f : ptx::ex2(m0 - m);

@@ -68,3 +68,41 @@ def test_infinity_that_some_rows_of_one_row_tile_see(D, L):
         O, status = pu.run_chunk(c)
         assert not any(status)
         assert torch.equal(O[inf].float(), want[inf]) and torch.isfinite(O[~inf]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("L,N", [([0], [700]), ([3000], [1]), ([1000, 30], [40, 200])], ids=["prompt", "token", "pieces"])
+@pytest.mark.parametrize("bits", [7, 12, 36, 300])
+def test_large_values_stay_finite(D, L, N, bits):
+    """Values of 2^120 and scores that grow by `bits` (in log2) along the sequence: outputs are weighted means of the values, and so finite; the sums
+    that they are the quotients of must not leave fp32 on the way."""
+    c = pu.make_case(L, N, Hq=4, Hkv=2, D=D, seed=43, poison=False)
+    top = max(l + n for l, n in zip(L, N))
+    c.vc = (c.vc.float() * 2.0 ** 120).to(BF16)                       # (randn: up to 5 of it, below 2^123)
+    for b, (l, n) in enumerate(zip(L, N)):
+        x = torch.arange(l + n)
+        grows = (x / top * bits * math.log(2.0) / (4 * D)).to(BF16)
+        c.kc[c.table[b, x // c.page].long(), x % c.page] = grows[:, None, None].expand(-1, 2, D)
+    c.q, c.scale = torch.full_like(c.q, 4.0), 1.0
+    ref, size = pu.chunk_reference(c)
+    for generic in (False, True):
+        O, status = pu.run_chunk(c, generic=generic)
+        assert not any(status) and torch.isfinite(O).all()
+        # (a score is D equal products of 4 and a bf16 number, exact in fp32; the factor to log2 is off by 2^-24, which moves keys of up to 30 below the
+        # maximum by 2^-19 of their weights, and exp by 2 steps: within the bounds' part for fp32)
+        pu.assert_chunk(c, O, ref, size, tensor_cores=not generic)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_small_values_keep_their_bits(D):
+    """Values about 2^-116, outputs down to bf16's last numbers."""
+    c = pu.make_case([0, 500], [300, 1], Hq=4, Hkv=2, D=D, seed=44, poison=False)
+    c.vc = (c.vc.double() * 2.0 ** -116).to(BF16)
+    ref, size = pu.chunk_reference(c)
+    # beside the bounds that are relative: an output's last step is 2^-133, and a sum of products (one for 16 keys) is off by 2^-149 at most, of which
+    # weights of 2^-14 and more make 2^-135
+    size = size + (501 / 16 * 2.0 ** -135 + 2.0 ** -134) / 2.0 ** -8
+    for generic in (False, True):
+        O, status = pu.run_chunk(c, generic=generic)
+        assert not any(status)
+        pu.assert_chunk(c, O, ref, size, tensor_cores=not generic)
