@@ -124,7 +124,10 @@ treewy_status_t treewy_pages_reserve(const treewy_page_pool_t *pool, int32_t B, 
  * Release: the pages of sequence b whose tokens all lie in first[b] .. end[b] - 1 go back to the stack, in such an order that a
  * reserve of the same entries takes the same ones again; their entries become -1.  A page that is only partly in
  * the range stays; first >= end releases nothing; end is cut to max_pages pages, a negative first counts as 0.  An entry out of range
- * (>= n_pages) becomes -1 with TREEWY_SEQ_BAD_PAGE, as does one that the stack has no room for (its page was released twice).
+ * (>= n_pages) becomes -1 with TREEWY_SEQ_BAD_PAGE, as does one that the stack has no room for.
+ * Who holds a page is not counted.  A page that stands in the tables of several sequences (a prompt that they share) goes back with the last of
+ * them only: for the others `first` lies behind it.  One that is released twice is on the stack twice and is handed out twice, to
+ * two sequences that then overwrite each other; that is not looked for, and shows only when the stack has no room.
  */
 treewy_status_t treewy_pages_release(const treewy_page_pool_t *pool, int32_t B, const int32_t *first, const int32_t *end,
                                      int32_t *seq_status, void *cuda_stream);

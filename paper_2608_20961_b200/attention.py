@@ -432,7 +432,9 @@ def treewy_attn_chunk(cache: KVCache, row_offsets: torch.Tensor, q: torch.Tensor
 
 class PagePool:
     """A page table kept on the GPU and the stack of pages that nobody holds (``treewy_page_pool_t``): page_table [B, max_pages]
-    (negative: no page), free_pages [n_pages], free_count [1], all int32.  The object refers to the tensors' memory."""
+    (negative: no page), free_pages [n_pages], free_count [1], all int32.  The object refers to the tensors' memory.
+    Who holds a page is not counted: one in the tables of several sequences (a shared prompt) is released for the last of them
+    only, with `first` behind it for the others."""
 
     def __init__(self, page_table: torch.Tensor, page_size: int, n_pages: int, free_pages: torch.Tensor, free_count: torch.Tensor):
         _require(page_table.dim() == 2 and page_table.is_contiguous() and page_table.dtype == torch.int32,
@@ -470,7 +472,7 @@ def treewy_pages_reserve(pool: PagePool, context_len: torch.Tensor, row_offsets:
 
 def treewy_pages_release(pool: PagePool, first: torch.Tensor, end: torch.Tensor, seq_status: torch.Tensor | None = None,
                          stream=None) -> None:
-    """The pages whose tokens all lie in first[b] .. end[b] - 1 go back to the pool."""
+    """The pages whose tokens all lie in first[b] .. end[b] - 1 go back to the pool (each once: see PagePool on shared ones)."""
     B, dev = pool.B, pool._dev
     _on_gpu(dev, B)
     tw._call("treewy_pages_release", load_library().treewy_pages_release, pool._ref, B, _int32(first, B, "first", dev),
