@@ -243,7 +243,7 @@ def treewy_kv_append(cache: KVCache, row_offsets: torch.Tensor, k: torch.Tensor,
     T, H_kv, d, dtype, dev = k.shape[0], cache.H_kv, cache.d_head, cache.dtype, cache._dev
     if rope is not None and (rope.T != T or rope._dev != dev):
         raise ValueError("rope: as many positions as rows, on the cache's device, wanted")
-    _on_gpu(dev, T)
+    _on_gpu(dev, T if seq_status is None else cache.B)
     ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
     H_q = ld_q = ld_qo = 0
     q_at = qo_at = None
@@ -384,7 +384,7 @@ def treewy_kv_append_norm(cache: KVCache, row_offsets: torch.Tensor, k: torch.Te
     T, H_kv, d, dtype, dev = k.shape[0], cache.H_kv, cache.d_head, cache.dtype, cache._dev
     if rope is not None and (rope.T != T or rope._dev != dev):
         raise ValueError("rope: as many positions as rows, on the cache's device, wanted")
-    _on_gpu(dev, T)
+    _on_gpu(dev, T if seq_status is None else cache.B)
     ld_k, ld_v = _rows(k, T, H_kv, d, dtype, "k", dev), _rows(v, T, H_kv, d, dtype, "v", dev)
     H_q = ld_q = ld_qo = 0
     q_at = qo_at = None
@@ -418,7 +418,7 @@ def treewy_attn_chunk(cache: KVCache, row_offsets: torch.Tensor, q: torch.Tensor
     (T, H_q, d), dtype, dev = q.shape, cache.dtype, cache._dev
     if d != cache.d_head:
         raise ValueError("q: the cache's d_head wanted")
-    _on_gpu(dev, T)
+    _on_gpu(dev, T if seq_status is None else cache.B)
     ld_q = _rows(q, T, H_q, d, dtype, "q", dev)
     if _rows(O, T, H_q, d, dtype, "O", dev) != H_q * d and T > 0:
         raise ValueError("O: contiguous rows wanted")

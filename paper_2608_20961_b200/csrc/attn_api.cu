@@ -125,7 +125,12 @@ treewy_status_t treewy_kv_append(const treewy_kv_cache_t *cache, const treewy_ro
         if (st != TREEWY_OK) return st;
     }
     if (seq_status && misaligned(seq_status)) return TREEWY_ERR_INVALID_ARG;
-    if (B == 0 || T == 0) return TREEWY_OK;
+    if (B == 0) return TREEWY_OK;
+    if (T == 0) {              // (ranges that claim rows are flagged all the same)
+        if (!seq_status) return TREEWY_OK;
+        if (bad_ptr(row_offsets)) return TREEWY_ERR_INVALID_ARG;
+        return launched(launch_no_rows(row_offsets, nullptr, B, 0, seq_status, static_cast<cudaStream_t>(cuda_stream)));
+    }
     const int e = elem_size(io_dtype);
     const int64_t kv_row = (int64_t)cache->H_kv * cache->d_head, q_row = (int64_t)H_q * cache->d_head;
     if (bad_ptr(row_offsets) || bad_ptr(k) || bad_ptr(v) || bad_stride(ld_k, kv_row, e) || bad_stride(ld_v, kv_row, e))

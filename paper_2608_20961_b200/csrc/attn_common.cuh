@@ -84,6 +84,8 @@ struct AttnArgs {
 };
 
 cudaError_t launch_rows(const RowsArgs &a, treewy_dtype_t io, cudaStream_t stream);
+// No packed rows: sequences whose range claims some are flagged, and (context_len not NULL) those whose length does not fit
+cudaError_t launch_no_rows(const int32_t *row_offsets, const int32_t *context_len, int B, long long capacity, int32_t *status, cudaStream_t stream);
 cudaError_t launch_kv_commit(const KvCommitArgs &a, treewy_dtype_t io, cudaStream_t stream);
 cudaError_t launch_attn_generic(const AttnArgs &a, treewy_dtype_t io, cudaStream_t stream);
 size_t attn_generic_workspace(const AttnArgs &a);

@@ -177,7 +177,24 @@ __global__ void __launch_bounds__(COMMIT_WARPS * 32) kv_commit_kernel(KvCommitAr
     }
 }
 
+__global__ void __launch_bounds__(256) no_rows_kernel(const int32_t *row_offsets, const int32_t *context_len, int B, long long capacity, int32_t *status)
+{
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    grid_dependency_wait();
+    grid_dependency_trigger();
+    if (b >= B) return;
+    const int lo = row_offsets[b], n = row_offsets[b + 1] - lo;
+    int bad = bad_offsets(lo, n, 0) ? TREEWY_SEQ_BAD_OFFSETS : 0;
+    if (!bad && context_len && (context_len[b] < 0 || context_len[b] > capacity)) bad = TREEWY_SEQ_BAD_LENGTH;
+    if (bad) atomicOr(&status[b], bad);
+}
+
 }  // namespace
+
+cudaError_t launch_no_rows(const int32_t *row_offsets, const int32_t *context_len, int B, long long capacity, int32_t *status, cudaStream_t stream)
+{
+    return launch_dependent(no_rows_kernel, dim3((B + 255) / 256), dim3(256), 0, stream, row_offsets, context_len, B, capacity, status);
+}
 
 cudaError_t launch_rows(const RowsArgs &a, treewy_dtype_t io, cudaStream_t stream)
 {

@@ -55,7 +55,12 @@ treewy_status_t chunk_common(bool force_generic, const treewy_kv_cache_t *cache,
     if (st != TREEWY_OK) return st;
     if (seq_status && misaligned(seq_status)) return TREEWY_ERR_INVALID_ARG;
     if (!(scale > 0.f) || scale > FLT_MAX) return TREEWY_ERR_INVALID_ARG;
-    if (B == 0 || T == 0) return TREEWY_OK;
+    if (B == 0) return TREEWY_OK;
+    if (T == 0) {              // (ranges that claim rows are flagged all the same)
+        if (!seq_status) return TREEWY_OK;
+        if (bad_ptr(row_offsets)) return TREEWY_ERR_INVALID_ARG;
+        return launched(launch_no_rows(row_offsets, a.c.context_len, B, (int64_t)a.c.max_pages * a.c.page_size, seq_status, static_cast<cudaStream_t>(cuda_stream)));
+    }
     if (bad_ptr(row_offsets) || bad_ptr(q) || bad_ptr(O) || bad_stride(ld_q, (int64_t)H_q * cache->d_head, elem_size(io)))
         return TREEWY_ERR_INVALID_ARG;
     const bool tc = !force_generic && chunk_tc_applies(a, io);
@@ -150,7 +155,12 @@ treewy_status_t treewy_kv_append_norm(const treewy_kv_cache_t *cache, const tree
     }
     if ((st = check_norm(q_norm, &na.q)) != TREEWY_OK || (st = check_norm(k_norm, &na.k)) != TREEWY_OK) return st;
     if (seq_status && misaligned(seq_status)) return TREEWY_ERR_INVALID_ARG;
-    if (B == 0 || T == 0) return TREEWY_OK;
+    if (B == 0) return TREEWY_OK;
+    if (T == 0) {              // (ranges that claim rows are flagged all the same)
+        if (!seq_status) return TREEWY_OK;
+        if (bad_ptr(row_offsets)) return TREEWY_ERR_INVALID_ARG;
+        return launched(launch_no_rows(row_offsets, nullptr, B, 0, seq_status, static_cast<cudaStream_t>(cuda_stream)));
+    }
     const int e = elem_size(io_dtype);
     const int64_t kv_row = (int64_t)cache->H_kv * cache->d_head, q_row = (int64_t)H_q * cache->d_head;
     if (bad_ptr(row_offsets) || bad_ptr(k) || bad_ptr(v) || bad_stride(ld_k, kv_row, e) || bad_stride(ld_v, kv_row, e))
