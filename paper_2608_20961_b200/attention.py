@@ -479,6 +479,11 @@ def treewy_pages_release(pool: PagePool, first: torch.Tensor, end: torch.Tensor,
              _int32(end, B, "end", dev), _int32(seq_status, B, "seq_status", dev), _stream(stream, pool.page_table))
 
 
+def _capturing(x: torch.Tensor) -> bool:
+    """Whether the call that x goes into is being captured into a graph."""
+    return x.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 class AttentionLayer:
     """One attention layer's side of a step -- a prompt or a piece of one, single tokens, a speculative round -- on the current
     stream: the paged cache, the rotary table, the norms and workspaces stay with the layer; each call takes the step's packed
@@ -515,7 +520,7 @@ class AttentionLayer:
         self._unseen = None                        # ancestor masks of nodes that see no draft row
         self._ws, self._ws_for = None, None
         self._rows_ws, self._rows_for = None, 0    # workspace of prefill, and the rows it is for
-        self._captured = []                        # those that graphs refer to stay
+        self._captured = []                        # workspaces that graphs refer to
 
     def _workspace(self, tree: Tree, shared_len: int) -> torch.Tensor:
         sizes = (tree.B, tree.T, tree.max_nodes, shared_len)
@@ -524,7 +529,13 @@ class AttentionLayer:
             if self._ws is None or ws.numel() > self._ws.numel():
                 self._ws = ws
             self._ws_for = sizes
-        return self._ws
+        return self._in_use(self._ws)
+
+    def _in_use(self, ws: torch.Tensor) -> torch.Tensor:
+        """A workspace that a call being captured takes stays, whatever later calls take: the graph writes to it at each replay."""
+        if _capturing(ws) and not any(w is ws for w in self._captured):
+            self._captured.append(ws)
+        return ws
 
     def _out(self, q: torch.Tensor) -> torch.Tensor:
         return torch.empty((q.shape[0], self.H_q, self.cache.d_head), dtype=q.dtype, device=q.device)
@@ -619,9 +630,7 @@ class AttentionLayer:
         self._append(offsets, positions, q, k, v, q_out, status)
         if self._rows_ws is None or self._rows_for < T:
             self._rows_ws, self._rows_for = attn_chunk_workspace(self.cache, T, self.H_q, self.window, self.sinks), T
-        if q.is_cuda and torch.cuda.is_current_stream_capturing() and not any(ws is self._rows_ws for ws in self._captured):
-            self._captured.append(self._rows_ws)
-        treewy_attn_chunk(self.cache, offsets, q_out, self.scale, O, self._rows_ws, self.window, self.sinks, status)
+        treewy_attn_chunk(self.cache, offsets, q_out, self.scale, O, self._in_use(self._rows_ws), self.window, self.sinks, status)
         if advance:
             self._len.add_(counts * (status == 0))
         return O
