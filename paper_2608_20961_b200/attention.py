@@ -484,10 +484,17 @@ def _capturing(x: torch.Tensor) -> bool:
     return x.is_cuda and torch.cuda.is_current_stream_capturing()
 
 
+def _let_go(ws: torch.Tensor | None) -> None:
+    """A workspace that a larger one replaces: calls on other streams than the one it was allocated on may still be at work in it.  All
+    of them are ahead of the current call, as the cache is theirs too, so its memory is free when the current stream has come here."""
+    if ws is not None and ws.is_cuda:
+        ws.record_stream(torch.cuda.current_stream(ws.device))
+
+
 class AttentionLayer:
     """One attention layer's side of a step -- a prompt or a piece of one, single tokens, a speculative round -- on the current
     stream: the paged cache, the rotary table, the norms and workspaces stay with the layer; each call takes the step's packed
-    rows.  The cache's ``context_len`` is advanced by ``prefill``, ``commit`` and ``append_and_attend``.  Layers of one model that share
+    rows.  Calls of one layer, replays of captured ones among them, share these: on several streams the caller orders them.  The cache's ``context_len`` is advanced by ``prefill``, ``commit`` and ``append_and_attend``.  Layers of one model that share
     a context_len array leave that to the last of them, since all of a step write at the same place: the others pass
     advance=False.
 
@@ -527,6 +534,7 @@ class AttentionLayer:
         if self._ws_for != sizes:
             ws = attn_workspace(self.cache, tree, self.H_q, shared_len)
             if self._ws is None or ws.numel() > self._ws.numel():
+                _let_go(self._ws)
                 self._ws = ws
             self._ws_for = sizes
         return self._in_use(self._ws)
@@ -629,6 +637,7 @@ class AttentionLayer:
             status |= (counts != 1) * tw.SEQ_TOO_MANY_NODES
         self._append(offsets, positions, q, k, v, q_out, status)
         if self._rows_ws is None or self._rows_for < T:
+            _let_go(self._rows_ws)
             self._rows_ws, self._rows_for = attn_chunk_workspace(self.cache, T, self.H_q, self.window, self.sinks), T
         treewy_attn_chunk(self.cache, offsets, q_out, self.scale, O, self._in_use(self._rows_ws), self.window, self.sinks, status)
         if advance:
