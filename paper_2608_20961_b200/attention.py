@@ -400,8 +400,15 @@ def treewy_kv_append_norm(cache: KVCache, row_offsets: torch.Tensor, k: torch.Te
              ld_qo, cache._dt, _int32(seq_status, cache.B, "seq_status", dev), _stream(stream, k))
 
 
+def _window(window: int, sinks: int) -> None:
+    """(ctypes would cut them to 32 bits without a word; the library refuses negative ones.)"""
+    if not (-1 << 31 <= window < 1 << 31 and -1 << 31 <= sinks < 1 << 31):
+        raise ValueError("window, sinks: 32 bits wanted")
+
+
 def attn_chunk_workspace(cache: KVCache, T: int, H_q: int, window: int = 0, sinks: int = 0) -> torch.Tensor:
     """A workspace for ``treewy_attn_chunk`` calls of up to T rows with this window (one per call in flight)."""
+    _window(window, sinks)
     n = load_library().treewy_attn_chunk_workspace(cache._ref, cache.B, T, H_q, window, sinks, cache._dt)
     return torch.empty((max(int(n), 16),), dtype=torch.uint8, device=cache.k.device)
 
@@ -418,6 +425,7 @@ def treewy_attn_chunk(cache: KVCache, row_offsets: torch.Tensor, q: torch.Tensor
     (T, H_q, d), dtype, dev = q.shape, cache.dtype, cache._dev
     if d != cache.d_head:
         raise ValueError("q: the cache's d_head wanted")
+    _window(window, sinks)
     _on_gpu(dev, T if seq_status is None else cache.B)
     ld_q = _rows(q, T, H_q, d, dtype, "q", dev)
     if _rows(O, T, H_q, d, dtype, "O", dev) != H_q * d and T > 0:
@@ -511,6 +519,7 @@ class AttentionLayer:
                  k_norm: HeadNorm | None = None, window: int = 0, sinks: int = 0):
         if H_q < 1 or H_q % cache.H_kv != 0:
             raise ValueError("H_q: a multiple of the cache's heads wanted")
+        _window(window, sinks)
         if window < 0 or sinks < 0:
             raise ValueError("window, sinks: not negative")
         _norm(q_norm, cache.d_head, "q_norm", cache._dev), _norm(k_norm, cache.d_head, "k_norm", cache._dev)
