@@ -28,7 +28,8 @@ enum {
 /*
  * Root-mean-square norm of one head's d_head elements ahead of the rotation,
  *       y = rotate(w x / sqrt(mean_c x_c^2 + eps)) ,   w = weight, or 1 + weight (plus_one),
- * in fp32 and rounded once.  weight [d_head] is the same for all heads; weight_dtype may differ from the data's.
+ * in fp32 and rounded once (the sum of squares too: a head whose elements reach some 2^60 leaves its range and becomes 0).  weight
+ * [d_head] is the same for all heads; weight_dtype may differ from the data's.
  */
 typedef struct {
     const void *weight; /* device */
@@ -80,7 +81,8 @@ treewy_status_t treewy_kv_append_norm(const treewy_kv_cache_t *cache, const tree
  * each) for the product with v.
  * A sequence whose range leaves the packed rows or runs backwards is flagged TREEWY_SEQ_BAD_OFFSETS, one whose rows do not fit
  * max_pages pages TREEWY_SEQ_BAD_LENGTH, one that sees a page out of range TREEWY_SEQ_BAD_PAGE, one with rows left
- * unwritten because a bounded wait gave up TREEWY_SEQ_TIMEOUT; the rows of O of a flagged sequence mean nothing.
+ * unwritten because a bounded wait gave up TREEWY_SEQ_TIMEOUT; the rows of O of a flagged sequence mean nothing.  (As in
+ * treewy_kv_append a row that two sequences claim, beside one that runs backwards, is computed for one of them.)
  */
 size_t treewy_attn_chunk_workspace(const treewy_kv_cache_t *cache, int32_t B, int32_t T, int32_t H_q, int32_t window,
                                    int32_t sinks, treewy_dtype_t io_dtype);

@@ -7,8 +7,8 @@
 // are joined by a second kernel with the same rule.  Only tiles that some row does not see whole are masked: a masked weight is
 // a negative number that the product skips, so what a row may not see is never multiplied.
 // It is bound by shared memory (4 x 4 scores to a thread, four keys of a row's weights at a time), small calls by the chain of one step and
-// the join: fp32, a prompt of 2048 with 32 / 8 heads of 128 2.06 ms, 17 TFLOP/s; one token over 8192 keys 68 us (157 in blocks of 64 rows); four pieces of up
-// to 77 rows with heads of 80 16.6.
+// the join: fp32, a prompt of 2048 with 32 / 8 heads of 128 2.06 ms, 17 TFLOP/s (bf16 with heads of 80 1.34 ms, 16); one token over 8192 keys 68-83 us (157 in
+// blocks of 64 rows); four pieces of up to 77 rows with heads of 80 16.6-22.
 #include <type_traits>
 
 #include "attn_common.cuh"

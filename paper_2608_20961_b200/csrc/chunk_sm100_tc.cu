@@ -17,13 +17,14 @@
 // whatever the values.  (Without the 14 and with a limit of 2^40 m moves less often still, but values from 2^88 on came out infinite.)  And the
 // roundings of O among fp32's last numbers, 2^-149, are 2^-135 in the output: less than bf16 tells apart.
 //
-// What bounds it.  Heads of 128, a prompt of 8192 over 32 / 8 heads (550 GFLOP), 520-540 us, 1040 TFLOP/s or 0.61 of the measured GEMM rate.
-// Without the exponentials it takes 446, without half of Q K^T 502, without both 380: three things are about equally long.  The
+// What bounds it.  Heads of 128, a prompt of 8192 over 32 / 8 heads (550 GFLOP), 525 us, 1050 TFLOP/s or 0.62 of the measured GEMM rate (up to
+// 587 where the power cap has lowered the clock).  Of 541 us 446 are left without the exponentials, 502 without half of Q K^T, 380 without both: three things are about equally long.  The
 // tensor cores: an MMA of Q K^T with both operands in shared memory takes 50 cycles for 64 keys where its arithmetic takes 32, since the
 // operands are 6 kB at 128 bytes a cycle; with P in tensor memory P V runs at its arithmetic.  The exponentials: 16 a cycle and SM, 1024 of some 2100 cycles a
-// tile of both streams.  And the softmax warps' own latency, 2 of them to a scheduler that issues 0.37 a cycle.  Heads of 64: 490 us (562
-// TFLOP/s), without exponentials 322.  Heads of 256 (one stream, four S buffers): 510-520 us (1060).  Decoding, 64 sequences
-// of 8192: 218 us, 6 TB/s, HBM.
+// tile of both streams.  And the softmax warps' own latency, 2 of them to a scheduler that issues 0.37 a cycle.  Heads of 64: 490 us (561
+// TFLOP/s), without exponentials 322.  Heads of 256 (one stream, four S buffers): 508-565 us (1083).  Decoding, 64 sequences
+// of 2048 to 8192 tokens: 222 us, 5.9 TB/s, HBM (all of 8192: 335, 6.4); with heads of 64 167-174 us, 3.9 TB/s: four rows of 128 are
+// used, four lanes of a warp take a tile's exponentials.  Short items pay their start: eight prompts of up to 512 46 us, window of 256 with heads of 64 154.
 //
 // Why so.  What else was built and measured on the prompt of 8192, heads of 128 (and 64), against this: a row split over two threads
 // 585; key tiles of 128 with one S buffer 773; two warpgroups a stream on alternate tiles, the reference passed between them, 1120 (1080); three S buffers for

@@ -5,9 +5,9 @@
 // A head is held in registers by a group of lanes (a power of two of them, so that its sums are a few exchanges), each
 // with UPL units: the vectors that hold VE pairs.  As in the rotation alone a warp takes heads of one token with the same pairs
 // in every lane, so cosines, sines, weights and dw's partial sums stay in registers over the heads.  Every row is read once and
-// written once.  15800 rows of 16 query and 2 + 2 key and value heads of 256 into a cache take 76 us, 4.25 TB/s or 0.66 of the copy rate: issue (0.55 a cycle)
-// and memory, about as long each.  Backward, 8199 rows of 32 heads of 128: 45 us, 4.5 TB/s.  A decoding step of 64 tokens 4.4 us: one launch
-// and its lookups.  Loads a step ahead in the forward pass cost registers (76 -> 81-92 us), over the ends of tokens in the backward pass too (45 -> 50).
+// written once.  15800 rows of 16 query and 2 + 2 key and value heads of 256 into a cache take 76 us, 4.25 TB/s or 0.66 of the copy rate, with 0.55
+// instructions issued a cycle: warps wait for loads, of which registers hold no more.  8199 rows of 32 heads of 128: forward alone 32 us, 4.3 TB/s, backward 45 us,
+// 4.5 TB/s.  A decoding step of 64 tokens 4.4 us (3.4 without a cache): one launch and its lookups.  Loads a step ahead in the forward pass cost registers (76 -> 81-92 us), over the ends of tokens in the backward pass too (45 -> 50).
 #include "ptx_sm100.cuh"
 #include "rows_common.cuh"
 
