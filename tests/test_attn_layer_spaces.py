@@ -77,10 +77,10 @@ def test_a_workspace_that_another_stream_is_at_is_not_handed_out(at, step):
     """Allocated on one stream, used on another, replaced there: the first stream's next allocation must not be that memory while the other
     has not come so far.  (Addresses alone are looked at.)"""
     dev = "cuda:0"
-    layer = _layer(at, dev)
+    layer, other = _layer(at, dev), _layer(at, dev)
     i32, rows = (lambda *x: torch.tensor(x, dtype=I32, device=dev)), (lambda T: [torch.zeros(T, h, 64, dtype=BF16, device=dev) for h in (8, 2, 2)])
 
-    def run(n, x):
+    def run(n, x, layer=layer):
         if step == "verify":
             layer.verify(trees[n], pos[2 * n], *x)
         else:
@@ -88,11 +88,12 @@ def test_a_workspace_that_another_stream_is_at_is_not_handed_out(at, step):
     trees, i32_of = {n: _tree(at, n, dev) for n in (2, 40)}, {n: i32(0, n, 2 * n) for n in (2, 40)}
     pos, data = {2 * n: torch.zeros(2 * n, dtype=I32, device=dev) for n in (2, 40)}, {n: rows(2 * n) for n in (2, 40)}
     space = lambda: layer._ws if step == "verify" else layer._rows_ws
+    run(40, data[40], other)                 # (what a first call loads is loaded here)
     run(2, data[2])
     where, size, side = space().data_ptr(), space().numel(), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
-        torch.cuda._sleep(200_000_000)       # (about a tenth of a second)
+        torch.cuda._sleep(600_000_000)       # (about a third of a second)
         run(2, data[2])
         run(40, data[40])
     assert space().numel() > size
